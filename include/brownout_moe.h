@@ -87,7 +87,8 @@ typedef enum bmoe_stage {
     BMOE_STAGE_DISPATCH = 1,
     BMOE_STAGE_FFN = 2,
     BMOE_STAGE_COMBINE = 3,
-    BMOE_STAGE_DOWN_COMBINE = 4  /* brownout_moe_ffn_down_combine */
+    BMOE_STAGE_DOWN_COMBINE = 4, /* brownout_moe_ffn_down_combine */
+    BMOE_STAGE_FEW = 5           /* brownout_moe_few */
 } bmoe_stage;
 
 /* Shape of one layer. */
@@ -392,6 +393,132 @@ BMOE_API bmoe_status brownout_moe_ffn_down_combine(const bmoe_desc* desc, const 
 BMOE_API bmoe_status brownout_moe_combine(const bmoe_desc* desc, const int32_t* slot_row,
                                  const float* slot_gate, const void* y_perm,
                                  const void* y_shared, void* out, void* stream);
+
+/*
+ * Norms around the layer: the RMS norm that makes the layer's input, and the
+ * one that returns its output to the residual stream.
+ *
+ * brownout_moe_pre_norm:
+ *   out[t,:] = rms(x[t,:]) * w,   rms(v) = v / sqrt(mean over j of v_j^2 + eps)
+ * brownout_moe_post_norm:
+ *   n[t,:] = rms(y[t,:]) * w_post  (norm_y 1)   or   y[t,:]  (norm_y 0)
+ *   r[t,:] = res_scale * x[t,:] + gate * n[t,:]
+ *   a[t,:] = rms(r[t,:]) * w_next   (when a is not NULL: the next block's norm;
+ *            it reads r before r is rounded to dtype)
+ * x, y, out, r, a [T,d] and w, w_post, w_next [d] in dtype; a NULL w, w_post or
+ * w_next stands for ones (w_post must be NULL when norm_y is 0, w_next when a
+ * is). gate by gate_mode: BMOE_GATE_NONE (NULL, 1), BMOE_GATE_CHANNEL ([d] in
+ * dtype), BMOE_GATE_TOKEN ([T] float) or BMOE_GATE_FULL ([T,d] in dtype).
+ * Sums in fp32 over the whole row, one rounding at each output. Every tensor
+ * except the per-token gate is 16-byte aligned. d is at most 32768; eps in
+ * [1e-12, 1]; res_scale finite. An output may be one of the input tensors of
+ * its shape (the residual stream updated in place); r and a differ. No workspace.
+ */
+typedef enum bmoe_gate_mode {
+    BMOE_GATE_NONE = 0,
+    BMOE_GATE_CHANNEL = 1,
+    BMOE_GATE_TOKEN = 2,
+    BMOE_GATE_FULL = 3
+} bmoe_gate_mode;
+#define BMOE_NORM_MAX_D 32768
+BMOE_API bmoe_status brownout_moe_pre_norm(int32_t dtype, int32_t T, int32_t d, float eps, const void* x,
+                                  const void* w, void* out, void* stream);
+BMOE_API bmoe_status brownout_moe_post_norm(int32_t dtype, int32_t T, int32_t d, float eps, int32_t norm_y,
+                                   float res_scale, int32_t gate_mode, const void* y, const void* x,
+                                   const void* w_post, const void* gate, void* r, const void* w_next, void* a,
+                                   void* stream);
+
+/*
+ * Weights held in 4 bits with group scales. A matrix stack [n, N, K] (K: the
+ * summed columns, a multiple of 8) is held as
+ *   codes  [n, N, P] uint8, P = 16 * ceil(K/32): byte b of a row holds column 2b
+ *          in its low four bits and column 2b+1 in its high four; the bytes past
+ *          K/2 are padding, their values do not matter;
+ *   scales [n, N, ceil(K/group)] bf16 (finite), group 32, 64 or 128;
+ *   zeros  [n, N, ceil(K/group)] uint8, or NULL: every zero point is 8.
+ * Column k of a row stands for  w = scale[k / group] * (code[k] - zero[k / group]).
+ * Products are exact in fp32 (bf16 activations on MFMA against code + 16, whose
+ * offset the sum of the activations takes back), sums in fp32, the group's sum
+ * is scaled in fp32. codes 16-byte aligned, scales 2-byte.
+ */
+#define BMOE_W4_ROW_BYTES(K) (((K) + 31) / 32 * 16)
+typedef struct bmoe_w4 {
+    const uint8_t* codes;
+    const void* scales;   /* bf16 */
+    const uint8_t* zeros; /* or NULL */
+    int32_t group;        /* 32, 64 or 128 */
+} bmoe_w4;
+
+/*
+ * brownout_moe_w4_quantize -- rounds w [n, N, K] (dtype) to that format. Per
+ * group of a row: without zeros, scale = max|w| / 7, code = 8 + round(w / scale)
+ * in 1..15; with zeros, scale = (max - min) / 15 over the group's values and 0,
+ * zero = round(-min / scale), code = zero + round(w / scale) clamped to 0..15.
+ * The scale is rounded to bf16 first, and w is divided by the rounded one;
+ * rounding is to nearest even. A group of zeros has scale 0 and codes 8 (0 and
+ * zero 0 with zeros). Padding bytes are written 0x88. Outputs as above.
+ */
+BMOE_API bmoe_status brownout_moe_w4_quantize(int32_t dtype, int32_t n, int32_t N, int32_t K, int32_t group,
+                                     const void* w, uint8_t* codes, void* scales, uint8_t* zeros, void* stream);
+
+/*
+ * Grouped products with 4-bit weights, for few rows per segment (each pass over
+ * a segment's weights serves up to 64 of its rows). dtype: BMOE_BF16 (the
+ * activations' and outputs'; others are BMOE_ERR_UNSUPPORTED). Segments as in
+ * brownout_moe_ffn: segment s covers rows offsets[s] .. offsets[s+1]-1; rows of
+ * no segment are left as they are. a_rows as in brownout_moe_ffn_gather, or NULL
+ * (row r reads a[r]; a then has rows_cap rows and a_count is not used). No workspace.
+ *   brownout_moe_w4_matmul   y[row,:] = a[row,:] W[s]^T                 W [n_seg, N, K]
+ *   brownout_moe_w4_gate_up  h[row,:] = silu(a[row,:] Wg[s]^T) * (a[row,:] Wu[s]^T)
+ *                            Wg, Wu [n_seg, d_ff, d], the same group and both with or without zeros
+ *   brownout_moe_w4_ffn      gate_up, then y[row,:] = h[row,:] Wd[s]^T   Wd [n_seg, d, d_ff]
+ */
+BMOE_API bmoe_status brownout_moe_w4_matmul(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t N, int32_t K,
+                                   const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,
+                                   const bmoe_w4* w, void* y, void* stream);
+BMOE_API bmoe_status brownout_moe_w4_gate_up(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t d, int32_t d_ff,
+                                    const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,
+                                    const bmoe_w4* w_gate, const bmoe_w4* w_up, void* h, void* stream);
+BMOE_API bmoe_status brownout_moe_w4_ffn(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t d, int32_t d_ff,
+                                const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,
+                                const bmoe_w4* w_gate, const bmoe_w4* w_up, const bmoe_w4* w_down, void* h, void* y,
+                                void* stream);
+
+/*
+ * brownout_moe_few -- the whole layer for 1 to BMOE_FEW_MAX_TOKENS tokens: the
+ * results of route, dispatch, FFN, the shared experts and combine, without the
+ * permutation and its buffers. Every token of a reached segment shares one read
+ * of the segment's weights.
+ *   topk_idx, topk_w, slot_group, slot_gate [T,k] as brownout_moe_route writes them
+ *   out[t,:] = sum over the valid slots i of t, segments ascending, of
+ *              W_down[g] (slot_gate[t,i] * silu(W_gate[g] x_t) * (W_up[g] x_t))
+ *              (+ W_down_sh (silu(W_gate_sh x_t) * (W_up_sh x_t)))
+ * The hidden values are held to 16 bits of significand (bf16 layers) or in fp32,
+ * the sum over experts in fp32; out is rounded once.
+ * x, out [T,d] (dtype). weights: w_router, bias, e2g as in brownout_moe_route;
+ * the six matrices either all plain (dtype, group 0; scales and zeros NULL) or
+ * all in 4 bits (dtype BMOE_BF16; `w` the codes, the same group for all six, and
+ * zeros for all or none). The *_sh matrices are read when d_ff_shared > 0.
+ * T above BMOE_FEW_MAX_TOKENS is BMOE_ERR_SHAPE.
+ * workspace: bmoe_workspace_bytes(desc, BMOE_STAGE_FEW) bytes, 256-byte aligned,
+ * no initialisation; calls that can overlap in time must not share one.
+ */
+#define BMOE_FEW_MAX_TOKENS 16
+typedef struct bmoe_matrix {
+    const void* w;
+    const void* scales;
+    const uint8_t* zeros;
+} bmoe_matrix;
+typedef struct bmoe_few_weights {
+    const void* w_router;
+    const float* bias;
+    const int32_t* e2g;
+    bmoe_matrix gate, up, down, gate_sh, up_sh, down_sh;
+    int32_t group; /* 0: plain weights; 32, 64 or 128: 4-bit weights */
+} bmoe_few_weights;
+BMOE_API bmoe_status brownout_moe_few(const bmoe_desc* desc, const bmoe_few_weights* weights, const void* x,
+                             int32_t* topk_idx, float* topk_w, int32_t* slot_group, float* slot_gate, void* out,
+                             void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

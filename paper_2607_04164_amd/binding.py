@@ -18,7 +18,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libbrownout_moe.so")
 
 BMOE_F32, BMOE_BF16 = 0, 1
-STAGE_ROUTE, STAGE_DISPATCH, STAGE_FFN, STAGE_COMBINE, STAGE_DOWN_COMBINE = 0, 1, 2, 3, 4
+STAGE_ROUTE, STAGE_DISPATCH, STAGE_FFN, STAGE_COMBINE, STAGE_DOWN_COMBINE, STAGE_FEW = 0, 1, 2, 3, 4, 5
 ROUTE_RECHECK_GAP = 1.0 / 16384.0
 MAX_EXPERTS, MAX_TOPK = 256, 16
 
@@ -29,9 +29,14 @@ EXPORTED = ("bmoe_validate", "bmoe_validate_map", "bmoe_workspace_bytes", "bmoe_
             "bmoe_version", "brownout_moe_route", "brownout_moe_dispatch", "brownout_moe_ffn",
             "brownout_moe_ffn_gate_up", "brownout_moe_ffn_down", "brownout_moe_combine",
             "brownout_moe_ffn_gather", "brownout_moe_ffn_gate_up_gather", "brownout_moe_united_init",
-            "brownout_moe_distill_mse", "brownout_moe_ffn_ex", "bmoe_partial_segment_map", "brownout_moe_dispatch_noalloc", "brownout_moe_ffn_down_combine")
+            "brownout_moe_distill_mse", "brownout_moe_ffn_ex", "bmoe_partial_segment_map", "brownout_moe_dispatch_noalloc", "brownout_moe_ffn_down_combine",
+            "brownout_moe_pre_norm", "brownout_moe_post_norm", "brownout_moe_w4_quantize", "brownout_moe_w4_matmul",
+            "brownout_moe_w4_gate_up", "brownout_moe_w4_ffn", "brownout_moe_few")
 STATUS_CODES = {v: k for k, v in STATUS.items()}
 DISTILL_WS_BYTES = 32768
+FEW_MAX_TOKENS = 16
+NORM_MAX_D = 32768
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_FULL = 0, 1, 2, 3
 DISPATCH_SCRATCH_BYTES = 1048576  # the array behind brownout_moe_dispatch_noalloc
 
 
@@ -61,6 +66,21 @@ def make_desc(T, d, E, top_k, G, d_ff, d_ff_shared=0, norm_topk=0, dtype="bf16")
     dt = {"bf16": BMOE_BF16, "f32": BMOE_F32, BMOE_BF16: BMOE_BF16, BMOE_F32: BMOE_F32}[dtype]
     return Desc(int(T), int(d), int(E), int(top_k), int(G), int(d_ff), int(d_ff_shared),
                 int(norm_topk), dt)
+
+
+class _W4Struct(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p),
+                ("group", ctypes.c_int32)]
+
+
+class _Matrix(ctypes.Structure):
+    _fields_ = [("w", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p)]
+
+
+class _FewWeights(ctypes.Structure):
+    _fields_ = [("w_router", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("e2g", ctypes.c_void_p),
+                *((n, _Matrix) for n in ("gate", "up", "down", "gate_sh", "up_sh", "down_sh")),
+                ("group", ctypes.c_int32)]
 
 
 _lib = None
@@ -113,6 +133,21 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.brownout_moe_ffn_down_combine.restype = I32
     lib.bmoe_partial_segment_map.argtypes = [P, P, I32, I32, ctypes.c_double, P, P, P, P]
     lib.bmoe_partial_segment_map.restype = I32
+    F32, WP = ctypes.c_float, ctypes.POINTER(_W4Struct)
+    lib.brownout_moe_pre_norm.argtypes = [I32] * 3 + [F32] + [P] * 4
+    lib.brownout_moe_pre_norm.restype = I32
+    lib.brownout_moe_post_norm.argtypes = [I32] * 3 + [F32, I32, F32, I32] + [P] * 8
+    lib.brownout_moe_post_norm.restype = I32
+    lib.brownout_moe_w4_quantize.argtypes = [I32] * 5 + [P] * 5
+    lib.brownout_moe_w4_quantize.restype = I32
+    lib.brownout_moe_w4_matmul.argtypes = [I32] * 5 + [P, P, I32, P, WP, P, P]
+    lib.brownout_moe_w4_matmul.restype = I32
+    lib.brownout_moe_w4_gate_up.argtypes = [I32] * 5 + [P, P, I32, P, WP, WP, P, P]
+    lib.brownout_moe_w4_gate_up.restype = I32
+    lib.brownout_moe_w4_ffn.argtypes = [I32] * 5 + [P, P, I32, P, WP, WP, WP, P, P, P]
+    lib.brownout_moe_w4_ffn.restype = I32
+    lib.brownout_moe_few.argtypes = [DP, ctypes.POINTER(_FewWeights)] + [P] * 7 + [SZ, P]
+    lib.brownout_moe_few.restype = I32
     _lib = lib
     return lib
 
@@ -489,6 +524,219 @@ def ffn_down_combine(desc: Desc, offsets, h, w_down, perm_token, slot_row, slot_
 
 
 # ---------------------------------------------------------------------------
+# decode-side operators: 4-bit weights, the norms around the layer
+
+def _fits(t, name: str, dtype, shape, device: int) -> int:
+    """Data pointer of a contiguous tensor of this type and shape on GPU `device`; raises otherwise."""
+    if not (isinstance(t, torch.Tensor) and t.get_device() == device and t.dtype is dtype and t.shape == shape
+            and t.is_contiguous()):
+        _dev(t, name, dtype, shape)
+        raise ValueError(f"{name} must be on GPU {device}")
+    return t.data_ptr()
+
+
+def _device_of(t, name: str) -> int:
+    """The GPU of a tensor, which has to be the current one (the library launches there)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    device = t.get_device()
+    if device != torch.cuda.current_device():
+        raise ValueError(f"{name} is on GPU {device}, the current GPU is {torch.cuda.current_device()}")
+    return device
+
+
+_DTYPES = {torch.bfloat16: BMOE_BF16, torch.float32: BMOE_F32}
+
+
+def _dtype_of(t) -> int:
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None:
+        raise ValueError(f"unsupported dtype {t.dtype}")
+    return dtype
+
+
+def w4_row_bytes(K: int) -> int:
+    """Bytes of a row of K codes."""
+    return 16 * ((K + 31) // 32)
+
+
+class W4:
+    """A matrix stack [n, N, K] held in 4 bits with group scales:
+    w = scale * (code - zero), by groups of `group` columns.
+
+    codes [n, N, w4_row_bytes(K)] uint8 (byte b of a row: column 2b in the low
+    four bits, 2b+1 in the high four), scales [n, N, ceil(K/group)] bf16, zeros
+    the same shape in uint8, or None (every zero point is 8). The tensors are
+    checked once here; they are kept, not copied."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None, *, K: int,
+                 group: int):
+        if group not in (32, 64, 128):
+            raise ValueError("group must be 32, 64 or 128")
+        if K < 8 or K % 8:
+            raise ValueError("K must be a positive multiple of 8")
+        if not isinstance(codes, torch.Tensor) or codes.dim() != 3:
+            raise ValueError("codes must be [n, N, row bytes]")
+        n, N, _ = codes.shape
+        self.device = _device_of(codes, "codes")
+        ng = -(-K // group)
+        _fits(codes, "codes", torch.uint8, (n, N, w4_row_bytes(K)), self.device)
+        _fits(scales, "scales", torch.bfloat16, (n, N, ng), self.device)
+        if zeros is not None:
+            _fits(zeros, "zeros", torch.uint8, (n, N, ng), self.device)
+        self.codes, self.scales, self.zeros = codes, scales, zeros
+        self.shape, self.group = (n, N, int(K)), int(group)
+        self._struct = _W4Struct(codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(),
+                                 self.group)
+        self._ref = ctypes.byref(self._struct)
+
+    def matrix(self) -> _Matrix:
+        return _Matrix(self._struct.codes, self._struct.scales, self._struct.zeros)
+
+
+def w4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, *, stream=None) -> W4:
+    """w [n, N, K] (bf16 or fp32) rounded to 4 bits; zeros: with a zero point per group."""
+    device = _device_of(w, "w")
+    if w.dim() != 3:
+        raise ValueError("w must be [n, N, K]")
+    n, N, K = w.shape
+    dtype = _dtype_of(w)
+    wp = _fits(w, "w", w.dtype, (n, N, K), device)
+    if group not in (32, 64, 128) or K < 8 or K % 8:
+        raise ValueError("group must be 32, 64 or 128 and K a multiple of 8")
+    ng = -(-K // group)
+    codes = _empty((n, N, w4_row_bytes(K)), torch.uint8, w.device)
+    scales = _empty((n, N, ng), torch.bfloat16, w.device)
+    z = _empty((n, N, ng), torch.uint8, w.device) if zeros else None
+    _check(load_library().brownout_moe_w4_quantize(dtype, n, N, K, int(group), wp, codes.data_ptr(), scales.data_ptr(),
+                                                   None if z is None else z.data_ptr(), _stream(stream)),
+           "brownout_moe_w4_quantize")
+    return W4(codes, scales, z, K=K, group=group)
+
+
+def _w4_rows(offsets, a, a_rows, n: int, K: int, device: int):
+    """Checks the row arguments of a 4-bit product: (rows_cap, offsets, a_rows, a_count, a) as the call takes them."""
+    if not isinstance(a, torch.Tensor) or a.dim() != 2:
+        raise ValueError("a must be [rows, K]")
+    m = a.shape[0]
+    ap = _fits(a, "a", torch.bfloat16, (m, K), device)
+    op = _fits(offsets, "offsets", torch.int32, (n + 1,), device)
+    if a_rows is None:
+        return m, op, None, 0, ap
+    rows = a_rows.numel()
+    if rows and not m:
+        raise ValueError("a_rows names rows of an empty a")
+    return rows, op, _fits(a_rows, "a_rows", torch.int32, (rows,), device), m, ap
+
+
+def _out(t, name, shape, a, device):
+    t = torch.empty(shape, dtype=a.dtype, device=a.device) if t is None else t
+    return t, _fits(t, name, a.dtype, shape, device)
+
+
+def w4_matmul(offsets: torch.Tensor, a: torch.Tensor, w: W4, *, a_rows: Optional[torch.Tensor] = None,
+              y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """y[row] = a[row] W[s]^T for the rows of segment s (offsets [n+1], as in ffn); a_rows as in ffn_gather.
+    bf16 activations. Rows of no segment are left as they are (unspecified in a new y)."""
+    device = _device_of(a, "a")
+    n, N, K = w.shape
+    rows, op, rp, m, ap = _w4_rows(offsets, a, a_rows, n, K, device)
+    y, yp = _out(y, "y", (rows, N), a, device)
+    _check(load_library().brownout_moe_w4_matmul(BMOE_BF16, n, rows, N, K, op, rp, m, ap, w._ref, yp, _stream(stream)),
+           "brownout_moe_w4_matmul")
+    return y
+
+
+def _w4_gated(w_gate: W4, w_up: W4):
+    if w_gate.shape != w_up.shape:
+        raise ValueError(f"w_gate {w_gate.shape} and w_up {w_up.shape} differ")
+    return w_gate.shape
+
+
+def w4_gate_up(offsets: torch.Tensor, a: torch.Tensor, w_gate: W4, w_up: W4, *, a_rows=None, h=None, stream=None):
+    """h[row] = silu(a[row] Wg[s]^T) * (a[row] Wu[s]^T); arguments as w4_matmul."""
+    device = _device_of(a, "a")
+    n, f, d = _w4_gated(w_gate, w_up)
+    rows, op, rp, m, ap = _w4_rows(offsets, a, a_rows, n, d, device)
+    h, hp = _out(h, "h", (rows, f), a, device)
+    _check(load_library().brownout_moe_w4_gate_up(BMOE_BF16, n, rows, d, f, op, rp, m, ap, w_gate._ref, w_up._ref, hp,
+                                                  _stream(stream)), "brownout_moe_w4_gate_up")
+    return h
+
+
+def w4_ffn(offsets: torch.Tensor, a: torch.Tensor, w_gate: W4, w_up: W4, w_down: W4, *, a_rows=None, h=None, y=None,
+           stream=None):
+    """The grouped SwiGLU FFN with 4-bit weights: (y, h); arguments as w4_matmul."""
+    device = _device_of(a, "a")
+    n, f, d = _w4_gated(w_gate, w_up)
+    if w_down.shape != (n, d, f):
+        raise ValueError(f"w_down must be {(n, d, f)}, got {w_down.shape}")
+    rows, op, rp, m, ap = _w4_rows(offsets, a, a_rows, n, d, device)
+    h, hp = _out(h, "h", (rows, f), a, device)
+    y, yp = _out(y, "y", (rows, d), a, device)
+    _check(load_library().brownout_moe_w4_ffn(BMOE_BF16, n, rows, d, f, op, rp, m, ap, w_gate._ref, w_up._ref,
+                                              w_down._ref, hp, yp, _stream(stream)), "brownout_moe_w4_ffn")
+    return y, h
+
+
+def pre_norm(x: torch.Tensor, w: Optional[torch.Tensor] = None, eps: float = 1e-6, *,
+             out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """rms(x) * w over the rows of x [T, d] (w [d], None: ones). out may be x."""
+    device = _device_of(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [T, d]")
+    T, d = shape = x.shape
+    dt, dtype = x.dtype, _dtype_of(x)
+    xp = _fits(x, "x", dt, shape, device)
+    wp = None if w is None else _fits(w, "w", dt, (d,), device)
+    out, op = _out(out, "out", shape, x, device)
+    _check(load_library().brownout_moe_pre_norm(dtype, T, d, eps, xp, wp, op, _stream(stream)), "brownout_moe_pre_norm")
+    return out
+
+
+def _gate_mode(gate: torch.Tensor, T: int, d: int, dt, device: int):
+    """(mode, pointer) of a gate that broadcasts against [T, d]: (d,) per channel, (T, 1) float per token, (T, d)."""
+    shape = tuple(gate.shape)
+    if shape == (d,):
+        return GATE_CHANNEL, _fits(gate, "gate", dt, shape, device)
+    if shape == (T, 1):
+        return GATE_TOKEN, _fits(gate, "gate", torch.float32, shape, device)
+    if shape == (T, d):
+        return GATE_FULL, _fits(gate, "gate", dt, shape, device)
+    raise ValueError(f"gate must be ({d},), ({T}, 1) or ({T}, {d}), got {shape}")
+
+
+def post_norm(y: torch.Tensor, x: torch.Tensor, norm: bool = True, *, w_post: Optional[torch.Tensor] = None,
+              gate: Optional[torch.Tensor] = None, res_scale: float = 1.0, next_norm: bool = False,
+              w_next: Optional[torch.Tensor] = None, eps: float = 1e-6, out: Optional[torch.Tensor] = None,
+              out_next: Optional[torch.Tensor] = None, stream=None):
+    """A block's output y back into the residual stream x (both [T, d]):
+    r = res_scale * x + gate * n, n = rms(y) * w_post (norm) or y; with next_norm also
+    a = rms(r) * w_next, the next block's input, in the same pass. Returns (r, a or None).
+    gate: None, [d], [T, 1] (fp32) or [T, d]. out may be x or y."""
+    device = _device_of(y, "y")
+    if y.dim() != 2:
+        raise ValueError("y must be [T, d]")
+    T, d = shape = y.shape
+    dt, dtype = y.dtype, _dtype_of(y)
+    yp, xp = _fits(y, "y", dt, shape, device), _fits(x, "x", dt, shape, device)
+    if w_post is not None and not norm:
+        raise ValueError("w_post without norm")
+    if not next_norm and (w_next is not None or out_next is not None):
+        raise ValueError("w_next and out_next belong to next_norm")
+    wp = None if w_post is None else _fits(w_post, "w_post", dt, (d,), device)
+    mode, gp = (GATE_NONE, None) if gate is None else _gate_mode(gate, T, d, dt, device)
+    out, rp = _out(out, "out", shape, y, device)
+    np_, ap = None, None
+    if next_norm:
+        np_ = None if w_next is None else _fits(w_next, "w_next", dt, (d,), device)
+        out_next, ap = _out(out_next, "out_next", shape, y, device)
+    _check(load_library().brownout_moe_post_norm(dtype, T, d, eps, 1 if norm else 0, res_scale, mode, yp, xp, wp, gp,
+                                                 rp, np_, ap, _stream(stream)), "brownout_moe_post_norm")
+    return out, out_next
+
+
+# ---------------------------------------------------------------------------
 
 # top_k from which LayerForward takes the fused gather by default
 FUSED_GATHER_MIN_TOP_K = 3
@@ -528,12 +776,35 @@ class LayerForward:
     the stream-K workspace (whole tiles; with a split its last bits could
     differ from the one-stream forward, which splits where the workspace
     allows).
+
+    few_tokens=True (T <= FEW_MAX_TOKENS): a forward is the one call
+    brownout_moe_few, without the permutation and its buffers; route, dispatch,
+    ffn, shared and combine are then not there. The routing is in
+    bufs["route"] as ever. Hidden values are rounded less than on the four-call
+    path, so the outputs differ in their last bits.
+
+    4-bit weights: the FFN matrices (the shared ones too) given as W4 objects,
+    all of one group size and all with or without zero points, bf16 layers. The
+    routed FFN then gathers its rows (fused_gather) and takes no stream-K
+    workspace; fold_combine does not go with them.
     """
 
     def __init__(self, desc: Desc, weights: Dict[str, torch.Tensor], device="cuda", stream_k: bool = True,
-                 fused_gather: Optional[bool] = None, fold_combine: bool = False, concurrent_shared: bool = True):
+                 fused_gather: Optional[bool] = None, fold_combine: bool = False, concurrent_shared: bool = True,
+                 few_tokens: bool = False):
         self.desc = desc
         self.w = weights
+        self.few_tokens = bool(few_tokens)
+        self.w4 = isinstance(weights["w_gate"], W4)
+        if self.w4 or self.few_tokens:
+            if fold_combine or (self.w4 and fused_gather is False):
+                raise ValueError("fold_combine and fused_gather=False do not go with few_tokens or 4-bit weights")
+            self._check_few_and_w4()
+        if self.few_tokens:
+            self._plan_few(device)
+            return
+        if self.w4:
+            fused_gather, stream_k = True, False
         if fused_gather is None:
             # (the gathered copies address x with 32-bit byte offsets)
             x_bytes = desc.T * desc.d * (2 if desc.dtype == BMOE_BF16 else 4)
@@ -571,6 +842,73 @@ class LayerForward:
                 self._side = torch.cuda.Stream(device=device)
         self._plan()
 
+    def _check_few_and_w4(self):
+        """Checks the weights of a few_tokens or 4-bit layer."""
+        desc, w = self.desc, self.w
+        _check(validate(desc), "bmoe_validate")
+        dt, d, E, G = desc.torch_dtype, desc.d, desc.E, desc.G
+        if self.w4 and desc.dtype != BMOE_BF16:
+            raise ValueError("4-bit weights need a bf16 layer")
+        _dev(w["w_router"], "w_router", dt, (E, d))
+        _dev(w["e2g"], "e2g", torch.int32, (E,))
+        if w.get("bias") is not None:
+            _dev(w["bias"], "bias", torch.float32, (E,))
+        shapes = {"w_gate": (G, desc.d_ff, d), "w_up": (G, desc.d_ff, d), "w_down": (G, d, desc.d_ff)}
+        if desc.d_ff_shared:
+            fs = desc.d_ff_shared
+            shapes.update(w_gate_sh=(1, fs, d), w_up_sh=(1, fs, d), w_down_sh=(1, d, fs))
+        for name, shape in shapes.items():
+            if not self.w4:
+                _dev(w[name], name, dt, shape)
+                continue
+            m, first = w[name], w["w_gate"]
+            if not isinstance(m, W4):
+                raise ValueError(f"{name} must be a W4, as w_gate is")
+            if m.shape != shape:
+                raise ValueError(f"{name} must have shape {shape}, got {m.shape}")
+            if m.group != first.group or (m.zeros is None) != (first.zeros is None):
+                raise ValueError(f"{name} must have w_gate's group size, and zero points as it has")
+        self._few_names = tuple(shapes)
+
+    def _plan_few(self, device):
+        """Buffers and the marshalled arguments of a few_tokens layer."""
+        desc, w = self.desc, self.w
+        T, k, d, dt = desc.T, desc.top_k, desc.d, desc.torch_dtype
+        if T > FEW_MAX_TOKENS:
+            raise ValueError(f"few_tokens takes at most {FEW_MAX_TOKENS} tokens, got {T}")
+        self.bufs = {"route": {n: _empty((T, k), t, device) for n, t in
+                               (("topk_idx", torch.int32), ("topk_w", torch.float32),
+                                ("slot_group", torch.int32), ("slot_gate", torch.float32))},
+                     "out": _empty((T, d), dt, device)}
+        self.ws = _empty((max(workspace_bytes(desc, STAGE_FEW), 256),), torch.uint8, device)
+        ptr = lambda t: None if t is None else t.data_ptr()
+        s = _FewWeights(w_router=ptr(w["w_router"]), bias=ptr(w.get("bias")), e2g=ptr(w["e2g"]),
+                        group=w["w_gate"].group if self.w4 else 0)
+        for name in self._few_names:
+            m = w[name]
+            setattr(s, name[2:], m.matrix() if self.w4 else _Matrix(ptr(m), None, None))
+        self._few_weights = s
+        self._lib = load_library()
+        self._xshape, self._dt = (T, d), dt
+        r = self.bufs["route"]
+        self._few_head = (ctypes.byref(desc), ctypes.byref(s))
+        self._few_tail = (*(ptr(r[n]) for n in ("topk_idx", "topk_w", "slot_group", "slot_gate")),
+                          ptr(self.bufs["out"]), ptr(self.ws), self.ws.numel())
+
+        def no_parts(*args, **kwargs):
+            raise ValueError("a few_tokens layer runs as one call: use few or the layer itself")
+        for name in ("route", "dispatch", "ffn", "ffn_gate_up", "ffn_down", "shared", "shared_fork", "shared_join",
+                     "combine", "down_combine"):
+            setattr(self, name, no_parts)
+
+    def few(self, x, stream=None):
+        """The whole layer in one call (few_tokens layers)."""
+        if not self.few_tokens:
+            raise ValueError("few needs a layer made with few_tokens=True")
+        _check(self._lib.brownout_moe_few(*self._few_head, self._x(x), *self._few_tail, self._s(stream)),
+               "brownout_moe_few")
+        return self.bufs["out"]
+
     def _plan(self):
         """Checks every fixed tensor and marshals the fixed arguments of each call."""
         desc, w, b = self.desc, self.w, self.bufs
@@ -581,10 +919,11 @@ class LayerForward:
         _dev(w["e2g"], "e2g", torch.int32, (E,))
         if w.get("bias") is not None:
             _dev(w["bias"], "bias", torch.float32, (E,))
-        _dev(w["w_gate"], "w_gate", dt, (G, f, d))
-        _dev(w["w_up"], "w_up", dt, (G, f, d))
-        _dev(w["w_down"], "w_down", dt, (G, d, f))
-        ptr = lambda t: None if t is None else t.data_ptr()
+        if not self.w4:
+            _dev(w["w_gate"], "w_gate", dt, (G, f, d))
+            _dev(w["w_up"], "w_up", dt, (G, f, d))
+            _dev(w["w_down"], "w_down", dt, (G, d, f))
+        ptr = lambda t: None if t is None else t._ref if isinstance(t, W4) else t.data_ptr()
         wsp, wsn = (ptr(self.ffn_ws), self.ffn_ws.numel()) if self.ffn_ws is not None else (None, 0)
         self._lib = load_library()
         self._desc_ref = ctypes.byref(desc)
@@ -604,6 +943,17 @@ class LayerForward:
                            wsp, wsn)
         self._ffn_args = (dtype, G, rows, d, f, ptr(dp["offsets"]), *a_src, ptr(w["w_gate"]),
                           ptr(w["w_up"]), ptr(w["w_down"]), ptr(b["h"]), ptr(b["y"]), wsp, wsn)
+        lib = self._lib
+        names = ["brownout_moe_ffn", "brownout_moe_ffn_gate_up", "brownout_moe_ffn_down"]
+        if fused:
+            names[:2] = ["brownout_moe_ffn_gather", "brownout_moe_ffn_gate_up_gather"]
+        if self.w4:  # (no workspace; the down product's rows are not gathered)
+            names = ["brownout_moe_w4_ffn", "brownout_moe_w4_gate_up", "brownout_moe_w4_matmul"]
+            self._ffn_args, self._gate_up_args = self._ffn_args[:-2], self._gate_up_args[:-2]
+            self._down_args = (dtype, G, rows, d, f, ptr(dp["offsets"]), None, 0, ptr(b["h"]), ptr(w["w_down"]),
+                               ptr(b["y"]))
+        self._ffn_names = names
+        self._ffn_calls = [getattr(lib, n) for n in names]
         self._a_at = 8 if fused else None  # where x's pointer goes in the fused argument lists
         self._combine_args = (ptr(dp["slot_row"]), ptr(r["slot_gate"]), ptr(b["y"]),
                               ptr(b["y_sh"]) if desc.d_ff_shared else None, ptr(b["out"]))
@@ -612,11 +962,18 @@ class LayerForward:
                                        ptr(dp["perm_token"]), ptr(dp["slot_row"]), ptr(r["slot_gate"]),
                                        ptr(b["y_sh"]) if desc.d_ff_shared else None, ptr(b["out"]),
                                        ptr(self.fold_ws), self.fold_ws.numel())
-        if desc.d_ff_shared:
+        if desc.d_ff_shared and self.w4:
+            fs = desc.d_ff_shared
+            self._shared_name, self._shared_at = "brownout_moe_w4_ffn", 8
+            self._shared_args = (dtype, 1, T, d, fs, ptr(self.sh_offsets), None, 0, ptr(w["w_gate_sh"]),
+                                 ptr(w["w_up_sh"]), ptr(w["w_down_sh"]), ptr(b["h_sh"]), ptr(b["y_sh"]))
+            self._shared_side_args = self._shared_args
+        elif desc.d_ff_shared:
             fs = desc.d_ff_shared
             _dev(w["w_gate_sh"], "w_gate_sh", dt, (1, fs, d))
             _dev(w["w_up_sh"], "w_up_sh", dt, (1, fs, d))
             _dev(w["w_down_sh"], "w_down_sh", dt, (1, d, fs))
+            self._shared_name, self._shared_at = "brownout_moe_ffn", 6
             self._shared_args = (dtype, 1, T, d, fs, ptr(self.sh_offsets), ptr(w["w_gate_sh"]),
                                  ptr(w["w_up_sh"]), ptr(w["w_down_sh"]), ptr(b["h_sh"]), ptr(b["y_sh"]), wsp, wsn)
             # on the side stream without the stream-K workspace, which the
@@ -651,30 +1008,26 @@ class LayerForward:
         return (*args[:i], self._x(x), *args[i:])
 
     def ffn(self, stream=None, x=None):
-        if self.fused_gather:
-            _check(self._lib.brownout_moe_ffn_gather(*self._fused_args(self._ffn_args, x), self._s(stream)),
-                   "brownout_moe_ffn_gather")
-        else:
-            _check(self._lib.brownout_moe_ffn(*self._ffn_args, self._s(stream)), "brownout_moe_ffn")
+        args = self._fused_args(self._ffn_args, x) if self.fused_gather else self._ffn_args
+        _check(self._ffn_calls[0](*args, self._s(stream)), self._ffn_names[0])
         return self.bufs["y"], self.bufs["h"]
 
     def ffn_gate_up(self, stream=None, x=None):
-        if self.fused_gather:
-            _check(self._lib.brownout_moe_ffn_gate_up_gather(*self._fused_args(self._gate_up_args, x),
-                                                             self._s(stream)), "brownout_moe_ffn_gate_up_gather")
-        else:
-            _check(self._lib.brownout_moe_ffn_gate_up(*self._gate_up_args, self._s(stream)),
-                   "brownout_moe_ffn_gate_up")
+        args = self._fused_args(self._gate_up_args, x) if self.fused_gather else self._gate_up_args
+        _check(self._ffn_calls[1](*args, self._s(stream)), self._ffn_names[1])
         return self.bufs["h"]
 
     def ffn_down(self, stream=None):
-        _check(self._lib.brownout_moe_ffn_down(*self._down_args, self._s(stream)), "brownout_moe_ffn_down")
+        _check(self._ffn_calls[2](*self._down_args, self._s(stream)), self._ffn_names[2])
         return self.bufs["y"]
+
+    def _run_shared(self, args, x, stream: int):
+        i = self._shared_at  # where x's pointer goes
+        _check(getattr(self._lib, self._shared_name)(*args[:i], x.data_ptr(), *args[i:], stream), self._shared_name)
 
     def shared(self, x, stream=None):
         self._x(x)  # the shared experts read x in token order: the layer's own input
-        a = self._shared_args
-        _check(self._lib.brownout_moe_ffn(*a[:6], x.data_ptr(), *a[6:], self._s(stream)), "brownout_moe_ffn")
+        self._run_shared(self._shared_args, x, self._s(stream))
         return self.bufs["y_sh"], self.bufs["h_sh"]
 
     def shared_fork(self, x, stream=None):
@@ -688,9 +1041,7 @@ class LayerForward:
             return self.shared(x, stream)
         self._x(x)
         self._side.wait_stream(stream if stream is not None else torch.cuda.current_stream())
-        a = self._shared_side_args
-        _check(self._lib.brownout_moe_ffn(*a[:6], x.data_ptr(), *a[6:], self._side.cuda_stream),
-               "brownout_moe_ffn")
+        self._run_shared(self._shared_side_args, x, self._side.cuda_stream)
         return self.bufs["y_sh"], self.bufs["h_sh"]
 
     def shared_join(self, stream=None):
@@ -710,6 +1061,8 @@ class LayerForward:
         return self.bufs["out"]
 
     def __call__(self, x: torch.Tensor, stream=None) -> torch.Tensor:
+        if self.few_tokens:
+            return self.few(x, stream)
         shared = bool(self.desc.d_ff_shared)
         if shared:
             self.shared_fork(x, stream)
@@ -724,3 +1077,34 @@ class LayerForward:
         if shared:
             self.shared_join(stream)
         return self.combine(stream)
+
+
+class ResidualBlock:
+    """A layer inside its residual block: x -> r = res_scale * x + gate * rms(layer(rms(x) w_pre)) w_post.
+
+    layer: a LayerForward. norms: dict with any of w_pre, w_post, w_next [d] (the layer's dtype; None or
+    missing: ones), gate ([d] or [T, d] in the layer's dtype, or [T, 1] fp32). post_norm False leaves the
+    layer's output unnormalised; next_norm also forms the next block's input a' = rms(r) w_next in the
+    same pass. r and a' are the block's own buffers, rewritten by every call."""
+
+    def __init__(self, layer: LayerForward, norms: Optional[Dict[str, torch.Tensor]] = None, *, eps: float = 1e-6,
+                 res_scale: float = 1.0, post_norm: bool = True, next_norm: bool = False, device="cuda"):
+        norms = dict(norms or {})
+        unknown = set(norms) - {"w_pre", "w_post", "w_next", "gate"}
+        if unknown:
+            raise ValueError(f"unknown norms {sorted(unknown)}")
+        self.layer, self.norms = layer, norms
+        self.eps, self.res_scale, self.norm_y, self.next_norm = float(eps), float(res_scale), post_norm, next_norm
+        desc = layer.desc
+        new = lambda: _empty((desc.T, desc.d), desc.torch_dtype, device)  # noqa: E731
+        self.bufs = {"a": new(), "r": new(), "a_next": new() if next_norm else None}
+
+    def __call__(self, x: torch.Tensor, a: Optional[torch.Tensor] = None, stream=None):
+        """(r, a'): a is this block's normed input where the block before formed it already (its a')."""
+        n, b = self.norms, self.bufs
+        if a is None:
+            a = pre_norm(x, n.get("w_pre"), self.eps, out=b["a"], stream=stream)
+        y = self.layer(a, stream)
+        return post_norm(y, x, self.norm_y, w_post=n.get("w_post"), gate=n.get("gate"), res_scale=self.res_scale,
+                         next_norm=self.next_norm, w_next=n.get("w_next"), eps=self.eps, out=b["r"],
+                         out_next=b["a_next"], stream=stream)

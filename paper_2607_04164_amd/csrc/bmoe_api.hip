@@ -1,6 +1,7 @@
 // Host side of the C ABI: argument checks (host only, before anything is
 // enqueued), workspace sizing, status strings and the four entry points.
 #include <limits.h>
+#include <math.h>
 
 #include "bmoe_common.h"
 
@@ -11,6 +12,37 @@ using namespace bmoe;
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 inline int elem_bytes(int dtype) { return dtype == BMOE_BF16 ? 2 : 4; }
+
+bmoe_status norm_check(int32_t dtype, int32_t T, int32_t d, float eps) {
+    if (dtype != BMOE_F32 && dtype != BMOE_BF16) return BMOE_ERR_UNSUPPORTED;
+    if (T < 0 || d < 8 || d % 8 != 0 || d > BMOE_NORM_MAX_D) return BMOE_ERR_SHAPE;
+    if (!(eps >= 1e-12f && eps <= 1.f)) return BMOE_ERR_SHAPE;
+    return BMOE_OK;
+}
+
+inline bool w4_group_ok(int32_t group) { return group == 32 || group == 64 || group == 128; }
+
+// One grouped product with 4-bit weights [n_seg, N, K] (w1: the second matrix of a gated one, or nullptr)
+bmoe_status w4_check(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t N, int32_t K, const int32_t* offsets,
+                     const int32_t* a_rows, int32_t a_count, const void* a, const bmoe_w4* w0, const bmoe_w4* w1,
+                     const void* c) {
+    if (dtype != BMOE_BF16) return BMOE_ERR_UNSUPPORTED;
+    if (n_seg < 1 || n_seg > BMOE_MAX_EXPERTS || rows_cap < 0) return BMOE_ERR_SHAPE;
+    if (N < 8 || N % 8 != 0 || N > (1 << 20) || K < 8 || K % 8 != 0 || K > (1 << 20)) return BMOE_ERR_SHAPE;
+    if ((int64_t)n_seg * ((N + 15) / 16) > kMaxBlocks256) return BMOE_ERR_SHAPE;
+    if (rows_cap == 0) return BMOE_OK;
+    if (!offsets || !a || !w0 || !c) return BMOE_ERR_NULL;
+    if (a_rows && a_count < 1) return BMOE_ERR_SHAPE;
+    for (const bmoe_w4* w : {w0, w1}) {
+        if (!w) continue;
+        if (!w->codes || !w->scales) return BMOE_ERR_NULL;
+        if (!w4_group_ok(w->group) || w->group != w0->group || (w->zeros != nullptr) != (w0->zeros != nullptr))
+            return BMOE_ERR_UNSUPPORTED;
+        if (!aligned16(w->codes) || ((uintptr_t)w->scales & 1u)) return BMOE_ERR_ALIGN;
+    }
+    if (!aligned16(a) || !aligned16(c)) return BMOE_ERR_ALIGN;
+    return BMOE_OK;
+}
 
 inline bmoe_status hip_status(hipError_t e) { return e == hipSuccess ? BMOE_OK : BMOE_ERR_HIP; }
 
@@ -62,6 +94,8 @@ size_t bmoe_workspace_bytes(const bmoe_desc* d, int32_t stage) {
     if (stage == BMOE_STAGE_DISPATCH) return dispatch_ws_bytes(d->T, d->G);
     if (stage == BMOE_STAGE_FFN && d->dtype == BMOE_BF16) return ffn_workspace_bytes();
     if (stage == BMOE_STAGE_DOWN_COMBINE) return down_combine_ws_bytes(d->T, d->d);
+    if (stage == BMOE_STAGE_FEW && d->T <= BMOE_FEW_MAX_TOKENS)
+        return few_ws_bytes(d->T, d->top_k, d->d_ff, d->d_ff_shared);
     return 0;
 }
 
@@ -286,6 +320,110 @@ bmoe_status brownout_moe_combine(const bmoe_desc* d, const int32_t* slot_row, co
     CombineArgs a{slot_row, slot_gate, y_perm, y_shared, out, d->T, d->top_k, d->d, elem_bytes(d->dtype),
                   (int64_t)d->T * d->top_k};
     return hip_status(launch_combine(a, (hipStream_t)stream));
+}
+
+bmoe_status brownout_moe_pre_norm(int32_t dtype, int32_t T, int32_t d, float eps, const void* x, const void* w,
+                                  void* out, void* stream) {
+    bmoe_status st = norm_check(dtype, T, d, eps);
+    if (st != BMOE_OK || T == 0) return st;
+    if (!x || !out) return BMOE_ERR_NULL;
+    if (!aligned16(x) || !aligned16(out) || !aligned16(w)) return BMOE_ERR_ALIGN;
+    return hip_status(bmoe::launch_pre_norm(bmoe::PreNormArgs{x, w, out, T, d, dtype, eps}, (hipStream_t)stream));
+}
+
+bmoe_status brownout_moe_post_norm(int32_t dtype, int32_t T, int32_t d, float eps, int32_t norm_y, float res_scale,
+                                   int32_t gate_mode, const void* y, const void* x, const void* w_post,
+                                   const void* gate, void* r, const void* w_next, void* a, void* stream) {
+    bmoe_status st = norm_check(dtype, T, d, eps);
+    if (st != BMOE_OK) return st;
+    if (gate_mode < BMOE_GATE_NONE || gate_mode > BMOE_GATE_FULL || (norm_y != 0 && norm_y != 1))
+        return BMOE_ERR_UNSUPPORTED;
+    if (!isfinite(res_scale)) return BMOE_ERR_SHAPE;
+    if (T == 0) return BMOE_OK;
+    if (!y || !x || !r || (gate_mode != BMOE_GATE_NONE && !gate)) return BMOE_ERR_NULL;
+    // what would not be read is not taken; r and a would overwrite each other
+    if ((gate_mode == BMOE_GATE_NONE && gate) || (!norm_y && w_post) || (!a && w_next) || a == r)
+        return BMOE_ERR_UNSUPPORTED;
+    for (const void* p : {y, x, w_post, (const void*)r, w_next, (const void*)a})
+        if (!aligned16(p)) return BMOE_ERR_ALIGN;
+    if (gate && ((uintptr_t)gate & (gate_mode == BMOE_GATE_TOKEN ? 3u : 15u))) return BMOE_ERR_ALIGN;
+    return hip_status(bmoe::launch_post_norm(
+        bmoe::PostNormArgs{y, x, w_post, gate, w_next, r, a, T, d, dtype, norm_y, gate_mode, eps, res_scale},
+        (hipStream_t)stream));
+}
+
+bmoe_status brownout_moe_w4_quantize(int32_t dtype, int32_t n, int32_t N, int32_t K, int32_t group, const void* w,
+                                     uint8_t* codes, void* scales, uint8_t* zeros, void* stream) {
+    if (dtype != BMOE_F32 && dtype != BMOE_BF16) return BMOE_ERR_UNSUPPORTED;
+    if (!w4_group_ok(group)) return BMOE_ERR_UNSUPPORTED;
+    if (n < 1 || n > BMOE_MAX_EXPERTS || N < 1 || N > (1 << 20) || K < 8 || K % 8 != 0 || K > (1 << 20))
+        return BMOE_ERR_SHAPE;
+    if (!w || !codes || !scales) return BMOE_ERR_NULL;
+    if (!aligned16(w) || !aligned16(codes) || ((uintptr_t)scales & 1u)) return BMOE_ERR_ALIGN;
+    return hip_status(bmoe::launch_w4_quantize(
+        bmoe::W4QuantizeArgs{w, codes, scales, zeros, n, N, K, group, dtype}, (hipStream_t)stream));
+}
+
+bmoe_status brownout_moe_w4_matmul(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t N, int32_t K,
+                                   const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,
+                                   const bmoe_w4* w, void* y, void* stream) {
+    bmoe_status st = w4_check(dtype, n_seg, rows_cap, N, K, offsets, a_rows, a_count, a, w, nullptr, y);
+    if (st != BMOE_OK || rows_cap == 0) return st;
+    return hip_status(bmoe::launch_w4_gemm(
+        bmoe::W4GemmArgs{offsets, a_rows, a_count, a, w, nullptr, y, n_seg, rows_cap, N, K}, (hipStream_t)stream));
+}
+
+bmoe_status brownout_moe_w4_gate_up(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t d, int32_t d_ff,
+                                    const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,
+                                    const bmoe_w4* w_gate, const bmoe_w4* w_up, void* h, void* stream) {
+    if (rows_cap > 0 && !w_up) return BMOE_ERR_NULL;
+    bmoe_status st = w4_check(dtype, n_seg, rows_cap, d_ff, d, offsets, a_rows, a_count, a, w_gate, w_up, h);
+    if (st != BMOE_OK || rows_cap == 0) return st;
+    return hip_status(bmoe::launch_w4_gemm(
+        bmoe::W4GemmArgs{offsets, a_rows, a_count, a, w_gate, w_up, h, n_seg, rows_cap, d_ff, d},
+        (hipStream_t)stream));
+}
+
+bmoe_status brownout_moe_w4_ffn(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t d, int32_t d_ff,
+                                const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,
+                                const bmoe_w4* w_gate, const bmoe_w4* w_up, const bmoe_w4* w_down, void* h, void* y,
+                                void* stream) {
+    if (rows_cap > 0 && !w_up) return BMOE_ERR_NULL;
+    bmoe_status st = w4_check(dtype, n_seg, rows_cap, d_ff, d, offsets, a_rows, a_count, a, w_gate, w_up, h);
+    if (st == BMOE_OK) st = w4_check(dtype, n_seg, rows_cap, d, d_ff, offsets, nullptr, 0, h, w_down, nullptr, y);
+    if (st != BMOE_OK || rows_cap == 0) return st;
+    const hipError_t e = bmoe::launch_w4_gemm(
+        bmoe::W4GemmArgs{offsets, a_rows, a_count, a, w_gate, w_up, h, n_seg, rows_cap, d_ff, d}, (hipStream_t)stream);
+    if (e != hipSuccess) return BMOE_ERR_HIP;
+    return hip_status(bmoe::launch_w4_gemm(
+        bmoe::W4GemmArgs{offsets, nullptr, 0, h, w_down, nullptr, y, n_seg, rows_cap, d, d_ff}, (hipStream_t)stream));
+}
+
+bmoe_status brownout_moe_few(const bmoe_desc* d, const bmoe_few_weights* w, const void* x, int32_t* topk_idx,
+                             float* topk_w, int32_t* slot_group, float* slot_gate, void* out, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+    bmoe_status st = bmoe_validate(d);
+    if (st != BMOE_OK) return st;
+    if (!w) return BMOE_ERR_NULL;
+    if (d->T > BMOE_FEW_MAX_TOKENS || !few_grid_fits(d->T, d->top_k, d->G, d->d_ff, d->d_ff_shared))
+        return BMOE_ERR_SHAPE;
+    if (w->group != 0 && (!w4_group_ok(w->group) || d->dtype != BMOE_BF16)) return BMOE_ERR_UNSUPPORTED;
+    if (d->T == 0) return BMOE_OK;
+    if (!w->w_router || !w->e2g || !x || !topk_idx || !topk_w || !slot_group || !slot_gate || !out) return BMOE_ERR_NULL;
+    if (!aligned16(x) || !aligned16(w->w_router) || !aligned16(out)) return BMOE_ERR_ALIGN;
+    const bmoe_matrix* m[6] = {&w->gate, &w->up, &w->down, &w->gate_sh, &w->up_sh, &w->down_sh};
+    const int used = d->d_ff_shared > 0 ? 6 : 3;
+    for (int i = 0; i < used; ++i) {
+        if (!m[i]->w || (w->group != 0 && !m[i]->scales)) return BMOE_ERR_NULL;
+        if (!aligned16(m[i]->w) || ((uintptr_t)m[i]->scales & 1u)) return BMOE_ERR_ALIGN;
+        if (w->group == 0 ? (m[i]->scales || m[i]->zeros) : ((m[i]->zeros != nullptr) != (m[0]->zeros != nullptr)))
+            return BMOE_ERR_UNSUPPORTED;
+    }
+    if (!workspace || workspace_bytes < few_ws_bytes(d->T, d->top_k, d->d_ff, d->d_ff_shared)) return BMOE_ERR_WORKSPACE;
+    if ((uintptr_t)workspace & 255u) return BMOE_ERR_ALIGN;
+    bmoe::FewArgs a{*w, x, topk_idx, topk_w, slot_group, slot_gate, out, workspace,
+                    d->T, d->d, d->E, d->top_k, d->G, d->d_ff, d->d_ff_shared, d->norm_topk, d->dtype};
+    return hip_status(bmoe::launch_few(a, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -254,4 +254,62 @@ struct CombineArgs {
 };
 hipError_t launch_combine(const CombineArgs& a, hipStream_t s);
 
+struct PreNormArgs {
+    const void *x, *w;
+    void* out;
+    int T, d, dtype;
+    float eps;
+};
+hipError_t launch_pre_norm(const PreNormArgs& a, hipStream_t s);
+
+struct PostNormArgs {
+    const void *y, *x, *w_post, *gate, *w_next;
+    void *r, *a;
+    int T, d, dtype, norm_y, gate_mode;
+    float eps, res_scale;
+};
+hipError_t launch_post_norm(const PostNormArgs& a, hipStream_t s);
+
+struct W4QuantizeArgs {
+    const void* w;
+    uint8_t* codes;
+    void* scales;
+    uint8_t* zeros;  // or nullptr
+    int n, N, K, group, dtype;
+};
+hipError_t launch_w4_quantize(const W4QuantizeArgs& a, hipStream_t s);
+
+// workgroups of 256 threads that one launch can hold (its threads are counted in 32 bits)
+constexpr int64_t kMaxBlocks256 = ((int64_t)1 << 24) - 1;
+
+// c[row] = a[row] W^T, or silu(a Wg^T) * (a Wu^T) with w1
+struct W4GemmArgs {
+    const int32_t* offsets;
+    const int32_t* a_rows;  // or nullptr
+    int a_count;
+    const void* a;
+    const bmoe_w4* w0;
+    const bmoe_w4* w1;  // or nullptr
+    void* c;
+    int n_seg, rows_cap, N, K;
+};
+hipError_t launch_w4_gemm(const W4GemmArgs& a, hipStream_t s);
+
+struct FewArgs {
+    bmoe_few_weights w;
+    const void* x;
+    int32_t* topk_idx;
+    float* topk_w;
+    int32_t* slot_group;
+    float* slot_gate;
+    void* out;
+    void* ws;
+    int T, d, E, k, G, f, fs, norm, dtype;
+};
+// hidden values of the slots and of the shared experts
+size_t few_ws_bytes(int T, int k, int f, int fs);
+// whether one launch holds a workgroup per 16 hidden columns of every segment that can be reached
+bool few_grid_fits(int T, int k, int G, int f, int fs);
+hipError_t launch_few(const FewArgs& a, hipStream_t s);
+
 }  // namespace bmoe

@@ -1,0 +1,213 @@
+"""Products with 4-bit weights and the quantizer, against 64 bits."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import decode_ref as R
+from paper_2607_04164_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.load_library()
+
+
+def _w4(t, K, group):
+    return B.W4(t[0].cuda(), t[1].cuda(), None if t[2] is None else t[2].cuda(), K=K, group=group)
+
+
+def _sum_error(K, group):
+    """Rounding of one output's sums, relative to the sum of its terms' magnitudes (w4_magnitude): a group's
+    chain of additions, then the groups', each step at most 2^-23."""
+    return (group + -(-K // group) + 8) * 2.0 ** -23
+
+
+def _segments(rng, rows, n, first=0):
+    cut = np.sort(rng.integers(0, rows + 1, n - 1))
+    return np.concatenate([[0], cut, [rows]]).astype(np.int32) + first
+
+
+def _check(y, want, err, rows, what):
+    got = R.np64(y)[rows]
+    assert np.isfinite(got).all(), what
+    tol = R.HALF["bf16"] * (np.abs(want) + err) + err
+    assert (np.abs(got - want) <= tol).all(), f"{what}: {float((np.abs(got - want) / np.maximum(tol, 1e-300)).max())}"
+    # the sums are far below the one rounding: over all values the error is that of a rounding (at most half a step)
+    if want.size and np.linalg.norm(want):
+        assert np.linalg.norm(got - want) <= R.HALF["bf16"] * np.linalg.norm(want), what
+
+
+# rows a tile and a pass of 64 end in, K that ends inside a chunk, a group and 32 columns, N inside a tile
+CASES = [(1, 1, 8, 8), (1, 1, 4096, 1408), (1, 17, 24, 264), (1, 65, 72, 136), (3, 7, 40, 128), (5, 130, 16, 1408),
+         (8, 64, 256, 2048), (4, 300, 56, 40), (60, 48, 176, 352)]
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros", [False, True], ids=["sym", "zeros"])
+@pytest.mark.parametrize("n,rows,N,K", CASES)
+def test_w4_matmul(n, rows, N, K, group, zeros):
+    rng = np.random.default_rng(n * 1000 + rows + K)
+    t = R.w4_random(rng, n, N, K, group, zeros)
+    offs = _segments(rng, rows, n) if n > 1 else np.array([0, rows], np.int32)
+    m = rows // 3 + 1
+    a = R.rand(rng, (m, K), 1.0, "bf16")
+    src = rng.integers(0, m, rows).astype(np.int32)
+    w64, mag, a64 = R.w4_values(*t, K, group), R.w4_magnitude(*t, K, group), R.np64(a)[src]
+    w = _w4(t, K, group)
+    gathered = B.w4_matmul(torch.from_numpy(offs).cuda(), a.cuda(), w, a_rows=torch.from_numpy(src).cuda())
+    plain = B.w4_matmul(torch.from_numpy(offs).cuda(), a[src.astype(np.int64)].contiguous().cuda(), w)
+    assert torch.equal(gathered, plain)
+    for s in range(n):
+        sl = slice(offs[s], offs[s + 1])
+        err = _sum_error(K, group) * np.abs(a64[sl]) @ mag[s].T
+        _check(gathered, a64[sl] @ w64[s].T, err, sl, f"segment {s}")
+
+
+@pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True)])
+@pytest.mark.parametrize("n,rows,f,d", [(1, 1, 24, 40), (1, 1, 1408, 2048), (4, 33, 200, 264), (8, 250, 72, 1408)])
+def test_w4_ffn(n, rows, f, d, group, zeros):
+    rng = np.random.default_rng(rows + f)
+    tg, tu = (R.w4_random(rng, n, f, d, group, zeros) for _ in range(2))
+    td = R.w4_random(rng, n, d, f, group, zeros)
+    offs = _segments(rng, rows, n) if n > 1 else np.array([0, rows], np.int32)
+    a = R.rand(rng, (rows, d), 1.0, "bf16")
+    wg, wu, wd = _w4(tg, d, group), _w4(tu, d, group), _w4(td, f, group)
+    o = torch.from_numpy(offs).cuda()
+    y, h = B.w4_ffn(o, a.cuda(), wg, wu, wd)
+    assert torch.equal(h, B.w4_gate_up(o, a.cuda(), wg, wu))
+    a64, h64 = R.np64(a), R.np64(h)
+    e = _sum_error(d, group)
+    for s in range(n):
+        sl = slice(offs[s], offs[s + 1])
+        g, u = a64[sl] @ R.w4_values(*tg, d, group)[s].T, a64[sl] @ R.w4_values(*tu, d, group)[s].T
+        eg = e * np.abs(a64[sl]) @ R.w4_magnitude(*tg, d, group)[s].T
+        eu = e * np.abs(a64[sl]) @ R.w4_magnitude(*tu, d, group)[s].T
+        want = R.silu(g) * u
+        # |silu'| <= 1.1; exp, reciprocal and products of silu within 2^-20
+        err = 1.1 * np.abs(u) * eg + (np.abs(R.silu(g)) + 1.1 * eg) * eu + 2.0 ** -20 * np.abs(want)
+        _check(h, want, err, sl, f"h of segment {s}")
+        # y from the h that the call stored
+        _check(y, h64[sl] @ R.w4_values(*td, f, group)[s].T,
+               _sum_error(f, group) * np.abs(h64[sl]) @ R.w4_magnitude(*td, f, group)[s].T, sl, f"y of segment {s}")
+
+
+def test_rows_of_no_segment_stay_as_they_are():
+    rng = np.random.default_rng(2)
+    n, N, K, rows = 3, 40, 160, 90
+    t = R.w4_random(rng, n, N, K, 32, True)
+    a = R.rand(rng, (rows, K), 1.0, "bf16").cuda()
+    y = torch.full((rows, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.w4_matmul(torch.tensor([5, 20, 20, 61], dtype=torch.int32, device="cuda"), a, _w4(t, K, 32), y=y)
+    assert bool((y[:5] == 7).all()) and bool((y[61:] == 7).all())
+    w64 = R.w4_values(*t, K, 32)
+    np.testing.assert_allclose(R.np64(y)[20:61], R.np64(a)[20:61] @ w64[2].T, rtol=0.01, atol=0.01)
+    # offsets past the capacity or out of order touch nothing outside, and empty calls nothing at all
+    y.fill_(7.0)
+    B.w4_matmul(torch.tensor([90, 90, 90, 500], dtype=torch.int32, device="cuda"), a, _w4(t, K, 32), y=y)
+    assert bool((y == 7).all())
+    assert B.w4_matmul(torch.zeros(4, dtype=torch.int32, device="cuda"), a[:0], _w4(t, K, 32)).shape == (0, N)
+
+
+def test_source_rows_out_of_range_are_clamped():
+    rng = np.random.default_rng(4)
+    t = R.w4_random(rng, 1, 32, 64, 64, False)
+    a = R.rand(rng, (4, 64), 1.0, "bf16").cuda()
+    rows = torch.tensor([-5, 0, 3, 1000], dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+    y = B.w4_matmul(off, a, _w4(t, 64, 64), a_rows=rows)
+    want = B.w4_matmul(off, a, _w4(t, 64, 64), a_rows=rows.clamp(0, 3))
+    assert torch.equal(y, want)
+
+
+def test_extreme_codes_scales_and_zeros():
+    """All codes 0 and 15, scale 0 and large, zero points past the codes; one hot activation row."""
+    K, N, group = 256, 16, 64
+    codes = torch.zeros((1, N, 128), dtype=torch.uint8)
+    codes[:, 1::2] = 0xFF
+    scales = torch.tensor([0.0, 1.0, -2.0, 1e30]).to(torch.bfloat16).repeat(1, N, 1)
+    zeros = torch.tensor([3, 0, 15, 255], dtype=torch.uint8).repeat(1, N, 1)
+    a = torch.zeros((5, K), dtype=torch.bfloat16)
+    for i, k in enumerate((0, 63, 64, 191, 255)):
+        a[i, k] = 1.0
+    y = B.w4_matmul(torch.tensor([0, 5], dtype=torch.int32, device="cuda"), a.cuda(),
+                    _w4((codes, scales, zeros), K, group))
+    want = R.np64(a) @ R.w4_values(codes, scales, zeros, K, group)[0].T
+    np.testing.assert_allclose(R.np64(y), want, rtol=2.0 ** -8)
+
+
+def quantize_ref(w32, group, zeros):
+    """The quantizer's definition, element by element in fp32."""
+    n, N, K = w32.shape
+    ng, pitch = -(-K // group), 16 * (-(-K // 32))
+    codes = np.full((n, N, 2 * pitch), 8, np.int64)
+    scales, zps = np.zeros((n, N, ng), np.float32), np.zeros((n, N, ng), np.uint8)
+    for g in range(ng):
+        v = w32[:, :, g * group:min(K, (g + 1) * group)]
+        lo, hi = np.minimum(v.min(-1), 0), np.maximum(v.max(-1), 0)
+        s = ((hi - lo) / np.float32(15) if zeros else np.maximum(hi, -lo) / np.float32(7)).astype(np.float32)
+        s = torch.from_numpy(s).to(torch.bfloat16).float().numpy()
+        safe = np.where(s > 0, s, np.float32(1))
+        z = np.clip(np.rint(-lo / safe), 0, 15) if zeros else np.full(s.shape, 8.0)
+        if zeros:
+            z = np.where(s > 0, z, 0)
+        q = np.where(s[..., None] > 0, np.rint(v / safe[..., None]), 0) + z[..., None]
+        codes[:, :, g * group:g * group + v.shape[-1]] = np.clip(q, 0 if zeros else 1, 15)
+        scales[:, :, g], zps[:, :, g] = s, z
+    packed = (codes[:, :, 0::2] | (codes[:, :, 1::2] << 4)).astype(np.uint8)
+    return packed, scales, zps
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("zeros", [False, True], ids=["sym", "zeros"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("n,N,K", [(1, 3, 8), (2, 5, 40), (1, 16, 256), (3, 7, 1408)])
+def test_w4_quantize(n, N, K, group, zeros, dtype):
+    rng = np.random.default_rng(K + group)
+    w = R.rand(rng, (n, N, K), 0.02, dtype)
+    w[0, 0, :] = 0  # groups of zeros
+    w[0, N - 1] = w[0, N - 1].abs()  # one-sided groups
+    q = B.w4_quantize(w.cuda(), group, zeros)
+    codes, scales, zps = quantize_ref(w.float().numpy(), group, zeros)
+    assert np.array_equal(q.codes.cpu().numpy(), codes)
+    assert np.array_equal(q.scales.float().cpu().numpy(), scales)
+    if zeros:
+        assert np.array_equal(q.zeros.cpu().numpy(), zps)
+    else:
+        assert q.zeros is None
+    # a code is at most half a step off (the bf16 scale moves the ends by 2^-8 of 7 or 15 steps)
+    back = R.w4_values(q.codes, q.scales, q.zeros, K, group)
+    step = np.repeat(scales.astype(np.float64), group, axis=2)[:, :, :K]
+    assert (np.abs(back - R.np64(w)) <= (0.5 + (1.0 if zeros else 0.0) * 0.5 + 15 * 2.0 ** -8) * step + 1e-30).all()
+
+
+def test_w4_graph_and_stream():
+    rng = np.random.default_rng(9)
+    n, rows, f, d = 4, 40, 96, 256
+    tg, tu, td = (R.w4_random(rng, n, *s, 64, True) for s in ((f, d), (f, d), (d, f)))
+    ws = _w4(tg, d, 64), _w4(tu, d, 64), _w4(td, f, 64)
+    o = torch.from_numpy(_segments(rng, rows, n)).cuda()
+    a = R.rand(rng, (rows, d), 1.0, "bf16").cuda()
+    y, h = B.w4_ffn(o, a, *ws)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    y1, h1 = torch.zeros_like(y), torch.zeros_like(h)
+    B.w4_ffn(o, a, *ws, y=y1, h=h1, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(y, y1) and torch.equal(h, h1)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.w4_ffn(o, a, *ws, y=y1, h=h1)
+    for k in range(3):
+        a.copy_(R.rand(rng, (rows, d), 1.0, "bf16"))
+        want = B.w4_ffn(o, a, *ws)
+        y1.zero_(), h1.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y1, want[0]) and torch.equal(h1, want[1]), f"replay {k}"
