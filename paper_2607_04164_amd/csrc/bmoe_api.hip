@@ -95,7 +95,7 @@ size_t bmoe_workspace_bytes(const bmoe_desc* d, int32_t stage) {
     if (stage == BMOE_STAGE_FFN && d->dtype == BMOE_BF16) return ffn_workspace_bytes();
     if (stage == BMOE_STAGE_DOWN_COMBINE) return down_combine_ws_bytes(d->T, d->d);
     if (stage == BMOE_STAGE_FEW && d->T <= BMOE_FEW_MAX_TOKENS)
-        return few_ws_bytes(d->T, d->top_k, d->d_ff, d->d_ff_shared);
+        return few_ws_bytes(d->T, d->E, d->top_k, d->d, d->d_ff, d->d_ff_shared);
     return 0;
 }
 
@@ -405,8 +405,7 @@ bmoe_status brownout_moe_few(const bmoe_desc* d, const bmoe_few_weights* w, cons
     bmoe_status st = bmoe_validate(d);
     if (st != BMOE_OK) return st;
     if (!w) return BMOE_ERR_NULL;
-    if (d->T > BMOE_FEW_MAX_TOKENS || !few_grid_fits(d->T, d->top_k, d->G, d->d_ff, d->d_ff_shared))
-        return BMOE_ERR_SHAPE;
+    if (d->T > BMOE_FEW_MAX_TOKENS) return BMOE_ERR_SHAPE;
     if (w->group != 0 && (!w4_group_ok(w->group) || d->dtype != BMOE_BF16)) return BMOE_ERR_UNSUPPORTED;
     if (d->T == 0) return BMOE_OK;
     if (!w->w_router || !w->e2g || !x || !topk_idx || !topk_w || !slot_group || !slot_gate || !out) return BMOE_ERR_NULL;
@@ -419,7 +418,7 @@ bmoe_status brownout_moe_few(const bmoe_desc* d, const bmoe_few_weights* w, cons
         if (w->group == 0 ? (m[i]->scales || m[i]->zeros) : ((m[i]->zeros != nullptr) != (m[0]->zeros != nullptr)))
             return BMOE_ERR_UNSUPPORTED;
     }
-    if (!workspace || workspace_bytes < few_ws_bytes(d->T, d->top_k, d->d_ff, d->d_ff_shared)) return BMOE_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < few_ws_bytes(d->T, d->E, d->top_k, d->d, d->d_ff, d->d_ff_shared)) return BMOE_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 255u) return BMOE_ERR_ALIGN;
     bmoe::FewArgs a{*w, x, topk_idx, topk_w, slot_group, slot_gate, out, workspace,
                     d->T, d->d, d->E, d->top_k, d->G, d->d_ff, d->d_ff_shared, d->norm_topk, d->dtype};

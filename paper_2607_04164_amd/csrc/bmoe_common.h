@@ -306,10 +306,8 @@ struct FewArgs {
     void* ws;
     int T, d, E, k, G, f, fs, norm, dtype;
 };
-// hidden values of the slots and of the shared experts
-size_t few_ws_bytes(int T, int k, int f, int fs);
-// whether one launch holds a workgroup per 16 hidden columns of every segment that can be reached
-bool few_grid_fits(int T, int k, int G, int f, int fs);
+// gate logits, counters and partial sums, hidden values of the slots and of the shared experts
+size_t few_ws_bytes(int T, int E, int k, int d, int f, int fs);
 hipError_t launch_few(const FewArgs& a, hipStream_t s);
 
 }  // namespace bmoe

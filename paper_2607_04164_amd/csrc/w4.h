@@ -52,33 +52,82 @@ __device__ __forceinline__ f32x4 mfma16(v4u a, v4u b, f32x4 c) {
                                                    0, 0);
 }
 
-// One matrix stack and the sizes that address it.
+// One matrix stack.
 struct W4Stack {
     const uint8_t* codes;
     const uint16_t* scales;
-    const uint8_t* zeros;  // or nullptr
+    const uint8_t* zeros;  // where there are none: any memory that can be read like them
+    int64_t groups;        // of all rows
+    int has_zeros;
 };
 
-// A chunk of one lane's W row: 128 columns' codes (the lane's 32 of them) and the chunk's groups.
+inline W4Stack w4_stack(const void* codes, const void* scales, const uint8_t* zeros, int64_t rows, int K, int group) {
+    return W4Stack{(const uint8_t*)codes, (const uint16_t*)scales, zeros ? zeros : (const uint8_t*)scales,
+                   rows * ceil_div(K, group), zeros != nullptr};
+}
+
+// the unsigned integer of N bytes
+template <int N>
+struct UintOf;
+template <>
+struct UintOf<1> { typedef uint8_t type; };
+template <>
+struct UintOf<2> { typedef uint16_t type; };
+template <>
+struct UintOf<4> { typedef uint32_t type; };
+template <>
+struct UintOf<8> { typedef uint64_t type; };
+
+// 16 bytes at a 32-bit offset from an address that the whole wave shares
+__device__ __forceinline__ v4u load_at(const void* base, uint32_t off) {
+    return *(const v4u*)((const char*)base + off);
+}
+
+// 16 rows of a stack (fewer at its end), from row `first` on
+template <int GROUP>
+struct W4Rows {
+    static constexpr int NG = kW4Chunk / GROUP;
+    const uint8_t* codes;
+    const uint16_t* scales;
+    const uint8_t* zeros;
+    int last;  // the place of the stack's last NG groups, from the first row's first
+    __device__ __forceinline__ W4Rows(const W4Stack& w, int64_t first, int K) {
+        const int64_t j = first * ceil_div(K, GROUP);
+        codes = w.codes + first * BMOE_W4_ROW_BYTES(K);
+        scales = w.scales + j;
+        zeros = w.zeros + j;
+        last = (int)(w.groups - NG - j < 0x7fffffff ? w.groups - NG - j : 0x7fffffff);
+    }
+};
+
+// A chunk of one lane's W row: 128 columns' codes (the lane's 32 of them) and the
+// chunk's groups, in one load each and without a branch (zeros are loaded where
+// there are none too). Rows of groups have any alignment.
 template <int GROUP>
 struct W4Chunk {
     static constexpr int NG = kW4Chunk / GROUP;
     v4u codes;
-    uint16_t s[NG];
-    uint8_t z[NG];
+    typename UintOf<2 * NG>::type s;
+    typename UintOf<NG>::type z;
 
-    // chunk c of matrix row `row` (of all rows of the stack); K columns
-    __device__ __forceinline__ void load(const W4Stack& w, size_t row, int c, int K, int q) {
+    // chunk c of row r of the rows; K columns
+    __device__ __forceinline__ void load(const W4Rows<GROUP>& w, int r, int c, int K, int q) {
         const int pitch = BMOE_W4_ROW_BYTES(K), ng = ceil_div(K, GROUP);
-        const int at = 64 * c + 16 * q;
-        codes = *(const v4u*)(w.codes + row * pitch + (at < pitch ? at : 0));
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            // (groups past the last one: their activations are zero)
-            const size_t j = row * ng + min(c * NG + g, ng - 1);
-            s[g] = w.scales[j];
-            z[g] = w.zeros ? w.zeros[j] : (uint8_t)8;
+        codes = load_at(w.codes, (uint32_t)(r * pitch + min(64 * c + 16 * q, pitch - 16)));
+        // groups past the row's last one are another row's, or 0 past the stack's
+        // end (a stack has at least 8 rows): their activations are zero
+        const int j = r * ng + c * NG, from = min(j, w.last);
+        __builtin_memcpy(&s, (const char*)w.scales + (uint32_t)(from * 2), sizeof s);
+        __builtin_memcpy(&z, w.zeros + (uint32_t)from, sizeof z);
+        if constexpr (NG > 1) {
+            s = (decltype(s))(s >> (16 * (j - from)));
+            z = (decltype(z))(z >> (8 * (j - from)));
         }
+    }
+    __device__ __forceinline__ float scale(int g) const { return bf16_to_f32((uint16_t)(s >> (16 * g))); }
+    // 16 + the zero point of group g
+    __device__ __forceinline__ float offset(bool has_zeros, int g) const {
+        return has_zeros ? 16.f + (float)(uint8_t)(z >> (8 * g)) : 24.f;
     }
 };
 

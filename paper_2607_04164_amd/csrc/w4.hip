@@ -38,7 +38,8 @@ __global__ __launch_bounds__(kW4Threads, 2) void w4_gemm_kernel(W4Params p) {
     const int beg = min(max(p.offsets[s], 0), p.rows_cap);
     const int end = min(max(p.offsets[s + 1], beg), p.rows_cap);
     if (end <= beg) return;
-    const size_t wrow = (size_t)s * N + min(n0 + r16, N - 1);
+    const W4Rows<GROUP> rows0(p.w[0], (int64_t)s * N + n0, K), rows1(p.w[NMAT - 1], (int64_t)s * N + n0, K);
+    const int wrow = min(r16, N - 1 - n0);
     const int nch = ceil_div(K, kW4Chunk);
     const v4u ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 
@@ -58,7 +59,7 @@ __global__ __launch_bounds__(kW4Threads, 2) void w4_gemm_kernel(W4Params p) {
         for (int c = wave; c < nch; c += kW4Waves) {
             W4Chunk<GROUP> w[NMAT];
 #pragma unroll
-            for (int m = 0; m < NMAT; ++m) w[m].load(p.w[m], wrow, c, K, q);
+            for (int m = 0; m < NMAT; ++m) w[m].load(m ? rows1 : rows0, wrow, c, K, q);
 #pragma unroll
             for (int m = 0; m < NMAT; ++m) w[m].codes = w4_transpose(w[m].codes);
 #pragma unroll
@@ -80,7 +81,7 @@ __global__ __launch_bounds__(kW4Threads, 2) void w4_gemm_kernel(W4Params p) {
                     }
 #pragma unroll
                     for (int m = 0; m < NMAT; ++m) {
-                        const float sc = bf16_to_f32(w[m].s[g]), off = 16.f + (float)w[m].z[g];
+                        const float sc = w[m].scale(g), off = w[m].offset(p.w[0].has_zeros, g);
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             tot[m][nt][i] = fmaf(sc, fmaf(-off, xs[i], acc[m][i]), tot[m][nt][i]);
@@ -195,8 +196,6 @@ hipError_t launch_w4(const W4Params& p, int group, hipStream_t s) {
     return hipGetLastError();
 }
 
-W4Stack stack_of(const bmoe_w4* w) { return w ? W4Stack{w->codes, (const uint16_t*)w->scales, w->zeros} : W4Stack{}; }
-
 }  // namespace
 
 hipError_t launch_w4_quantize(const W4QuantizeArgs& a, hipStream_t s) {
@@ -213,7 +212,10 @@ hipError_t launch_w4_quantize(const W4QuantizeArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_w4_gemm(const W4GemmArgs& a, hipStream_t s) {
-    W4Params p{(const uint16_t*)a.a, {stack_of(a.w0), stack_of(a.w1)}, (uint16_t*)a.c, a.offsets, a.a_rows, a.a_count,
+    auto stack = [&](const bmoe_w4* w) {
+        return w ? w4_stack(w->codes, w->scales, w->zeros, (int64_t)a.n_seg * a.N, a.K, w->group) : W4Stack{};
+    };
+    W4Params p{(const uint16_t*)a.a, {stack(a.w0), stack(a.w1)}, (uint16_t*)a.c, a.offsets, a.a_rows, a.a_count,
                a.n_seg, a.rows_cap, a.N, a.K};
     return a.w1 ? launch_w4<true>(p, a.w0->group, s) : launch_w4<false>(p, a.w0->group, s);
 }
