@@ -463,7 +463,7 @@ BMOE_API bmoe_status brownout_moe_w4_quantize(int32_t dtype, int32_t n, int32_t 
 
 /*
  * Grouped products with 4-bit weights, for few rows per segment (each pass over
- * a segment's weights serves up to 64 of its rows). dtype: BMOE_BF16 (the
+ * a segment's weights serves up to 32 of its rows). dtype: BMOE_BF16 (the
  * activations' and outputs'; others are BMOE_ERR_UNSUPPORTED). Segments as in
  * brownout_moe_ffn: segment s covers rows offsets[s] .. offsets[s+1]-1; rows of
  * no segment are left as they are. a_rows as in brownout_moe_ffn_gather, or NULL

@@ -279,8 +279,8 @@ struct W4QuantizeArgs {
 };
 hipError_t launch_w4_quantize(const W4QuantizeArgs& a, hipStream_t s);
 
-// workgroups of 256 threads that one launch can hold (its threads are counted in 32 bits)
-constexpr int64_t kMaxBlocks256 = ((int64_t)1 << 24) - 1;
+// workgroups of 512 threads that one launch can hold (its threads are counted in 32 bits)
+constexpr int64_t kMaxBlocks512 = ((int64_t)1 << 23) - 1;
 
 // c[row] = a[row] W^T, or silu(a Wg^T) * (a Wu^T) with w1
 struct W4GemmArgs {
@@ -309,5 +309,8 @@ struct FewArgs {
 // gate logits, counters and partial sums, hidden values of the slots and of the shared experts
 size_t few_ws_bytes(int T, int E, int k, int d, int f, int fs);
 hipError_t launch_few(const FewArgs& a, hipStream_t s);
+hipError_t launch_few_w4(const FewArgs& a, hipStream_t s);
+// logits to the start of a.ws; clears the counters of the down kernel
+hipError_t launch_few_logits(const FewArgs& a, int32_t* done, hipStream_t s);
 
 }  // namespace bmoe

@@ -1,0 +1,816 @@
+// The whole layer for at most 16 tokens (Sec. 2.1 with the map of Eq. 2).
+//
+// With so few tokens all of them fit one MFMA tile, so nothing is permuted: a
+// reached segment's weights are multiplied with every token, and a token that
+// does not call the segment is left out where its hidden values would be stored.
+//   few_logits_kernel  one workgroup per expert (and four tokens): the gate logits
+//                      in float64 (bf16 and fp32 products are exact there), so
+//                      near ties need no second look;
+//   few_up_kernel      items of 16 hidden columns of a reached segment (or of the
+//                      shared experts), dealt out to the workgroups. Every
+//                      workgroup selects the top-k from the logits by itself, which
+//                      costs less than another launch: silu(Wg x) * (Wu x), times
+//                      the token's gate of that segment, to the workspace;
+//   few_down_kernel    16 output columns a workgroup: the sum over the reached
+//                      segments and their hidden columns is one long K, so the
+//                      gate-weighted sum over experts falls out of it. K is split
+//                      over several workgroups where the columns alone are too few
+//                      for the chip; the last one to finish adds the parts in order.
+// The last two are bound by reading the weights. A workgroup's waves split K; each
+// wave reads units of the weight rows into one register buffer while it multiplies
+// the other. Their partial tiles are added through LDS in wave order. The tokens
+// are the A operand, the weight rows the B operand: D[token 4q+i][weight row r16] in
+// element i of lane (r16, q). Rows of the A operand past the last token (or of
+// tokens that do not call the segment) hold what is at hand: a row of D depends on
+// its own row of A alone, and theirs are not used.
+// A unit is the columns that a wave takes at once, UK of them: 64 of bf16 and 32
+// of fp32 weights, 256 of 4-bit ones (see w4.h): a 128-byte line of each row.
+// Hidden values of bf16 layers are kept as the sum of two bf16 (16 bits of
+// significand) and multiplied as such, since the matrix cores idle here anyway;
+// so the layer's output is rounded once. Up to eight tokens have their high parts
+// in rows 0..7 of the A operand and their low parts in rows 8..15.
+#pragma once
+
+#include <math.h>
+
+#include "bmoe_common.h"
+#include "route_select.h"
+#include "w4.h"
+
+namespace bmoe {
+namespace {
+
+constexpr int kFewTok = BMOE_FEW_MAX_TOKENS;
+constexpr int kFewCols = 16;
+constexpr int kLogitThreads = 256, kUpThreads = 512, kDownThreads = 256;
+constexpr int kUpWgsPerCu = 2, kDownWgsPerCu = 3;  // by their registers
+constexpr int kSplitMax = 8;     // workgroups that share 16 output columns
+constexpr int kLogitTokens = 4;  // tokens of a few_logits_kernel workgroup
+constexpr int kMaxSlots = kFewTok * BMOE_MAX_TOPK;
+static_assert(kFewTok == 16, "one MFMA tile of tokens");
+constexpr int kTile = kFewTok * kFewCols;  // outputs of a tile, a thread each
+static_assert(kMaxSlots <= kTile && BMOE_MAX_EXPERTS <= kTile, "a thread per slot and per expert");
+static_assert(kTile <= kUpThreads && kTile == kDownThreads, "a thread per output");
+
+// A value that the wave shares, in a scalar register: left to itself the compiler
+// keeps some of them, and the addresses that follow from them, in vector registers
+// (up kernel: 203 registers, 130 this way).
+__device__ __forceinline__ int scalar(int v) {
+    asm("" : "+v"(v));  // (nothing is known of v here, so the next step stays)
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int div_uniform(int a, int b) { return scalar((int)((unsigned)a / (unsigned)b)); }
+
+// ---- selection and the reached segments
+//
+// The 16 lanes of a row of lanes hold one token's logits, V each (experts s, s + 16, ..).
+
+constexpr int kSetWords = BMOE_MAX_EXPERTS / 32;
+
+struct SelectSmem {
+    int pk[kFewTok][BMOE_MAX_TOPK];    // picks, best first
+    float pe[kFewTok][BMOE_MAX_TOPK];  // exp(logit - best)
+    float sum[kFewTok];                // of exp(logit - best) over all experts
+    float gate[kMaxSlots];             // by slot, of a segment's first slot of the token
+    uint32_t reached[kSetWords];       // the reached segments as a bit set
+    int16_t segs[BMOE_MAX_EXPERTS];    // and ascending
+    int16_t slot_of[BMOE_MAX_EXPERTS][kFewTok];  // [place in segs][token], -1: does not call it
+};
+
+__device__ __forceinline__ int members_below(const uint32_t* set, int g) {
+    int n = 0;
+    for (int i = 0; i < g >> 5; ++i) n += __popc(set[i]);
+    return n + __popc(set[g >> 5] & ((1u << (g & 31)) - 1));
+}
+__device__ __forceinline__ int members(const uint32_t* set) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kSetWords; ++i) n += __popc(set[i]);
+    return scalar(n);
+}
+
+// picks of tokens 4 * wave .. 4 * wave + 3; the set was cleared before
+template <int V>
+__device__ __forceinline__ void few_select(const double* logits, const int32_t* e2g, SelectSmem& sm, int T, int E, int G,
+                                           int k, int wave, int lane) {
+    const int s = lane & 15, t = wave * 4 + (lane >> 4), tl = min(t, T - 1);
+    const int vpl = (E - s + 15) / 16;
+    double v[V];
+    int key[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int e = min(s + 16 * j, E - 1);
+        v[j] = logits[tl * E + e];
+        key[j] = (e << 16) | (e2g[e] + 1);
+    }
+    unsigned taken = vpl >= V ? 0u : ~0u << vpl;
+    double top = 0.0;
+    for (int r = 0; r < k; ++r) {
+        // ascending expert order, strict >: the lower index wins a tie; the first
+        // untaken one is taken even at -inf
+        double bv = -INFINITY;
+        int be = kNoPick;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const bool in = !((taken >> j) & 1u) && (v[j] > bv || be == kNoPick);
+            bv = in ? v[j] : bv;
+            be = in ? key[j] : be;
+        }
+        group_argmax<16>(bv, be);
+        const int e = pick_expert(be);
+        if ((e & 15) == s) taken |= 1u << ((e >> 4) & 31);
+        top = r == 0 ? bv : top;
+        if (s == 0) {
+            sm.pk[t][r] = be;
+            sm.pe[t][r] = __expf((float)(bv - top));
+            const int g = pick_group(be);
+            if (t < T && (unsigned)g < (unsigned)G) atomicOr(&sm.reached[g >> 5], 1u << (g & 31));
+        }
+    }
+    float se = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) se += j < vpl ? __expf((float)(v[j] - top)) : 0.f;
+    se = group_sum<16>(se);
+    if (s == 0) sm.sum[t] = se;
+}
+
+// ---- weights of one format
+//
+// Rows: 16 weight rows (fewer at the matrix's end) of K columns; Unit: a wave's UK
+// columns of them, loaded at lane row r and the unit's first column; X: the same
+// columns of the tokens, from an address that the wave shares and the lane's row's
+// byte offset. RAGGED: columns past K read the row's last ones and tail() zeroes
+// them (in every unit: a branch would cost copies of the buffers). multiply() adds the products with NP parts of the activations (their sum is the value) to
+// tot. PARTS: parts of a hidden value; BATCH: units of a register buffer.
+struct FmtBf16 {
+    typedef uint16_t Act;
+    static constexpr int UK = 64, LD = 2, PARTS = 2, BATCH = 2;
+    static constexpr bool PAIRS = true;
+    struct Stack { const uint16_t* w; };
+    struct Rows {
+        const uint16_t* w;
+        Rows() = default;
+        __device__ __forceinline__ Rows(const Stack& st, int64_t first, int K) : w(st.w + first * K) {}
+    };
+    struct X {
+        v4u x[LD];
+        template <bool RAGGED>
+        __device__ __forceinline__ void load(const Act* base, uint32_t row, int k, int K, int q) {
+#pragma unroll
+            for (int u = 0; u < LD; ++u) x[u] = load_at(base, row + 2 * (RAGGED ? min(k + u * 32 + q * 8, K - 8) : k + u * 32 + q * 8));
+        }
+        __device__ __forceinline__ void tail(int k, int K, int q) {
+#pragma unroll
+            for (int u = 0; u < LD; ++u) x[u] &= k + u * 32 + q * 8 < K ? ~0u : 0u;
+        }
+    };
+    struct Unit {
+        X w;
+        template <bool RAGGED>
+        __device__ __forceinline__ void load(const Rows& rows, int r, int k, int K, int q) {
+            w.template load<RAGGED>(rows.w, (uint32_t)(r * K) * 2, k, K, q);
+        }
+        __device__ __forceinline__ void tail(int k, int K, int q) { w.tail(k, K, q); }
+    };
+    template <int NM, int NP>
+    __device__ static __forceinline__ void multiply(f32x4 (&tot)[NM], const Unit (&w)[NM], const X (&x)[NP],
+                                                    const Stack&) {
+#pragma unroll
+        for (int u = 0; u < LD; ++u)
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int m = 0; m < NM; ++m) tot[m] = mfma16(x[p].x[u], w[m].w.x[u], tot[m]);
+    }
+};
+
+struct FmtF32 {
+    typedef float Act;
+    static constexpr int UK = 32, LD = 2, PARTS = 1, BATCH = 2;
+    static constexpr bool PAIRS = true;
+    struct Stack { const float* w; };
+    struct Rows {
+        const float* w;
+        Rows() = default;
+        __device__ __forceinline__ Rows(const Stack& st, int64_t first, int K) : w(st.w + first * K) {}
+    };
+    struct X {
+        v4u x[LD];
+        template <bool RAGGED>
+        __device__ __forceinline__ void load(const Act* base, uint32_t row, int k, int K, int q) {
+#pragma unroll
+            for (int u = 0; u < LD; ++u) x[u] = load_at(base, row + 4 * (RAGGED ? min(k + u * 16 + q * 4, K - 4) : k + u * 16 + q * 4));
+        }
+        __device__ __forceinline__ void tail(int k, int K, int q) {
+#pragma unroll
+            for (int u = 0; u < LD; ++u) x[u] &= k + u * 16 + q * 4 < K ? ~0u : 0u;
+        }
+    };
+    struct Unit {
+        X w;
+        template <bool RAGGED>
+        __device__ __forceinline__ void load(const Rows& rows, int r, int k, int K, int q) {
+            w.template load<RAGGED>(rows.w, (uint32_t)(r * K) * 4, k, K, q);
+        }
+        __device__ __forceinline__ void tail(int k, int K, int q) { w.tail(k, K, q); }
+    };
+    template <int NM, int NP>
+    __device__ static __forceinline__ void multiply(f32x4 (&tot)[NM], const Unit (&w)[NM], const X (&x)[NP],
+                                                    const Stack&) {
+        static_assert(NP == 1, "fp32 activations are whole");
+#pragma unroll
+        for (int u = 0; u < LD; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int m = 0; m < NM; ++m)
+                    tot[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[0].x[u][j]),
+                                                                  __uint_as_float(w[m].w.x[u][j]), tot[m], 0, 0, 0);
+    }
+};
+
+template <int GROUP>
+struct FmtW4 {
+    typedef uint16_t Act;
+    static constexpr int UK = kW4Unit, LD = UK / 32, PARTS = 2, BATCH = 1;
+    static constexpr bool PAIRS = false;
+    static constexpr int NG = W4Unit<GROUP>::NG, STEPS = GROUP / 32;
+    typedef W4Stack Stack;
+    typedef W4Rows<GROUP> Rows;
+    struct X {
+        v4u x[LD];
+        template <bool RAGGED>
+        __device__ __forceinline__ void load(const Act* base, uint32_t row, int k, int K, int q) {
+#pragma unroll
+            for (int u = 0; u < LD; ++u)
+                x[u] = load_at(base, row + 2 * (RAGGED ? min(k + u * 32 + q * 8, K - 8) : k + u * 32 + q * 8));
+        }
+        __device__ __forceinline__ void tail(int k, int K, int q) {
+#pragma unroll
+            for (int u = 0; u < LD; ++u) x[u] &= k + u * 32 + q * 8 < K ? ~0u : 0u;
+        }
+    };
+    struct Unit {
+        W4Unit<GROUP> w;
+        template <bool RAGGED>
+        __device__ __forceinline__ void load(const Rows& rows, int r, int k, int K, int q) {
+            w.load(rows, r, k / kW4Unit, K, q);
+        }
+        __device__ __forceinline__ void tail(int, int, int) { w.settle(); }  // (codes are finite)
+    };
+    template <int NM, int NP>
+    __device__ static __forceinline__ void multiply(f32x4 (&tot)[NM], const Unit (&w)[NM], const X (&x)[NP],
+                                                    const Stack& st) {
+        const v4u ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+        v4u c[2][NM];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int m = 0; m < NM; ++m) c[h][m] = w4_transpose(w[m].w.codes[h]);
+        // A group is scaled while the next one is multiplied. (The fences keep the
+        // compiler from running more groups side by side than there are registers.)
+        f32x4 acc[2][NM], xs[2];
+        auto flush = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+            for (int m = 0; m < NM; ++m) {
+                const float sc = w[m].w.scale(g), off = w[m].w.offset(st.has_zeros, g);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    tot[m][i] = fmaf(sc, fmaf(-off, xs[g & 1][i], acc[g & 1][m][i]), tot[m][i]);
+                asm volatile("" : "+v"(tot[m]));  // here, and not where tot is used next
+            }
+        };
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            xs[g & 1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int m = 0; m < NM; ++m) acc[g & 1][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = g * STEPS; u < (g + 1) * STEPS; ++u) {
+                v4u b[NM];
+#pragma unroll
+                for (int m = 0; m < NM; ++m) b[m] = w4_unpack(c[u / 4][m][u % 4]);
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    const v4u a = w4_order(x[p].x[u]);
+                    xs[g & 1] = mfma16(a, ones, xs[g & 1]);
+#pragma unroll
+                    for (int m = 0; m < NM; ++m) acc[g & 1][m] = mfma16(a, b[m], acc[g & 1][m]);
+                }
+            }
+            if (g > 0) flush(g - 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        flush(NG - 1);
+    }
+};
+
+// one of two by value (a conditional between two kernel arguments themselves would
+// become a load through a chosen address, which waits for every load before it)
+template <typename T>
+__device__ __forceinline__ T pick(bool first, T a, T b) { return first ? a : b; }
+__device__ __forceinline__ FmtBf16::Stack pick(bool first, FmtBf16::Stack a, FmtBf16::Stack b) {
+    return {pick(first, a.w, b.w)};
+}
+__device__ __forceinline__ FmtF32::Stack pick(bool first, FmtF32::Stack a, FmtF32::Stack b) {
+    return {pick(first, a.w, b.w)};
+}
+__device__ __forceinline__ W4Stack pick(bool first, W4Stack a, W4Stack b) {
+    return {pick(first, a.codes, b.codes), pick(first, a.scales, b.scales), pick(first, a.zeros, b.zeros),
+            pick(first, a.groups, b.groups), a.has_zeros};
+}
+
+template <class F>
+struct FewParams {
+    typedef typename F::Act Act;
+    typename F::Stack up[2], up_sh[2], down, down_sh;  // up: W_gate, W_up
+    const Act* x;
+    const double* logits;  // [T, E]
+    const int32_t* e2g;
+    int32_t* topk_idx;
+    float* topk_w;
+    int32_t* slot_group;
+    float* slot_gate;
+    // hidden values, [T*k, f] of the slots then [T, fs] of the shared experts;
+    // bf16 layers: the high parts, then as many low parts
+    Act* h;
+    Act* out;
+    int32_t* done;   // [tiles of d] workgroups that have finished, when split > 1
+    float* partial;  // [tiles of d][split][16 tokens][16 columns]
+    int T, k, G, E, d, f, fs, norm, split;
+    int64_t h_part;  // elements of one part
+};
+
+// Neither loads nor multiplies move past a fence. (The memory clobber keeps the
+// loads in front of a loop and at its end from being merged into ones at its start,
+// which would be waited for at once.)
+__device__ __forceinline__ void step_fence() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Both run n steps over two register buffers of weights. Every load of their loops
+// is issued on every path (a step past the last loads the last one again), so that
+// the compiler can count the loads that are younger than the ones it waits for.
+//
+// stream_pairs: the activations have two buffers too; the loads of step i + 2 follow
+// the multiply of step i.
+template <class W, class X, class LoadW, class LoadX, class Multiply>
+__device__ __forceinline__ void stream_pairs(int n, LoadW load_w, LoadX load_x, Multiply multiply) {
+    W w0, w1;
+    X x0, x1;
+    load_w(w0, 0);
+    load_x(x0, 0);
+    load_w(w1, min(1, n - 1));
+    load_x(x1, min(1, n - 1));
+    step_fence();
+    int i = 0;
+    for (; i + 2 < n; i += 2) {
+        multiply(w0, x0);
+        step_fence();
+        load_w(w0, i + 2);
+        load_x(x0, i + 2);
+        step_fence();
+        multiply(w1, x1);
+        step_fence();
+        load_w(w1, min(i + 3, n - 1));
+        load_x(x1, min(i + 3, n - 1));
+        step_fence();
+    }
+    multiply(w0, x0);
+    if (i + 1 < n) multiply(w1, x1);
+}
+// stream_weights: one buffer of activations, which come from the L2 cache; they are
+// loaded just before the next step's weights (loads return in order: after them they
+// would be waited for together).
+template <class W, class X, class LoadW, class LoadX, class Multiply>
+__device__ __forceinline__ void stream_weights(int n, LoadW load_w, LoadX load_x, Multiply multiply) {
+    W w0, w1;
+    X x;
+    load_w(w0, 0);
+    step_fence();
+    int i = 0;
+    for (; i + 1 < n; i += 2) {
+        load_x(x, i);
+        step_fence();
+        load_w(w1, i + 1);
+        step_fence();
+        multiply(w0, x);
+        step_fence();
+        load_x(x, i + 1);
+        step_fence();
+        load_w(w0, min(i + 2, n - 1));
+        step_fence();
+        multiply(w1, x);
+        step_fence();
+    }
+    if (i < n) {
+        load_x(x, i);
+        multiply(w0, x);
+    }
+}
+// Plain weights: 15.7 us (one token, up) by pairs, 19.0 with one buffer of
+// activations; 4-bit weights, whose units hold four times the columns, have no
+// registers for the second one.
+template <class F, class W, class X, class LoadW, class LoadX, class Multiply>
+__device__ __forceinline__ void stream_steps(int n, LoadW load_w, LoadX load_x, Multiply multiply) {
+    if (n <= 0) return;
+    if constexpr (F::PAIRS) stream_pairs<W, X>(n, load_w, load_x, multiply);
+    else stream_weights<W, X>(n, load_w, load_x, multiply);
+}
+
+template <class F, int NM>
+struct FewW {
+    typename F::Unit w[F::BATCH][NM];
+};
+template <class F, int NP>
+struct FewX {
+    typename F::X x[F::BATCH][NP];
+};
+
+// sum of the waves' partials of D element (row, col)
+template <int WAVES>
+__device__ __forceinline__ float tile_sum(const f32x4 (*part)[64], int row, int col) {
+    const float* p = (const float*)&part[0][(row >> 2) * 16 + col] + (row & 3);
+    float v = p[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v += p[w * 256];
+    return v;
+}
+
+__device__ __forceinline__ void store_hidden(float* h, int64_t, int64_t at, float v) { h[at] = v; }
+__device__ __forceinline__ void store_hidden(uint16_t* h, int64_t part, int64_t at, float v) {
+    const uint16_t hi = f32_to_bf16(v);
+    const float rest = v - bf16_to_f32(hi);
+    h[at] = hi;
+    h[part + at] = isfinite(rest) ? f32_to_bf16(rest) : (uint16_t)0;  // (an infinite value stays one)
+}
+
+// What a workgroup of few_up_kernel works on: item i is 16 hidden columns, of the
+// shared experts first, then of the reached segments in turn.
+struct UpItem {
+    bool shared;
+    int place, n0;  // place among the reached segments
+    __device__ __forceinline__ UpItem(int i, int sh_tiles, int tiles) {
+        shared = i < sh_tiles;
+        place = shared ? 0 : div_uniform(i - sh_tiles, tiles);
+        n0 = (shared ? i : i - sh_tiles - place * tiles) * kFewCols;
+    }
+};
+
+// RAGGED: d is not whole units, or they do not go evenly over the waves' buffers
+template <class F, bool RAGGED>
+__global__ __launch_bounds__(kUpThreads, kUpWgsPerCu * kUpThreads / 256) void few_up_kernel(FewParams<F> p) {
+    constexpr int WAVES = kUpThreads / 64, BATCH = F::BATCH;
+    __shared__ __align__(16) f32x4 part[2][2][WAVES][64];  // [parity of the item][matrix]
+    __shared__ SelectSmem sm;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int r16 = lane & 15, q = lane >> 4;
+    const int T = p.T, k = p.k, d = p.d, f = p.f, fs = p.fs;
+    const int sh_tiles = ceil_div(fs, kFewCols), tiles = ceil_div(f, kFewCols);
+
+    // the picks, the reached segments, and where each token's gate of a segment is
+    if (tid < kSetWords) sm.reached[tid] = 0;
+    for (int i = tid; i < BMOE_MAX_EXPERTS * kFewTok / 2; i += kUpThreads) ((uint32_t*)sm.slot_of)[i] = ~0u;
+    __syncthreads();
+    if (wave * 4 < T) {
+        if (p.E <= 64) few_select<4>(p.logits, p.e2g, sm, T, p.E, p.G, k, wave, lane);
+        else few_select<16>(p.logits, p.e2g, sm, T, p.E, p.G, k, wave, lane);
+    }
+    __syncthreads();
+    if (tid < p.G && (sm.reached[tid >> 5] >> (tid & 31)) & 1u) sm.segs[members_below(sm.reached, tid)] = (int16_t)tid;
+    if (tid < T * k) {
+        const int t = tid / k, i = tid - t * k;
+        const int g = pick_group(sm.pk[t][i]);
+        const bool known = (unsigned)g < (unsigned)p.G;
+        float mine = 0.f, all = 0.f;
+        bool first = known;
+        for (int j = 0; j < k; ++j) {
+            const float e = sm.pe[t][j];
+            const bool same = pick_group(sm.pk[t][j]) == g;
+            all += e;
+            if (same && j < i) first = false;
+            mine += same && j >= i ? e : 0.f;
+        }
+        const float inv = 1.f / (p.norm ? all : sm.sum[t]);
+        sm.gate[tid] = mine * inv;
+        if (first) sm.slot_of[members_below(sm.reached, g)][t] = (int16_t)tid;
+        if (blockIdx.x == 0) {
+            p.topk_idx[tid] = pick_expert(sm.pk[t][i]);
+            p.topk_w[tid] = sm.pe[t][i] * inv;
+            p.slot_group[tid] = first ? g : -1;
+            p.slot_gate[tid] = first ? mine * inv : 0.f;
+        }
+    }
+    const int items = sh_tiles + members(sm.reached) * tiles;
+    __syncthreads();
+
+    const uint32_t xr = (uint32_t)(min(r16, T - 1) * d) * sizeof(typename F::Act);
+    const int units = ceil_div(d, F::UK), steps = ceil_div(ceil_div(units, WAVES), BATCH);  // steps of an item
+    const int wg = scalar(blockIdx.x), wgs = scalar(gridDim.x);
+    const int mine = scalar(wg < items ? div_uniform(items - 1 - wg, wgs) + 1 : 0);
+    typedef FewW<F, 2> W;
+    typedef FewX<F, 1> X;
+    // the place of the loads: step l_step of item l_item, whose weight rows are
+    // gate and up (lane row l_row)
+    int l_item = wg, l_step = 0, l_at = 0, l_row = 0;
+    typename F::Rows gate, up;
+    auto enter = [&]() __attribute__((always_inline)) {
+        const UpItem it(l_item, sh_tiles, tiles);
+        const int seg = it.shared ? 0 : scalar(sm.segs[it.place]), N = pick(it.shared, fs, f);
+        gate = typename F::Rows(pick(it.shared, p.up_sh[0], p.up[0]), (int64_t)seg * N + it.n0, d);
+        up = typename F::Rows(pick(it.shared, p.up_sh[1], p.up[1]), (int64_t)seg * N + it.n0, d);
+        l_row = min(r16, N - 1 - it.n0);
+    };
+    auto load_w = [&](W& b, int at) __attribute__((always_inline)) {
+        if (at != l_at) {
+            l_at = at;
+            if (++l_step == steps) {
+                l_step = 0;
+                l_item += wgs;
+                enter();
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            int u = wave + WAVES * (BATCH * l_step + i);
+            if constexpr (RAGGED) u = min(u, units - 1);
+            b.w[i][0].template load<RAGGED>(gate, l_row, u * F::UK, d, q);
+            b.w[i][1].template load<RAGGED>(up, l_row, u * F::UK, d, q);
+        }
+    };
+    f32x4 tot[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    int item = wg, step = 0, parity = 0;
+    int x_at = 0, x_step = 0;  // and of the activations'
+    auto load_x = [&](X& b, int at) __attribute__((always_inline)) {
+        if (at != x_at) {
+            x_at = at;
+            if (++x_step == steps) x_step = 0;
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            int u = wave + WAVES * (BATCH * x_step + i);
+            if constexpr (RAGGED) u = min(u, units - 1);
+            b.x[i][0].template load<RAGGED>(p.x, xr, u * F::UK, d, q);
+        }
+    };
+    auto multiply = [&](W& b, X& x) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            if constexpr (RAGGED) {
+                const int kk = (wave + WAVES * (BATCH * step + i)) * F::UK;
+                b.w[i][0].tail(kk, d, q);
+                b.w[i][1].tail(kk, d, q);
+                x.x[i][0].tail(kk, d, q);
+            }
+            F::multiply(tot, b.w[i], x.x[i], p.up[0]);
+        }
+        if (++step < steps) return;
+        step = 0;
+        part[parity][0][wave][lane] = tot[0];
+        part[parity][1][wave][lane] = tot[1];
+        tot[0] = tot[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // one barrier an item: the other parity's partials were read before it
+        lds_reads_done();
+        wg_barrier();
+        const UpItem it(item, sh_tiles, tiles);
+        const int N = pick(it.shared, fs, f), col = it.n0 + (tid & 15), token = tid >> 4;
+        if (token < T && col < N) {
+            const int slot = it.shared ? token : sm.slot_of[it.place][token];
+            if (slot >= 0) {
+                const float g = tile_sum<WAVES>(part[parity][0], token, tid & 15);
+                const float u = tile_sum<WAVES>(part[parity][1], token, tid & 15);
+                const float v = silu_mul(g, u) * (it.shared ? 1.f : sm.gate[slot]);
+                const int64_t at = (it.shared ? (int64_t)T * k * f : 0) + (int64_t)slot * N + col;
+                store_hidden(p.h, p.h_part, at, v);
+            }
+        }
+        parity ^= 1;
+        item += wgs;
+    };
+    if (mine > 0) enter();
+    stream_steps<F, W, X>(mine * steps, load_w, load_x, multiply);
+}
+
+// The long K of few_down_kernel: unit k of place a among the reached segments; a ==
+// segments: of the shared experts.
+struct DownUnit {
+    int a, k;
+    __device__ __forceinline__ void advance(int n, int segments, int per) {
+        k += n;
+#pragma clang loop unroll(disable) vectorize(disable)
+        while (a < segments && k >= per) {
+            k -= per;
+            ++a;
+        }
+    }
+};
+
+// PACK: at most 8 tokens, both parts of their hidden values in one A operand
+// RAGGED: d_ff or d_ff_shared is not whole units
+template <class F, bool PACK, bool RAGGED>
+__global__ __launch_bounds__(kDownThreads, kDownWgsPerCu * kDownThreads / 256) void few_down_kernel(FewParams<F> p) {
+    constexpr int WAVES = kDownThreads / 64, BATCH = F::BATCH, NP = PACK ? 1 : F::PARTS;
+    __shared__ __align__(16) f32x4 part[WAVES][64];
+    __shared__ uint32_t reached[kSetWords];
+    // by place among the reached segments (ascending): the segment, the tokens that
+    // call it, each token's slot (0 where it has none)
+    __shared__ int16_t segs[BMOE_MAX_EXPERTS];
+    __shared__ uint32_t callers[BMOE_MAX_EXPERTS + 1];
+    __shared__ uint8_t slot_of[BMOE_MAX_EXPERTS][kFewTok];
+    __shared__ int last_s;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int r16 = lane & 15, q = lane >> 4;
+    const int T = p.T, k = p.k, d = p.d, f = p.f, fs = p.fs;
+    const int wg = scalar(blockIdx.x), tile = div_uniform(wg, p.split), n0 = tile * kFewCols;
+    const int g = tid < T * k ? p.slot_group[tid] : -1;
+    const bool valid = (unsigned)g < (unsigned)p.G;
+    if (tid < kSetWords) reached[tid] = 0;
+    callers[tid] = 0;
+    for (int i = tid; i < BMOE_MAX_EXPERTS * kFewTok / 4; i += kDownThreads) ((uint32_t*)slot_of)[i] = 0;
+    __syncthreads();
+    if (valid) atomicOr(&reached[g >> 5], 1u << (g & 31));
+    __syncthreads();
+    const int segments = members(reached);
+    if (valid) {
+        const int place = members_below(reached, g), t = tid / k;
+        segs[place] = (int16_t)g;
+        atomicOr(&callers[place], 1u << t);
+        slot_of[place][t] = (uint8_t)tid;
+    }
+    if (tid == 0) callers[segments] = 0xffffu;  // the shared experts
+    const int per = ceil_div(f, F::UK), per_sh = ceil_div(fs, F::UK), units = segments * per + per_sh;
+    __syncthreads();
+    // the waves of the tile's workgroups take the units in turn
+    const int first = (wg - tile * p.split) * WAVES + wave, stride = p.split * WAVES;
+    const int steps = ceil_div(div_uniform(units + stride - 1, stride), BATCH);
+    const int wr = min(r16, d - 1 - n0), token = PACK ? r16 & 7 : r16;
+    typedef FewW<F, 1> W;
+    typedef FewX<F, NP> X;
+    DownUnit lu{0, 0}, xu, mu;  // of the weights' loads, the activations' and the products
+    lu.advance(first, segments, per);
+    xu = mu = lu;
+    int l_at = 0, x_at = 0;
+    auto load_w = [&](W& b, int at) __attribute__((always_inline)) {
+        if (at != l_at) {
+            l_at = at;
+            lu.advance(stride, segments, per);
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            if (i) lu.advance(stride, segments, per);
+            // (past the last unit: the first one again, its products are dropped)
+            const bool past = lu.a == segments && lu.k >= per_sh, sh = lu.a == segments && !past;
+            const int seg = sh ? 0 : scalar(segs[past ? 0 : lu.a]), width = pick(sh, fs, f);
+            const typename F::Rows rows(pick(sh, p.down_sh, p.down), (int64_t)seg * d + n0, width);
+            b.w[i][0].template load<RAGGED>(rows, wr, past ? 0 : lu.k * F::UK, width, q);
+        }
+    };
+    auto load_x = [&](X& b, int at) __attribute__((always_inline)) {
+        if (at != x_at) {
+            x_at = at;
+            xu.advance(stride, segments, per);
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            if (i) xu.advance(stride, segments, per);
+            const bool past = xu.a == segments && xu.k >= per_sh, sh = xu.a == segments && !past;
+            const int slot = sh ? min(token, T - 1) : slot_of[past ? 0 : xu.a][token], width = pick(sh, fs, f);
+            // (hidden values are below 2^32 bytes: 16 tokens, 16 slots, 2^20 columns)
+            const uint32_t hr = (uint32_t)((sh ? (int64_t)T * k * f : 0) + (int64_t)slot * width +
+                                           (PACK && r16 >= 8 ? p.h_part : 0)) * sizeof(typename F::Act);
+#pragma unroll
+            for (int j = 0; j < NP; ++j)
+                b.x[i][j].template load<RAGGED>(p.h + j * p.h_part, hr, past ? 0 : xu.k * F::UK, width, q);
+        }
+    };
+    f32x4 tot = {0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](W& b, X& x) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const bool past = mu.a == segments && mu.k >= per_sh;
+            if constexpr (RAGGED) {
+                const int kk = mu.k * F::UK, width = pick(mu.a == segments, fs, f);
+                b.w[i][0].tail(kk, width, q);
+#pragma unroll
+                for (int j = 0; j < NP; ++j) x.x[i][j].tail(kk, width, q);
+            }
+            f32x4 acc[1] = {{0.f, 0.f, 0.f, 0.f}};
+            F::multiply(acc, b.w[i], x.x[i], p.down);
+            // only the tokens that call the segment take its products
+            const uint32_t who = past ? 0u : callers[mu.a];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) tot[j] += (who >> ((PACK ? 4 * (q & 1) : 4 * q) + j)) & 1u ? acc[0][j] : 0.f;
+            mu.advance(stride, segments, per);
+        }
+    };
+    stream_steps<F, W, X>(steps, load_w, load_x, multiply);
+    part[wave][lane] = tot;
+    __syncthreads();
+    const int t = tid >> 4, col = tid & 15;
+    float v = tile_sum<WAVES>(part, t, col);
+    if constexpr (PACK) v += t < 8 ? tile_sum<WAVES>(part, t + 8, col) : 0.f;
+    if (p.split > 1) {
+        // the parts meet in memory; the workgroup that finishes last adds them in
+        // order. Relaxed accesses of agent scope go past the caches of one XCD, and
+        // the wait orders them; fences would write back and drop whole L2 caches
+        // (81 us instead of 9 for one token of the fine-grained layer).
+        float* mine = p.partial + (size_t)wg * kTile;
+        __hip_atomic_store(mine + tid, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        wait_vmcnt<0>();  // (this wave's part is written)
+        __syncthreads();
+        if (tid == 0)
+            last_s = __hip_atomic_fetch_add(p.done + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == p.split - 1;
+        __syncthreads();
+        if (!last_s) return;
+        const float* all = p.partial + (size_t)tile * p.split * kTile;
+        float parts[kSplitMax];
+#pragma unroll
+        for (int i = 0; i < kSplitMax; ++i)
+            if (i < p.split)
+                parts[i] = __hip_atomic_load(all + i * kTile + tid, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        v = parts[0];
+#pragma unroll
+        for (int i = 1; i < kSplitMax; ++i)
+            if (i < p.split) v += parts[i];
+    }
+    if (t < T && n0 + col < d) {
+        typename F::Act* o = p.out + (size_t)t * d + n0 + col;
+        if constexpr (sizeof(typename F::Act) == 2) *o = f32_to_bf16(v);
+        else *o = v;
+    }
+}
+
+// Workgroups that share 16 output columns: as many as the chip holds at once, where
+// the columns are fewer
+inline int most_splits(int d) {
+    const int tiles = ceil_div(d, kFewCols), n = kDownWgsPerCu * 256 / tiles;
+    return n < 1 ? 1 : n > kSplitMax ? kSplitMax : n;
+}
+
+inline size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+inline size_t logit_bytes(int T, int E) { return round256((size_t)T * E * sizeof(double)); }
+inline size_t done_bytes(int d) { return round256((size_t)ceil_div(d, kFewCols) * sizeof(int32_t)); }
+inline size_t partial_bytes(int d) {
+    return most_splits(d) == 1 ? 0 : (size_t)ceil_div(d, kFewCols) * most_splits(d) * kTile * sizeof(float);
+}
+
+template <class F, class ToStack>
+hipError_t launch_few_t(const FewArgs& a, ToStack st, hipStream_t s) {
+    typedef typename F::Act Act;
+    FewParams<F> p;
+    p.up[0] = st(a.w.gate, (int64_t)a.G * a.f, a.d);
+    p.up[1] = st(a.w.up, (int64_t)a.G * a.f, a.d);
+    p.down = st(a.w.down, (int64_t)a.G * a.d, a.f);
+    p.up_sh[0] = st(a.w.gate_sh, a.fs, a.d);
+    p.up_sh[1] = st(a.w.up_sh, a.fs, a.d);
+    p.down_sh = st(a.w.down_sh, a.d, a.fs);
+    p.x = (const Act*)a.x;
+    p.logits = (const double*)a.ws;
+    p.e2g = a.w.e2g;
+    p.topk_idx = a.topk_idx;
+    p.topk_w = a.topk_w;
+    p.slot_group = a.slot_group;
+    p.slot_gate = a.slot_gate;
+    char* ws = (char*)a.ws + logit_bytes(a.T, a.E);
+    p.done = (int32_t*)ws;
+    ws += done_bytes(a.d);
+    p.partial = (float*)ws;
+    p.h = (Act*)(ws + partial_bytes(a.d));
+    p.out = (Act*)a.out;
+    p.T = a.T;
+    p.k = a.k;
+    p.G = a.G;
+    p.E = a.E;
+    p.d = a.d;
+    p.f = a.f;
+    p.fs = a.fs;
+    p.norm = a.norm;
+    p.h_part = (int64_t)a.T * a.k * a.f + (int64_t)a.T * a.fs;
+    const int64_t slots = (int64_t)a.T * a.k, most = slots < a.G ? slots : a.G;
+    const int64_t units = most * ceil_div(a.f, F::UK) + ceil_div(a.fs, F::UK);
+    p.split = most_splits(a.d);
+    if (units < (int64_t)p.split * (kDownThreads / 64)) p.split = (int)ceil_div64(units, kDownThreads / 64);  // a unit a wave
+    hipError_t e = launch_few_logits(a, p.done, s);
+    if (e != hipSuccess) return e;
+    const int64_t items = most * ceil_div(a.f, kFewCols) + ceil_div(a.fs, kFewCols);
+    const int64_t room = (int64_t)kUpWgsPerCu * persistent_workgroups();
+    const dim3 up((unsigned)(items < room ? items : room)), down((unsigned)(ceil_div(a.d, kFewCols) * p.split));
+    const bool up_ragged = a.d % (F::UK * F::BATCH * (kUpThreads / 64)) != 0;
+    const bool down_ragged = a.f % F::UK != 0 || a.fs % F::UK != 0;
+    if (up_ragged) hipLaunchKernelGGL((few_up_kernel<F, true>), up, dim3(kUpThreads), 0, s, p);
+    else hipLaunchKernelGGL((few_up_kernel<F, false>), up, dim3(kUpThreads), 0, s, p);
+    constexpr bool kParts = F::PARTS == 2;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, down, dim3(kDownThreads), 0, s, p); };
+    if (kParts && a.T <= 8) {
+        if (down_ragged) go(few_down_kernel<F, kParts, true>);
+        else go(few_down_kernel<F, kParts, false>);
+    } else {
+        if (down_ragged) go(few_down_kernel<F, false, true>);
+        else go(few_down_kernel<F, false, false>);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace bmoe

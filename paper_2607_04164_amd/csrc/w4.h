@@ -9,12 +9,13 @@
 // below the bf16 output's.
 //
 // A wave owns 16 rows of W (the B operand) and up to TILES tiles of 16
-// activation rows (the A operand). It takes the columns in chunks of 128: lane
-// (r, q) loads the 16 bytes of row r, columns 32q .. 32q+31. Two exchanges of
-// lane rows then give step u (one MFMA of 32 columns) the columns 32u .. 32u+31,
-// eight of them in each lane, so that a group of 32 is one step. In a lane the
-// eight codes come out as columns 0,4,1,5,2,6,3,7; the activations are put into
-// the same order (w4_order).
+// activation rows (the A operand). It takes the columns in units of 256, a 128-byte
+// line of each row: lane (r, q) loads the 16 bytes of columns 32q .. 32q+31 and of
+// 128 + 32q .., row r. Two exchanges of lane rows then give step u of a half (one
+// MFMA of 32 columns) the columns 32u .. 32u+31, eight of them in each lane, so that
+// a group of 32 is one step. In a lane the eight codes come out as columns
+// 0,4,1,5,2,6,3,7; the activations are put into the same order (w4_order). A unit's
+// scales are one load of each lane, and so are its zero points.
 #pragma once
 
 #include "bmoe_common.h"
@@ -23,12 +24,16 @@ namespace bmoe {
 
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));  // native vector: stays in registers
 
-constexpr int kW4Chunk = 128;  // columns per chunk
+constexpr int kW4Unit = 256;  // columns per unit
 
 __device__ __forceinline__ v4u w4_unpack(uint32_t c) {
-    constexpr uint32_t kMask = 0x00780078u, kSixteen = 0x41804180u;
-    return v4u{((c << 3) & kMask) | kSixteen, ((c >> 1) & kMask) | kSixteen, ((c >> 5) & kMask) | kSixteen,
-               ((c >> 9) & kMask) | kSixteen};
+    constexpr uint32_t kMask = 0x00780078u;
+    // (in a vector register: an instruction takes one scalar operand, and with both
+    // constants scalar the and and the or would be two)
+    uint32_t sixteen;
+    asm("v_mov_b32 %0, 0x41804180" : "=v"(sixteen));
+    return v4u{((c << 3) & kMask) | sixteen, ((c >> 1) & kMask) | sixteen, ((c >> 5) & kMask) | sixteen,
+               ((c >> 9) & kMask) | sixteen};
 }
 
 // eight activations in the order of w4_unpack
@@ -66,18 +71,6 @@ inline W4Stack w4_stack(const void* codes, const void* scales, const uint8_t* ze
                    rows * ceil_div(K, group), zeros != nullptr};
 }
 
-// the unsigned integer of N bytes
-template <int N>
-struct UintOf;
-template <>
-struct UintOf<1> { typedef uint8_t type; };
-template <>
-struct UintOf<2> { typedef uint16_t type; };
-template <>
-struct UintOf<4> { typedef uint32_t type; };
-template <>
-struct UintOf<8> { typedef uint64_t type; };
-
 // 16 bytes at a 32-bit offset from an address that the whole wave shares
 __device__ __forceinline__ v4u load_at(const void* base, uint32_t off) {
     return *(const v4u*)((const char*)base + off);
@@ -86,11 +79,12 @@ __device__ __forceinline__ v4u load_at(const void* base, uint32_t off) {
 // 16 rows of a stack (fewer at its end), from row `first` on
 template <int GROUP>
 struct W4Rows {
-    static constexpr int NG = kW4Chunk / GROUP;
+    static constexpr int NG = kW4Unit / GROUP;
     const uint8_t* codes;
     const uint16_t* scales;
     const uint8_t* zeros;
     int last;  // the place of the stack's last NG groups, from the first row's first
+    W4Rows() = default;
     __device__ __forceinline__ W4Rows(const W4Stack& w, int64_t first, int K) {
         const int64_t j = first * ceil_div(K, GROUP);
         codes = w.codes + first * BMOE_W4_ROW_BYTES(K);
@@ -100,34 +94,68 @@ struct W4Rows {
     }
 };
 
-// A chunk of one lane's W row: 128 columns' codes (the lane's 32 of them) and the
-// chunk's groups, in one load each and without a branch (zeros are loaded where
-// there are none too). Rows of groups have any alignment.
-template <int GROUP>
-struct W4Chunk {
-    static constexpr int NG = kW4Chunk / GROUP;
-    v4u codes;
-    typename UintOf<2 * NG>::type s;
-    typename UintOf<NG>::type z;
-
-    // chunk c of row r of the rows; K columns
-    __device__ __forceinline__ void load(const W4Rows<GROUP>& w, int r, int c, int K, int q) {
-        const int pitch = BMOE_W4_ROW_BYTES(K), ng = ceil_div(K, GROUP);
-        codes = load_at(w.codes, (uint32_t)(r * pitch + min(64 * c + 16 * q, pitch - 16)));
-        // groups past the row's last one are another row's, or 0 past the stack's
-        // end (a stack has at least 8 rows): their activations are zero
-        const int j = r * ng + c * NG, from = min(j, w.last);
-        __builtin_memcpy(&s, (const char*)w.scales + (uint32_t)(from * 2), sizeof s);
-        __builtin_memcpy(&z, w.zeros + (uint32_t)from, sizeof z);
-        if constexpr (NG > 1) {
-            s = (decltype(s))(s >> (16 * (j - from)));
-            z = (decltype(z))(z >> (8 * (j - from)));
+// N bytes of group values from any address
+template <int N>
+struct W4Groups {
+    static constexpr int WORDS = (N + 3) / 4;
+    uint32_t v[WORDS];
+    __device__ __forceinline__ void load(const void* p) {
+        if constexpr (N == 2) {
+            uint16_t h;
+            __builtin_memcpy(&h, p, 2);
+            v[0] = h;
+        } else {
+            __builtin_memcpy(v, p, N);
         }
     }
-    __device__ __forceinline__ float scale(int g) const { return bf16_to_f32((uint16_t)(s >> (16 * g))); }
+    // drops the first `bits` of the first word (below 32)
+    template <int BITS>
+    __device__ __forceinline__ void drop() {
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) v[j] = v[j] >> BITS | (j + 1 < WORDS ? v[j + 1 < WORDS ? j + 1 : j] << (32 - BITS) : 0u);
+    }
+};
+
+// A unit of one lane's W row: 256 columns' codes (the lane's 64 of them) and the
+// unit's groups, without a branch (zeros are loaded where there are none too). Rows
+// of groups have any alignment.
+template <int GROUP>
+struct W4Unit {
+    static constexpr int NG = kW4Unit / GROUP;
+    v4u codes[2];
+    W4Groups<2 * NG> s;
+    W4Groups<NG> z;
+    int back;  // groups that s and z start before the unit's first one
+
+    // unit c of row r of the rows; K columns
+    __device__ __forceinline__ void load(const W4Rows<GROUP>& w, int r, int c, int K, int q) {
+        const int pitch = BMOE_W4_ROW_BYTES(K), ng = ceil_div(K, GROUP);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            codes[h] = load_at(w.codes, (uint32_t)(r * pitch + min(128 * c + 64 * h + 16 * q, pitch - 16)));
+        // Groups past the row's last one are another row's: their activations are
+        // zero. A unit that would reach past the stack's end starts further back (a
+        // stack has at least 8 rows).
+        const int j = r * ng + c * NG, from = min(j, w.last);
+        back = j - from;
+        s.load((const char*)w.scales + (uint32_t)(from * 2));
+        z.load(w.zeros + (uint32_t)from);
+    }
+    // moves the groups to their places: after the load, where K is not whole units
+    __device__ __forceinline__ void settle() {
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+            if (i < back) {
+                s.template drop<16>();
+                z.template drop<8>();
+            }
+    }
+    __device__ __forceinline__ float scale(int g) const {
+        return __uint_as_float(g & 1 ? s.v[g >> 1] & 0xffff0000u : s.v[g >> 1] << 16);
+    }
     // 16 + the zero point of group g
     __device__ __forceinline__ float offset(bool has_zeros, int g) const {
-        return has_zeros ? 16.f + (float)(uint8_t)(z >> (8 * g)) : 24.f;
+        return has_zeros ? 16.f + (float)((z.v[g >> 2] >> (8 * (g & 3))) & 0xffu) : 24.f;
     }
 };
 

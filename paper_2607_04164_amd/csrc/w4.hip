@@ -1,20 +1,22 @@
 // Weights in 4 bits with group scales: the quantizer and the grouped products
 // of few rows (see w4.h for the arithmetic).
 //
-// The products are bound by reading the codes: one workgroup (4 waves) owns a
-// segment and 16 output columns, its waves split K by chunks of 128 columns, and
-// a segment's rows are taken 64 at a time, so that up to 64 rows share one read
-// of the weights. The waves' partial tiles are added through LDS in wave order.
+// One workgroup (8 waves) owns a segment and 16 output columns; its waves split K by
+// units of 256 columns. A segment's rows are taken up to 32 at a time; later passes
+// find the weights in the L2 cache. A wave loads WB units of weights, then takes their
+// columns step by step; the activations of the next XS steps (from the L2 cache) are
+// loaded while these are multiplied. The waves' partial tiles are added through LDS
+// in wave order.
 #include "bmoe_common.h"
 #include "w4.h"
 
 namespace bmoe {
 namespace {
 
-constexpr int kW4Threads = 256;
+constexpr int kW4Threads = 512;
 constexpr int kW4Waves = kW4Threads / 64;
 constexpr int kW4Cols = 16;
-constexpr int kW4Tiles = 4;  // tiles of 16 rows per pass
+constexpr int kW4Tiles = 2;  // tiles of 16 rows per pass
 
 struct W4Params {
     const uint16_t* A;  // [rows_cap or a_count, K]
@@ -26,94 +28,143 @@ struct W4Params {
     int n_seg, rows_cap, N, K;
 };
 
-template <bool GATED, int GROUP>
-__global__ __launch_bounds__(kW4Threads, 2) void w4_gemm_kernel(W4Params p) {
-    constexpr int NMAT = GATED ? 2 : 1, TILES = kW4Tiles, NG = W4Chunk<GROUP>::NG, STEPS = GROUP / 32;
-    __shared__ __align__(16) f32x4 part[kW4Waves][NMAT * TILES][64];
+// One pass: rows m0 .. m0 + 16 * TILES - 1 (fewer: the segment's last), this wave's
+// units. RAGGED: K is not whole units; WB > 1 needs units that go evenly over the waves.
+template <bool GATED, int GROUP, int TILES, int WB, bool RAGGED>
+__device__ __forceinline__ void w4_pass(const W4Params& p, const W4Rows<GROUP>& rows0, const W4Rows<GROUP>& rows1, int wrow,
+                                        int m0, int end, int wave, int r16, int q, f32x4 (*part)[64]) {
+    constexpr int NMAT = GATED ? 2 : 1, GS = GROUP / 32;
+    constexpr int XS = 4 / TILES, NX = WB * 8 / XS;
+    const int K = p.K, units = ceil_div(K, kW4Unit);
+    const v4u ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+    const uint16_t* xp[TILES];
+#pragma unroll
+    for (int nt = 0; nt < TILES; ++nt) {
+        const int r = min(m0 + nt * 16 + r16, end - 1);
+        xp[nt] = p.A + (size_t)gathered_row(p.a_rows, p.a_count, r) * K;
+    }
+    f32x4 tot[NMAT][TILES];
+#pragma unroll
+    for (int m = 0; m < NMAT; ++m)
+#pragma unroll
+        for (int nt = 0; nt < TILES; ++nt) tot[m][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int u0 = wave; u0 < units; u0 += kW4Waves * WB) {
+        v4u x[2][XS][TILES];
+        auto load_x = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < XS; ++j) {
+                const int step = i * XS + j;
+                int col = (u0 + kW4Waves * (step / 8)) * kW4Unit + (step % 8) * 32 + q * 8;
+                if constexpr (RAGGED) col = min(col, K - 8);
+#pragma unroll
+                for (int nt = 0; nt < TILES; ++nt) x[i & 1][j][nt] = *(const v4u*)(xp[nt] + col);
+            }
+        };
+        load_x(0);
+        W4Unit<GROUP> w[WB][NMAT];
+#pragma unroll
+        for (int b = 0; b < WB; ++b)
+#pragma unroll
+            for (int m = 0; m < NMAT; ++m) w[b][m].load(m ? rows1 : rows0, wrow, u0 + kW4Waves * b, K, q);
+        f32x4 acc[NMAT][TILES], xs[TILES];
+        v4u c[NMAT];
+#pragma unroll
+        for (int i = 0; i < NX; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + 1 < NX) load_x(i + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < XS; ++j) {
+                const int step = i * XS + j, b = step / 8, s8 = step % 8, g = s8 / GS;
+                if (s8 == 0 && RAGGED) {
+#pragma unroll
+                    for (int m = 0; m < NMAT; ++m) w[b][m].settle();
+                }
+                if (s8 % 4 == 0) {
+#pragma unroll
+                    for (int m = 0; m < NMAT; ++m) c[m] = w4_transpose(w[b][m].codes[s8 / 4]);
+                }
+                if (s8 % GS == 0) {
+#pragma unroll
+                    for (int nt = 0; nt < TILES; ++nt) {
+                        xs[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int m = 0; m < NMAT; ++m) acc[m][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    }
+                }
+                v4u wv[NMAT];
+#pragma unroll
+                for (int m = 0; m < NMAT; ++m) wv[m] = w4_unpack(c[m][s8 % 4]);
+#pragma unroll
+                for (int nt = 0; nt < TILES; ++nt) {
+                    v4u xv = x[i & 1][j][nt];
+                    if constexpr (RAGGED) xv &= (u0 + kW4Waves * b) * kW4Unit + s8 * 32 + q * 8 < K ? ~0u : 0u;
+                    xv = w4_order(xv);
+                    xs[nt] = mfma16(xv, ones, xs[nt]);
+#pragma unroll
+                    for (int m = 0; m < NMAT; ++m) acc[m][nt] = mfma16(xv, wv[m], acc[m][nt]);
+                }
+                if (s8 % GS == GS - 1) {
+#pragma unroll
+                    for (int m = 0; m < NMAT; ++m) {
+                        const float sc = w[b][m].scale(g), off = w[b][m].offset(p.w[0].has_zeros, g);
+#pragma unroll
+                        for (int nt = 0; nt < TILES; ++nt) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                tot[m][nt][e] = fmaf(sc, fmaf(-off, xs[nt][e], acc[m][nt][e]), tot[m][nt][e]);
+                            asm volatile("" : "+v"(tot[m][nt]));  // here, and not where tot is used next
+                        }
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);  // (registers: no step runs ahead of the one before)
+            }
+        }
+    }
+    const int lane = r16 + 16 * q;
+#pragma unroll
+    for (int nt = 0; nt < TILES; ++nt)
+#pragma unroll
+        for (int m = 0; m < NMAT; ++m) part[(wave * kW4Tiles + nt) * NMAT + m][lane] = tot[m][nt];
+}
+
+template <bool GATED, int GROUP, bool RAGGED>
+__global__ __launch_bounds__(kW4Threads, 4) void w4_gemm_kernel(W4Params p) {
+    constexpr int NMAT = GATED ? 2 : 1;
+    __shared__ __align__(16) f32x4 part[kW4Waves * kW4Tiles * NMAT][64];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int r16 = lane & 15, q = lane >> 4;
     const int K = p.K, N = p.N;
     const int ncb = ceil_div(N, kW4Cols);
-    const int s = blockIdx.x / ncb, n0 = (blockIdx.x % ncb) * kW4Cols;
+    const int s = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)ncb)), n0 = ((int)blockIdx.x - s * ncb) * kW4Cols;
     const int beg = min(max(p.offsets[s], 0), p.rows_cap);
     const int end = min(max(p.offsets[s + 1], beg), p.rows_cap);
     if (end <= beg) return;
     const W4Rows<GROUP> rows0(p.w[0], (int64_t)s * N + n0, K), rows1(p.w[NMAT - 1], (int64_t)s * N + n0, K);
     const int wrow = min(r16, N - 1 - n0);
-    const int nch = ceil_div(K, kW4Chunk);
-    const v4u ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 
-    for (int m0 = beg; m0 < end; m0 += 16 * TILES) {
-        const int tiles = min(ceil_div(end - m0, 16), TILES);
-        const uint16_t* xp[TILES];
-#pragma unroll
-        for (int nt = 0; nt < TILES; ++nt) {
-            const int r = min(m0 + nt * 16 + r16, end - 1);
-            xp[nt] = p.A + (size_t)gathered_row(p.a_rows, p.a_count, r) * K;
-        }
-        f32x4 tot[NMAT][TILES];
-#pragma unroll
-        for (int m = 0; m < NMAT; ++m)
-#pragma unroll
-            for (int nt = 0; nt < TILES; ++nt) tot[m][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int c = wave; c < nch; c += kW4Waves) {
-            W4Chunk<GROUP> w[NMAT];
-#pragma unroll
-            for (int m = 0; m < NMAT; ++m) w[m].load(m ? rows1 : rows0, wrow, c, K, q);
-#pragma unroll
-            for (int m = 0; m < NMAT; ++m) w[m].codes = w4_transpose(w[m].codes);
-#pragma unroll
-            for (int nt = 0; nt < TILES; ++nt) {
-                if (nt >= tiles) break;
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    f32x4 acc[NMAT], xs = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int m = 0; m < NMAT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int u = g * STEPS; u < (g + 1) * STEPS; ++u) {
-                        const int col = c * kW4Chunk + u * 32 + q * 8;
-                        v4u x = col < K ? *(const v4u*)(xp[nt] + col) : v4u{0, 0, 0, 0};
-                        x = w4_order(x);
-                        xs = mfma16(x, ones, xs);
-#pragma unroll
-                        for (int m = 0; m < NMAT; ++m) acc[m] = mfma16(x, w4_unpack(w[m].codes[u]), acc[m]);
-                    }
-#pragma unroll
-                    for (int m = 0; m < NMAT; ++m) {
-                        const float sc = w[m].scale(g), off = w[m].offset(p.w[0].has_zeros, g);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            tot[m][nt][i] = fmaf(sc, fmaf(-off, xs[i], acc[m][i]), tot[m][nt][i]);
-                    }
-                }
-            }
-        }
-#pragma unroll
-        for (int nt = 0; nt < TILES; ++nt)
-            if (nt < tiles) {
-#pragma unroll
-                for (int m = 0; m < NMAT; ++m) part[wave][m * TILES + nt][lane] = tot[m][nt];
-            }
+    for (int m0 = beg; m0 < end; m0 += 16 * kW4Tiles) {
+        const int rows = min(end - m0, 16 * kW4Tiles);
+        if (rows > 16) w4_pass<GATED, GROUP, 2, 1, RAGGED>(p, rows0, rows1, wrow, m0, end, wave, r16, q, part);
+        else if (!RAGGED && K % (kW4Unit * kW4Waves * 2) == 0)
+            w4_pass<GATED, GROUP, 1, 2, false>(p, rows0, rows1, wrow, m0, end, wave, r16, q, part);
+        else w4_pass<GATED, GROUP, 1, 1, RAGGED>(p, rows0, rows1, wrow, m0, end, wave, r16, q, part);
         __syncthreads();
-        // wave nt finishes row tile nt: the lane holds rows 4q .. 4q+3, column r16
-        if (wave < tiles && n0 + r16 < N) {
-            f32x4 sum[NMAT];
+        // a thread per output of the pass
+        const int row = tid >> 4, col = tid & 15, nt = row >> 4;
+        if (row < rows && n0 + col < N) {
+            const float* at = (const float*)&part[nt * NMAT][((row & 15) >> 2) * 16 + col] + (row & 3);
+            float sum[NMAT];
 #pragma unroll
             for (int m = 0; m < NMAT; ++m) {
-                sum[m] = part[0][m * TILES + wave][lane];
+                sum[m] = at[m * 256];
 #pragma unroll
-                for (int w = 1; w < kW4Waves; ++w) sum[m] += part[w][m * TILES + wave][lane];
+                for (int w = 1; w < kW4Waves; ++w) sum[m] += at[(w * kW4Tiles * NMAT + m) * 256];
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = m0 + wave * 16 + 4 * q + i;
-                if (row >= end) continue;
-                float v;
-                if constexpr (GATED) v = silu_mul(sum[0][i], sum[NMAT - 1][i]);
-                else v = sum[0][i];
-                p.C[(size_t)row * N + n0 + r16] = f32_to_bf16(v);
-            }
+            float v;
+            if constexpr (GATED) v = silu_mul(sum[0], sum[NMAT - 1]);
+            else v = sum[0];
+            p.C[(size_t)(m0 + row) * N + n0 + col] = f32_to_bf16(v);
         }
         __syncthreads();  // the partials are rewritten by the next pass
     }
@@ -188,11 +239,13 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ 
 template <bool GATED>
 hipError_t launch_w4(const W4Params& p, int group, hipStream_t s) {
     const int64_t blocks = (int64_t)p.n_seg * ceil_div(p.N, kW4Cols);
-    if (blocks > kMaxBlocks256) return hipErrorInvalidValue;
+    if (blocks > kMaxBlocks512) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks), block(kW4Threads);
-    if (group == 32) hipLaunchKernelGGL((w4_gemm_kernel<GATED, 32>), grid, block, 0, s, p);
-    else if (group == 64) hipLaunchKernelGGL((w4_gemm_kernel<GATED, 64>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((w4_gemm_kernel<GATED, 128>), grid, block, 0, s, p);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, p); };
+    const bool ragged = p.K % kW4Unit != 0;
+    if (group == 32) ragged ? go(w4_gemm_kernel<GATED, 32, true>) : go(w4_gemm_kernel<GATED, 32, false>);
+    else if (group == 64) ragged ? go(w4_gemm_kernel<GATED, 64, true>) : go(w4_gemm_kernel<GATED, 64, false>);
+    else ragged ? go(w4_gemm_kernel<GATED, 128, true>) : go(w4_gemm_kernel<GATED, 128, false>);
     return hipGetLastError();
 }
 

@@ -21,6 +21,8 @@ CASES = {
     "wide-hidden": dict(T=3, d=64, E=8, top_k=2, G=4, f=2048, norm=1),
     "wide-model": dict(T=2, d=2048, E=16, top_k=4, G=8, f=40, fs=16),
     "shared-wider": dict(T=7, d=192, E=20, top_k=5, G=6, f=56, fs=488),
+    "whole-units-9": dict(T=9, d=1024, E=60, top_k=4, G=15, f=256, fs=128),
+    "whole-units-8": dict(T=8, d=1024, E=24, top_k=6, G=20, f=384, norm=1),
     "few-columns": dict(T=13, d=40, E=33, top_k=7, G=11, f=16),
 }
 FORMATS = [("bf16", 0, False), ("f32", 0, False), ("bf16", 32, False), ("bf16", 64, True), ("bf16", 128, False),
