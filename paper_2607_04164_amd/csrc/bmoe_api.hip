@@ -29,7 +29,6 @@ bmoe_status w4_check(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t N, 
     if (dtype != BMOE_BF16) return BMOE_ERR_UNSUPPORTED;
     if (n_seg < 1 || n_seg > BMOE_MAX_EXPERTS || rows_cap < 0) return BMOE_ERR_SHAPE;
     if (N < 8 || N % 8 != 0 || N > (1 << 20) || K < 8 || K % 8 != 0 || K > (1 << 20)) return BMOE_ERR_SHAPE;
-    if ((int64_t)n_seg * ((N + 15) / 16) > kMaxBlocks512) return BMOE_ERR_SHAPE;
     if (rows_cap == 0) return BMOE_OK;
     if (!offsets || !a || !w0 || !c) return BMOE_ERR_NULL;
     if (a_rows && a_count < 1) return BMOE_ERR_SHAPE;

@@ -279,9 +279,6 @@ struct W4QuantizeArgs {
 };
 hipError_t launch_w4_quantize(const W4QuantizeArgs& a, hipStream_t s);
 
-// workgroups of 512 threads that one launch can hold (its threads are counted in 32 bits)
-constexpr int64_t kMaxBlocks512 = ((int64_t)1 << 23) - 1;
-
 // c[row] = a[row] W^T, or silu(a Wg^T) * (a Wu^T) with w1
 struct W4GemmArgs {
     const int32_t* offsets;

@@ -1,9 +1,11 @@
 // Weights in 4 bits with group scales: the quantizer and the grouped products
 // of few rows (see w4.h for the arithmetic).
 //
-// One workgroup (8 waves) owns a segment and 16 output columns; its waves split K by
-// units of 256 columns. A segment's rows are taken up to 32 at a time; later passes
-// find the weights in the L2 cache. A wave loads WB units of weights, then takes their
+// One workgroup (8 waves) takes up to 32 rows of a segment (a pass) and 16 output
+// columns; its waves split K by units of 256 columns. The passes of a segment run side
+// by side: a loop over them inside a workgroup would make the longest segment's time
+// the kernel's. Their weights meet in the L2 cache (column blocks of a multiple of 8
+// keep them on one XCD). A wave loads WB units of weights, then takes their
 // columns step by step; the activations of the next XS steps (from the L2 cache) are
 // loaded while these are multiplied. The waves' partial tiles are added through LDS
 // in wave order.
@@ -128,6 +130,37 @@ __device__ __forceinline__ void w4_pass(const W4Params& p, const W4Rows<GROUP>& 
         for (int m = 0; m < NMAT; ++m) part[(wave * kW4Tiles + nt) * NMAT + m][lane] = tot[m][nt];
 }
 
+// Finds pass `at` of all segments' passes: its segment and its place among them, or
+// returns the number of passes there are (`at` then past them). One wave's work, the
+// same in every wave.
+__device__ __forceinline__ int find_pass(const int32_t* offsets, int n_seg, int rows_cap, int at, int lane, int* seg,
+                                         int* nth) {
+    int before = 0;
+    for (int base = 0; base < n_seg; base += 64) {
+        int passes = 0;
+        if (base + lane < n_seg) {
+            const int beg = min(max(offsets[base + lane], 0), rows_cap);
+            const int end = min(max(offsets[base + lane + 1], beg), rows_cap);
+            passes = ceil_div(end - beg, 16 * kW4Tiles);
+        }
+        int upto = passes;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int v = __shfl_up(upto, off);
+            if (lane >= off) upto += v;
+        }
+        const unsigned long long past = __ballot(before + upto > at);
+        if (past) {
+            const int l = __ffsll(past) - 1;
+            *seg = __builtin_amdgcn_readfirstlane(base + l);
+            *nth = __builtin_amdgcn_readfirstlane(at - before - __shfl(upto - passes, l));
+            return -1;
+        }
+        before += __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+    }
+    return before;
+}
+
 template <bool GATED, int GROUP, bool RAGGED>
 __global__ __launch_bounds__(kW4Threads, 4) void w4_gemm_kernel(W4Params p) {
     constexpr int NMAT = GATED ? 2 : 1;
@@ -136,15 +169,16 @@ __global__ __launch_bounds__(kW4Threads, 4) void w4_gemm_kernel(W4Params p) {
     const int r16 = lane & 15, q = lane >> 4;
     const int K = p.K, N = p.N;
     const int ncb = ceil_div(N, kW4Cols);
-    const int s = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)ncb)), n0 = ((int)blockIdx.x - s * ncb) * kW4Cols;
-    const int beg = min(max(p.offsets[s], 0), p.rows_cap);
-    const int end = min(max(p.offsets[s + 1], beg), p.rows_cap);
-    if (end <= beg) return;
-    const W4Rows<GROUP> rows0(p.w[0], (int64_t)s * N + n0, K), rows1(p.w[NMAT - 1], (int64_t)s * N + n0, K);
-    const int wrow = min(r16, N - 1 - n0);
-
-    for (int m0 = beg; m0 < end; m0 += 16 * kW4Tiles) {
-        const int rows = min(end - m0, 16 * kW4Tiles);
+    for (int64_t at = blockIdx.x;; at += gridDim.x) {  // (a launch that holds all of them makes one turn)
+        const int pass = __builtin_amdgcn_readfirstlane((int)(at / ncb));
+        int s, nth;
+        if (find_pass(p.offsets, p.n_seg, p.rows_cap, pass, lane, &s, &nth) >= 0) return;
+        const int n0 = __builtin_amdgcn_readfirstlane((int)(at - (int64_t)pass * ncb)) * kW4Cols;
+        const int beg = min(max(p.offsets[s], 0), p.rows_cap);
+        const int end = min(max(p.offsets[s + 1], beg), p.rows_cap);
+        const W4Rows<GROUP> rows0(p.w[0], (int64_t)s * N + n0, K), rows1(p.w[NMAT - 1], (int64_t)s * N + n0, K);
+        const int wrow = min(r16, N - 1 - n0);
+        const int m0 = beg + nth * 16 * kW4Tiles, rows = min(end - m0, 16 * kW4Tiles);
         if (rows > 16) w4_pass<GATED, GROUP, 2, 1, RAGGED>(p, rows0, rows1, wrow, m0, end, wave, r16, q, part);
         else if (!RAGGED && K % (kW4Unit * kW4Waves * 2) == 0)
             w4_pass<GATED, GROUP, 1, 2, false>(p, rows0, rows1, wrow, m0, end, wave, r16, q, part);
@@ -153,20 +187,20 @@ __global__ __launch_bounds__(kW4Threads, 4) void w4_gemm_kernel(W4Params p) {
         // a thread per output of the pass
         const int row = tid >> 4, col = tid & 15, nt = row >> 4;
         if (row < rows && n0 + col < N) {
-            const float* at = (const float*)&part[nt * NMAT][((row & 15) >> 2) * 16 + col] + (row & 3);
+            const float* d = (const float*)&part[nt * NMAT][((row & 15) >> 2) * 16 + col] + (row & 3);
             float sum[NMAT];
 #pragma unroll
             for (int m = 0; m < NMAT; ++m) {
-                sum[m] = at[m * 256];
+                sum[m] = d[m * 256];
 #pragma unroll
-                for (int w = 1; w < kW4Waves; ++w) sum[m] += at[(w * kW4Tiles * NMAT + m) * 256];
+                for (int w = 1; w < kW4Waves; ++w) sum[m] += d[(w * kW4Tiles * NMAT + m) * 256];
             }
             float v;
             if constexpr (GATED) v = silu_mul(sum[0], sum[NMAT - 1]);
             else v = sum[0];
             p.C[(size_t)(m0 + row) * N + n0 + col] = f32_to_bf16(v);
         }
-        __syncthreads();  // the partials are rewritten by the next pass
+        __syncthreads();  // the partials are rewritten by the next turn
     }
 }
 
@@ -238,9 +272,10 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ 
 
 template <bool GATED>
 hipError_t launch_w4(const W4Params& p, int group, hipStream_t s) {
-    const int64_t blocks = (int64_t)p.n_seg * ceil_div(p.N, kW4Cols);
-    if (blocks > kMaxBlocks512) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks), block(kW4Threads);
+    // passes: at most one for 32 rows, and one more for the rest of each segment's rows
+    const int64_t passes = (int64_t)p.rows_cap / (16 * kW4Tiles) + (p.n_seg < p.rows_cap ? p.n_seg : p.rows_cap);
+    const int64_t blocks = passes * ceil_div(p.N, kW4Cols), room = (int64_t)1 << 22;
+    const dim3 grid((unsigned)(blocks < room ? blocks : room)), block(kW4Threads);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, p); };
     const bool ragged = p.K % kW4Unit != 0;
     if (group == 32) ragged ? go(w4_gemm_kernel<GATED, 32, true>) : go(w4_gemm_kernel<GATED, 32, false>);
