@@ -43,14 +43,13 @@ namespace {
 constexpr int kFewTok = BMOE_FEW_MAX_TOKENS;
 constexpr int kFewCols = 16;
 constexpr int kLogitThreads = 256, kUpThreads = 512, kDownThreads = 256;
-constexpr int kUpWgsPerCu = 2, kDownWgsPerCu = 3;  // by their registers
-constexpr int kSplitMax = 8;     // workgroups that share 16 output columns
+constexpr int kSplitMax = 8;  // workgroups that share their output columns
 constexpr int kLogitTokens = 4;  // tokens of a few_logits_kernel workgroup
 constexpr int kMaxSlots = kFewTok * BMOE_MAX_TOPK;
 static_assert(kFewTok == 16, "one MFMA tile of tokens");
-constexpr int kTile = kFewTok * kFewCols;  // outputs of a tile, a thread each
+constexpr int kTile = kFewTok * kFewCols;  // outputs of a tile
 static_assert(kMaxSlots <= kTile && BMOE_MAX_EXPERTS <= kTile, "a thread per slot and per expert");
-static_assert(kTile <= kUpThreads && kTile == kDownThreads, "a thread per output");
+static_assert(2 * kTile <= kUpThreads && kTile == kDownThreads, "a thread per output of a tile");
 
 // A value that the wave shares, in a scalar register: left to itself the compiler
 // keeps some of them, and the addresses that follow from them, in vector registers
@@ -141,11 +140,16 @@ __device__ __forceinline__ void few_select(const double* logits, const int32_t* 
 // columns of the tokens, from an address that the wave shares and the lane's row's
 // byte offset. RAGGED: columns past K read the row's last ones and tail() zeroes
 // them (in every unit: a branch would cost copies of the buffers). multiply() adds the products with NP parts of the activations (their sum is the value) to
-// tot. PARTS: parts of a hidden value; BATCH: units of a register buffer.
+// tot. PARTS: parts of a hidden value; BATCH: units of a register buffer; UP_TILES,
+// DOWN_TILES: tiles of 16 columns that a wave takes with the same activations (4-bit
+// weights are a quarter of the bytes, and with one tile the activations' loads, not
+// the weights', bound them: 86 and 58 us for six tokens of wide experts); UP_WAVES,
+// DOWN_WAVES: waves per SIMD, by registers.
 struct FmtBf16 {
     typedef uint16_t Act;
     static constexpr int UK = 64, LD = 2, PARTS = 2, BATCH = 2;
     static constexpr bool PAIRS = true;
+    static constexpr int UP_TILES = 1, DOWN_TILES = 1, UP_WAVES = 4, DOWN_WAVES = 3;
     struct Stack { const uint16_t* w; };
     struct Rows {
         const uint16_t* w;
@@ -188,6 +192,7 @@ struct FmtF32 {
     typedef float Act;
     static constexpr int UK = 32, LD = 2, PARTS = 1, BATCH = 2;
     static constexpr bool PAIRS = true;
+    static constexpr int UP_TILES = 1, DOWN_TILES = 1, UP_WAVES = 4, DOWN_WAVES = 3;
     struct Stack { const float* w; };
     struct Rows {
         const float* w;
@@ -234,6 +239,7 @@ struct FmtW4 {
     typedef uint16_t Act;
     static constexpr int UK = kW4Unit, LD = UK / 32, PARTS = 2, BATCH = 1;
     static constexpr bool PAIRS = false;
+    static constexpr int UP_TILES = 2, DOWN_TILES = 4, UP_WAVES = 2, DOWN_WAVES = 2;
     static constexpr int NG = W4Unit<GROUP>::NG, STEPS = GROUP / 32;
     typedef W4Stack Stack;
     typedef W4Rows<GROUP> Rows;
@@ -446,28 +452,28 @@ __device__ __forceinline__ void store_hidden(uint16_t* h, int64_t part, int64_t 
     h[part + at] = isfinite(rest) ? f32_to_bf16(rest) : (uint16_t)0;  // (an infinite value stays one)
 }
 
-// What a workgroup of few_up_kernel works on: item i is 16 hidden columns, of the
+// What a workgroup of few_up_kernel works on: item i is `cols` hidden columns, of the
 // shared experts first, then of the reached segments in turn.
 struct UpItem {
     bool shared;
     int place, n0;  // place among the reached segments
-    __device__ __forceinline__ UpItem(int i, int sh_tiles, int tiles) {
+    __device__ __forceinline__ UpItem(int i, int cols, int sh_tiles, int tiles) {
         shared = i < sh_tiles;
         place = shared ? 0 : div_uniform(i - sh_tiles, tiles);
-        n0 = (shared ? i : i - sh_tiles - place * tiles) * kFewCols;
+        n0 = (shared ? i : i - sh_tiles - place * tiles) * cols;
     }
 };
 
 // RAGGED: d is not whole units, or they do not go evenly over the waves' buffers
 template <class F, bool RAGGED>
-__global__ __launch_bounds__(kUpThreads, kUpWgsPerCu * kUpThreads / 256) void few_up_kernel(FewParams<F> p) {
-    constexpr int WAVES = kUpThreads / 64, BATCH = F::BATCH;
-    __shared__ __align__(16) f32x4 part[2][2][WAVES][64];  // [parity of the item][matrix]
+__global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewParams<F> p) {
+    constexpr int WAVES = kUpThreads / 64, BATCH = F::BATCH, TILES = F::UP_TILES, COLS = TILES * kFewCols;
+    __shared__ __align__(16) f32x4 part[2][2 * TILES][WAVES][64];  // [parity of the item][matrix, tile]
     __shared__ SelectSmem sm;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int r16 = lane & 15, q = lane >> 4;
     const int T = p.T, k = p.k, d = p.d, f = p.f, fs = p.fs;
-    const int sh_tiles = ceil_div(fs, kFewCols), tiles = ceil_div(f, kFewCols);
+    const int sh_tiles = ceil_div(fs, COLS), tiles = ceil_div(f, COLS);
 
     // the picks, the reached segments, and where each token's gate of a segment is
     if (tid < kSetWords) sm.reached[tid] = 0;
@@ -509,18 +515,19 @@ __global__ __launch_bounds__(kUpThreads, kUpWgsPerCu * kUpThreads / 256) void fe
     const int units = ceil_div(d, F::UK), steps = ceil_div(ceil_div(units, WAVES), BATCH);  // steps of an item
     const int wg = scalar(blockIdx.x), wgs = scalar(gridDim.x);
     const int mine = scalar(wg < items ? div_uniform(items - 1 - wg, wgs) + 1 : 0);
-    typedef FewW<F, 2> W;
+    typedef FewW<F, 2 * TILES> W;
     typedef FewX<F, 1> X;
     // the place of the loads: step l_step of item l_item, whose weight rows are
-    // gate and up (lane row l_row)
-    int l_item = wg, l_step = 0, l_at = 0, l_row = 0;
+    // gate and up (the lane's rows l_row)
+    int l_item = wg, l_step = 0, l_at = 0, l_row[TILES];
     typename F::Rows gate, up;
     auto enter = [&]() __attribute__((always_inline)) {
-        const UpItem it(l_item, sh_tiles, tiles);
+        const UpItem it(l_item, COLS, sh_tiles, tiles);
         const int seg = it.shared ? 0 : scalar(sm.segs[it.place]), N = pick(it.shared, fs, f);
         gate = typename F::Rows(pick(it.shared, p.up_sh[0], p.up[0]), (int64_t)seg * N + it.n0, d);
         up = typename F::Rows(pick(it.shared, p.up_sh[1], p.up[1]), (int64_t)seg * N + it.n0, d);
-        l_row = min(r16, N - 1 - it.n0);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) l_row[t] = min(16 * t + r16, N - 1 - it.n0);
     };
     auto load_w = [&](W& b, int at) __attribute__((always_inline)) {
         if (at != l_at) {
@@ -535,11 +542,16 @@ __global__ __launch_bounds__(kUpThreads, kUpWgsPerCu * kUpThreads / 256) void fe
         for (int i = 0; i < BATCH; ++i) {
             int u = wave + WAVES * (BATCH * l_step + i);
             if constexpr (RAGGED) u = min(u, units - 1);
-            b.w[i][0].template load<RAGGED>(gate, l_row, u * F::UK, d, q);
-            b.w[i][1].template load<RAGGED>(up, l_row, u * F::UK, d, q);
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                b.w[i][2 * t].template load<RAGGED>(gate, l_row[t], u * F::UK, d, q);
+                b.w[i][2 * t + 1].template load<RAGGED>(up, l_row[t], u * F::UK, d, q);
+            }
         }
     };
-    f32x4 tot[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    f32x4 tot[2 * TILES];
+#pragma unroll
+    for (int m = 0; m < 2 * TILES; ++m) tot[m] = f32x4{0.f, 0.f, 0.f, 0.f};
     int item = wg, step = 0, parity = 0;
     int x_at = 0, x_step = 0;  // and of the activations'
     auto load_x = [&](X& b, int at) __attribute__((always_inline)) {
@@ -559,27 +571,29 @@ __global__ __launch_bounds__(kUpThreads, kUpWgsPerCu * kUpThreads / 256) void fe
         for (int i = 0; i < BATCH; ++i) {
             if constexpr (RAGGED) {
                 const int kk = (wave + WAVES * (BATCH * step + i)) * F::UK;
-                b.w[i][0].tail(kk, d, q);
-                b.w[i][1].tail(kk, d, q);
+#pragma unroll
+                for (int m = 0; m < 2 * TILES; ++m) b.w[i][m].tail(kk, d, q);
                 x.x[i][0].tail(kk, d, q);
             }
             F::multiply(tot, b.w[i], x.x[i], p.up[0]);
         }
         if (++step < steps) return;
         step = 0;
-        part[parity][0][wave][lane] = tot[0];
-        part[parity][1][wave][lane] = tot[1];
-        tot[0] = tot[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int m = 0; m < 2 * TILES; ++m) {
+            part[parity][m][wave][lane] = tot[m];
+            tot[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
         // one barrier an item: the other parity's partials were read before it
         lds_reads_done();
         wg_barrier();
-        const UpItem it(item, sh_tiles, tiles);
-        const int N = pick(it.shared, fs, f), col = it.n0 + (tid & 15), token = tid >> 4;
+        const UpItem it(item, COLS, sh_tiles, tiles);
+        const int N = pick(it.shared, fs, f), at_col = tid % COLS, col = it.n0 + at_col, token = tid / COLS;
         if (token < T && col < N) {
             const int slot = it.shared ? token : sm.slot_of[it.place][token];
             if (slot >= 0) {
-                const float g = tile_sum<WAVES>(part[parity][0], token, tid & 15);
-                const float u = tile_sum<WAVES>(part[parity][1], token, tid & 15);
+                const float g = tile_sum<WAVES>(part[parity][2 * (at_col >> 4)], token, at_col & 15);
+                const float u = tile_sum<WAVES>(part[parity][2 * (at_col >> 4) + 1], token, at_col & 15);
                 const float v = silu_mul(g, u) * (it.shared ? 1.f : sm.gate[slot]);
                 const int64_t at = (it.shared ? (int64_t)T * k * f : 0) + (int64_t)slot * N + col;
                 store_hidden(p.h, p.h_part, at, v);
@@ -609,9 +623,10 @@ struct DownUnit {
 // PACK: at most 8 tokens, both parts of their hidden values in one A operand
 // RAGGED: d_ff or d_ff_shared is not whole units
 template <class F, bool PACK, bool RAGGED>
-__global__ __launch_bounds__(kDownThreads, kDownWgsPerCu * kDownThreads / 256) void few_down_kernel(FewParams<F> p) {
+__global__ __launch_bounds__(kDownThreads, F::DOWN_WAVES) void few_down_kernel(FewParams<F> p) {
     constexpr int WAVES = kDownThreads / 64, BATCH = F::BATCH, NP = PACK ? 1 : F::PARTS;
-    __shared__ __align__(16) f32x4 part[WAVES][64];
+    constexpr int TILES = F::DOWN_TILES, COLS = TILES * kFewCols;
+    __shared__ __align__(16) f32x4 part[TILES][WAVES][64];
     __shared__ uint32_t reached[kSetWords];
     // by place among the reached segments (ascending): the segment, the tokens that
     // call it, each token's slot (0 where it has none)
@@ -622,7 +637,7 @@ __global__ __launch_bounds__(kDownThreads, kDownWgsPerCu * kDownThreads / 256) v
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int r16 = lane & 15, q = lane >> 4;
     const int T = p.T, k = p.k, d = p.d, f = p.f, fs = p.fs;
-    const int wg = scalar(blockIdx.x), tile = div_uniform(wg, p.split), n0 = tile * kFewCols;
+    const int wg = scalar(blockIdx.x), tile = div_uniform(wg, p.split), n0 = tile * COLS;
     const int g = tid < T * k ? p.slot_group[tid] : -1;
     const bool valid = (unsigned)g < (unsigned)p.G;
     if (tid < kSetWords) reached[tid] = 0;
@@ -644,8 +659,11 @@ __global__ __launch_bounds__(kDownThreads, kDownWgsPerCu * kDownThreads / 256) v
     // the waves of the tile's workgroups take the units in turn
     const int first = (wg - tile * p.split) * WAVES + wave, stride = p.split * WAVES;
     const int steps = ceil_div(div_uniform(units + stride - 1, stride), BATCH);
-    const int wr = min(r16, d - 1 - n0), token = PACK ? r16 & 7 : r16;
-    typedef FewW<F, 1> W;
+    const int token = PACK ? r16 & 7 : r16;
+    int wr[TILES];
+#pragma unroll
+    for (int m = 0; m < TILES; ++m) wr[m] = min(16 * m + r16, d - 1 - n0);
+    typedef FewW<F, TILES> W;
     typedef FewX<F, NP> X;
     DownUnit lu{0, 0}, xu, mu;  // of the weights' loads, the activations' and the products
     lu.advance(first, segments, per);
@@ -663,7 +681,9 @@ __global__ __launch_bounds__(kDownThreads, kDownWgsPerCu * kDownThreads / 256) v
             const bool past = lu.a == segments && lu.k >= per_sh, sh = lu.a == segments && !past;
             const int seg = sh ? 0 : scalar(segs[past ? 0 : lu.a]), width = pick(sh, fs, f);
             const typename F::Rows rows(pick(sh, p.down_sh, p.down), (int64_t)seg * d + n0, width);
-            b.w[i][0].template load<RAGGED>(rows, wr, past ? 0 : lu.k * F::UK, width, q);
+#pragma unroll
+            for (int m = 0; m < TILES; ++m)
+                b.w[i][m].template load<RAGGED>(rows, wr[m], past ? 0 : lu.k * F::UK, width, q);
         }
     };
     auto load_x = [&](X& b, int at) __attribute__((always_inline)) {
@@ -684,75 +704,109 @@ __global__ __launch_bounds__(kDownThreads, kDownWgsPerCu * kDownThreads / 256) v
                 b.x[i][j].template load<RAGGED>(p.h + j * p.h_part, hr, past ? 0 : xu.k * F::UK, width, q);
         }
     };
-    f32x4 tot = {0.f, 0.f, 0.f, 0.f};
+    f32x4 tot[TILES];
+#pragma unroll
+    for (int m = 0; m < TILES; ++m) tot[m] = f32x4{0.f, 0.f, 0.f, 0.f};
     auto multiply = [&](W& b, X& x) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
             const bool past = mu.a == segments && mu.k >= per_sh;
             if constexpr (RAGGED) {
                 const int kk = mu.k * F::UK, width = pick(mu.a == segments, fs, f);
-                b.w[i][0].tail(kk, width, q);
+#pragma unroll
+                for (int m = 0; m < TILES; ++m) b.w[i][m].tail(kk, width, q);
 #pragma unroll
                 for (int j = 0; j < NP; ++j) x.x[i][j].tail(kk, width, q);
             }
-            f32x4 acc[1] = {{0.f, 0.f, 0.f, 0.f}};
+            f32x4 acc[TILES];
+#pragma unroll
+            for (int m = 0; m < TILES; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
             F::multiply(acc, b.w[i], x.x[i], p.down);
             // only the tokens that call the segment take its products
             const uint32_t who = past ? 0u : callers[mu.a];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) tot[j] += (who >> ((PACK ? 4 * (q & 1) : 4 * q) + j)) & 1u ? acc[0][j] : 0.f;
+            for (int j = 0; j < 4; ++j) {
+                const bool takes = (who >> ((PACK ? 4 * (q & 1) : 4 * q) + j)) & 1u;
+#pragma unroll
+                for (int m = 0; m < TILES; ++m) tot[m][j] += takes ? acc[m][j] : 0.f;
+            }
             mu.advance(stride, segments, per);
         }
     };
     stream_steps<F, W, X>(steps, load_w, load_x, multiply);
-    part[wave][lane] = tot;
+#pragma unroll
+    for (int m = 0; m < TILES; ++m) part[m][wave][lane] = tot[m];
     __syncthreads();
     const int t = tid >> 4, col = tid & 15;
-    float v = tile_sum<WAVES>(part, t, col);
-    if constexpr (PACK) v += t < 8 ? tile_sum<WAVES>(part, t + 8, col) : 0.f;
+    float v[TILES];
+#pragma unroll
+    for (int m = 0; m < TILES; ++m) {
+        v[m] = tile_sum<WAVES>(part[m], t, col);
+        if constexpr (PACK) v[m] += t < 8 ? tile_sum<WAVES>(part[m], t + 8, col) : 0.f;
+    }
     if (p.split > 1) {
         // the parts meet in memory; the workgroup that finishes last adds them in
         // order. Relaxed accesses of agent scope go past the caches of one XCD, and
         // the wait orders them; fences would write back and drop whole L2 caches
         // (81 us instead of 9 for one token of the fine-grained layer).
-        float* mine = p.partial + (size_t)wg * kTile;
-        __hip_atomic_store(mine + tid, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        float* mine = p.partial + (size_t)wg * (TILES * kTile) + tid;
+#pragma unroll
+        for (int m = 0; m < TILES; ++m)
+            __hip_atomic_store(mine + m * kTile, v[m], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         wait_vmcnt<0>();  // (this wave's part is written)
         __syncthreads();
         if (tid == 0)
             last_s = __hip_atomic_fetch_add(p.done + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == p.split - 1;
         __syncthreads();
         if (!last_s) return;
-        const float* all = p.partial + (size_t)tile * p.split * kTile;
-        float parts[kSplitMax];
+        const float* all = p.partial + (size_t)tile * p.split * (TILES * kTile) + tid;
+        float parts[kSplitMax][TILES];
 #pragma unroll
         for (int i = 0; i < kSplitMax; ++i)
-            if (i < p.split)
-                parts[i] = __hip_atomic_load(all + i * kTile + tid, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        v = parts[0];
+            if (i < p.split) {
 #pragma unroll
-        for (int i = 1; i < kSplitMax; ++i)
-            if (i < p.split) v += parts[i];
+                for (int m = 0; m < TILES; ++m)
+                    parts[i][m] = __hip_atomic_load(all + (i * TILES + m) * kTile, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+#pragma unroll
+        for (int m = 0; m < TILES; ++m) {
+            v[m] = parts[0][m];
+#pragma unroll
+            for (int i = 1; i < kSplitMax; ++i)
+                if (i < p.split) v[m] += parts[i][m];
+        }
     }
-    if (t < T && n0 + col < d) {
-        typename F::Act* o = p.out + (size_t)t * d + n0 + col;
-        if constexpr (sizeof(typename F::Act) == 2) *o = f32_to_bf16(v);
-        else *o = v;
+#pragma unroll
+    for (int m = 0; m < TILES; ++m) {
+        const int c = n0 + 16 * m + col;
+        if (t < T && c < d) {
+            typename F::Act* o = p.out + (size_t)t * d + c;
+            if constexpr (sizeof(typename F::Act) == 2) *o = f32_to_bf16(v[m]);
+            else *o = v[m];
+        }
     }
 }
 
-// Workgroups that share 16 output columns: as many as the chip holds at once, where
-// the columns are fewer
-inline int most_splits(int d) {
-    const int tiles = ceil_div(d, kFewCols), n = kDownWgsPerCu * 256 / tiles;
+// Workgroups that share `cols` output columns: as many as two or three a CU, where the
+// columns are fewer
+inline int most_splits(int d, int cols, int per_cu) {
+    const int tiles = ceil_div(d, cols), n = per_cu * 256 / tiles;
     return n < 1 ? 1 : n > kSplitMax ? kSplitMax : n;
 }
 
 inline size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 inline size_t logit_bytes(int T, int E) { return round256((size_t)T * E * sizeof(double)); }
 inline size_t done_bytes(int d) { return round256((size_t)ceil_div(d, kFewCols) * sizeof(int32_t)); }
+template <class F>
+size_t partial_of(int d) {
+    constexpr int cols = F::DOWN_TILES * kFewCols;
+    const int split = most_splits(d, cols, F::DOWN_WAVES);
+    return split == 1 ? 0 : (size_t)ceil_div(d, cols) * split * F::DOWN_TILES * kTile * sizeof(float);
+}
+// (enough for any format)
 inline size_t partial_bytes(int d) {
-    return most_splits(d) == 1 ? 0 : (size_t)ceil_div(d, kFewCols) * most_splits(d) * kTile * sizeof(float);
+    const size_t a = partial_of<FmtBf16>(d), b = partial_of<FmtF32>(d), c = partial_of<FmtW4<32>>(d);
+    return a > b ? (a > c ? a : c) : (b > c ? b : c);
 }
 
 template <class F, class ToStack>
@@ -789,13 +843,14 @@ hipError_t launch_few_t(const FewArgs& a, ToStack st, hipStream_t s) {
     p.h_part = (int64_t)a.T * a.k * a.f + (int64_t)a.T * a.fs;
     const int64_t slots = (int64_t)a.T * a.k, most = slots < a.G ? slots : a.G;
     const int64_t units = most * ceil_div(a.f, F::UK) + ceil_div(a.fs, F::UK);
-    p.split = most_splits(a.d);
+    constexpr int kUpCols = F::UP_TILES * kFewCols, kDownCols = F::DOWN_TILES * kFewCols;
+    p.split = most_splits(a.d, kDownCols, F::DOWN_WAVES);
     if (units < (int64_t)p.split * (kDownThreads / 64)) p.split = (int)ceil_div64(units, kDownThreads / 64);  // a unit a wave
     hipError_t e = launch_few_logits(a, p.done, s);
     if (e != hipSuccess) return e;
-    const int64_t items = most * ceil_div(a.f, kFewCols) + ceil_div(a.fs, kFewCols);
-    const int64_t room = (int64_t)kUpWgsPerCu * persistent_workgroups();
-    const dim3 up((unsigned)(items < room ? items : room)), down((unsigned)(ceil_div(a.d, kFewCols) * p.split));
+    const int64_t items = most * ceil_div(a.f, kUpCols) + ceil_div(a.fs, kUpCols);
+    const int64_t room = (int64_t)F::UP_WAVES * 256 / kUpThreads * persistent_workgroups();
+    const dim3 up((unsigned)(items < room ? items : room)), down((unsigned)(ceil_div(a.d, kDownCols) * p.split));
     const bool up_ragged = a.d % (F::UK * F::BATCH * (kUpThreads / 64)) != 0;
     const bool down_ragged = a.f % F::UK != 0 || a.fs % F::UK != 0;
     if (up_ragged) hipLaunchKernelGGL((few_up_kernel<F, true>), up, dim3(kUpThreads), 0, s, p);
