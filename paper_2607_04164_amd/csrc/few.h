@@ -135,118 +135,106 @@ __device__ __forceinline__ void few_select(const double* logits, const int32_t* 
 
 // ---- weights of one format
 //
-// Rows: 16 weight rows (fewer at the matrix's end) of K columns; Unit: a wave's UK
-// columns of them, loaded at lane row r and the unit's first column; X: the same
-// columns of the tokens, from an address that the wave shares and the lane's row's
-// byte offset. RAGGED: columns past K read the row's last ones and tail() zeroes
-// them (in every unit: a branch would cost copies of the buffers). multiply() adds the products with NP parts of the activations (their sum is the value) to
-// tot. PARTS: parts of a hidden value; BATCH: units of a register buffer; UP_TILES,
-// DOWN_TILES: tiles of 16 columns that a wave takes with the same activations (4-bit
-// weights are a quarter of the bytes, and with one tile the activations' loads, not
-// the weights', bound them: 86 and 58 us for six tokens of wide experts); UP_WAVES,
+// Place: tiles of 16 rows (fewer at the matrix's end) of NR matrices, from row `first`
+// of each on; tile m is rows 16 (m / NR) .. of matrix m % NR. Set: a wave's unit of UK
+// columns of NM such tiles; X: the same columns of the tokens, from an address that the
+// wave shares and the lane's row's byte offset. RAGGED: columns past K read the row's
+// last ones and tail() zeroes them (in every unit: a branch would cost copies of the
+// buffers). multiply() adds the products with NP parts of the activations (their sum is
+// the value) to tot. PARTS: parts of a hidden value; BATCH: units of a register buffer;
+// UP_TILES, DOWN_TILES: tiles of 16 columns that a wave takes with the same activations
+// (4-bit weights are a quarter of the bytes, and with one tile the activations' loads,
+// not the weights', bound them: 86 and 58 us for six tokens of wide experts); UP_WAVES,
 // DOWN_WAVES: waves per SIMD, by registers.
-struct FmtBf16 {
-    typedef uint16_t Act;
-    static constexpr int UK = 64, LD = 2, PARTS = 2, BATCH = 2;
-    static constexpr bool PAIRS = true;
-    static constexpr int UP_TILES = 1, DOWN_TILES = 1, UP_WAVES = 4, DOWN_WAVES = 3;
-    struct Stack { const uint16_t* w; };
-    struct Rows {
-        const uint16_t* w;
-        Rows() = default;
-        __device__ __forceinline__ Rows(const Stack& st, int64_t first, int K) : w(st.w + first * K) {}
-    };
-    struct X {
-        v4u x[LD];
-        template <bool RAGGED>
-        __device__ __forceinline__ void load(const Act* base, uint32_t row, int k, int K, int q) {
-#pragma unroll
-            for (int u = 0; u < LD; ++u) x[u] = load_at(base, row + 2 * (RAGGED ? min(k + u * 32 + q * 8, K - 8) : k + u * 32 + q * 8));
-        }
-        __device__ __forceinline__ void tail(int k, int K, int q) {
-#pragma unroll
-            for (int u = 0; u < LD; ++u) x[u] &= k + u * 32 + q * 8 < K ? ~0u : 0u;
-        }
-    };
-    struct Unit {
-        X w;
-        template <bool RAGGED>
-        __device__ __forceinline__ void load(const Rows& rows, int r, int k, int K, int q) {
-            w.template load<RAGGED>(rows.w, (uint32_t)(r * K) * 2, k, K, q);
-        }
-        __device__ __forceinline__ void tail(int k, int K, int q) { w.tail(k, K, q); }
-    };
-    template <int NM, int NP>
-    __device__ static __forceinline__ void multiply(f32x4 (&tot)[NM], const Unit (&w)[NM], const X (&x)[NP],
-                                                    const Stack&) {
-#pragma unroll
-        for (int u = 0; u < LD; ++u)
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
-#pragma unroll
-                for (int m = 0; m < NM; ++m) tot[m] = mfma16(x[p].x[u], w[m].w.x[u], tot[m]);
-    }
-};
 
-struct FmtF32 {
-    typedef float Act;
-    static constexpr int UK = 32, LD = 2, PARTS = 1, BATCH = 2;
-    static constexpr bool PAIRS = true;
+// bf16 and fp32 weights: 16 bytes of a row are EPC columns
+template <typename ActT>
+struct FmtPlain {
+    typedef ActT Act;
+    static constexpr bool kBf16 = sizeof(Act) == 2;
+    static constexpr int EPC = 16 / sizeof(Act), LD = 2, UK = 4 * EPC * LD, PARTS = kBf16 ? 2 : 1, BATCH = 2;
+    static constexpr bool PAIRS = true, X_IN_LDS = false;
     static constexpr int UP_TILES = 1, DOWN_TILES = 1, UP_WAVES = 4, DOWN_WAVES = 3;
-    struct Stack { const float* w; };
-    struct Rows {
-        const float* w;
-        Rows() = default;
-        __device__ __forceinline__ Rows(const Stack& st, int64_t first, int K) : w(st.w + first * K) {}
+    struct Stack {
+        const Act* w;
+        bool has_zeros;  // (no meaning here)
+    };
+    template <int NR>
+    struct Place {
+        const Act* w[NR];
+        uint32_t row;  // the lane's row, in bytes
+        __device__ __forceinline__ void set(const Stack& s0, const Stack& s1, int64_t first, int left, int K, int r16, int) {
+            w[0] = s0.w + first * K;
+            if constexpr (NR == 2) w[NR - 1] = s1.w + first * K;
+            row = (uint32_t)(min(r16, left - 1) * K) * sizeof(Act);
+        }
     };
     struct X {
         v4u x[LD];
         template <bool RAGGED>
-        __device__ __forceinline__ void load(const Act* base, uint32_t row, int k, int K, int q) {
+        __device__ __forceinline__ void load(const void* base, uint32_t row, int k, int K, int q) {
 #pragma unroll
-            for (int u = 0; u < LD; ++u) x[u] = load_at(base, row + 4 * (RAGGED ? min(k + u * 16 + q * 4, K - 4) : k + u * 16 + q * 4));
+            for (int u = 0; u < LD; ++u) {
+                const int col = k + (u * 4 + q) * EPC;
+                x[u] = load_at(base, row + sizeof(Act) * (RAGGED ? min(col, K - EPC) : col));
+            }
         }
         __device__ __forceinline__ void tail(int k, int K, int q) {
 #pragma unroll
-            for (int u = 0; u < LD; ++u) x[u] &= k + u * 16 + q * 4 < K ? ~0u : 0u;
+            for (int u = 0; u < LD; ++u) x[u] &= k + (u * 4 + q) * EPC < K ? ~0u : 0u;
         }
     };
-    struct Unit {
-        X w;
-        template <bool RAGGED>
-        __device__ __forceinline__ void load(const Rows& rows, int r, int k, int K, int q) {
-            w.template load<RAGGED>(rows.w, (uint32_t)(r * K) * 4, k, K, q);
+    template <int NM>
+    struct Set {
+        X w[NM];
+        template <bool RAGGED, int NR>
+        __device__ __forceinline__ void load(const Place<NR>& at, int k, int K, int q) {
+            static_assert(NM == NR, "one tile of each matrix");
+#pragma unroll
+            for (int m = 0; m < NM; ++m) w[m].template load<RAGGED>(at.w[m], at.row, k, K, q);
         }
-        __device__ __forceinline__ void tail(int k, int K, int q) { w.tail(k, K, q); }
+        __device__ __forceinline__ void tail(int k, int K, int q) {
+#pragma unroll
+            for (int m = 0; m < NM; ++m) w[m].tail(k, K, q);
+        }
     };
     template <int NM, int NP>
-    __device__ static __forceinline__ void multiply(f32x4 (&tot)[NM], const Unit (&w)[NM], const X (&x)[NP],
-                                                    const Stack&) {
-        static_assert(NP == 1, "fp32 activations are whole");
+    __device__ static __forceinline__ void multiply(f32x4 (&tot)[NM], const Set<NM>& w, const X (&x)[NP], bool) {
 #pragma unroll
         for (int u = 0; u < LD; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int p = 0; p < NP; ++p) {
+                if constexpr (kBf16) {
 #pragma unroll
-                for (int m = 0; m < NM; ++m)
-                    tot[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[0].x[u][j]),
-                                                                  __uint_as_float(w[m].w.x[u][j]), tot[m], 0, 0, 0);
+                    for (int m = 0; m < NM; ++m) tot[m] = mfma16(x[p].x[u], w.w[m].x[u], tot[m]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int m = 0; m < NM; ++m)
+                            tot[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                                __uint_as_float(x[p].x[u][j]), __uint_as_float(w.w[m].x[u][j]), tot[m], 0, 0, 0);
+                }
+            }
     }
 };
+typedef FmtPlain<uint16_t> FmtBf16;
+typedef FmtPlain<float> FmtF32;
 
 template <int GROUP>
 struct FmtW4 {
     typedef uint16_t Act;
     static constexpr int UK = kW4Unit, LD = UK / 32, PARTS = 2, BATCH = 1;
-    static constexpr bool PAIRS = false;
+    static constexpr bool PAIRS = false, X_IN_LDS = true;
     static constexpr int UP_TILES = 2, DOWN_TILES = 4, UP_WAVES = 2, DOWN_WAVES = 2;
     static constexpr int NG = W4Unit<GROUP>::NG, STEPS = GROUP / 32;
     typedef W4Stack Stack;
-    typedef W4Rows<GROUP> Rows;
+    template <int NR>
+    using Place = W4Place<GROUP, NR>;
     struct X {
         v4u x[LD];
         template <bool RAGGED>
-        __device__ __forceinline__ void load(const Act* base, uint32_t row, int k, int K, int q) {
+        __device__ __forceinline__ void load(const void* base, uint32_t row, int k, int K, int q) {
 #pragma unroll
             for (int u = 0; u < LD; ++u)
                 x[u] = load_at(base, row + 2 * (RAGGED ? min(k + u * 32 + q * 8, K - 8) : k + u * 32 + q * 8));
@@ -256,30 +244,28 @@ struct FmtW4 {
             for (int u = 0; u < LD; ++u) x[u] &= k + u * 32 + q * 8 < K ? ~0u : 0u;
         }
     };
-    struct Unit {
+    template <int NM>
+    struct Set {
         W4Unit<GROUP> w;
-        template <bool RAGGED>
-        __device__ __forceinline__ void load(const Rows& rows, int r, int k, int K, int q) {
-            w.load(rows, r, k / kW4Unit, K, q);
+        template <bool RAGGED, int NR>
+        __device__ __forceinline__ void load(const Place<NR>& at, int k, int K, int q) {
+            static_assert(NM == 4, "four tiles");
+            w.load(at, k / kW4Unit, K, q);
         }
         __device__ __forceinline__ void tail(int, int, int) { w.settle(); }  // (codes are finite)
     };
     template <int NM, int NP>
-    __device__ static __forceinline__ void multiply(f32x4 (&tot)[NM], const Unit (&w)[NM], const X (&x)[NP],
-                                                    const Stack& st) {
+    __device__ static __forceinline__ void multiply(f32x4 (&tot)[NM], const Set<NM>& w, const X (&x)[NP], bool has_zeros) {
         const v4u ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-        v4u c[2][NM];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int m = 0; m < NM; ++m) c[h][m] = w4_transpose(w[m].w.codes[h]);
+        const W4Spread<GROUP> groups(w.w);
+        v4u c[NM];
         // A group is scaled while the next one is multiplied. (The fences keep the
         // compiler from running more groups side by side than there are registers.)
         f32x4 acc[2][NM], xs[2];
         auto flush = [&](int g) __attribute__((always_inline)) {
 #pragma unroll
             for (int m = 0; m < NM; ++m) {
-                const float sc = w[m].w.scale(g), off = w[m].w.offset(st.has_zeros, g);
+                const float sc = groups.scale(m, g), off = groups.offset(has_zeros, m, g);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     tot[m][i] = fmaf(sc, fmaf(-off, xs[g & 1][i], acc[g & 1][m][i]), tot[m][i]);
@@ -293,9 +279,13 @@ struct FmtW4 {
             for (int m = 0; m < NM; ++m) acc[g & 1][m] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int u = g * STEPS; u < (g + 1) * STEPS; ++u) {
+                if (u % 4 == 0) {
+#pragma unroll
+                    for (int m = 0; m < NM; ++m) c[m] = w4_transpose(w.w.codes[m][u / 4]);
+                }
                 v4u b[NM];
 #pragma unroll
-                for (int m = 0; m < NM; ++m) b[m] = w4_unpack(c[u / 4][m][u % 4]);
+                for (int m = 0; m < NM; ++m) b[m] = w4_unpack(c[m][u % 4]);
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
                     const v4u a = w4_order(x[p].x[u]);
@@ -315,11 +305,16 @@ struct FmtW4 {
 // become a load through a chosen address, which waits for every load before it)
 template <typename T>
 __device__ __forceinline__ T pick(bool first, T a, T b) { return first ? a : b; }
+template <typename Act>
+__device__ __forceinline__ typename FmtPlain<Act>::Stack pick_stack(bool first, typename FmtPlain<Act>::Stack a,
+                                                                    typename FmtPlain<Act>::Stack b) {
+    return {pick(first, a.w, b.w), false};
+}
 __device__ __forceinline__ FmtBf16::Stack pick(bool first, FmtBf16::Stack a, FmtBf16::Stack b) {
-    return {pick(first, a.w, b.w)};
+    return pick_stack<uint16_t>(first, a, b);
 }
 __device__ __forceinline__ FmtF32::Stack pick(bool first, FmtF32::Stack a, FmtF32::Stack b) {
-    return {pick(first, a.w, b.w)};
+    return pick_stack<float>(first, a, b);
 }
 __device__ __forceinline__ W4Stack pick(bool first, W4Stack a, W4Stack b) {
     return {pick(first, a.codes, b.codes), pick(first, a.scales, b.scales), pick(first, a.zeros, b.zeros),
@@ -427,7 +422,7 @@ __device__ __forceinline__ void stream_steps(int n, LoadW load_w, LoadX load_x, 
 
 template <class F, int NM>
 struct FewW {
-    typename F::Unit w[F::BATCH][NM];
+    typename F::template Set<NM> w[F::BATCH];
 };
 template <class F, int NP>
 struct FewX {
@@ -465,16 +460,27 @@ struct UpItem {
 };
 
 // RAGGED: d is not whole units, or they do not go evenly over the waves' buffers
-template <class F, bool RAGGED>
+// X_LDS: the tokens are kept in LDS (up to kXBytes of them)
+constexpr int kXPad = 16;  // bytes between the rows there, so that they start on other banks
+constexpr int kXBytes = 16 * (2 * 2048 + kXPad);
+template <class F, bool RAGGED, bool X_LDS>
 __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewParams<F> p) {
     constexpr int WAVES = kUpThreads / 64, BATCH = F::BATCH, TILES = F::UP_TILES, COLS = TILES * kFewCols;
     __shared__ __align__(16) f32x4 part[2][2 * TILES][WAVES][64];  // [parity of the item][matrix, tile]
     __shared__ SelectSmem sm;
+    __shared__ __align__(16) char x_lds[X_LDS ? kXBytes : 16];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int r16 = lane & 15, q = lane >> 4;
     const int T = p.T, k = p.k, d = p.d, f = p.f, fs = p.fs;
     const int sh_tiles = ceil_div(fs, COLS), tiles = ceil_div(f, COLS);
 
+    if constexpr (X_LDS) {
+        const int nch = d * (int)sizeof(typename F::Act) / 16;
+        for (int i = tid; i < T * nch; i += kUpThreads) {
+            const int t = i / nch;
+            *(v4u*)(x_lds + t * (nch * 16 + kXPad) + (i - t * nch) * 16) = ((const v4u*)p.x)[i];
+        }
+    }
     // the picks, the reached segments, and where each token's gate of a segment is
     if (tid < kSetWords) sm.reached[tid] = 0;
     for (int i = tid; i < BMOE_MAX_EXPERTS * kFewTok / 2; i += kUpThreads) ((uint32_t*)sm.slot_of)[i] = ~0u;
@@ -511,23 +517,20 @@ __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewPara
     const int items = sh_tiles + members(sm.reached) * tiles;
     __syncthreads();
 
-    const uint32_t xr = (uint32_t)(min(r16, T - 1) * d) * sizeof(typename F::Act);
+    const uint32_t xr = min(r16, T - 1) * (d * (uint32_t)sizeof(typename F::Act) + (X_LDS ? kXPad : 0));
     const int units = ceil_div(d, F::UK), steps = ceil_div(ceil_div(units, WAVES), BATCH);  // steps of an item
     const int wg = scalar(blockIdx.x), wgs = scalar(gridDim.x);
     const int mine = scalar(wg < items ? div_uniform(items - 1 - wg, wgs) + 1 : 0);
     typedef FewW<F, 2 * TILES> W;
     typedef FewX<F, 1> X;
-    // the place of the loads: step l_step of item l_item, whose weight rows are
-    // gate and up (the lane's rows l_row)
-    int l_item = wg, l_step = 0, l_at = 0, l_row[TILES];
-    typename F::Rows gate, up;
+    // the place of the loads: step l_step of item l_item
+    int l_item = wg, l_step = 0, l_at = 0;
+    typename F::template Place<2> rows;  // of W_gate and W_up
     auto enter = [&]() __attribute__((always_inline)) {
         const UpItem it(l_item, COLS, sh_tiles, tiles);
         const int seg = it.shared ? 0 : scalar(sm.segs[it.place]), N = pick(it.shared, fs, f);
-        gate = typename F::Rows(pick(it.shared, p.up_sh[0], p.up[0]), (int64_t)seg * N + it.n0, d);
-        up = typename F::Rows(pick(it.shared, p.up_sh[1], p.up[1]), (int64_t)seg * N + it.n0, d);
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) l_row[t] = min(16 * t + r16, N - 1 - it.n0);
+        rows.set(pick(it.shared, p.up_sh[0], p.up[0]), pick(it.shared, p.up_sh[1], p.up[1]), (int64_t)seg * N + it.n0,
+                 N - it.n0, d, r16, q);
     };
     auto load_w = [&](W& b, int at) __attribute__((always_inline)) {
         if (at != l_at) {
@@ -542,11 +545,7 @@ __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewPara
         for (int i = 0; i < BATCH; ++i) {
             int u = wave + WAVES * (BATCH * l_step + i);
             if constexpr (RAGGED) u = min(u, units - 1);
-#pragma unroll
-            for (int t = 0; t < TILES; ++t) {
-                b.w[i][2 * t].template load<RAGGED>(gate, l_row[t], u * F::UK, d, q);
-                b.w[i][2 * t + 1].template load<RAGGED>(up, l_row[t], u * F::UK, d, q);
-            }
+            b.w[i].template load<RAGGED>(rows, u * F::UK, d, q);
         }
     };
     f32x4 tot[2 * TILES];
@@ -563,7 +562,7 @@ __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewPara
         for (int i = 0; i < BATCH; ++i) {
             int u = wave + WAVES * (BATCH * x_step + i);
             if constexpr (RAGGED) u = min(u, units - 1);
-            b.x[i][0].template load<RAGGED>(p.x, xr, u * F::UK, d, q);
+            b.x[i][0].template load<RAGGED>(X_LDS ? (const void*)x_lds : (const void*)p.x, xr, u * F::UK, d, q);
         }
     };
     auto multiply = [&](W& b, X& x) __attribute__((always_inline)) {
@@ -571,11 +570,10 @@ __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewPara
         for (int i = 0; i < BATCH; ++i) {
             if constexpr (RAGGED) {
                 const int kk = (wave + WAVES * (BATCH * step + i)) * F::UK;
-#pragma unroll
-                for (int m = 0; m < 2 * TILES; ++m) b.w[i][m].tail(kk, d, q);
+                b.w[i].tail(kk, d, q);
                 x.x[i][0].tail(kk, d, q);
             }
-            F::multiply(tot, b.w[i], x.x[i], p.up[0]);
+            F::multiply(tot, b.w[i], x.x[i], p.up[0].has_zeros);
         }
         if (++step < steps) return;
         step = 0;
@@ -660,9 +658,6 @@ __global__ __launch_bounds__(kDownThreads, F::DOWN_WAVES) void few_down_kernel(F
     const int first = (wg - tile * p.split) * WAVES + wave, stride = p.split * WAVES;
     const int steps = ceil_div(div_uniform(units + stride - 1, stride), BATCH);
     const int token = PACK ? r16 & 7 : r16;
-    int wr[TILES];
-#pragma unroll
-    for (int m = 0; m < TILES; ++m) wr[m] = min(16 * m + r16, d - 1 - n0);
     typedef FewW<F, TILES> W;
     typedef FewX<F, NP> X;
     DownUnit lu{0, 0}, xu, mu;  // of the weights' loads, the activations' and the products
@@ -680,10 +675,10 @@ __global__ __launch_bounds__(kDownThreads, F::DOWN_WAVES) void few_down_kernel(F
             // (past the last unit: the first one again, its products are dropped)
             const bool past = lu.a == segments && lu.k >= per_sh, sh = lu.a == segments && !past;
             const int seg = sh ? 0 : scalar(segs[past ? 0 : lu.a]), width = pick(sh, fs, f);
-            const typename F::Rows rows(pick(sh, p.down_sh, p.down), (int64_t)seg * d + n0, width);
-#pragma unroll
-            for (int m = 0; m < TILES; ++m)
-                b.w[i][m].template load<RAGGED>(rows, wr[m], past ? 0 : lu.k * F::UK, width, q);
+            typename F::template Place<1> rows;
+            const typename F::Stack st = pick(sh, p.down_sh, p.down);
+            rows.set(st, st, (int64_t)seg * d + n0, d - n0, width, r16, q);
+            b.w[i].template load<RAGGED>(rows, past ? 0 : lu.k * F::UK, width, q);
         }
     };
     auto load_x = [&](X& b, int at) __attribute__((always_inline)) {
@@ -713,15 +708,14 @@ __global__ __launch_bounds__(kDownThreads, F::DOWN_WAVES) void few_down_kernel(F
             const bool past = mu.a == segments && mu.k >= per_sh;
             if constexpr (RAGGED) {
                 const int kk = mu.k * F::UK, width = pick(mu.a == segments, fs, f);
-#pragma unroll
-                for (int m = 0; m < TILES; ++m) b.w[i][m].tail(kk, width, q);
+                b.w[i].tail(kk, width, q);
 #pragma unroll
                 for (int j = 0; j < NP; ++j) x.x[i][j].tail(kk, width, q);
             }
             f32x4 acc[TILES];
 #pragma unroll
             for (int m = 0; m < TILES; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
-            F::multiply(acc, b.w[i], x.x[i], p.down);
+            F::multiply(acc, b.w[i], x.x[i], p.down.has_zeros);
             // only the tokens that call the segment take its products
             const uint32_t who = past ? 0u : callers[mu.a];
 #pragma unroll
@@ -853,8 +847,15 @@ hipError_t launch_few_t(const FewArgs& a, ToStack st, hipStream_t s) {
     const dim3 up((unsigned)(items < room ? items : room)), down((unsigned)(ceil_div(a.d, kDownCols) * p.split));
     const bool up_ragged = a.d % (F::UK * F::BATCH * (kUpThreads / 64)) != 0;
     const bool down_ragged = a.f % F::UK != 0 || a.fs % F::UK != 0;
-    if (up_ragged) hipLaunchKernelGGL((few_up_kernel<F, true>), up, dim3(kUpThreads), 0, s, p);
-    else hipLaunchKernelGGL((few_up_kernel<F, false>), up, dim3(kUpThreads), 0, s, p);
+    const bool x_fits = F::X_IN_LDS && (int64_t)a.T * (a.d * (int)sizeof(Act) + kXPad) <= kXBytes;
+    auto go_up = [&](auto kernel) { hipLaunchKernelGGL(kernel, up, dim3(kUpThreads), 0, s, p); };
+    if (x_fits) {
+        if (up_ragged) go_up(few_up_kernel<F, true, F::X_IN_LDS>);
+        else go_up(few_up_kernel<F, false, F::X_IN_LDS>);
+    } else {
+        if (up_ragged) go_up(few_up_kernel<F, true, false>);
+        else go_up(few_up_kernel<F, false, false>);
+    }
     constexpr bool kParts = F::PARTS == 2;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, down, dim3(kDownThreads), 0, s, p); };
     if (kParts && a.T <= 8) {

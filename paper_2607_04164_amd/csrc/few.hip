@@ -78,9 +78,9 @@ hipError_t launch_few(const FewArgs& a, hipStream_t s) {
     if (a.w.group) return launch_few_w4(a, s);
     if (a.dtype == BMOE_BF16)
         return launch_few_t<FmtBf16>(
-            a, [](const bmoe_matrix& m, int64_t, int) { return FmtBf16::Stack{(const uint16_t*)m.w}; }, s);
+            a, [](const bmoe_matrix& m, int64_t, int) { return FmtBf16::Stack{(const uint16_t*)m.w, false}; }, s);
     return launch_few_t<FmtF32>(
-        a, [](const bmoe_matrix& m, int64_t, int) { return FmtF32::Stack{(const float*)m.w}; }, s);
+        a, [](const bmoe_matrix& m, int64_t, int) { return FmtF32::Stack{(const float*)m.w, false}; }, s);
 }
 
 }  // namespace bmoe

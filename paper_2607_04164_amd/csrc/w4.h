@@ -8,14 +8,17 @@
 // costs about 5 times the rounding of the plain sum (16 + q against q - z), far
 // below the bf16 output's.
 //
-// A wave owns 16 rows of W (the B operand) and up to TILES tiles of 16
-// activation rows (the A operand). It takes the columns in units of 256, a 128-byte
-// line of each row: lane (r, q) loads the 16 bytes of columns 32q .. 32q+31 and of
+// A wave owns MT = 4 tiles of 16 rows of W (the B operands; of one matrix, or two of
+// each of two; where that makes too few workgroups, one tile of each matrix) and one
+// or two tiles of 16 activation rows (the A operands). It takes the columns in units
+// of 256, a 128-byte line of each row: lane (r, q) loads the 16 bytes of columns 32q .. 32q+31 and of
 // 128 + 32q .., row r. Two exchanges of lane rows then give step u of a half (one
 // MFMA of 32 columns) the columns 32u .. 32u+31, eight of them in each lane, so that
 // a group of 32 is one step. In a lane the eight codes come out as columns
-// 0,4,1,5,2,6,3,7; the activations are put into the same order (w4_order). A unit's
-// scales are one load of each lane, and so are its zero points.
+// 0,4,1,5,2,6,3,7; the activations are put into the same order (w4_order). The scales
+// of a unit are one load: lane row q brings those of tile q, and three exchanges hand
+// them to all lanes; the zero points likewise. (Loads are what is scarce: an
+// instruction of 64 lanes takes 16 cycles of the address unit however little it brings.)
 #pragma once
 
 #include "bmoe_common.h"
@@ -76,24 +79,6 @@ __device__ __forceinline__ v4u load_at(const void* base, uint32_t off) {
     return *(const v4u*)((const char*)base + off);
 }
 
-// 16 rows of a stack (fewer at its end), from row `first` on
-template <int GROUP>
-struct W4Rows {
-    static constexpr int NG = kW4Unit / GROUP;
-    const uint8_t* codes;
-    const uint16_t* scales;
-    const uint8_t* zeros;
-    int last;  // the place of the stack's last NG groups, from the first row's first
-    W4Rows() = default;
-    __device__ __forceinline__ W4Rows(const W4Stack& w, int64_t first, int K) {
-        const int64_t j = first * ceil_div(K, GROUP);
-        codes = w.codes + first * BMOE_W4_ROW_BYTES(K);
-        scales = w.scales + j;
-        zeros = w.zeros + j;
-        last = (int)(w.groups - NG - j < 0x7fffffff ? w.groups - NG - j : 0x7fffffff);
-    }
-};
-
 // N bytes of group values from any address
 template <int N>
 struct W4Groups {
@@ -116,30 +101,80 @@ struct W4Groups {
     }
 };
 
-// A unit of one lane's W row: 256 columns' codes (the lane's 64 of them) and the
-// unit's groups, without a branch (zeros are loaded where there are none too). Rows
-// of groups have any alignment.
-template <int GROUP>
+// MT tiles of 16 rows: of NR stacks, from row `first` of each on, `left` rows there
+// (at least 8). Tile m is rows 16 (m / NR) .. of stack m % NR.
+template <int GROUP, int NR, int MT = 4>
+struct W4Place {
+    static constexpr int NG = kW4Unit / GROUP;
+    const uint8_t* codes[NR];  // the first row
+    uint32_t row[MT / NR];     // the lane's row of a tile, in bytes
+    const uint16_t* scales;    // the lane's row of tile q % MT
+    const uint8_t* zeros;
+    int last;                  // from there: the stack's last NG groups
+
+    __device__ __forceinline__ void set(const W4Stack& s0, const W4Stack& s1, int64_t first, int left, int K, int r16, int q) {
+        const int pitch = BMOE_W4_ROW_BYTES(K), ng = ceil_div(K, GROUP);
+        codes[0] = s0.codes + first * pitch;
+        if constexpr (NR == 2) codes[NR - 1] = s1.codes + first * pitch;
+#pragma unroll
+        for (int t = 0; t < MT / NR; ++t) row[t] = (uint32_t)(min(16 * t + r16, left - 1) * pitch);
+        const bool second = NR == 2 && (q & 1);
+        const int64_t j = (first + min(16 * (q % MT / NR) + r16, left - 1)) * ng;
+        scales = (second ? s1.scales : s0.scales) + j;
+        zeros = (second ? s1.zeros : s0.zeros) + j;
+        const int64_t rest = s0.groups - NG - j;
+        last = (int)(rest < 0x7fffffff ? rest : 0x7fffffff);
+    }
+};
+
+// out[i]: lane row i's value in every lane row, where row q has the value of q % MT
+template <int MT>
+__device__ __forceinline__ void w4_spread(uint32_t v, uint32_t (&out)[MT]) {
+    typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+    out[0] = v;
+    if constexpr (MT == 2) {
+        const v2u a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        out[0] = a[0];
+        out[MT - 1] = a[1];
+    }
+    if constexpr (MT != 4) return;
+    const v2u a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    const v2u b = __builtin_amdgcn_permlane16_swap(a[0], a[0], false, false);
+    const v2u c = __builtin_amdgcn_permlane16_swap(a[1], a[1], false, false);
+    out[0] = b[0];
+    out[MT > 1 ? 1 : 0] = b[1];
+    out[MT > 2 ? 2 : 0] = c[0];
+    out[MT > 3 ? 3 : 0] = c[1];
+}
+
+// A unit of the tiles: 256 columns' codes (the lane's 64 of them) and the unit's
+// groups, without a branch (zeros are loaded where there are none too). Rows of groups
+// have any alignment.
+template <int GROUP, int MT = 4>
 struct W4Unit {
     static constexpr int NG = kW4Unit / GROUP;
-    v4u codes[2];
-    W4Groups<2 * NG> s;
-    W4Groups<NG> z;
+    typedef W4Groups<2 * NG> Scales;
+    typedef W4Groups<NG> Zeros;
+    v4u codes[MT][2];
+    Scales s;  // of tile q % MT
+    Zeros z;
     int back;  // groups that s and z start before the unit's first one
 
-    // unit c of row r of the rows; K columns
-    __device__ __forceinline__ void load(const W4Rows<GROUP>& w, int r, int c, int K, int q) {
-        const int pitch = BMOE_W4_ROW_BYTES(K), ng = ceil_div(K, GROUP);
+    template <int NR>
+    __device__ __forceinline__ void load(const W4Place<GROUP, NR, MT>& w, int c, int K, int q) {
+        const int pitch = BMOE_W4_ROW_BYTES(K);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            codes[h] = load_at(w.codes, (uint32_t)(r * pitch + min(128 * c + 64 * h + 16 * q, pitch - 16)));
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                codes[m][h] = load_at(w.codes[m % NR], w.row[m / NR] + min(128 * c + 64 * h + 16 * q, pitch - 16));
         // Groups past the row's last one are another row's: their activations are
         // zero. A unit that would reach past the stack's end starts further back (a
         // stack has at least 8 rows).
-        const int j = r * ng + c * NG, from = min(j, w.last);
-        back = j - from;
-        s.load((const char*)w.scales + (uint32_t)(from * 2));
-        z.load(w.zeros + (uint32_t)from);
+        const int from = min(c * NG, w.last);
+        back = c * NG - from;
+        s.load(w.scales + from);
+        z.load(w.zeros + from);
     }
     // moves the groups to their places: after the load, where K is not whole units
     __device__ __forceinline__ void settle() {
@@ -150,12 +185,25 @@ struct W4Unit {
                 z.template drop<8>();
             }
     }
-    __device__ __forceinline__ float scale(int g) const {
-        return __uint_as_float(g & 1 ? s.v[g >> 1] & 0xffff0000u : s.v[g >> 1] << 16);
+};
+
+// the groups of all tiles, in every lane of their rows
+template <int GROUP, int MT = 4>
+struct W4Spread {
+    static constexpr int NG = kW4Unit / GROUP;
+    uint32_t s[(2 * NG + 3) / 4][MT], z[(NG + 3) / 4][MT];
+    __device__ __forceinline__ explicit W4Spread(const W4Unit<GROUP, MT>& u) {
+#pragma unroll
+        for (int i = 0; i < (2 * NG + 3) / 4; ++i) w4_spread<MT>(u.s.v[i], s[i]);
+#pragma unroll
+        for (int i = 0; i < (NG + 3) / 4; ++i) w4_spread<MT>(u.z.v[i], z[i]);
+    }
+    __device__ __forceinline__ float scale(int m, int g) const {
+        return __uint_as_float(g & 1 ? s[g >> 1][m] & 0xffff0000u : s[g >> 1][m] << 16);
     }
     // 16 + the zero point of group g
-    __device__ __forceinline__ float offset(bool has_zeros, int g) const {
-        return has_zeros ? 16.f + (float)((z.v[g >> 2] >> (8 * (g & 3))) & 0xffu) : 24.f;
+    __device__ __forceinline__ float offset(bool has_zeros, int m, int g) const {
+        return has_zeros ? 16.f + (float)((z[g >> 2][m] >> (8 * (g & 3))) & 0xffu) : 24.f;
     }
 };
 

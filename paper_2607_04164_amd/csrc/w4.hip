@@ -1,24 +1,23 @@
 // Weights in 4 bits with group scales: the quantizer and the grouped products
 // of few rows (see w4.h for the arithmetic).
 //
-// One workgroup (8 waves) takes up to 32 rows of a segment (a pass) and 16 output
-// columns; its waves split K by units of 256 columns. The passes of a segment run side
-// by side: a loop over them inside a workgroup would make the longest segment's time
-// the kernel's. Their weights meet in the L2 cache (column blocks of a multiple of 8
-// keep them on one XCD). A wave loads WB units of weights, then takes their
-// columns step by step; the activations of the next XS steps (from the L2 cache) are
-// loaded while these are multiplied. The waves' partial tiles are added through LDS
-// in wave order.
+// One workgroup takes up to 32 rows of a segment (a pass) and four tiles of 16 weight
+// rows: 32 columns of a gated product (both matrices), 64 of a plain one. Its waves
+// split K by units of 256 columns. The passes of a segment run side by side: a loop over
+// them inside a workgroup would make the longest segment's time the kernel's. Their
+// weights meet in the L2 cache (column blocks of a multiple of 8 keep them on one XCD).
+// A wave loads a unit of weights, then takes its columns step by step; the activations
+// of the next steps (from the L2 cache) are loaded while these are multiplied. The
+// waves' partial tiles are added through LDS in wave order.
 #include "bmoe_common.h"
 #include "w4.h"
 
 namespace bmoe {
 namespace {
 
-constexpr int kW4Threads = 512;
-constexpr int kW4Waves = kW4Threads / 64;
-constexpr int kW4Cols = 16;
 constexpr int kW4Tiles = 2;  // tiles of 16 rows per pass
+constexpr int kW4Rows = 16 * kW4Tiles;
+constexpr int w4_waves(int mt) { return mt == 1 ? 16 : 8; }  // per workgroup
 
 struct W4Params {
     const uint16_t* A;  // [rows_cap or a_count, K]
@@ -31,85 +30,77 @@ struct W4Params {
 };
 
 // One pass: rows m0 .. m0 + 16 * TILES - 1 (fewer: the segment's last), this wave's
-// units. RAGGED: K is not whole units; WB > 1 needs units that go evenly over the waves.
-template <bool GATED, int GROUP, int TILES, int WB, bool RAGGED>
-__device__ __forceinline__ void w4_pass(const W4Params& p, const W4Rows<GROUP>& rows0, const W4Rows<GROUP>& rows1, int wrow,
-                                        int m0, int end, int wave, int r16, int q, f32x4 (*part)[64]) {
-    constexpr int NMAT = GATED ? 2 : 1, GS = GROUP / 32;
-    constexpr int XS = 4 / TILES, NX = WB * 8 / XS;
+// units. RAGGED: K is not whole units.
+template <int NR, int MT, int GROUP, int TILES, bool RAGGED>
+__device__ __forceinline__ void w4_pass(const W4Params& p, const W4Place<GROUP, NR, MT>& place, int m0, int end, int wave,
+                                        int r16, int q, f32x4 (*part)[64]) {
+    constexpr int GS = GROUP / 32, XS = 4 / TILES, NX = 8 / XS;
     const int K = p.K, units = ceil_div(K, kW4Unit);
     const v4u ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-    const uint16_t* xp[TILES];
+    int row[TILES];  // (gathered while the first weights are loaded)
 #pragma unroll
-    for (int nt = 0; nt < TILES; ++nt) {
-        const int r = min(m0 + nt * 16 + r16, end - 1);
-        xp[nt] = p.A + (size_t)gathered_row(p.a_rows, p.a_count, r) * K;
-    }
-    f32x4 tot[NMAT][TILES];
+    for (int nt = 0; nt < TILES; ++nt) row[nt] = gathered_row(p.a_rows, p.a_count, min(m0 + nt * 16 + r16, end - 1));
+    f32x4 tot[MT][TILES];
 #pragma unroll
-    for (int m = 0; m < NMAT; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int nt = 0; nt < TILES; ++nt) tot[m][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int u0 = wave; u0 < units; u0 += kW4Waves * WB) {
+    for (int unit = wave; unit < units; unit += w4_waves(MT)) {
         v4u x[2][XS][TILES];
         auto load_x = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
             for (int j = 0; j < XS; ++j) {
-                const int step = i * XS + j;
-                int col = (u0 + kW4Waves * (step / 8)) * kW4Unit + (step % 8) * 32 + q * 8;
+                int col = unit * kW4Unit + (i * XS + j) * 32 + q * 8;
                 if constexpr (RAGGED) col = min(col, K - 8);
 #pragma unroll
-                for (int nt = 0; nt < TILES; ++nt) x[i & 1][j][nt] = *(const v4u*)(xp[nt] + col);
+                for (int nt = 0; nt < TILES; ++nt) x[i & 1][j][nt] = *(const v4u*)(p.A + (size_t)row[nt] * K + col);
             }
         };
+        W4Unit<GROUP, MT> w;
+        w.load(place, unit, K, q);
+        __builtin_amdgcn_sched_barrier(0);
         load_x(0);
-        W4Unit<GROUP> w[WB][NMAT];
-#pragma unroll
-        for (int b = 0; b < WB; ++b)
-#pragma unroll
-            for (int m = 0; m < NMAT; ++m) w[b][m].load(m ? rows1 : rows0, wrow, u0 + kW4Waves * b, K, q);
-        f32x4 acc[NMAT][TILES], xs[TILES];
-        v4u c[NMAT];
+        load_x(1);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (RAGGED) w.settle();
+        const W4Spread<GROUP, MT> groups(w);
+        f32x4 acc[MT][TILES], xs[TILES];
+        v4u c[MT];
 #pragma unroll
         for (int i = 0; i < NX; ++i) {
-            __builtin_amdgcn_sched_barrier(0);
-            if (i + 1 < NX) load_x(i + 1);
-            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < XS; ++j) {
-                const int step = i * XS + j, b = step / 8, s8 = step % 8, g = s8 / GS;
-                if (s8 == 0 && RAGGED) {
+                const int step = i * XS + j, g = step / GS;
+                if (step % 4 == 0) {
 #pragma unroll
-                    for (int m = 0; m < NMAT; ++m) w[b][m].settle();
+                    for (int m = 0; m < MT; ++m) c[m] = w4_transpose(w.codes[m][step / 4]);
                 }
-                if (s8 % 4 == 0) {
-#pragma unroll
-                    for (int m = 0; m < NMAT; ++m) c[m] = w4_transpose(w[b][m].codes[s8 / 4]);
-                }
-                if (s8 % GS == 0) {
+                if (step % GS == 0) {
 #pragma unroll
                     for (int nt = 0; nt < TILES; ++nt) {
                         xs[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int m = 0; m < NMAT; ++m) acc[m][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        for (int m = 0; m < MT; ++m) acc[m][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
                     }
                 }
-                v4u wv[NMAT];
-#pragma unroll
-                for (int m = 0; m < NMAT; ++m) wv[m] = w4_unpack(c[m][s8 % 4]);
+                v4u xv[TILES];
 #pragma unroll
                 for (int nt = 0; nt < TILES; ++nt) {
-                    v4u xv = x[i & 1][j][nt];
-                    if constexpr (RAGGED) xv &= (u0 + kW4Waves * b) * kW4Unit + s8 * 32 + q * 8 < K ? ~0u : 0u;
-                    xv = w4_order(xv);
-                    xs[nt] = mfma16(xv, ones, xs[nt]);
-#pragma unroll
-                    for (int m = 0; m < NMAT; ++m) acc[m][nt] = mfma16(xv, wv[m], acc[m][nt]);
+                    xv[nt] = x[i & 1][j][nt];
+                    if constexpr (RAGGED) xv[nt] &= unit * kW4Unit + step * 32 + q * 8 < K ? ~0u : 0u;
+                    xv[nt] = w4_order(xv[nt]);
+                    xs[nt] = mfma16(xv[nt], ones, xs[nt]);
                 }
-                if (s8 % GS == GS - 1) {
 #pragma unroll
-                    for (int m = 0; m < NMAT; ++m) {
-                        const float sc = w[b][m].scale(g), off = w[b][m].offset(p.w[0].has_zeros, g);
+                for (int m = 0; m < MT; ++m) {
+                    const v4u wv = w4_unpack(c[m][step % 4]);
+#pragma unroll
+                    for (int nt = 0; nt < TILES; ++nt) acc[m][nt] = mfma16(xv[nt], wv, acc[m][nt]);
+                }
+                if (step % GS == GS - 1) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        const float sc = groups.scale(m, g), off = groups.offset(p.w[0].has_zeros, m, g);
 #pragma unroll
                         for (int nt = 0; nt < TILES; ++nt) {
 #pragma unroll
@@ -121,84 +112,82 @@ __device__ __forceinline__ void w4_pass(const W4Params& p, const W4Rows<GROUP>& 
                 }
                 __builtin_amdgcn_sched_barrier(0);  // (registers: no step runs ahead of the one before)
             }
+            if (i + 2 < NX) load_x(i + 2);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     const int lane = r16 + 16 * q;
 #pragma unroll
     for (int nt = 0; nt < TILES; ++nt)
 #pragma unroll
-        for (int m = 0; m < NMAT; ++m) part[(wave * kW4Tiles + nt) * NMAT + m][lane] = tot[m][nt];
+        for (int m = 0; m < MT; ++m) part[(wave * kW4Tiles + nt) * MT + m][lane] = tot[m][nt];
 }
 
-// Finds pass `at` of all segments' passes: its segment and its place among them, or
-// returns the number of passes there are (`at` then past them). One wave's work, the
-// same in every wave.
-__device__ __forceinline__ int find_pass(const int32_t* offsets, int n_seg, int rows_cap, int at, int lane, int* seg,
-                                         int* nth) {
+// inclusive sum over the lanes of a wave
+__device__ __forceinline__ int wave_prefix(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // lane 15 to row 1, lane 47 to row 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2 and 3
+    return v;
+}
+
+struct W4Pass {
+    int seg, beg, end;  // the pass's rows; seg -1: there are fewer passes
+};
+// Pass `at` of all segments' passes. One wave's work, the same in every wave.
+__device__ __forceinline__ W4Pass find_pass(const int32_t* offsets, int n_seg, int rows_cap, int at, int lane) {
     int before = 0;
     for (int base = 0; base < n_seg; base += 64) {
-        int passes = 0;
-        if (base + lane < n_seg) {
-            const int beg = min(max(offsets[base + lane], 0), rows_cap);
-            const int end = min(max(offsets[base + lane + 1], beg), rows_cap);
-            passes = ceil_div(end - beg, 16 * kW4Tiles);
-        }
-        int upto = passes;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int v = __shfl_up(upto, off);
-            if (lane >= off) upto += v;
-        }
-        const unsigned long long past = __ballot(before + upto > at);
+        const int s = min(base + lane, n_seg - 1);
+        const int beg = min(max(offsets[s], 0), rows_cap), end = min(max(offsets[s + 1], beg), rows_cap);
+        const int passes = base + lane < n_seg ? ceil_div(end - beg, kW4Rows) : 0;
+        const int upto = before + wave_prefix(passes);
+        const unsigned long long past = __ballot(upto > at);
         if (past) {
             const int l = __ffsll(past) - 1;
-            *seg = __builtin_amdgcn_readfirstlane(base + l);
-            *nth = __builtin_amdgcn_readfirstlane(at - before - __shfl(upto - passes, l));
-            return -1;
+            const int nth = at - __builtin_amdgcn_readlane(upto - passes, l);
+            const int from = __builtin_amdgcn_readlane(beg, l) + nth * kW4Rows, last = __builtin_amdgcn_readlane(end, l);
+            return {base + l, from, min(from + kW4Rows, last)};
         }
-        before += __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+        before = __builtin_amdgcn_readlane(upto, 63);
     }
-    return before;
+    return {-1, 0, 0};
 }
 
-template <bool GATED, int GROUP, bool RAGGED>
-__global__ __launch_bounds__(kW4Threads, 4) void w4_gemm_kernel(W4Params p) {
-    constexpr int NMAT = GATED ? 2 : 1;
-    __shared__ __align__(16) f32x4 part[kW4Waves * kW4Tiles * NMAT][64];
+template <int NR, int MT, int GROUP, bool RAGGED>
+__global__ __launch_bounds__(64 * w4_waves(MT), w4_waves(MT) / 4) void w4_gemm_kernel(W4Params p) {
+    constexpr int WAVES = w4_waves(MT), COLS = 16 * MT / NR;
+    __shared__ __align__(16) f32x4 part[WAVES * kW4Tiles * MT][64];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int r16 = lane & 15, q = lane >> 4;
     const int K = p.K, N = p.N;
-    const int ncb = ceil_div(N, kW4Cols);
-    for (int64_t at = blockIdx.x;; at += gridDim.x) {  // (a launch that holds all of them makes one turn)
-        const int pass = __builtin_amdgcn_readfirstlane((int)(at / ncb));
-        int s, nth;
-        if (find_pass(p.offsets, p.n_seg, p.rows_cap, pass, lane, &s, &nth) >= 0) return;
-        const int n0 = __builtin_amdgcn_readfirstlane((int)(at - (int64_t)pass * ncb)) * kW4Cols;
-        const int beg = min(max(p.offsets[s], 0), p.rows_cap);
-        const int end = min(max(p.offsets[s + 1], beg), p.rows_cap);
-        const W4Rows<GROUP> rows0(p.w[0], (int64_t)s * N + n0, K), rows1(p.w[NMAT - 1], (int64_t)s * N + n0, K);
-        const int wrow = min(r16, N - 1 - n0);
-        const int m0 = beg + nth * 16 * kW4Tiles, rows = min(end - m0, 16 * kW4Tiles);
-        if (rows > 16) w4_pass<GATED, GROUP, 2, 1, RAGGED>(p, rows0, rows1, wrow, m0, end, wave, r16, q, part);
-        else if (!RAGGED && K % (kW4Unit * kW4Waves * 2) == 0)
-            w4_pass<GATED, GROUP, 1, 2, false>(p, rows0, rows1, wrow, m0, end, wave, r16, q, part);
-        else w4_pass<GATED, GROUP, 1, 1, RAGGED>(p, rows0, rows1, wrow, m0, end, wave, r16, q, part);
+    for (int pass = blockIdx.y;; pass += gridDim.y) {  // (a launch that holds all of them makes one turn)
+        const W4Pass at = find_pass(p.offsets, p.n_seg, p.rows_cap, pass, lane);
+        if (at.seg < 0) return;
+        const int n0 = blockIdx.x * COLS, rows = at.end - at.beg;
+        W4Place<GROUP, NR, MT> place;
+        place.set(p.w[0], p.w[NR - 1], (int64_t)at.seg * N + n0, N - n0, K, r16, q);
+        if (rows > 16) w4_pass<NR, MT, GROUP, 2, RAGGED>(p, place, at.beg, at.end, wave, r16, q, part);
+        else w4_pass<NR, MT, GROUP, 1, RAGGED>(p, place, at.beg, at.end, wave, r16, q, part);
         __syncthreads();
-        // a thread per output of the pass
-        const int row = tid >> 4, col = tid & 15, nt = row >> 4;
-        if (row < rows && n0 + col < N) {
-            const float* d = (const float*)&part[nt * NMAT][((row & 15) >> 2) * 16 + col] + (row & 3);
-            float sum[NMAT];
+        for (int i = tid; i < rows * COLS; i += 64 * WAVES) {
+            const int row = i / COLS, col = i % COLS, nt = row >> 4;
+            // element (row, col & 15) of the tiles of column block col / 16
+            const float* d = (const float*)&part[nt * MT + col / 16 * NR][((row & 15) >> 2) * 16 + (col & 15)] + (row & 3);
+            float sum[NR];
 #pragma unroll
-            for (int m = 0; m < NMAT; ++m) {
+            for (int m = 0; m < NR; ++m) {
                 sum[m] = d[m * 256];
 #pragma unroll
-                for (int w = 1; w < kW4Waves; ++w) sum[m] += d[(w * kW4Tiles * NMAT + m) * 256];
+                for (int w = 1; w < WAVES; ++w) sum[m] += d[(w * kW4Tiles * MT + m) * 256];
             }
             float v;
-            if constexpr (GATED) v = silu_mul(sum[0], sum[NMAT - 1]);
+            if constexpr (NR == 2) v = silu_mul(sum[0], sum[NR - 1]);
             else v = sum[0];
-            p.C[(size_t)(m0 + row) * N + n0 + col] = f32_to_bf16(v);
+            if (n0 + col < N) p.C[(size_t)(at.beg + row) * N + n0 + col] = f32_to_bf16(v);
         }
         __syncthreads();  // the partials are rewritten by the next turn
     }
@@ -270,18 +259,27 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ 
     }
 }
 
-template <bool GATED>
-hipError_t launch_w4(const W4Params& p, int group, hipStream_t s) {
-    // passes: at most one for 32 rows, and one more for the rest of each segment's rows
-    const int64_t passes = (int64_t)p.rows_cap / (16 * kW4Tiles) + (p.n_seg < p.rows_cap ? p.n_seg : p.rows_cap);
-    const int64_t blocks = passes * ceil_div(p.N, kW4Cols), room = (int64_t)1 << 22;
-    const dim3 grid((unsigned)(blocks < room ? blocks : room)), block(kW4Threads);
+template <int NR, int MT>
+hipError_t launch_w4_tiles(const W4Params& p, int group, int64_t passes, hipStream_t s) {
+    const int blocks = ceil_div(p.N, 16 * MT / NR);
+    // (a launch counts its threads in 32 bits, and at most 65535 rows of workgroups)
+    int64_t room = ((int64_t)1 << 21) / blocks;
+    room = room < 1 ? 1 : room > 65535 ? 65535 : room;
+    const dim3 grid((unsigned)blocks, (unsigned)(passes < room ? passes : room)), block(64 * w4_waves(MT));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, p); };
     const bool ragged = p.K % kW4Unit != 0;
-    if (group == 32) ragged ? go(w4_gemm_kernel<GATED, 32, true>) : go(w4_gemm_kernel<GATED, 32, false>);
-    else if (group == 64) ragged ? go(w4_gemm_kernel<GATED, 64, true>) : go(w4_gemm_kernel<GATED, 64, false>);
-    else ragged ? go(w4_gemm_kernel<GATED, 128, true>) : go(w4_gemm_kernel<GATED, 128, false>);
+    if (group == 32) ragged ? go(w4_gemm_kernel<NR, MT, 32, true>) : go(w4_gemm_kernel<NR, MT, 32, false>);
+    else if (group == 64) ragged ? go(w4_gemm_kernel<NR, MT, 64, true>) : go(w4_gemm_kernel<NR, MT, 64, false>);
+    else ragged ? go(w4_gemm_kernel<NR, MT, 128, true>) : go(w4_gemm_kernel<NR, MT, 128, false>);
     return hipGetLastError();
+}
+
+template <int NR>
+hipError_t launch_w4(const W4Params& p, int group, hipStream_t s) {
+    // passes: at most one for 32 rows, and one more for the rest of each segment's rows
+    const int64_t passes = (int64_t)p.rows_cap / kW4Rows + (p.n_seg < p.rows_cap ? p.n_seg : p.rows_cap);
+    if (passes * ceil_div(p.N, 64 / NR) < 256) return launch_w4_tiles<NR, NR>(p, group, passes, s);
+    return launch_w4_tiles<NR, 4>(p, group, passes, s);
 }
 
 }  // namespace
@@ -305,7 +303,7 @@ hipError_t launch_w4_gemm(const W4GemmArgs& a, hipStream_t s) {
     };
     W4Params p{(const uint16_t*)a.a, {stack(a.w0), stack(a.w1)}, (uint16_t*)a.c, a.offsets, a.a_rows, a.a_count,
                a.n_seg, a.rows_cap, a.N, a.K};
-    return a.w1 ? launch_w4<true>(p, a.w0->group, s) : launch_w4<false>(p, a.w0->group, s);
+    return a.w1 ? launch_w4<2>(p, a.w0->group, s) : launch_w4<1>(p, a.w0->group, s);
 }
 
 }  // namespace bmoe
