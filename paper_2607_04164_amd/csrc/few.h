@@ -252,23 +252,26 @@ struct FmtW4 {
             static_assert(NM == 4, "four tiles");
             w.load(at, k / kW4Unit, K, q);
         }
-        __device__ __forceinline__ void tail(int, int, int) { w.settle(); }  // (codes are finite)
+        __device__ __forceinline__ void tail(int k, int K, int) { w.settle(k, K); }  // (codes are finite)
     };
     template <int NM, int NP>
     __device__ static __forceinline__ void multiply(f32x4 (&tot)[NM], const Set<NM>& w, const X (&x)[NP], bool has_zeros) {
         const v4u ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-        const W4Spread<GROUP> groups(w.w);
+        const W4Spread<GROUP> groups(w.w, has_zeros);
+        const int q = (threadIdx.x & 63) >> 4;
         v4u c[NM];
         // A group is scaled while the next one is multiplied. (The fences keep the
         // compiler from running more groups side by side than there are registers.)
         f32x4 acc[2][NM], xs[2];
+        float xa = 0.f;  // xs of group 4i + q
         auto flush = [&](int g) __attribute__((always_inline)) {
+            xa = q == (g & 3) ? xs[g & 1][0] : xa;
 #pragma unroll
             for (int m = 0; m < NM; ++m) {
-                const float sc = groups.scale(m, g), off = groups.offset(has_zeros, m, g);
+                const float sc = groups.scale(m, g);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    tot[m][i] = fmaf(sc, fmaf(-off, xs[g & 1][i], acc[g & 1][m][i]), tot[m][i]);
+                for (int i = 0; i < 4; ++i) tot[m][i] = fmaf(sc, acc[g & 1][m][i], tot[m][i]);
+                if (g % 4 == 3 || g == NG - 1) tot[m] = groups.add_offset(tot[m], xa, m, g);
                 asm volatile("" : "+v"(tot[m]));  // here, and not where tot is used next
             }
         };
@@ -289,7 +292,7 @@ struct FmtW4 {
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
                     const v4u a = w4_order(x[p].x[u]);
-                    xs[g & 1] = mfma16(a, ones, xs[g & 1]);
+                    xs[g & 1] = mfma16(ones, a, xs[g & 1]);
 #pragma unroll
                     for (int m = 0; m < NM; ++m) acc[g & 1][m] = mfma16(a, b[m], acc[g & 1][m]);
                 }

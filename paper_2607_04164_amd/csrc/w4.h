@@ -3,8 +3,11 @@
 // A code q becomes the bf16 value 16 + q by placing its four bits on top of the
 // mantissa of 16 (one shift, one and-or for two codes); q and 16 + q are exact in
 // bf16. Per group of columns the matrix cores form
-//   acc = sum_k x_k (16 + q_k)   and   xs = sum_k x_k   (B operand of ones),
-// and the group adds s (acc - (16 + z) xs) to the total, in fp32. The offset
+//   acc = sum_k x_k (16 + q_k)   and   xs = sum_k x_k   (A operand of ones),
+// and the group adds s acc - s (16 + z) xs to the total, in fp32: the first term by
+// one multiply-add an element, the second as a product over the groups on the fp32
+// matrix cores, four groups an instruction (s (16 + z) is exact in fp32; the vector
+// units, not the matrix cores, bound a product of more than a few rows). The offset
 // costs about 5 times the rounding of the plain sum (16 + q against q - z), far
 // below the bf16 output's.
 //
@@ -17,7 +20,7 @@
 // a group of 32 is one step. In a lane the eight codes come out as columns
 // 0,4,1,5,2,6,3,7; the activations are put into the same order (w4_order). The scales
 // of a unit are one load: lane row q brings those of tile q, and three exchanges hand
-// them to all lanes; the zero points likewise. (Loads are what is scarce: an
+// them to all lanes; the zero points likewise, into the fp32 product's B operand. (Loads are what is scarce: an
 // instruction of 64 lanes takes 16 cycles of the address unit however little it brings.)
 #pragma once
 
@@ -176,34 +179,51 @@ struct W4Unit {
         s.load(w.scales + from);
         z.load(w.zeros + from);
     }
-    // moves the groups to their places: after the load, where K is not whole units
-    __device__ __forceinline__ void settle() {
+    // After the load, where K is not whole units: moves the groups to their places and
+    // clears the scales of those past column K (another row's may be infinite).
+    __device__ __forceinline__ void settle(int k, int K) {
 #pragma unroll
         for (int i = 0; i < NG; ++i)
             if (i < back) {
                 s.template drop<16>();
                 z.template drop<8>();
             }
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+            if (k + i * GROUP >= K) s.v[i / 2] &= i & 1 ? 0xffffu : 0xffff0000u;
     }
 };
 
-// the groups of all tiles, in every lane of their rows
+// the groups of all tiles: their scales in every lane, and - s (16 + z) as B operands
+// of the fp32 matrix cores (group 4 i + q in lane row q of offset[i])
 template <int GROUP, int MT = 4>
 struct W4Spread {
-    static constexpr int NG = kW4Unit / GROUP;
-    uint32_t s[(2 * NG + 3) / 4][MT], z[(NG + 3) / 4][MT];
-    __device__ __forceinline__ explicit W4Spread(const W4Unit<GROUP, MT>& u) {
+    static constexpr int NG = kW4Unit / GROUP, NC = (NG + 3) / 4;
+    uint32_t s[(2 * NG + 3) / 4][MT];
+    v4u offset[NC];  // of tiles 0 .. 3 (beyond MT: repeated)
+    __device__ __forceinline__ W4Spread(const W4Unit<GROUP, MT>& u, bool has_zeros) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            v4u own = {0u, 0u, 0u, 0u};  // of the tile of this lane row, groups 4 i .. 4 i + 3
+#pragma unroll
+            for (int j = 0; j < 4 && 4 * i + j < NG; ++j) {
+                const int g = 4 * i + j;
+                const float z = has_zeros ? (float)((u.z.v[i] >> (8 * j)) & 0xffu) : 8.f;
+                own[j] = __float_as_uint(-value(u.s.v[g >> 1], g) * (16.f + z));
+            }
+            offset[i] = w4_transpose(own);
+        }
 #pragma unroll
         for (int i = 0; i < (2 * NG + 3) / 4; ++i) w4_spread<MT>(u.s.v[i], s[i]);
-#pragma unroll
-        for (int i = 0; i < (NG + 3) / 4; ++i) w4_spread<MT>(u.z.v[i], z[i]);
     }
-    __device__ __forceinline__ float scale(int m, int g) const {
-        return __uint_as_float(g & 1 ? s[g >> 1][m] & 0xffff0000u : s[g >> 1][m] << 16);
+    __device__ __forceinline__ static float value(uint32_t pair, int g) {
+        return __uint_as_float(g & 1 ? pair & 0xffff0000u : pair << 16);
     }
-    // 16 + the zero point of group g
-    __device__ __forceinline__ float offset(bool has_zeros, int m, int g) const {
-        return has_zeros ? 16.f + (float)((z[g >> 2][m] >> (8 * (g & 3))) & 0xffu) : 24.f;
+    __device__ __forceinline__ float scale(int m, int g) const { return value(s[g >> 1][m], g); }
+    // after group g, the last or every fourth: adds the offsets' part of tile m; xs:
+    // the A operand, group 4 (g / 4) + q's sum of the token r16 in lane (r16, q)
+    __device__ __forceinline__ f32x4 add_offset(f32x4 tot, float xs, int m, int g) const {
+        return __builtin_amdgcn_mfma_f32_16x16x4f32(xs, __uint_as_float(offset[g >> 2][m]), tot, 0, 0, 0);
     }
 };
 

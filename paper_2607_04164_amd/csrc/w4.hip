@@ -62,9 +62,12 @@ __device__ __forceinline__ void w4_pass(const W4Params& p, const W4Place<GROUP, 
         load_x(0);
         load_x(1);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (RAGGED) w.settle();
-        const W4Spread<GROUP, MT> groups(w);
+        if constexpr (RAGGED) w.settle(unit * kW4Unit, K);
+        const W4Spread<GROUP, MT> groups(w, p.w[0].has_zeros);
         f32x4 acc[MT][TILES], xs[TILES];
+        float xa[TILES];  // xs of group 4i + q
+#pragma unroll
+        for (int nt = 0; nt < TILES; ++nt) xa[nt] = 0.f;
         v4u c[MT];
 #pragma unroll
         for (int i = 0; i < NX; ++i) {
@@ -89,7 +92,7 @@ __device__ __forceinline__ void w4_pass(const W4Params& p, const W4Place<GROUP, 
                     xv[nt] = x[i & 1][j][nt];
                     if constexpr (RAGGED) xv[nt] &= unit * kW4Unit + step * 32 + q * 8 < K ? ~0u : 0u;
                     xv[nt] = w4_order(xv[nt]);
-                    xs[nt] = mfma16(xv[nt], ones, xs[nt]);
+                    xs[nt] = mfma16(ones, xv[nt], xs[nt]);
                 }
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
@@ -99,13 +102,15 @@ __device__ __forceinline__ void w4_pass(const W4Params& p, const W4Place<GROUP, 
                 }
                 if (step % GS == GS - 1) {
 #pragma unroll
+                    for (int nt = 0; nt < TILES; ++nt) xa[nt] = q == (g & 3) ? xs[nt][0] : xa[nt];
+#pragma unroll
                     for (int m = 0; m < MT; ++m) {
-                        const float sc = groups.scale(m, g), off = groups.offset(p.w[0].has_zeros, m, g);
+                        const float sc = groups.scale(m, g);
 #pragma unroll
                         for (int nt = 0; nt < TILES; ++nt) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                tot[m][nt][e] = fmaf(sc, fmaf(-off, xs[nt][e], acc[m][nt][e]), tot[m][nt][e]);
+                            for (int e = 0; e < 4; ++e) tot[m][nt][e] = fmaf(sc, acc[m][nt][e], tot[m][nt][e]);
+                            if (g % 4 == 3 || step == 7) tot[m][nt] = groups.add_offset(tot[m][nt], xa[nt], m, g);
                             asm volatile("" : "+v"(tot[m][nt]));  // here, and not where tot is used next
                         }
                     }
@@ -173,21 +178,24 @@ __global__ __launch_bounds__(64 * w4_waves(MT), w4_waves(MT) / 4) void w4_gemm_k
         if (rows > 16) w4_pass<NR, MT, GROUP, 2, RAGGED>(p, place, at.beg, at.end, wave, r16, q, part);
         else w4_pass<NR, MT, GROUP, 1, RAGGED>(p, place, at.beg, at.end, wave, r16, q, part);
         __syncthreads();
-        for (int i = tid; i < rows * COLS; i += 64 * WAVES) {
-            const int row = i / COLS, col = i % COLS, nt = row >> 4;
-            // element (row, col & 15) of the tiles of column block col / 16
-            const float* d = (const float*)&part[nt * MT + col / 16 * NR][((row & 15) >> 2) * 16 + (col & 15)] + (row & 3);
-            float sum[NR];
+        // a thread: one lane's four rows of a tile of each matrix
+        for (int i = tid; i < kW4Tiles * MT / NR * 64; i += 64 * WAVES) {
+            const int l = i & 63, t = (i >> 6) % (MT / NR), nt = (i >> 6) / (MT / NR);
+            const int row = nt * 16 + (l >> 4) * 4, col = n0 + t * 16 + (l & 15);
+            if (row >= rows || col >= N) continue;
+            f32x4 sum[NR];
 #pragma unroll
             for (int m = 0; m < NR; ++m) {
-                sum[m] = d[m * 256];
+                const f32x4* d = &part[nt * MT + t * NR + m][l];
+                sum[m] = d[0];
 #pragma unroll
-                for (int w = 1; w < WAVES; ++w) sum[m] += d[(w * kW4Tiles * MT + m) * 256];
+                for (int w = 1; w < WAVES; ++w) sum[m] += d[w * kW4Tiles * MT * 64];
             }
-            float v;
-            if constexpr (NR == 2) v = silu_mul(sum[0], sum[NR - 1]);
-            else v = sum[0];
-            if (n0 + col < N) p.C[(size_t)(at.beg + row) * N + n0 + col] = f32_to_bf16(v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v = NR == 2 ? silu_mul(sum[0][e], sum[NR - 1][e]) : sum[0][e];
+                if (row + e < rows) p.C[(size_t)(at.beg + row + e) * N + col] = f32_to_bf16(v);
+            }
         }
         __syncthreads();  // the partials are rewritten by the next turn
     }

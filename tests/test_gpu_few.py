@@ -23,6 +23,7 @@ CASES = {
     "shared-wider": dict(T=7, d=192, E=20, top_k=5, G=6, f=56, fs=488),
     "whole-units-9": dict(T=9, d=1024, E=60, top_k=4, G=15, f=256, fs=128),
     "whole-units-8": dict(T=8, d=1024, E=24, top_k=6, G=20, f=384, norm=1),
+    "wider-than-lds": dict(T=16, d=2056, E=8, top_k=1, G=4, f=40),
     "few-columns": dict(T=13, d=40, E=33, top_k=7, G=11, f=16),
 }
 FORMATS = [("bf16", 0, False), ("f32", 0, False), ("bf16", 32, False), ("bf16", 64, True), ("bf16", 128, False),
@@ -133,6 +134,34 @@ def test_tokens_do_not_mix():
     out = layer(x)
     keep = [t for t in range(8) if t != 3]
     assert torch.equal(out[keep], clean[keep])
+
+
+@pytest.mark.parametrize("T", [5, 12])
+@pytest.mark.parametrize("group,zeros", [(32, False), (64, True), (128, True)])
+def test_nan_scales_do_not_spread(T, group, zeros):
+    """A row of NaN scales reaches one output column of the tokens that call its segment, and units that end
+    inside a row (200 columns) take nothing of the next row."""
+    case = dict(T=T, d=264, E=6, top_k=1, G=6, f=200, fs=72)
+    c, vals = R.make_case(21, group=group, zeros=zeros, **case)
+    ref = reference(c, vals, case)
+    w, x = to_gpu(c, case, group)
+    layer = B.LayerForward(desc_of(case, "bf16"), w, few_tokens=True)
+    clean = layer(x).float().cpu().numpy()
+    g0 = ref["slot_group"][0, 0]
+    hit = (ref["slot_group"] == g0).any(axis=1)
+    assert hit.any() and not hit.all()
+    c["w_down"][1][g0, 7] = float("nan")
+    w, x = to_gpu(c, case, group)
+    out = B.LayerForward(desc_of(case, "bf16"), w, few_tokens=True)(x).float().cpu().numpy()
+    assert np.isnan(out[hit, 7]).all()
+    bad = np.zeros_like(out, dtype=bool)
+    bad[hit, 7] = True
+    assert np.array_equal(out[~bad], clean[~bad])
+    c, vals = R.make_case(21, group=group, zeros=zeros, **case)
+    c["w_gate"][1][g0, 9] = float("nan")  # a hidden column of the callers, so all of their outputs
+    w, x = to_gpu(c, case, group)
+    out = B.LayerForward(desc_of(case, "bf16"), w, few_tokens=True)(x).float().cpu().numpy()
+    assert np.isnan(out[hit]).all() and np.array_equal(out[~hit], clean[~hit])
 
 
 def test_same_as_the_four_calls():

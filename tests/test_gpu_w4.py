@@ -142,6 +142,28 @@ def test_extreme_codes_scales_and_zeros():
     np.testing.assert_allclose(R.np64(y), want, rtol=2.0 ** -8)
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("N,K", [(40, 264), (40, 1408), (72, 40)])
+def test_a_row_with_nan_scales_is_the_only_one(N, K, group):
+    """Also where a unit of columns ends inside the row, so that the next row's scales are loaded with it."""
+    rng = np.random.default_rng(N + K + group)
+    t = R.w4_random(rng, 2, N, K, group, True)
+    a = R.rand(rng, (60, K), 1.0, "bf16").cuda()
+    off = torch.tensor([0, 20, 60], dtype=torch.int32, device="cuda")
+    clean = B.w4_matmul(off, a, _w4(t, K, group))
+    scales = t[1].clone()
+    scales[0, 5] = float("nan")
+    scales[1, 0] = float("inf")
+    scales[1, N - 1] = float("nan")
+    y = B.w4_matmul(off, a, _w4((t[0], scales, t[2]), K, group))
+    bad = torch.zeros_like(y, dtype=torch.bool)
+    bad[:20, 5] = True
+    bad[20:, 0] = True
+    bad[20:, N - 1] = True
+    assert not torch.isfinite(y[bad].float()).any()
+    assert torch.equal(y[~bad], clean[~bad])
+
+
 def quantize_ref(w32, group, zeros):
     """The quantizer's definition, element by element in fp32."""
     n, N, K = w32.shape
