@@ -477,20 +477,23 @@ __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewPara
     const int T = p.T, k = p.k, d = p.d, f = p.f, fs = p.fs;
     const int sh_tiles = ceil_div(fs, COLS), tiles = ceil_div(f, COLS);
 
-    if constexpr (X_LDS) {
-        const int nch = d * (int)sizeof(typename F::Act) / 16;
-        for (int i = tid; i < T * nch; i += kUpThreads) {
-            const int t = i / nch;
-            *(v4u*)(x_lds + t * (nch * 16 + kXPad) + (i - t * nch) * 16) = ((const v4u*)p.x)[i];
-        }
-    }
     // the picks, the reached segments, and where each token's gate of a segment is
     if (tid < kSetWords) sm.reached[tid] = 0;
-    for (int i = tid; i < BMOE_MAX_EXPERTS * kFewTok / 2; i += kUpThreads) ((uint32_t*)sm.slot_of)[i] = ~0u;
     __syncthreads();
-    if (wave * 4 < T) {
+    const int selecting = ceil_div(T, 4) * 64, idle = tid - selecting;
+    if (idle < 0) {
         if (p.E <= 64) few_select<4>(p.logits, p.e2g, sm, T, p.E, p.G, k, wave, lane);
         else few_select<16>(p.logits, p.e2g, sm, T, p.E, p.G, k, wave, lane);
+    } else {
+        for (int i = idle; i < BMOE_MAX_EXPERTS * kFewTok / 2; i += kUpThreads - selecting)
+            ((uint32_t*)sm.slot_of)[i] = ~0u;
+        if constexpr (X_LDS) {
+            const int nch = d * (int)sizeof(typename F::Act) / 16;
+            for (int i = idle; i < T * nch; i += kUpThreads - selecting) {
+                const int t = i / nch;
+                *(v4u*)(x_lds + t * (nch * 16 + kXPad) + (i - t * nch) * 16) = ((const v4u*)p.x)[i];
+            }
+        }
     }
     __syncthreads();
     if (tid < p.G && (sm.reached[tid >> 5] >> (tid & 31)) & 1u) sm.segs[members_below(sm.reached, tid)] = (int16_t)tid;
@@ -642,6 +645,7 @@ __global__ __launch_bounds__(kDownThreads, F::DOWN_WAVES) void few_down_kernel(F
     const int g = tid < T * k ? p.slot_group[tid] : -1;
     const bool valid = (unsigned)g < (unsigned)p.G;
     if (tid < kSetWords) reached[tid] = 0;
+    if (tid == 0) segs[0] = 0;  // (read for its address where no segment is reached)
     callers[tid] = 0;
     for (int i = tid; i < BMOE_MAX_EXPERTS * kFewTok / 4; i += kDownThreads) ((uint32_t*)slot_of)[i] = 0;
     __syncthreads();

@@ -136,6 +136,26 @@ def test_tokens_do_not_mix():
     assert torch.equal(out[keep], clean[keep])
 
 
+@pytest.mark.parametrize("dtype,group,zeros", FORMATS[:3], ids=IDS[:3])
+@pytest.mark.parametrize("fs", [0, 72])
+def test_experts_of_no_segment(dtype, group, zeros, fs):
+    """Experts that the map sends nowhere give nothing: one segment of four left, then none, so that the output
+    is the shared experts' or zero."""
+    case = dict(T=6, d=136, E=8, top_k=3, G=4, f=48, fs=fs)
+    for left in (1, 0):
+        c, vals = R.make_case(31, dtype=dtype, group=group, zeros=zeros, **case)
+        c["e2g"][c["e2g"] >= left] = -1
+        w, x = to_gpu(c, case, group)
+        layer = B.LayerForward(desc_of(case, dtype), w, few_tokens=True)
+        layer.ws.fill_(0xFF)
+        out = layer(x)
+        ref = reference(c, vals, case)
+        ref["slot_gate"] = np.where(ref["slot_group"] >= 0, ref["slot_gate"], 0)  # as the route kernels write it
+        check(layer, out, ref, dtype, f"{left} left")
+        if not left and not fs:
+            assert not out.any()
+
+
 @pytest.mark.parametrize("T", [5, 12])
 @pytest.mark.parametrize("group,zeros", [(32, False), (64, True), (128, True)])
 def test_nan_scales_do_not_spread(T, group, zeros):
