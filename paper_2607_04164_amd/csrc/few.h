@@ -6,12 +6,12 @@
 //   few_logits_kernel  one workgroup per expert (and four tokens): the gate logits
 //                      in float64 (bf16 and fp32 products are exact there), so
 //                      near ties need no second look;
-//   few_up_kernel      items of 16 hidden columns of a reached segment (or of the
-//                      shared experts), dealt out to the workgroups. Every
+//   few_up_kernel      items of 16 or 32 hidden columns of a reached segment (or of
+//                      the shared experts), dealt out to the workgroups. Every
 //                      workgroup selects the top-k from the logits by itself, which
 //                      costs less than another launch: silu(Wg x) * (Wu x), times
 //                      the token's gate of that segment, to the workspace;
-//   few_down_kernel    16 output columns a workgroup: the sum over the reached
+//   few_down_kernel    16 to 64 output columns a workgroup: the sum over the reached
 //                      segments and their hidden columns is one long K, so the
 //                      gate-weighted sum over experts falls out of it. K is split
 //                      over several workgroups where the columns alone are too few
@@ -141,32 +141,36 @@ __device__ __forceinline__ void few_select(const double* logits, const int32_t* 
 // wave shares and the lane's row's byte offset. RAGGED: columns past K read the row's
 // last ones and tail() zeroes them (in every unit: a branch would cost copies of the
 // buffers). multiply() adds the products with NP parts of the activations (their sum is
-// the value) to tot. PARTS: parts of a hidden value; BATCH: units of a register buffer;
-// UP_TILES, DOWN_TILES: tiles of 16 columns that a wave takes with the same activations
-// (4-bit weights are a quarter of the bytes, and with one tile the activations' loads,
-// not the weights', bound them: 86 and 58 us for six tokens of wide experts); UP_WAVES,
-// DOWN_WAVES: waves per SIMD, by registers.
+// the value) to tot. PARTS: parts of a hidden value; DOWN_BATCH: units of a register
+// buffer there; UP_TILES (at most), DOWN_TILES: tiles of 16 columns that a wave takes with
+// the same activations, PACK_TILES: for up to eight tokens; UP_WAVES, DOWN_WAVES: waves per
+// SIMD, by registers. 4-bit weights are a quarter of the bytes, and with one tile the
+// activations' loads, not the weights', bound them: 86 and 58 us for six tokens of wide
+// experts. bf16, down: two tiles take 58.6 us for the layer of 16 tokens, one 63.2, but
+// 28.7 against 27.1 for the layer of one token, where they leave fewer waves.
 
 // bf16 and fp32 weights: 16 bytes of a row are EPC columns
 template <typename ActT>
 struct FmtPlain {
     typedef ActT Act;
     static constexpr bool kBf16 = sizeof(Act) == 2;
-    static constexpr int EPC = 16 / sizeof(Act), LD = 2, UK = 4 * EPC * LD, PARTS = kBf16 ? 2 : 1, BATCH = 2;
+    static constexpr int EPC = 16 / sizeof(Act), LD = 2, UK = 4 * EPC * LD, PARTS = kBf16 ? 2 : 1;
     static constexpr bool PAIRS = true, X_IN_LDS = false;
-    static constexpr int UP_TILES = 1, DOWN_TILES = 1, UP_WAVES = 4, DOWN_WAVES = 3;
+    static constexpr int UP_TILES = PARTS, UP_WAVES = 4;  // (at most, of bf16)
+    static constexpr int DOWN_TILES = PARTS, PACK_TILES = 1, DOWN_BATCH = 2, DOWN_WAVES = 3;
     struct Stack {
         const Act* w;
         bool has_zeros;  // (no meaning here)
     };
-    template <int NR>
+    template <int NR, int NM>
     struct Place {
         const Act* w[NR];
-        uint32_t row;  // the lane's row, in bytes
+        uint32_t row[NM / NR];  // the lane's row of a tile, in bytes
         __device__ __forceinline__ void set(const Stack& s0, const Stack& s1, int64_t first, int left, int K, int r16, int) {
             w[0] = s0.w + first * K;
             if constexpr (NR == 2) w[NR - 1] = s1.w + first * K;
-            row = (uint32_t)(min(r16, left - 1) * K) * sizeof(Act);
+#pragma unroll
+            for (int t = 0; t < NM / NR; ++t) row[t] = (uint32_t)(min(16 * t + r16, left - 1) * K) * sizeof(Act);
         }
     };
     struct X {
@@ -188,10 +192,9 @@ struct FmtPlain {
     struct Set {
         X w[NM];
         template <bool RAGGED, int NR>
-        __device__ __forceinline__ void load(const Place<NR>& at, int k, int K, int q) {
-            static_assert(NM == NR, "one tile of each matrix");
+        __device__ __forceinline__ void load(const Place<NR, NM>& at, int k, int K, int q) {
 #pragma unroll
-            for (int m = 0; m < NM; ++m) w[m].template load<RAGGED>(at.w[m], at.row, k, K, q);
+            for (int m = 0; m < NM; ++m) w[m].template load<RAGGED>(at.w[m % NR], at.row[m / NR], k, K, q);
         }
         __device__ __forceinline__ void tail(int k, int K, int q) {
 #pragma unroll
@@ -224,13 +227,14 @@ typedef FmtPlain<float> FmtF32;
 template <int GROUP>
 struct FmtW4 {
     typedef uint16_t Act;
-    static constexpr int UK = kW4Unit, LD = UK / 32, PARTS = 2, BATCH = 1;
+    static constexpr int UK = kW4Unit, LD = UK / 32, PARTS = 2;
     static constexpr bool PAIRS = false, X_IN_LDS = true;
-    static constexpr int UP_TILES = 2, DOWN_TILES = 4, UP_WAVES = 2, DOWN_WAVES = 2;
+    static constexpr int UP_TILES = 2, UP_WAVES = 2;
+    static constexpr int DOWN_TILES = 4, PACK_TILES = 4, DOWN_BATCH = 1, DOWN_WAVES = 2;
     static constexpr int NG = W4Unit<GROUP>::NG, STEPS = GROUP / 32;
     typedef W4Stack Stack;
-    template <int NR>
-    using Place = W4Place<GROUP, NR>;
+    template <int NR, int NM>
+    using Place = W4Place<GROUP, NR, NM>;
     struct X {
         v4u x[LD];
         template <bool RAGGED>
@@ -246,10 +250,10 @@ struct FmtW4 {
     };
     template <int NM>
     struct Set {
+        static_assert(NM == 4, "four tiles");
         W4Unit<GROUP> w;
         template <bool RAGGED, int NR>
-        __device__ __forceinline__ void load(const Place<NR>& at, int k, int K, int q) {
-            static_assert(NM == 4, "four tiles");
+        __device__ __forceinline__ void load(const Place<NR, NM>& at, int k, int K, int q) {
             w.load(at, k / kW4Unit, K, q);
         }
         __device__ __forceinline__ void tail(int k, int K, int) { w.settle(k, K); }  // (codes are finite)
@@ -423,13 +427,13 @@ __device__ __forceinline__ void stream_steps(int n, LoadW load_w, LoadX load_x, 
     else stream_weights<W, X>(n, load_w, load_x, multiply);
 }
 
-template <class F, int NM>
+template <class F, int BATCH, int NM>
 struct FewW {
-    typename F::template Set<NM> w[F::BATCH];
+    typename F::template Set<NM> w[BATCH];
 };
-template <class F, int NP>
+template <class F, int BATCH, int NP>
 struct FewX {
-    typename F::X x[F::BATCH][NP];
+    typename F::X x[BATCH][NP];
 };
 
 // sum of the waves' partials of D element (row, col)
@@ -462,13 +466,14 @@ struct UpItem {
     }
 };
 
-// RAGGED: d is not whole units, or they do not go evenly over the waves' buffers
+// TILES: of a matrix an item has; a register buffer holds two units, of one tile or one of
+// each of two. RAGGED: d is not whole units, or they do not go evenly over the waves' buffers
 // X_LDS: the tokens are kept in LDS (up to kXBytes of them)
 constexpr int kXPad = 16;  // bytes between the rows there, so that they start on other banks
 constexpr int kXBytes = 16 * (2 * 2048 + kXPad);
-template <class F, bool RAGGED, bool X_LDS>
+template <class F, int TILES, bool RAGGED, bool X_LDS>
 __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewParams<F> p) {
-    constexpr int WAVES = kUpThreads / 64, BATCH = F::BATCH, TILES = F::UP_TILES, COLS = TILES * kFewCols;
+    constexpr int WAVES = kUpThreads / 64, BATCH = 2 / TILES, COLS = TILES * kFewCols;
     __shared__ __align__(16) f32x4 part[2][2 * TILES][WAVES][64];  // [parity of the item][matrix, tile]
     __shared__ SelectSmem sm;
     __shared__ __align__(16) char x_lds[X_LDS ? kXBytes : 16];
@@ -527,11 +532,16 @@ __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewPara
     const int units = ceil_div(d, F::UK), steps = ceil_div(ceil_div(units, WAVES), BATCH);  // steps of an item
     const int wg = scalar(blockIdx.x), wgs = scalar(gridDim.x);
     const int mine = scalar(wg < items ? div_uniform(items - 1 - wg, wgs) + 1 : 0);
-    typedef FewW<F, 2 * TILES> W;
-    typedef FewX<F, 1> X;
+    // A workgroup starts an item at a step of its own and goes around: rows are often a
+    // power of two long, and from one column the workgroups would ask a few memory
+    // channels for all of them.
+    const int turn = scalar((int)((unsigned)wg % (unsigned)steps));
+    auto turned = [&](int s) __attribute__((always_inline)) { return s + turn < steps ? s + turn : s + turn - steps; };
+    typedef FewW<F, BATCH, 2 * TILES> W;
+    typedef FewX<F, BATCH, 1> X;
     // the place of the loads: step l_step of item l_item
     int l_item = wg, l_step = 0, l_at = 0;
-    typename F::template Place<2> rows;  // of W_gate and W_up
+    typename F::template Place<2, 2 * TILES> rows;  // of W_gate and W_up
     auto enter = [&]() __attribute__((always_inline)) {
         const UpItem it(l_item, COLS, sh_tiles, tiles);
         const int seg = it.shared ? 0 : scalar(sm.segs[it.place]), N = pick(it.shared, fs, f);
@@ -549,7 +559,7 @@ __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewPara
         }
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            int u = wave + WAVES * (BATCH * l_step + i);
+            int u = wave + WAVES * (BATCH * turned(l_step) + i);
             if constexpr (RAGGED) u = min(u, units - 1);
             b.w[i].template load<RAGGED>(rows, u * F::UK, d, q);
         }
@@ -566,7 +576,7 @@ __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewPara
         }
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            int u = wave + WAVES * (BATCH * x_step + i);
+            int u = wave + WAVES * (BATCH * turned(x_step) + i);
             if constexpr (RAGGED) u = min(u, units - 1);
             b.x[i][0].template load<RAGGED>(X_LDS ? (const void*)x_lds : (const void*)p.x, xr, u * F::UK, d, q);
         }
@@ -575,7 +585,7 @@ __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewPara
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
             if constexpr (RAGGED) {
-                const int kk = (wave + WAVES * (BATCH * step + i)) * F::UK;
+                const int kk = (wave + WAVES * (BATCH * turned(step) + i)) * F::UK;
                 b.w[i].tail(kk, d, q);
                 x.x[i][0].tail(kk, d, q);
             }
@@ -628,8 +638,8 @@ struct DownUnit {
 // RAGGED: d_ff or d_ff_shared is not whole units
 template <class F, bool PACK, bool RAGGED>
 __global__ __launch_bounds__(kDownThreads, F::DOWN_WAVES) void few_down_kernel(FewParams<F> p) {
-    constexpr int WAVES = kDownThreads / 64, BATCH = F::BATCH, NP = PACK ? 1 : F::PARTS;
-    constexpr int TILES = F::DOWN_TILES, COLS = TILES * kFewCols;
+    constexpr int WAVES = kDownThreads / 64, BATCH = F::DOWN_BATCH, NP = PACK ? 1 : F::PARTS;
+    constexpr int TILES = PACK ? F::PACK_TILES : F::DOWN_TILES, COLS = TILES * kFewCols;
     __shared__ __align__(16) f32x4 part[TILES][WAVES][64];
     __shared__ uint32_t reached[kSetWords];
     // by place among the reached segments (ascending): the segment, the tokens that
@@ -665,8 +675,8 @@ __global__ __launch_bounds__(kDownThreads, F::DOWN_WAVES) void few_down_kernel(F
     const int first = (wg - tile * p.split) * WAVES + wave, stride = p.split * WAVES;
     const int steps = ceil_div(div_uniform(units + stride - 1, stride), BATCH);
     const int token = PACK ? r16 & 7 : r16;
-    typedef FewW<F, TILES> W;
-    typedef FewX<F, NP> X;
+    typedef FewW<F, BATCH, TILES> W;
+    typedef FewX<F, BATCH, NP> X;
     DownUnit lu{0, 0}, xu, mu;  // of the weights' loads, the activations' and the products
     lu.advance(first, segments, per);
     xu = mu = lu;
@@ -682,7 +692,7 @@ __global__ __launch_bounds__(kDownThreads, F::DOWN_WAVES) void few_down_kernel(F
             // (past the last unit: the first one again, its products are dropped)
             const bool past = lu.a == segments && lu.k >= per_sh, sh = lu.a == segments && !past;
             const int seg = sh ? 0 : scalar(segs[past ? 0 : lu.a]), width = pick(sh, fs, f);
-            typename F::template Place<1> rows;
+            typename F::template Place<1, TILES> rows;
             const typename F::Stack st = pick(sh, p.down_sh, p.down);
             rows.set(st, st, (int64_t)seg * d + n0, d - n0, width, r16, q);
             b.w[i].template load<RAGGED>(rows, past ? 0 : lu.k * F::UK, width, q);
@@ -798,16 +808,15 @@ inline int most_splits(int d, int cols, int per_cu) {
 inline size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 inline size_t logit_bytes(int T, int E) { return round256((size_t)T * E * sizeof(double)); }
 inline size_t done_bytes(int d) { return round256((size_t)ceil_div(d, kFewCols) * sizeof(int32_t)); }
-template <class F>
-size_t partial_of(int d) {
-    constexpr int cols = F::DOWN_TILES * kFewCols;
-    const int split = most_splits(d, cols, F::DOWN_WAVES);
-    return split == 1 ? 0 : (size_t)ceil_div(d, cols) * split * F::DOWN_TILES * kTile * sizeof(float);
-}
-// (enough for any format)
+// (of the partials, enough for any format: 1, 2 or 4 tiles of columns, 2 or 3 workgroups a CU)
 inline size_t partial_bytes(int d) {
-    const size_t a = partial_of<FmtBf16>(d), b = partial_of<FmtF32>(d), c = partial_of<FmtW4<32>>(d);
-    return a > b ? (a > c ? a : c) : (b > c ? b : c);
+    size_t most = 0;
+    for (int tiles = 1; tiles <= 4; tiles *= 2) {
+        const int split = most_splits(d, tiles * kFewCols, 3);
+        const size_t n = split == 1 ? 0 : (size_t)ceil_div(d, tiles * kFewCols) * split * tiles * kTile * sizeof(float);
+        most = n > most ? n : most;
+    }
+    return most;
 }
 
 template <class F, class ToStack>
@@ -844,28 +853,42 @@ hipError_t launch_few_t(const FewArgs& a, ToStack st, hipStream_t s) {
     p.h_part = (int64_t)a.T * a.k * a.f + (int64_t)a.T * a.fs;
     const int64_t slots = (int64_t)a.T * a.k, most = slots < a.G ? slots : a.G;
     const int64_t units = most * ceil_div(a.f, F::UK) + ceil_div(a.fs, F::UK);
-    constexpr int kUpCols = F::UP_TILES * kFewCols, kDownCols = F::DOWN_TILES * kFewCols;
-    p.split = most_splits(a.d, kDownCols, F::DOWN_WAVES);
+    const bool pack = F::PARTS == 2 && a.T <= 8;
+    const int down_cols = (pack ? F::PACK_TILES : F::DOWN_TILES) * kFewCols;
+    p.split = most_splits(a.d, down_cols, F::DOWN_WAVES);
     if (units < (int64_t)p.split * (kDownThreads / 64)) p.split = (int)ceil_div64(units, kDownThreads / 64);  // a unit a wave
     hipError_t e = launch_few_logits(a, p.done, s);
     if (e != hipSuccess) return e;
-    const int64_t items = most * ceil_div(a.f, kUpCols) + ceil_div(a.fs, kUpCols);
+    // Pairs of tiles of bf16 weights: for many tokens, whose activations they save loads of
+    // (16 tokens: 52.1 us for the layer, single tiles 55.3), and where they leave a CU no
+    // more than one workgroup (one token: 25.5 and 26.7). In between single tiles keep the
+    // workgroups' shares closer (two tokens of wide experts: 206 and 228).
+    auto items_of = [&](int tiles) {
+        const int cols = tiles * kFewCols;
+        return most * ceil_div(a.f, cols) + ceil_div(a.fs, cols);
+    };
+    const int up_tiles = F::PAIRS && a.T <= 8 && items_of(F::UP_TILES) > 256 ? 1 : F::UP_TILES;
+    const int64_t items = items_of(up_tiles);
     const int64_t room = (int64_t)F::UP_WAVES * 256 / kUpThreads * persistent_workgroups();
-    const dim3 up((unsigned)(items < room ? items : room)), down((unsigned)(ceil_div(a.d, kDownCols) * p.split));
-    const bool up_ragged = a.d % (F::UK * F::BATCH * (kUpThreads / 64)) != 0;
+    const dim3 up((unsigned)(items < room ? items : room)), down((unsigned)(ceil_div(a.d, down_cols) * p.split));
+    const bool up_ragged = a.d % (F::UK * (2 / up_tiles) * (kUpThreads / 64)) != 0;
     const bool down_ragged = a.f % F::UK != 0 || a.fs % F::UK != 0;
     const bool x_fits = F::X_IN_LDS && (int64_t)a.T * (a.d * (int)sizeof(Act) + kXPad) <= kXBytes;
     auto go_up = [&](auto kernel) { hipLaunchKernelGGL(kernel, up, dim3(kUpThreads), 0, s, p); };
+    constexpr int kSingle = F::PAIRS ? 1 : F::UP_TILES;
     if (x_fits) {
-        if (up_ragged) go_up(few_up_kernel<F, true, F::X_IN_LDS>);
-        else go_up(few_up_kernel<F, false, F::X_IN_LDS>);
+        if (up_ragged) go_up(few_up_kernel<F, F::UP_TILES, true, F::X_IN_LDS>);
+        else go_up(few_up_kernel<F, F::UP_TILES, false, F::X_IN_LDS>);
+    } else if (up_tiles == F::UP_TILES) {
+        if (up_ragged) go_up(few_up_kernel<F, F::UP_TILES, true, false>);
+        else go_up(few_up_kernel<F, F::UP_TILES, false, false>);
     } else {
-        if (up_ragged) go_up(few_up_kernel<F, true, false>);
-        else go_up(few_up_kernel<F, false, false>);
+        if (up_ragged) go_up(few_up_kernel<F, kSingle, true, false>);
+        else go_up(few_up_kernel<F, kSingle, false, false>);
     }
     constexpr bool kParts = F::PARTS == 2;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, down, dim3(kDownThreads), 0, s, p); };
-    if (kParts && a.T <= 8) {
+    if (pack) {
         if (down_ragged) go(few_down_kernel<F, kParts, true>);
         else go(few_down_kernel<F, kParts, false>);
     } else {

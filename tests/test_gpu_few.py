@@ -23,6 +23,8 @@ CASES = {
     "shared-wider": dict(T=7, d=192, E=20, top_k=5, G=6, f=56, fs=488),
     "whole-units-9": dict(T=9, d=1024, E=60, top_k=4, G=15, f=256, fs=128),
     "whole-units-8": dict(T=8, d=1024, E=24, top_k=6, G=20, f=384, norm=1),
+    "many-items": dict(T=4, d=1024, E=64, top_k=8, G=32, f=288),
+    "many-items-odd": dict(T=5, d=200, E=64, top_k=8, G=40, f=296, fs=24),
     "wider-than-lds": dict(T=16, d=2056, E=8, top_k=1, G=4, f=40),
     "few-columns": dict(T=13, d=40, E=33, top_k=7, G=11, f=16),
 }
