@@ -142,10 +142,15 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void post_norm_kernel(PostPara
 template <int V>
 using Int = std::integral_constant<int, V>;
 
-// runs f(NT, CH) with the row split that fits: a wave a row where there are rows
-// for every wave of the chip, else four; sixteen where a row needs them
+// runs f(NT, CH) with the row split that fits: a wave a row where there are rows for
+// every wave of the chip and a lane's share of the row is at most wave_chunks, else four
+// waves; sixteen where a row needs them. wave_chunks: 4 for pre_norm, 2 for post_norm,
+// which holds three rows; with more, too few waves fit a SIMD to keep its loads going
+// (8192 bf16 rows, a wave and four waves a row: pre_norm 6.8 and 10.0 us of 1024
+// columns, 11.7 and 13.2 of 2048, 22.7 and 20.5 of 4096; post_norm 17.4 and 24.8, 39.7
+// and 34.0, 116.7 and 70.4).
 template <typename F>
-hipError_t with_split(int64_t T, int nch, F f) {
+hipError_t with_split(int64_t T, int nch, int wave_chunks, F f) {
     auto with_ch = [&](auto nt) {
         const int per = ceil_div(nch, decltype(nt)::value);
         if (per <= 1) f(nt, Int<1>{});
@@ -153,7 +158,7 @@ hipError_t with_split(int64_t T, int nch, F f) {
         else if (per <= 4) f(nt, Int<4>{});
         else f(nt, Int<8>{});
     };
-    if (nch <= 64 || (nch <= 512 && T >= 1024)) with_ch(Int<64>{});
+    if (nch <= 64 || (nch <= 64 * wave_chunks && T >= 1024)) with_ch(Int<64>{});
     else if (nch <= 2048) with_ch(Int<256>{});
     else with_ch(Int<1024>{});
     return hipGetLastError();
@@ -170,7 +175,7 @@ unsigned grid_of(int64_t T) {
 
 hipError_t launch_pre_norm(const PreNormArgs& a, hipStream_t s) {
     const int nch = a.d / (a.dtype == BMOE_BF16 ? 8 : 4);
-    return with_split(a.T, nch, [&](auto nt, auto ch) {
+    return with_split(a.T, nch, 4, [&](auto nt, auto ch) {
         constexpr int NT = decltype(nt)::value, CH = decltype(ch)::value;
         const dim3 grid(grid_of<NT>(a.T)), block(NT > 256 ? NT : 256);
         if (a.dtype == BMOE_BF16)
@@ -186,7 +191,7 @@ hipError_t launch_post_norm(const PostNormArgs& a, hipStream_t s) {
     const int nch = a.d / (a.dtype == BMOE_BF16 ? 8 : 4);
     const PostParams p{(const uint4*)a.y, (const uint4*)a.x, (const uint4*)a.w_post, (const uint4*)a.w_next, a.gate,
                        (uint4*)a.r, (uint4*)a.a, a.T, nch, a.norm_y, a.gate_mode, a.eps, a.res_scale};
-    return with_split(a.T, nch, [&](auto nt, auto ch) {
+    return with_split(a.T, nch, 2, [&](auto nt, auto ch) {
         constexpr int NT = decltype(nt)::value, CH = decltype(ch)::value;
         const dim3 grid(grid_of<NT>(a.T)), block(NT > 256 ? NT : 256);
         if (a.dtype == BMOE_BF16) hipLaunchKernelGGL((post_norm_kernel<uint16_t, NT, CH>), grid, block, 0, s, p);
