@@ -602,6 +602,12 @@ class W4:
                                  self.group)
         self._ref = ctypes.byref(self._struct)
 
+    def _on(self, device: int):
+        """The call's argument, for a call on GPU `device`."""
+        if self.device != device:
+            raise ValueError(f"4-bit weights are on GPU {self.device}, the call is on GPU {device}")
+        return self._ref
+
     def matrix(self) -> _Matrix:
         return _Matrix(self._struct.codes, self._struct.scales, self._struct.zeros)
 
@@ -654,7 +660,7 @@ def w4_matmul(offsets: torch.Tensor, a: torch.Tensor, w: W4, *, a_rows: Optional
     n, N, K = w.shape
     rows, op, rp, m, ap = _w4_rows(offsets, a, a_rows, n, K, device)
     y, yp = _out(y, "y", (rows, N), a, device)
-    _check(load_library().brownout_moe_w4_matmul(BMOE_BF16, n, rows, N, K, op, rp, m, ap, w._ref, yp, _stream_ptr(stream, device)),
+    _check(load_library().brownout_moe_w4_matmul(BMOE_BF16, n, rows, N, K, op, rp, m, ap, w._on(device), yp, _stream_ptr(stream, device)),
            "brownout_moe_w4_matmul")
     return y
 
@@ -671,8 +677,8 @@ def w4_gate_up(offsets: torch.Tensor, a: torch.Tensor, w_gate: W4, w_up: W4, *, 
     n, f, d = _w4_gated(w_gate, w_up)
     rows, op, rp, m, ap = _w4_rows(offsets, a, a_rows, n, d, device)
     h, hp = _out(h, "h", (rows, f), a, device)
-    _check(load_library().brownout_moe_w4_gate_up(BMOE_BF16, n, rows, d, f, op, rp, m, ap, w_gate._ref, w_up._ref, hp,
-                                                  _stream_ptr(stream, device)), "brownout_moe_w4_gate_up")
+    _check(load_library().brownout_moe_w4_gate_up(BMOE_BF16, n, rows, d, f, op, rp, m, ap, w_gate._on(device),
+                                                  w_up._on(device), hp, _stream_ptr(stream, device)), "brownout_moe_w4_gate_up")
     return h
 
 
@@ -686,8 +692,8 @@ def w4_ffn(offsets: torch.Tensor, a: torch.Tensor, w_gate: W4, w_up: W4, w_down:
     rows, op, rp, m, ap = _w4_rows(offsets, a, a_rows, n, d, device)
     h, hp = _out(h, "h", (rows, f), a, device)
     y, yp = _out(y, "y", (rows, d), a, device)
-    _check(load_library().brownout_moe_w4_ffn(BMOE_BF16, n, rows, d, f, op, rp, m, ap, w_gate._ref, w_up._ref,
-                                              w_down._ref, hp, yp, _stream_ptr(stream, device)), "brownout_moe_w4_ffn")
+    _check(load_library().brownout_moe_w4_ffn(BMOE_BF16, n, rows, d, f, op, rp, m, ap, w_gate._on(device), w_up._on(device),
+                                              w_down._on(device), hp, yp, _stream_ptr(stream, device)), "brownout_moe_w4_ffn")
     return y, h
 
 
@@ -861,26 +867,28 @@ class LayerForward:
         dt, d, E, G = desc.torch_dtype, desc.d, desc.E, desc.G
         if self.w4 and desc.dtype != BMOE_BF16:
             raise ValueError("4-bit weights need a bf16 layer")
-        _dev(w["w_router"], "w_router", dt, (E, d))
-        _dev(w["e2g"], "e2g", torch.int32, (E,))
+        device = _device_of(w["e2g"], "e2g")
+        _fits(w["w_router"], "w_router", dt, (E, d), device)
+        _fits(w["e2g"], "e2g", torch.int32, (E,), device)
         if w.get("bias") is not None:
-            _dev(w["bias"], "bias", torch.float32, (E,))
+            _fits(w["bias"], "bias", torch.float32, (E,), device)
         shapes = {"w_gate": (G, desc.d_ff, d), "w_up": (G, desc.d_ff, d), "w_down": (G, d, desc.d_ff)}
         if desc.d_ff_shared:
             fs = desc.d_ff_shared
             shapes.update(w_gate_sh=(1, fs, d), w_up_sh=(1, fs, d), w_down_sh=(1, d, fs))
         for name, shape in shapes.items():
             if not self.w4:
-                _dev(w[name], name, dt, shape)
+                _fits(w[name], name, dt, shape, device)
                 continue
             m, first = w[name], w["w_gate"]
             if not isinstance(m, W4):
                 raise ValueError(f"{name} must be a W4, as w_gate is")
+            m._on(device)
             if m.shape != shape:
                 raise ValueError(f"{name} must have shape {shape}, got {m.shape}")
             if m.group != first.group or (m.zeros is None) != (first.zeros is None):
                 raise ValueError(f"{name} must have w_gate's group size, and zero points as it has")
-        self._few_names = tuple(shapes)
+        self._few_names, self._few_device = tuple(shapes), device
 
     def _plan_few(self, device):
         """Buffers and the marshalled arguments of a few_tokens layer."""
@@ -917,7 +925,10 @@ class LayerForward:
         """The whole layer in one call (few_tokens layers)."""
         if not self.few_tokens:
             raise ValueError("few needs a layer made with few_tokens=True")
-        _check(self._lib.brownout_moe_few(*self._few_head, self._x(x), *self._few_tail, self._s(stream)),
+        xp, device = self._x(x), _device_of(x, "x")
+        if device != self._few_device:
+            raise ValueError(f"x is on GPU {device}, the layer on GPU {self._few_device}")
+        _check(self._lib.brownout_moe_few(*self._few_head, xp, *self._few_tail, _stream_ptr(stream, device)),
                "brownout_moe_few")
         return self.bufs["out"]
 

@@ -294,3 +294,16 @@ def test_few_graph_and_streams(dtype, group, zeros):
         q = other(xs[1], stream=side)
         torch.cuda.synchronize()
         assert torch.equal(p, want[0]) and torch.equal(q, want[1])
+
+
+def test_another_device_is_refused():
+    case = CASES["one"]
+    c, _ = R.make_case(5, group=32, **case)
+    w, x = to_gpu(c, case, 32)
+    layer = B.LayerForward(desc_of(case, "bf16"), w, few_tokens=True)
+    layer._few_device += 1
+    with pytest.raises(ValueError, match="the layer on GPU"):
+        layer(x)
+    w["w_up"].device += 1
+    with pytest.raises(ValueError, match="4-bit weights are on GPU"):
+        B.LayerForward(desc_of(case, "bf16"), w, few_tokens=True)

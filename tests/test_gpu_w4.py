@@ -234,3 +234,13 @@ def test_w4_graph_and_stream():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(y1, want[0]) and torch.equal(h1, want[1]), f"replay {k}"
+
+
+def test_weights_of_another_device_are_refused():
+    rng = np.random.default_rng(8)
+    w = _w4(R.w4_random(rng, 1, 32, 32, 32, False), 32, 32)
+    a, off = R.rand(rng, (2, 32), 1.0, "bf16").cuda(), torch.tensor([0, 2], dtype=torch.int32, device="cuda")
+    w.device += 1
+    for call in (lambda: B.w4_matmul(off, a, w), lambda: B.w4_gate_up(off, a, w, w), lambda: B.w4_ffn(off, a, w, w, w)):
+        with pytest.raises(ValueError, match="4-bit weights are on GPU"):
+            call()
