@@ -20,6 +20,9 @@
  *   brownout_moe_dispatch  per-group histogram, prefix, stable permutation, row gather
  *   brownout_moe_ffn       grouped SwiGLU FFN over the united experts
  *   brownout_moe_combine   gate-weighted sum back into token order
+ * For up to 16 tokens one call does the same (brownout_moe_few). The experts may be held
+ * in 4 bits (bmoe_w4; brownout_moe_w4_ffn in place of brownout_moe_ffn, or brownout_moe_few).
+ * brownout_moe_pre_norm and brownout_moe_post_norm are the layer's two ends in a residual block.
  *
  * Conventions for every call:
  *   - Tensor pointers are DEVICE pointers, row-major, owned by the caller. The
