@@ -29,6 +29,12 @@
 // significand) and multiplied as such, since the matrix cores idle here anyway;
 // so the layer's output is rounded once. Up to eight tokens have their high parts
 // in rows 0..7 of the A operand and their low parts in rows 8..15.
+//
+// d 2048, 60 experts, top-4, 15 segments, d_ff 1408, kernel by kernel: one token 2.9 +
+// 14.4 + 9 us (63 MB; of the second 3.5 before its first weights), 16 tokens 4.6 + 30 +
+// 19 (177 MB), one token in 4 bits 2.8 + 10 + 7.8 (17 MB: latency). Two tokens of d 4096,
+// d_ff 14336: 4.6 + 121 + 65 (914 MB, 4.9 TB/s); six of them in 4 bits 4.8 + 63 + 42
+// (331 MB: two waves a SIMD by registers, each with one unit on its way).
 #pragma once
 
 #include <math.h>

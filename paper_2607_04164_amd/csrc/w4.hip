@@ -9,6 +9,13 @@
 // A wave loads a unit of weights, then takes its columns step by step; the activations
 // of the next steps (from the L2 cache) are loaded while these are multiplied. The
 // waves' partial tiles are added through LDS in wave order.
+//
+// Bound by latency: a workgroup takes about 10 us (its segment 1, the first loads 3,
+// products 3.3, sums and stores 2.5), one of them a CU by registers. 250 rows of 8
+// segments, gate and up 1408 x 2048, down 2048 x 1408, groups of 32: 24 + 15 us for
+// 43 MB; 1000 rows of 32 segments of 2048 x 2048: 49 us for 82 MB. Workgroups that stay
+// and load the next item's first unit before they add this one's partials need all 256
+// registers: 44 us for the second, but 39.2 against 37.4 for the first.
 #include "bmoe_common.h"
 #include "w4.h"
 
@@ -286,6 +293,8 @@ template <int NR>
 hipError_t launch_w4(const W4Params& p, int group, hipStream_t s) {
     // passes: at most one for 32 rows, and one more for the rest of each segment's rows
     const int64_t passes = (int64_t)p.rows_cap / kW4Rows + (p.n_seg < p.rows_cap ? p.n_seg : p.rows_cap);
+    // fewer workgroups than CUs: one tile of each matrix a wave (one row of 4096 x 4096, groups of
+    // 128: 7.0 us, with four tiles 9.5; where there are more, the FFN above takes 24.8 + 16.1 with two)
     if (passes * ceil_div(p.N, 64 / NR) < 256) return launch_w4_tiles<NR, NR>(p, group, passes, s);
     return launch_w4_tiles<NR, 4>(p, group, passes, s);
 }
