@@ -98,6 +98,18 @@ def test_every_token_count(dtype, group, zeros):
         check(layer, layer(x), reference(c, vals, case), dtype, f"T={T}")
 
 
+@pytest.mark.parametrize("dtype,group,zeros", [f for f in FORMATS if f[0] == "bf16"], ids=[i for i in IDS if i != "f32"])
+@pytest.mark.parametrize("T", [3, 11])
+def test_more_columns_than_the_chip_holds(T, dtype, group, zeros):
+    """16392 output columns: too many tiles for workgroups to share one, and activations past the LDS."""
+    case = dict(T=T, d=16392, E=4, top_k=2, G=2, f=72, fs=8)
+    c, vals = R.make_case(17, dtype=dtype, group=group, zeros=zeros, **case)
+    w, x = to_gpu(c, case, group)
+    layer = B.LayerForward(desc_of(case, dtype), w, few_tokens=True)
+    layer.ws.fill_(0xFF)
+    check(layer, layer(x), reference(c, vals, case), dtype, f"T={T}")
+
+
 def test_ties_and_masked_experts():
     """Equal router rows (the lower index wins) and experts masked by the lowest bias, fewer left than top_k."""
     case = dict(T=6, d=128, E=12, top_k=5, G=4, f=64)

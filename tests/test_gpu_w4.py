@@ -244,3 +244,36 @@ def test_weights_of_another_device_are_refused():
     for call in (lambda: B.w4_matmul(off, a, w), lambda: B.w4_gate_up(off, a, w, w), lambda: B.w4_ffn(off, a, w, w, w)):
         with pytest.raises(ValueError, match="4-bit weights are on GPU"):
             call()
+
+
+@pytest.mark.parametrize("n,rows", [(65, 64), (200, 300), (256, 1000)])
+def test_more_segments_than_lanes(n, rows):
+    rng = np.random.default_rng(n)
+    N, K, group = 24, 72, 32
+    t = R.w4_random(rng, n, N, K, group, True)
+    offs = _segments(rng, rows, n)
+    offs[n // 2:] = offs[n // 2]  # the second half's rows belong to the last segment
+    offs[n] = rows
+    a = R.rand(rng, (rows, K), 1.0, "bf16")
+    y = B.w4_matmul(torch.from_numpy(offs).cuda(), a.cuda(), _w4(t, K, group))
+    w64, mag, a64 = R.w4_values(*t, K, group), R.w4_magnitude(*t, K, group), R.np64(a)
+    for s in range(n):
+        sl = slice(offs[s], offs[s + 1])
+        _check(y, a64[sl] @ w64[s].T, _sum_error(K, group) * np.abs(a64[sl]) @ mag[s].T, sl, f"segment {s}")
+
+
+def test_more_passes_than_a_launch_has():
+    """160 segments of a row and 2^20 columns: 16384 blocks of columns, of which a launch holds 128 passes."""
+    n, N, K, group = 160, 1 << 20, 8, 32
+    g = torch.Generator(device="cuda").manual_seed(3)
+    codes = torch.randint(0, 256, (n, N, 16), generator=g, device="cuda", dtype=torch.uint8)
+    scales = (torch.rand((n, N, 1), generator=g, device="cuda") + 0.5).to(torch.bfloat16)
+    a = torch.randn((n, K), generator=g, device="cuda").to(torch.bfloat16)
+    y = B.w4_matmul(torch.arange(n + 1, dtype=torch.int32, device="cuda"), a, B.W4(codes, scales, K=K, group=group))
+    cols = torch.cat([torch.arange(40), torch.arange(40, N - 40, N // 41), torch.arange(N - 40, N)]).cuda()
+    t = codes[:, cols].cpu(), scales[:, cols].cpu(), None
+    w64, mag, a64 = R.w4_values(*t, K, group), R.w4_magnitude(*t, K, group), R.np64(a)
+    part = y[:, cols]
+    for s in range(n):
+        sl = slice(s, s + 1)
+        _check(part, a64[sl] @ w64[s].T, _sum_error(K, group) * np.abs(a64[sl]) @ mag[s].T, sl, f"segment {s}")
