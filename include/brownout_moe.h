@@ -470,7 +470,8 @@ BMOE_API bmoe_status brownout_moe_w4_quantize(int32_t dtype, int32_t n, int32_t 
  * activations' and outputs'; others are BMOE_ERR_UNSUPPORTED). Segments as in
  * brownout_moe_ffn: segment s covers rows offsets[s] .. offsets[s+1]-1; rows of
  * no segment are left as they are. a_rows as in brownout_moe_ffn_gather, or NULL
- * (row r reads a[r]; a then has rows_cap rows and a_count is not used). No workspace.
+ * (row r reads a[r]; a then has rows_cap rows and a_count is not used). A product's output
+ * is not its input (BMOE_ERR_UNSUPPORTED). No workspace.
  *   brownout_moe_w4_matmul   y[row,:] = a[row,:] W[s]^T                 W [n_seg, N, K]
  *   brownout_moe_w4_gate_up  h[row,:] = silu(a[row,:] Wg[s]^T) * (a[row,:] Wu[s]^T)
  *                            Wg, Wu [n_seg, d_ff, d], the same group and both with or without zeros

@@ -368,6 +368,7 @@ bmoe_status brownout_moe_w4_matmul(int32_t dtype, int32_t n_seg, int32_t rows_ca
                                    const bmoe_w4* w, void* y, void* stream) {
     bmoe_status st = w4_check(dtype, n_seg, rows_cap, N, K, offsets, a_rows, a_count, a, w, nullptr, y);
     if (st != BMOE_OK || rows_cap == 0) return st;
+    if (y == a) return BMOE_ERR_UNSUPPORTED;  // (other workgroups still read a)
     return hip_status(bmoe::launch_w4_gemm(
         bmoe::W4GemmArgs{offsets, a_rows, a_count, a, w, nullptr, y, n_seg, rows_cap, N, K}, (hipStream_t)stream));
 }
@@ -378,6 +379,7 @@ bmoe_status brownout_moe_w4_gate_up(int32_t dtype, int32_t n_seg, int32_t rows_c
     if (rows_cap > 0 && !w_up) return BMOE_ERR_NULL;
     bmoe_status st = w4_check(dtype, n_seg, rows_cap, d_ff, d, offsets, a_rows, a_count, a, w_gate, w_up, h);
     if (st != BMOE_OK || rows_cap == 0) return st;
+    if (h == a) return BMOE_ERR_UNSUPPORTED;
     return hip_status(bmoe::launch_w4_gemm(
         bmoe::W4GemmArgs{offsets, a_rows, a_count, a, w_gate, w_up, h, n_seg, rows_cap, d_ff, d},
         (hipStream_t)stream));
@@ -391,6 +393,7 @@ bmoe_status brownout_moe_w4_ffn(int32_t dtype, int32_t n_seg, int32_t rows_cap, 
     bmoe_status st = w4_check(dtype, n_seg, rows_cap, d_ff, d, offsets, a_rows, a_count, a, w_gate, w_up, h);
     if (st == BMOE_OK) st = w4_check(dtype, n_seg, rows_cap, d, d_ff, offsets, nullptr, 0, h, w_down, nullptr, y);
     if (st != BMOE_OK || rows_cap == 0) return st;
+    if (h == a || y == h) return BMOE_ERR_UNSUPPORTED;  // (y may be a: it is read before)
     const hipError_t e = bmoe::launch_w4_gemm(
         bmoe::W4GemmArgs{offsets, a_rows, a_count, a, w_gate, w_up, h, n_seg, rows_cap, d_ff, d}, (hipStream_t)stream);
     if (e != hipSuccess) return BMOE_ERR_HIP;

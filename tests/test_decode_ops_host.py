@@ -95,6 +95,15 @@ def test_w4_ffn_refusals(lib, wu, wd, code):
         assert lib.brownout_moe_w4_gate_up(1, 2, 5, 64, 32, A, None, 0, A, ctypes.byref(w4s()), ref(wu), A, None) == code
 
 
+def test_w4_outputs_are_not_their_inputs(lib):
+    assert matmul(lib, a=A, y=A) == UNSUP
+    ref, other = ctypes.byref(w4s()), A + 4096
+    gate_up = lambda a, h: lib.brownout_moe_w4_gate_up(1, 2, 5, 64, 64, A, None, 0, a, ref, ref, h, None)  # noqa: E731
+    ffn = lambda a, h, y: lib.brownout_moe_w4_ffn(1, 2, 5, 64, 64, A, None, 0, a, ref, ref, ref, h, y, None)  # noqa: E731
+    assert gate_up(A, A) == UNSUP
+    assert ffn(A, A, other) == UNSUP and ffn(A, other, other) == UNSUP
+
+
 @pytest.mark.parametrize("kw,code", [
     ({"dtype": 3}, UNSUP), ({"group": 16}, UNSUP), ({"n": 0}, SHAPE), ({"N": 0}, SHAPE), ({"K": 12}, SHAPE),
     ({"w": None}, NULL), ({"codes": None}, NULL), ({"scales": None}, NULL), ({"w": ODD}, ALIGN), ({"codes": ODD}, ALIGN),
