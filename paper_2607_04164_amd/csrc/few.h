@@ -106,7 +106,8 @@ __device__ __forceinline__ void few_select(const double* logits, const int32_t* 
     for (int j = 0; j < V; ++j) {
         const int e = min(s + 16 * j, E - 1);
         v[j] = logits[tl * E + e];
-        key[j] = (e << 16) | (e2g[e] + 1);
+        const int g = e2g[e];  // (outside [0, G): sent nowhere, as brownout_moe_route takes it)
+        key[j] = (e << 16) | ((unsigned)g < (unsigned)G ? g + 1 : 0);
     }
     unsigned taken = vpl >= V ? 0u : ~0u << vpl;
     double top = 0.0;

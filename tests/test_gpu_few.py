@@ -170,6 +170,35 @@ def test_experts_of_no_segment(dtype, group, zeros, fs):
             assert not out.any()
 
 
+@pytest.mark.parametrize("E,G", [(12, 5), (200, 30)])
+@pytest.mark.parametrize("T", [4, 16])
+def test_map_entries_out_of_range(T, E, G):
+    """An entry outside [0, G), whatever its bits, sends its expert nowhere, as brownout_moe_route takes it."""
+    case = dict(T=T, d=128, E=E, top_k=6, G=G, f=40)
+    wild = [-2, -100, -65536, -(2 ** 31), G, 300, 65535, 65536, 65537 + G, 70000, 131073, 2 ** 31 - 1]
+    c, vals = R.make_case(41, zipf=0.0, **case)
+    # every second of the experts that are picked most often
+    first = reference(c, vals, case)
+    order = np.argsort(-np.bincount(first["topk_idx"].ravel(), minlength=E), kind="stable")
+    for i, e in enumerate(order[:2 * len(wild):2]):
+        c["e2g"][int(e)] = wild[i % len(wild)]
+    w, x = to_gpu(c, case, 0)
+    desc = desc_of(case, "bf16")
+    layer = B.LayerForward(desc, w, few_tokens=True)
+    layer.ws.fill_(0xFF)
+    out = layer(x)
+    want = B.route(desc, x, w["w_router"], w["bias"], w["e2g"])
+    c["e2g"][(c["e2g"] < 0) | (c["e2g"] >= G)] = -1
+    ref = reference(c, vals, case)
+    ref["slot_gate"] = np.where(ref["slot_group"] >= 0, ref["slot_gate"], 0)
+    assert (ref["slot_group"] < 0).any() and (ref["slot_group"] >= 0).any()
+    check(layer, out, ref, "bf16", "map")
+    for n in ("topk_idx", "slot_group"):
+        assert torch.equal(layer.bufs["route"][n], want[n]), n
+    for n in ("topk_w", "slot_gate"):
+        assert_gates(layer.bufs["route"][n].cpu().numpy(), want[n].cpu().numpy(), n)
+
+
 @pytest.mark.parametrize("T", [5, 12])
 @pytest.mark.parametrize("group,zeros", [(32, False), (64, True), (128, True)])
 def test_nan_scales_do_not_spread(T, group, zeros):
