@@ -266,7 +266,8 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ 
             lo = fminf(lo, __shfl_xor(lo, off));
             hi = fmaxf(hi, __shfl_xor(hi, off));
         }
-        const float want = zeros ? (hi - lo) / 15.f : fmaxf(hi, -lo) / 7.f;
+        float want = zeros ? (hi - lo) / 15.f : fmaxf(hi, -lo) / 7.f;
+        if (zeros && isinf(want)) want = (0.5f * hi - 0.5f * lo) / 7.5f;  // (the range is past the largest value)
         const uint16_t sb = f32_to_bf16(want);
         const float s = bf16_to_f32(sb);
         const bool some = s > 0.f;

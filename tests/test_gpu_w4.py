@@ -277,3 +277,24 @@ def test_more_passes_than_a_launch_has():
     for s in range(n):
         sl = slice(s, s + 1)
         _check(part, a64[sl] @ w64[s].T, _sum_error(K, group) * np.abs(a64[sl]) @ mag[s].T, sl, f"segment {s}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_w4_quantize_of_a_range_past_the_largest_value(group, dtype):
+    """max - min is infinite in fp32, the scale is not."""
+    K = 264
+    rng = np.random.default_rng(group)
+    w = R.rand(rng, (1, 6, K), 1.0, dtype)
+    w[0, :, 3::group], w[0, :, 5::group] = 3.0e38, -2.5e38
+    w[0, 1] *= -1
+    q = B.w4_quantize(w.cuda(), group, True)
+    assert bool(torch.isfinite(q.scales).all())
+    w64, s, back = R.np64(w), R.np64(q.scales), R.w4_values(q.codes, q.scales, q.zeros, K, group)
+    ng = -(-K // group)
+    span = np.stack([np.maximum(v.max(-1), 0) - np.minimum(v.min(-1), 0)
+                     for v in (w64[..., g * group:(g + 1) * group] for g in range(ng))], -1) / 15
+    # rounded to bf16 from a value with the roundings of a difference and a quotient
+    assert (np.abs(s - span) <= (R.HALF["bf16"] + 2 * R.HALF["f32"]) * span).all()
+    step = np.repeat(s, group, axis=2)[:, :, :K]
+    assert (np.abs(back - w64) <= (1.0 + 15 * 2.0 ** -8) * step).all()
