@@ -437,7 +437,8 @@ BMOE_API bmoe_status brownout_moe_post_norm(int32_t dtype, int32_t T, int32_t d,
  *   codes  [n, N, P] uint8, P = 16 * ceil(K/32): byte b of a row holds column 2b
  *          in its low four bits and column 2b+1 in its high four; the bytes past
  *          K/2 are padding, their values do not matter;
- *   scales [n, N, ceil(K/group)] bf16 (finite), group 32, 64 or 128;
+ *   scales [n, N, ceil(K/group)] bf16 (finite, or NaN for weights that are not numbers),
+ *          group 32, 64 or 128;
  *   zeros  [n, N, ceil(K/group)] uint8, or NULL: every zero point is 8.
  * Column k of a row stands for  w = scale[k / group] * (code[k] - zero[k / group]).
  * Products are exact in fp32 (bf16 activations on MFMA against code + 16, whose
@@ -459,7 +460,9 @@ typedef struct bmoe_w4 {
  * zero = round(-min / scale), code = zero + round(w / scale) clamped to 0..15.
  * The scale is rounded to bf16 first, and w is divided by the rounded one;
  * rounding is to nearest even. A group of zeros has scale 0 and codes 8 (0 and
- * zero 0 with zeros). Padding bytes are written 0x88. Outputs as above.
+ * zero 0 with zeros). A group with a value that is not finite has scale NaN and the
+ * codes of a group of zeros: all of its weights read NaN, and so do the products with
+ * them. Padding bytes are written 0x88. Outputs as above.
  */
 BMOE_API bmoe_status brownout_moe_w4_quantize(int32_t dtype, int32_t n, int32_t N, int32_t K, int32_t group,
                                      const void* w, uint8_t* codes, void* scales, uint8_t* zeros, void* stream);

@@ -613,7 +613,8 @@ class W4:
 
 
 def w4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, *, stream=None) -> W4:
-    """w [n, N, K] (bf16 or fp32) rounded to 4 bits; zeros: with a zero point per group."""
+    """w [n, N, K] (bf16 or fp32) rounded to 4 bits; zeros: with a zero point per group. A group with a value that
+    is not finite reads NaN throughout."""
     device = _device_of(w, "w")
     if w.dim() != 3:
         raise ValueError("w must be [n, N, K]")

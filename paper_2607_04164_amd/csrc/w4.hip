@@ -249,7 +249,7 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ 
         const int k0 = g * GROUP + l * PER;  // this lane's columns
         const T* src = w + row * (int64_t)K;
         float f[PER / 4][4];
-        float lo = 0.f, hi = 0.f;
+        float lo = 0.f, hi = 0.f, odd = 0.f;  // odd: NaN once a value is not finite
 #pragma unroll
         for (int c = 0; c < PER / 4; ++c) {
             load4<T>(src + min(k0 + 4 * c, K - 4), f[c]);
@@ -258,6 +258,7 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ 
                 for (int j = 0; j < 4; ++j) {
                     lo = fminf(lo, f[c][j]);
                     hi = fmaxf(hi, f[c][j]);
+                    odd = fmaf(f[c][j], 0.f, odd);
                 }
             }
         }
@@ -268,6 +269,7 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ 
         }
         float want = zeros ? (hi - lo) / 15.f : fmaxf(hi, -lo) / 7.f;
         if (zeros && isinf(want)) want = (0.5f * hi - 0.5f * lo) / 7.5f;  // (the range is past the largest value)
+        if ((__ballot(isnan(odd)) >> (threadIdx.x & 56)) & 0xff) want = NAN;  // (any lane of the group)
         const uint16_t sb = f32_to_bf16(want);
         const float s = bf16_to_f32(sb);
         const bool some = s > 0.f;

@@ -298,3 +298,25 @@ def test_w4_quantize_of_a_range_past_the_largest_value(group, dtype):
     assert (np.abs(s - span) <= (R.HALF["bf16"] + 2 * R.HALF["f32"]) * span).all()
     step = np.repeat(s, group, axis=2)[:, :, :K]
     assert (np.abs(back - w64) <= (1.0 + 15 * 2.0 ** -8) * step).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("zeros", [False, True], ids=["sym", "zeros"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("K", [8, 200, 384])
+def test_w4_quantize_marks_groups_that_are_not_finite(K, group, zeros, dtype):
+    """A NaN or infinite weight makes its group's scale NaN; every other group is as without it."""
+    rng = np.random.default_rng(K + group)
+    w = R.rand(rng, (2, 9, K), 0.02, dtype)
+    clean = B.w4_quantize(w.cuda(), group, zeros)
+    ng = -(-K // group)
+    bad = np.zeros((2, 9, ng), bool)
+    for i, v in enumerate((float("nan"), float("inf"), -float("inf"), float("nan"))):
+        for row, k in ((2 * i, (7 * i + 3) % K), (2 * i, K - 1), (2 * i + 1, K // 2)):
+            w[i % 2, row, k] = v
+            bad[i % 2, row, k // group] = True
+    q = B.w4_quantize(w.cuda(), group, zeros)
+    back, was = (R.w4_values(t.codes, t.scales, t.zeros, K, group) for t in (q, clean))
+    cols = np.repeat(bad, group, axis=2)[:, :, :K]
+    assert np.isnan(back[cols]).all() and np.array_equal(back[~cols], was[~cols])
+    assert bool((q.codes[..., -(-K // 2):] == 0x88).all())  # (padding)
