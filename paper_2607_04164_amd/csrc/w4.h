@@ -10,6 +10,10 @@
 // units, not the matrix cores, bound a product of more than a few rows). The offset
 // costs about 5 times the rounding of the plain sum (16 + q against q - z), far
 // below the bf16 output's.
+// Where the terms leave fp32 though the product itself does not (activations near the
+// largest value), or an activation is infinite (acc and its offset are then infinities
+// of opposite signs), the result is not finite: such a result is computed again as it
+// is defined (w4_defined).
 //
 // A wave owns MT = 4 tiles of 16 rows of W (the B operands; of one matrix, or two of
 // each of two; where that makes too few workgroups, one tile of each matrix) and one
@@ -226,5 +230,30 @@ struct W4Spread {
         return __builtin_amdgcn_mfma_f32_16x16x4f32(xs, __uint_as_float(offset[g >> 2][m]), tot, 0, 0, 0);
     }
 };
+
+// sum over k of x_k s (q_k - z) for one row of W as it is defined, in float64 (every term
+// is exact there). load(k, f): columns k .. k + 7 of x. One lane's work, for the few
+// results that are not finite.
+template <int GROUP, class Load>
+__device__ __forceinline__ double w4_defined(const W4Stack& w, int64_t row, int K, Load load) {
+    const int ng = ceil_div(K, GROUP);
+    const uint8_t* codes = w.codes + row * BMOE_W4_ROW_BYTES(K);
+    double sum = 0.0;
+#pragma clang loop unroll(disable)
+    for (int k = 0; k < K && !isnan(sum); k += 8) {
+        const int64_t g = row * ng + k / GROUP;
+        const double s = bf16_to_f32(w.scales[g]);
+        const int z = w.has_zeros ? w.zeros[g] : 8;
+        uint32_t c = *(const uint32_t*)(codes + k / 2);
+        float f[8];
+        load(k, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            sum = fma(s * ((int)(c & 15u) - z), (double)f[j], sum);
+            c >>= 4;
+        }
+    }
+    return sum;
+}
 
 }  // namespace bmoe

@@ -19,6 +19,7 @@
 #include <type_traits>
 
 #include "bmoe_common.h"
+#include "chunk16.h"
 #include "w4.h"
 
 namespace bmoe {
@@ -200,10 +201,21 @@ __global__ __launch_bounds__(64 * w4_waves(MT), w4_waves(MT) / 4) void w4_gemm_k
 #pragma unroll
                 for (int w = 1; w < WAVES; ++w) sum[m] += d[w * kW4Tiles * MT * 64];
             }
+            unsigned again = 0;  // rows whose sums are not finite
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float v = NR == 2 ? silu_mul(sum[0][e], sum[NR - 1][e]) : sum[0][e];
-                if (row + e < rows) p.C[(size_t)(at.beg + row + e) * N + col] = f32_to_bf16(v);
+                if (row + e >= rows) continue;
+                p.C[(size_t)(at.beg + row + e) * N + col] = f32_to_bf16(v);
+                again |= isfinite(sum[0][e]) && isfinite(sum[NR - 1][e]) ? 0u : 1u << e;
+            }
+            for (; again; again &= again - 1) {
+                const int r = at.beg + row + __ffs(again) - 1;
+                const uint4* x = (const uint4*)(p.A + (size_t)gathered_row(p.a_rows, p.a_count, r) * K);
+                auto load = [&](int k, float* f) { Vec<uint16_t>::load(x[k / 8], f); };
+                float v = (float)w4_defined<GROUP>(p.w[0], (int64_t)at.seg * N + col, K, load);
+                if constexpr (NR == 2) v = silu_mul(v, (float)w4_defined<GROUP>(p.w[1], (int64_t)at.seg * N + col, K, load));
+                p.C[(size_t)r * N + col] = f32_to_bf16(v);
             }
         }
         __syncthreads();  // the partials are rewritten by the next turn

@@ -320,3 +320,90 @@ def test_w4_quantize_marks_groups_that_are_not_finite(K, group, zeros, dtype):
     cols = np.repeat(bad, group, axis=2)[:, :, :K]
     assert np.isnan(back[cols]).all() and np.array_equal(back[~cols], was[~cols])
     assert bool((q.codes[..., -(-K // 2):] == 0x88).all())  # (padding)
+
+
+def _same_beyond(got, want, what):
+    """Infinities and NaN where they belong."""
+    for f in (np.isnan, np.isposinf, np.isneginf):
+        assert np.array_equal(f(got), f(want)), f"{what}: {f.__name__}"
+
+
+# (n, rows, N, K): one tile of columns a wave, and four
+BEYOND = [(1, 5, 40, 264), (3, 40, 72, 512), (8, 60, 2048, 264), (8, 60, 2048, 256)]
+
+
+@pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True)])
+@pytest.mark.parametrize("n,rows,N,K", BEYOND)
+def test_activations_whose_sums_leave_fp32(n, rows, N, K, group, zeros):
+    """Finite products of activations near the largest value, whose sums with the codes + 16 would be infinite,
+    and infinite activations: what the definition gives. Rows beside them are as they would be alone."""
+    rng = np.random.default_rng(rows + K)
+    t = R.w4_random(rng, n, N, K, group, zeros)
+    offs = _segments(rng, rows, n) if n > 1 else np.array([0, rows], np.int32)
+    a = R.rand(rng, (rows, K), 1.0, "bf16")
+    off, w = torch.from_numpy(offs).cuda(), _w4(t, K, group)
+    clean = B.w4_matmul(off, a.cuda(), w)
+    kind = np.arange(rows) % 5  # 0: as it was
+    for r in range(rows):
+        k = rng.choice(K, 4, replace=False)
+        if kind[r] == 1:
+            a[r, k[0]] = 3.3e38 * (-1) ** r
+        elif kind[r] == 2:  # a sum that cancels
+            a[r, k[0]], a[r, k[1]], a[r, k[2]] = 3.0e38, 3.0e38, -3.0e38
+        elif kind[r] == 3:
+            a[r, k[0]] = float("inf") * (-1) ** r
+        elif kind[r] == 4:
+            a[r, k[3]] = float("nan") if r % 2 else float("inf")
+    y = B.w4_matmul(off, a.cuda(), w)
+    keep = torch.from_numpy(kind == 0).cuda()
+    assert torch.equal(y[keep], clean[keep])
+    with np.errstate(invalid="ignore"):
+        for s in range(n):
+            rs = np.arange(offs[s], offs[s + 1])
+            w64, mag = R.w4_values(*t, K, group)[s], R.w4_magnitude(*t, K, group)[s]
+            finite = rs[kind[rs] < 3]
+            a64 = R.np64(a)[finite]
+            _check(y, a64 @ w64.T, _sum_error(K, group) * np.abs(a64) @ mag.T, finite, f"segment {s}")
+            rest = rs[kind[rs] >= 3]
+            want = (R.np64(a)[rest][:, None, :] * w64[None]).sum(-1)
+            _same_beyond(R.np64(y)[rest], want, f"segment {s}")
+
+
+@pytest.mark.parametrize("n,rows,f,d", [(2, 9, 40, 264), (8, 70, 1024, 264)])
+@pytest.mark.parametrize("group,zeros", [(32, False), (64, True)])
+def test_hidden_values_whose_sums_leave_fp32(n, rows, f, d, group, zeros):
+    """gate_up of large activations, and a product of the infinite h that it stored."""
+    rng = np.random.default_rng(rows + f)
+    tg, tu = (R.w4_random(rng, n, f, d, group, zeros) for _ in range(2))
+    td = R.w4_random(rng, n, d, f, group, zeros)
+    tu[1][:, 1::2, 0] = 0  # every second hidden value has no part of the large activation in its factor
+    offs = _segments(rng, rows, n)
+    a = R.rand(rng, (rows, d), 1.0, "bf16")
+    a[::2, 3] = 3.0e38
+    off = torch.from_numpy(offs).cuda()
+    y, h = B.w4_ffn(off, a.cuda(), _w4(tg, d, group), _w4(tu, d, group), _w4(td, f, group))
+    a64, h64, y64 = R.np64(a), R.np64(h), R.np64(y)
+    e = _sum_error(d, group)
+    with np.errstate(invalid="ignore", over="ignore"):
+        for s in range(n):
+            sl = slice(offs[s], offs[s + 1])
+            wg, wu, wd = (R.w4_values(*t, K, group)[s] for t, K in ((tg, d), (tu, d), (td, f)))
+            g, u = a64[sl] @ wg.T, a64[sl] @ wu.T
+            eg = e * np.abs(a64[sl]) @ R.w4_magnitude(*tg, d, group)[s].T
+            eu = e * np.abs(a64[sl]) @ R.w4_magnitude(*tu, d, group)[s].T
+            want = R.silu(g) * u
+            # (a product past the type's largest value, by more than its error, is infinite)
+            err = 1.1 * np.abs(u) * eg + (np.abs(R.silu(g)) + 1.1 * eg) * eu + 2.0 ** -20 * np.abs(want)
+            tol = R.HALF["bf16"] * (np.abs(want) + err) + err
+            past = np.abs(want) - tol > float(torch.finfo(torch.bfloat16).max)
+            assert past.any() or sl.stop - sl.start < 2
+            assert np.array_equal(h64[sl][past], np.sign(want[past]) * np.inf)
+            sure = np.abs(want) + tol < float(torch.finfo(torch.bfloat16).max)
+            assert (np.abs(h64[sl] - want)[sure] <= tol[sure]).all()
+            hs = h64[sl]
+            wanty = (hs[:, None, :] * wd[None]).sum(-1)
+            fin = np.isfinite(hs).all(-1)
+            _same_beyond(y64[sl][~fin], wanty[~fin], f"segment {s}")
+            tol = _sum_error(f, group) * np.abs(hs[fin]) @ R.w4_magnitude(*td, f, group)[s].T
+            tol = R.HALF["bf16"] * (np.abs(wanty[fin]) + tol) + tol
+            assert (np.abs(y64[sl][fin] - wanty[fin]) <= tol).all()
