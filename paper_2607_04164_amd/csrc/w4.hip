@@ -201,16 +201,16 @@ __global__ __launch_bounds__(64 * w4_waves(MT), w4_waves(MT) / 4) void w4_gemm_k
 #pragma unroll
                 for (int w = 1; w < WAVES; ++w) sum[m] += d[w * kW4Tiles * MT * 64];
             }
-            unsigned again = 0;  // rows whose sums are not finite
+            unsigned again = 0;  // rows whose result is not finite
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float v = NR == 2 ? silu_mul(sum[0][e], sum[NR - 1][e]) : sum[0][e];
-                if (row + e >= rows) continue;
-                p.C[(size_t)(at.beg + row + e) * N + col] = f32_to_bf16(v);
-                again |= isfinite(sum[0][e]) && isfinite(sum[NR - 1][e]) ? 0u : 1u << e;
+                again |= isfinite(v) ? 0u : 1u << e;
+                if (row + e < rows) p.C[(size_t)(at.beg + row + e) * N + col] = f32_to_bf16(v);
             }
-            for (; again; again &= again - 1) {
+            for (; __builtin_expect(again != 0, 0); again &= again - 1) {
                 const int r = at.beg + row + __ffs(again) - 1;
+                if (r >= at.end) break;
                 const uint4* x = (const uint4*)(p.A + (size_t)gathered_row(p.a_rows, p.a_count, r) * K);
                 auto load = [&](int k, float* f) { Vec<uint16_t>::load(x[k / 8], f); };
                 float v = (float)w4_defined<GROUP>(p.w[0], (int64_t)at.seg * N + col, K, load);
@@ -274,14 +274,15 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T* __restrict__ 
                 }
             }
         }
+        hi = isnan(odd) ? INFINITY : hi;  // (neither minimum nor maximum keeps a NaN)
 #pragma unroll
         for (int off = 4; off; off >>= 1) {
             lo = fminf(lo, __shfl_xor(lo, off));
             hi = fmaxf(hi, __shfl_xor(hi, off));
         }
         float want = zeros ? (hi - lo) / 15.f : fmaxf(hi, -lo) / 7.f;
-        if (zeros && isinf(want)) want = (0.5f * hi - 0.5f * lo) / 7.5f;  // (the range is past the largest value)
-        if ((__ballot(isnan(odd)) >> (threadIdx.x & 56)) & 0xff) want = NAN;  // (any lane of the group)
+        // infinite with finite values: zeros, and the range is past the largest value
+        if (__builtin_expect(isinf(want), 0)) want = isinf(fmaxf(hi, -lo)) ? NAN : (0.5f * hi - 0.5f * lo) / 7.5f;
         const uint16_t sb = f32_to_bf16(want);
         const float s = bf16_to_f32(sb);
         const bool some = s > 0.f;
