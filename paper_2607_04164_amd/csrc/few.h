@@ -40,6 +40,7 @@
 #include <math.h>
 
 #include "bmoe_common.h"
+#include "chunk16.h"
 #include "route_select.h"
 #include "w4.h"
 
@@ -162,7 +163,7 @@ struct FmtPlain {
     typedef ActT Act;
     static constexpr bool kBf16 = sizeof(Act) == 2;
     static constexpr int EPC = 16 / sizeof(Act), LD = 2, UK = 4 * EPC * LD, PARTS = kBf16 ? 2 : 1;
-    static constexpr bool PAIRS = true, X_IN_LDS = false;
+    static constexpr bool PAIRS = true, X_IN_LDS = false, OFFSET = false;
     static constexpr int UP_TILES = PARTS, UP_WAVES = 4;  // (at most, of bf16)
     static constexpr int DOWN_TILES = PARTS, PACK_TILES = 1, DOWN_BATCH = 2, DOWN_WAVES = 3;
     struct Stack {
@@ -235,11 +236,24 @@ template <int GROUP>
 struct FmtW4 {
     typedef uint16_t Act;
     static constexpr int UK = kW4Unit, LD = UK / 32, PARTS = 2;
-    static constexpr bool PAIRS = false, X_IN_LDS = true;
+    static constexpr bool PAIRS = false, X_IN_LDS = true, OFFSET = true;
     static constexpr int UP_TILES = 2, UP_WAVES = 2;
     static constexpr int DOWN_TILES = 4, PACK_TILES = 4, DOWN_BATCH = 1, DOWN_WAVES = 2;
     static constexpr int NG = W4Unit<GROUP>::NG, STEPS = GROUP / 32;
     typedef W4Stack Stack;
+    // the product of a row of W with x (the sum of PARTS_OF_X parts, `part` apart), as defined
+    template <int PARTS_OF_X>
+    __device__ static __forceinline__ double defined(const Stack& w, int64_t row, int K, const uint16_t* x, int64_t part) {
+        return w4_defined<GROUP>(w, row, K, [&](int k, float* f) {
+            Vec<uint16_t>::load(*(const uint4*)(x + k), f);
+            if constexpr (PARTS_OF_X == 2) {
+                float low[8];
+                Vec<uint16_t>::load(*(const uint4*)(x + part + k), low);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] += low[j];  // (exact: 16 bits)
+            }
+        });
+    }
     template <int NR, int NM>
     using Place = W4Place<GROUP, NR, NM>;
     struct X {
@@ -332,7 +346,7 @@ __device__ __forceinline__ FmtF32::Stack pick(bool first, FmtF32::Stack a, FmtF3
 }
 __device__ __forceinline__ W4Stack pick(bool first, W4Stack a, W4Stack b) {
     return {pick(first, a.codes, b.codes), pick(first, a.scales, b.scales), pick(first, a.zeros, b.zeros),
-            pick(first, a.groups, b.groups), a.has_zeros};
+            pick(first, a.groups, b.groups), pick(first, a.has_zeros, b.has_zeros)};
 }
 
 template <class F>
@@ -615,7 +629,21 @@ __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewPara
             if (slot >= 0) {
                 const float g = tile_sum<WAVES>(part[parity][2 * (at_col >> 4)], token, at_col & 15);
                 const float u = tile_sum<WAVES>(part[parity][2 * (at_col >> 4) + 1], token, at_col & 15);
-                const float v = silu_mul(g, u) * (it.shared ? 1.f : sm.gate[slot]);
+                float v = silu_mul(g, u);
+                if constexpr (F::OFFSET) {
+                    if (__builtin_expect(!isfinite(v), 0)) {
+                        const int64_t row = (int64_t)(it.shared ? 0 : sm.segs[it.place]) * N + col;
+                        float g1 = g, u1 = u;
+#pragma clang loop unroll(disable)
+                        for (int m = 0; m < 2; ++m) {  // W_gate, then W_up
+                            g1 = u1;
+                            u1 = (float)F::template defined<1>(pick(it.shared, p.up_sh[m], p.up[m]), row, d,
+                                                               p.x + (size_t)token * d, 0);
+                        }
+                        v = silu_mul(g1, u1);
+                    }
+                }
+                v *= it.shared ? 1.f : sm.gate[slot];
                 const int64_t at = (it.shared ? (int64_t)T * k * f : 0) + (int64_t)slot * N + col;
                 store_hidden(p.h, p.h_part, at, v);
             }
@@ -640,6 +668,21 @@ struct DownUnit {
         }
     }
 };
+
+// column c of token t's output from the stored hidden values, as defined
+template <class F>
+__device__ __forceinline__ float defined_output(const FewParams<F>& p, int t, int c) {
+    double sum = 0.0;
+#pragma clang loop unroll(disable)
+    for (int i = 0; i <= p.k; ++i) {  // (the last one: the shared experts)
+        const bool sh = i == p.k;
+        const int slot = t * p.k + min(i, p.k - 1), g = sh ? 0 : p.slot_group[slot], width = pick(sh, p.fs, p.f);
+        if (sh ? p.fs == 0 : (unsigned)g >= (unsigned)p.G) continue;
+        const int64_t at = sh ? (int64_t)p.T * p.k * p.f + (int64_t)t * p.fs : (int64_t)slot * p.f;
+        sum += F::template defined<2>(pick(sh, p.down_sh, p.down), (int64_t)g * p.d + c, width, p.h + at, p.h_part);
+    }
+    return (float)sum;
+}
 
 // PACK: at most 8 tokens, both parts of their hidden values in one A operand
 // RAGGED: d_ff or d_ff_shared is not whole units
@@ -798,6 +841,9 @@ __global__ __launch_bounds__(kDownThreads, F::DOWN_WAVES) void few_down_kernel(F
     for (int m = 0; m < TILES; ++m) {
         const int c = n0 + 16 * m + col;
         if (t < T && c < d) {
+            if constexpr (F::OFFSET) {
+                if (__builtin_expect(!isfinite(v[m]), 0)) v[m] = defined_output(p, t, c);
+            }
             typename F::Act* o = p.out + (size_t)t * d + c;
             if constexpr (sizeof(typename F::Act) == 2) *o = f32_to_bf16(v[m]);
             else *o = v[m];

@@ -1,8 +1,6 @@
 // The few-token layer (see few.h): gate logits, sizes, and the layers of plain weights.
 #include "few.h"
 
-#include "chunk16.h"
-
 namespace bmoe {
 namespace {
 

@@ -348,3 +348,69 @@ def test_another_device_is_refused():
     w["w_up"].device += 1
     with pytest.raises(ValueError, match="4-bit weights are on GPU"):
         B.LayerForward(desc_of(case, "bf16"), w, few_tokens=True)
+
+
+def _hidden_then_out(x, slots, vals):
+    """One token's output from hidden values held in fp32, where they can be infinite; slots: (segment, gate, shared)."""
+    out = np.zeros(len(x))
+    with np.errstate(all="ignore"):
+        for g, gate, sh in slots:
+            wg, wu, wd = (vals[n + "_sh" * sh][g] for n in ("w_gate", "w_up", "w_down"))
+            h = (R.silu(wg @ x) * (wu @ x) * np.float64(gate)).astype(np.float32).astype(np.float64)
+            out += (wd * h).sum(1)
+    return out
+
+
+@pytest.mark.parametrize("T", [3, 8, 16])
+@pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True)])
+@pytest.mark.parametrize("fs", [0, 72])
+def test_sums_that_leave_fp32(T, group, zeros, fs):
+    """4-bit layers: activations and hidden values near the largest value, whose sums with the codes + 16 would be
+    infinite; then infinite hidden values. Tokens beside them are as they would be alone. (In one of the cases a
+    hidden value of the shared experts is past the largest value already with one large factor: -3.427e38.)"""
+    case = dict(T=T, d=264, E=6, top_k=2, G=3, f=200, fs=fs)
+    c, vals = R.make_case(51, group=group, zeros=zeros, **case)
+    K = {"w_gate": 264, "w_up": 264, "w_down": 200, "w_gate_sh": 264, "w_up_sh": 264, "w_down_sh": fs}
+    names = ["w_gate", "w_up"] + (["w_gate_sh", "w_up_sh"] if fs else [])
+    c["w_router"][:, 0] = 0
+    for n in names:
+        c[n][1][:, :, 0] = 0  # columns of the first group: only in the hidden columns below
+    for n in names:
+        c[n][0][:, 5, 0] |= 15  # (code 15 in column 0)
+        if zeros:
+            c[n][2][:, 5, 0] = 8
+    for n in names[::2]:
+        c[n][1][:, 5, 0] = 0.05  # a large factor of one hidden column, the other one stays as it is
+    w, x = to_gpu(c, case, group)
+    clean = B.LayerForward(desc_of(case, "bf16"), w, few_tokens=True)(x).clone()
+    hot = np.arange(T) % 3 == 1
+    c["x"][torch.from_numpy(hot), 0] = 3.0e38
+    x64, finite = R.np64(c["x"]), 0
+    for factors in (1, 2):
+        if factors == 2:
+            for n in names[1::2]:
+                c[n][1][:, 5, 0] = 0.05
+        for n in vals:
+            vals[n] = R.w4_values(*c[n], K[n], group)
+        with np.errstate(all="ignore"):
+            ref = reference(c, vals, case)
+        w, x = to_gpu(c, case, group)
+        layer = B.LayerForward(desc_of(case, "bf16"), w, few_tokens=True)
+        layer.ws.fill_(0xFF)
+        out = layer(x)
+        o64 = R.np64(out)
+        for t in np.flatnonzero(hot):
+            slots = [(g, gate, 0) for g, gate in zip(ref["slot_group"][t], ref["slot_gate"][t]) if g >= 0]
+            want = _hidden_then_out(x64[t], slots + ([(0, 1.0, 1)] if fs else []), vals)
+            if np.isfinite(want).all():
+                assert factors == 1 and np.abs(want).max() > 1e35
+                R.assert_few(out[t:t + 1], {"out": ref["out"][t:t + 1]}, "bf16", f"token {t}")
+                finite += 1
+                continue
+            assert not np.isfinite(want).any()
+            for f in (np.isnan, np.isposinf, np.isneginf):
+                assert np.array_equal(f(o64[t]), f(want)), f"token {t}: {f.__name__}"
+        keep = torch.from_numpy(~hot).cuda()
+        if factors == 1:
+            assert torch.equal(out[keep], clean[keep])
+    assert finite >= hot.sum() - 1
