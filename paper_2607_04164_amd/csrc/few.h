@@ -629,21 +629,21 @@ __global__ __launch_bounds__(kUpThreads, F::UP_WAVES) void few_up_kernel(FewPara
             if (slot >= 0) {
                 const float g = tile_sum<WAVES>(part[parity][2 * (at_col >> 4)], token, at_col & 15);
                 const float u = tile_sum<WAVES>(part[parity][2 * (at_col >> 4) + 1], token, at_col & 15);
-                float v = silu_mul(g, u);
-                if constexpr (F::OFFSET) {
-                    if (__builtin_expect(!isfinite(v), 0)) {
+                const float gate = it.shared ? 1.f : sm.gate[slot];
+                float v = silu_mul(g, u) * gate;
+                if (__builtin_expect(!isfinite(v), 0)) {
+                    float g1 = g, u1 = u;
+                    if constexpr (F::OFFSET) {
                         const int64_t row = (int64_t)(it.shared ? 0 : sm.segs[it.place]) * N + col;
-                        float g1 = g, u1 = u;
 #pragma clang loop unroll(disable)
                         for (int m = 0; m < 2; ++m) {  // W_gate, then W_up
                             g1 = u1;
                             u1 = (float)F::template defined<1>(pick(it.shared, p.up_sh[m], p.up[m]), row, d,
                                                                p.x + (size_t)token * d, 0);
                         }
-                        v = silu_mul(g1, u1);
                     }
+                    v = silu_mul(g1, u1 * gate);  // (may be finite where silu(g) u is not)
                 }
-                v *= it.shared ? 1.f : sm.gate[slot];
                 const int64_t at = (it.shared ? (int64_t)T * k * f : 0) + (int64_t)slot * N + col;
                 store_hidden(p.h, p.h_part, at, v);
             }

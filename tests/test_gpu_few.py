@@ -414,3 +414,35 @@ def test_sums_that_leave_fp32(T, group, zeros, fs):
         if factors == 1:
             assert torch.equal(out[keep], clean[keep])
     assert finite >= hot.sum() - 1
+
+
+@pytest.mark.parametrize("dtype,group,zeros", FORMATS[:3], ids=IDS[:3])
+def test_gate_keeps_a_hidden_value_finite(dtype, group, zeros):
+    """silu(g) u past the largest value, times the token's gate below it: the hidden value, so the output, is finite."""
+    case = dict(T=3, d=64, E=4, top_k=2, G=4, f=24)
+    c, vals = R.make_case(7, dtype=dtype, group=group, zeros=zeros, zipf=0.0, **case)
+    c["w_router"][:, :32] = 0
+    c["x"][:, :32] = 0
+    c["x"][1, 0], c["x"][1, 1] = 2.0 ** 127, 4.0
+    for n, k in (("w_gate", 0), ("w_up", 1)):
+        if group:
+            codes, scales, _ = c[n]
+            codes[:, 5, :16] = 0x88
+            codes[:, 5, 0] = 0x8A if k == 0 else 0xA8  # two steps in column k, none beside it
+            scales[:, 5, 0] = 0.5
+            codes[:, :5, 0], codes[:, 6:, 0] = 0x88, 0x88
+            vals[n] = R.w4_values(*c[n], 64, group)
+        else:
+            c[n][:, :, :2] = 0
+            c[n][:, 5, :32] = 0
+            c[n][:, 5, k] = 1.0
+            vals[n] = R.np64(c[n])
+    with np.errstate(over="ignore"):
+        ref = reference(c, vals, case)
+    g, gate = ref["slot_group"][1], ref["slot_gate"][1]
+    x = R.np64(c["x"])[1]
+    big = [(R.silu(vals["w_gate"][s] @ x) * (vals["w_up"][s] @ x))[5] for s in g]
+    w, x = to_gpu(c, case, group)
+    layer = B.LayerForward(desc_of(case, dtype), w, few_tokens=True)
+    assert any(b > 3.41e38 for b in big) and all(abs(b * y) < 3.3e38 for b, y in zip(big, gate))
+    check(layer, layer(x), ref, dtype, "gate")
