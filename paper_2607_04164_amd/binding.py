@@ -818,7 +818,7 @@ class LayerForward:
         if self.w4 or self.few_tokens:
             if fold_combine or (self.w4 and fused_gather is False):
                 raise ValueError("fold_combine and fused_gather=False do not go with few_tokens or 4-bit weights")
-            self._check_few_and_w4()
+            self._check_few_and_w4(device)
         if self.few_tokens:
             self._plan_few(device)
             return
@@ -861,14 +861,17 @@ class LayerForward:
                 self._side = torch.cuda.Stream(device=device)
         self._plan()
 
-    def _check_few_and_w4(self):
-        """Checks the weights of a few_tokens or 4-bit layer."""
+    def _check_few_and_w4(self, buffers):
+        """Checks the weights of a few_tokens or 4-bit layer, and that its buffers will be beside them."""
         desc, w = self.desc, self.w
         _check(validate(desc), "bmoe_validate")
         dt, d, E, G = desc.torch_dtype, desc.d, desc.E, desc.G
         if self.w4 and desc.dtype != BMOE_BF16:
             raise ValueError("4-bit weights need a bf16 layer")
         device = _device_of(w["e2g"], "e2g")
+        buffers = torch.device(buffers)
+        if buffers.type != "cuda" or buffers.index not in (None, device):
+            raise ValueError(f"the layer's buffers would be on {buffers}, its weights are on GPU {device}")
         _fits(w["w_router"], "w_router", dt, (E, d), device)
         _fits(w["e2g"], "e2g", torch.int32, (E,), device)
         if w.get("bias") is not None:

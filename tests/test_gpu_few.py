@@ -446,3 +446,15 @@ def test_gate_keeps_a_hidden_value_finite(dtype, group, zeros):
     layer = B.LayerForward(desc_of(case, dtype), w, few_tokens=True)
     assert any(b > 3.41e38 for b in big) and all(abs(b * y) < 3.3e38 for b, y in zip(big, gate))
     check(layer, layer(x), ref, dtype, "gate")
+
+
+@pytest.mark.parametrize("few", [True, False])
+@pytest.mark.parametrize("device", ["cpu", "cuda:1"])
+def test_buffers_on_another_device_are_refused(device, few):
+    case = CASES["one"]
+    c, _ = R.make_case(5, group=32, **case)
+    w, _ = to_gpu(c, case, 32)
+    with pytest.raises(ValueError, match="buffers would be on"):
+        B.LayerForward(desc_of(case, "bf16"), w, device=device, few_tokens=few)
+    for same in ("cuda", "cuda:0", torch.device("cuda", 0)):
+        B.LayerForward(desc_of(case, "bf16"), w, device=same, few_tokens=few)
