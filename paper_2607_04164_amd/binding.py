@@ -815,6 +815,7 @@ class LayerForward:
         self.w = weights
         self.few_tokens = bool(few_tokens)
         self.w4 = isinstance(weights["w_gate"], W4)
+        self._few_device = None  # the GPU of a few_tokens or 4-bit layer
         if self.w4 or self.few_tokens:
             if fold_combine or (self.w4 and fused_gather is False):
                 raise ValueError("fold_combine and fused_gather=False do not go with few_tokens or 4-bit weights")
@@ -929,10 +930,7 @@ class LayerForward:
         """The whole layer in one call (few_tokens layers)."""
         if not self.few_tokens:
             raise ValueError("few needs a layer made with few_tokens=True")
-        xp, device = self._x(x), _device_of(x, "x")
-        if device != self._few_device:
-            raise ValueError(f"x is on GPU {device}, the layer on GPU {self._few_device}")
-        _check(self._lib.brownout_moe_few(*self._few_head, xp, *self._few_tail, _stream_ptr(stream, device)),
+        _check(self._lib.brownout_moe_few(*self._few_head, self._x(x), *self._few_tail, self._s(stream)),
                "brownout_moe_few")
         return self.bufs["out"]
 
@@ -1011,11 +1009,15 @@ class LayerForward:
         if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dtype == self._dt
                 and tuple(x.shape) == self._xshape and x.is_contiguous()):
             _dev(x, "x", self._dt, self._xshape)
+        if self._few_device not in (None, x.get_device()):
+            raise ValueError(f"x is on GPU {x.get_device()}, the layer on GPU {self._few_device}")
         return x.data_ptr()
 
-    @staticmethod
-    def _s(stream) -> int:
-        return _stream_ptr(stream, torch.cuda.current_device() if stream is None else 0)
+    def _s(self, stream) -> int:
+        device = torch.cuda.current_device()
+        if self._few_device not in (None, device):
+            raise ValueError(f"the current GPU is {device}, the layer on GPU {self._few_device}")
+        return _stream_ptr(stream, device)
 
     def route(self, x, stream=None):
         _check(self._lib.brownout_moe_route(self._desc_ref, self._x(x), *self._route_args[:2], None,
@@ -1067,6 +1069,7 @@ class LayerForward:
         if self._side is None:
             return self.shared(x, stream)
         self._x(x)
+        self._s(stream)  # (for its check of the current GPU)
         self._side.wait_stream(stream if stream is not None else torch.cuda.current_stream())
         self._run_shared(self._shared_side_args, x, self._side.cuda_stream)
         return self.bufs["y_sh"], self.bufs["h_sh"]

@@ -458,3 +458,27 @@ def test_buffers_on_another_device_are_refused(device, few):
         B.LayerForward(desc_of(case, "bf16"), w, device=device, few_tokens=few)
     for same in ("cuda", "cuda:0", torch.device("cuda", 0)):
         B.LayerForward(desc_of(case, "bf16"), w, device=same, few_tokens=few)
+
+
+@pytest.mark.parametrize("few", [True, False])
+def test_calls_from_another_device_are_refused(few, monkeypatch):
+    """The parts of a 4-bit layer too: with x on another GPU, and with another GPU the current one."""
+    case = dict(T=4, d=64, E=6, top_k=2, G=3, f=40, fs=24)
+    c, _ = R.make_case(5, group=32, **case)
+    w, x = to_gpu(c, case, 32)
+    layer = B.LayerForward(desc_of(case, "bf16"), w, few_tokens=few)
+    want = layer(x).clone()
+    parts = [] if few else [lambda: layer.route(x), lambda: layer.dispatch(x), lambda: layer.ffn(x=x),
+                            lambda: layer.ffn_gate_up(x=x), lambda: layer.shared(x), lambda: layer.shared_fork(x)]
+    layer._few_device += 1
+    for call in (lambda: layer(x), *parts):
+        with pytest.raises(ValueError, match="the layer on GPU"):
+            call()
+    layer._few_device -= 1
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "current_device", lambda: 1)
+        side = torch.cuda.Stream(device=0)
+        for call in (lambda: layer(x), lambda: layer(x, side), *parts, *([] if few else [layer.ffn_down, layer.combine])):
+            with pytest.raises(ValueError, match="the layer on GPU"):
+                call()
+    assert torch.equal(layer(x), want)
