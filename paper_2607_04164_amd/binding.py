@@ -624,9 +624,9 @@ def w4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, *, strea
     if group not in (32, 64, 128) or K < 8 or K % 8:
         raise ValueError("group must be 32, 64 or 128 and K a multiple of 8")
     ng = -(-K // group)
-    codes = _empty((n, N, w4_row_bytes(K)), torch.uint8, w.device)
-    scales = _empty((n, N, ng), torch.bfloat16, w.device)
-    z = _empty((n, N, ng), torch.uint8, w.device) if zeros else None
+    codes = _new((n, N, w4_row_bytes(K)), torch.uint8, w.device, stream)
+    scales = _new((n, N, ng), torch.bfloat16, w.device, stream)
+    z = _new((n, N, ng), torch.uint8, w.device, stream) if zeros else None
     _check(load_library().brownout_moe_w4_quantize(dtype, n, N, K, int(group), wp, codes.data_ptr(), scales.data_ptr(),
                                                    None if z is None else z.data_ptr(), _stream_ptr(stream, device)),
            "brownout_moe_w4_quantize")
@@ -648,8 +648,17 @@ def _w4_rows(offsets, a, a_rows, n: int, K: int, device: int):
     return rows, op, _fits(a_rows, "a_rows", torch.int32, (rows,), device), m, ap
 
 
-def _out(t, name, shape, a, device):
-    t = torch.empty(shape, dtype=a.dtype, device=a.device) if t is None else t
+def _new(shape, dtype, device, stream):
+    """A tensor that a call on `stream` writes: memory of that stream, since what the current stream has freed it
+    may still be reading."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _out(t, name, shape, a, device, stream):
+    t = _new(shape, a.dtype, a.device, stream) if t is None else t
     return t, _fits(t, name, a.dtype, shape, device)
 
 
@@ -660,7 +669,7 @@ def w4_matmul(offsets: torch.Tensor, a: torch.Tensor, w: W4, *, a_rows: Optional
     device = _device_of(a, "a")
     n, N, K = w.shape
     rows, op, rp, m, ap = _w4_rows(offsets, a, a_rows, n, K, device)
-    y, yp = _out(y, "y", (rows, N), a, device)
+    y, yp = _out(y, "y", (rows, N), a, device, stream)
     _check(load_library().brownout_moe_w4_matmul(BMOE_BF16, n, rows, N, K, op, rp, m, ap, w._on(device), yp, _stream_ptr(stream, device)),
            "brownout_moe_w4_matmul")
     return y
@@ -677,7 +686,7 @@ def w4_gate_up(offsets: torch.Tensor, a: torch.Tensor, w_gate: W4, w_up: W4, *, 
     device = _device_of(a, "a")
     n, f, d = _w4_gated(w_gate, w_up)
     rows, op, rp, m, ap = _w4_rows(offsets, a, a_rows, n, d, device)
-    h, hp = _out(h, "h", (rows, f), a, device)
+    h, hp = _out(h, "h", (rows, f), a, device, stream)
     _check(load_library().brownout_moe_w4_gate_up(BMOE_BF16, n, rows, d, f, op, rp, m, ap, w_gate._on(device),
                                                   w_up._on(device), hp, _stream_ptr(stream, device)), "brownout_moe_w4_gate_up")
     return h
@@ -691,8 +700,8 @@ def w4_ffn(offsets: torch.Tensor, a: torch.Tensor, w_gate: W4, w_up: W4, w_down:
     if w_down.shape != (n, d, f):
         raise ValueError(f"w_down must be {(n, d, f)}, got {w_down.shape}")
     rows, op, rp, m, ap = _w4_rows(offsets, a, a_rows, n, d, device)
-    h, hp = _out(h, "h", (rows, f), a, device)
-    y, yp = _out(y, "y", (rows, d), a, device)
+    h, hp = _out(h, "h", (rows, f), a, device, stream)
+    y, yp = _out(y, "y", (rows, d), a, device, stream)
     _check(load_library().brownout_moe_w4_ffn(BMOE_BF16, n, rows, d, f, op, rp, m, ap, w_gate._on(device), w_up._on(device),
                                               w_down._on(device), hp, yp, _stream_ptr(stream, device)), "brownout_moe_w4_ffn")
     return y, h
@@ -708,7 +717,7 @@ def pre_norm(x: torch.Tensor, w: Optional[torch.Tensor] = None, eps: float = 1e-
     dt, dtype = x.dtype, _dtype_of(x)
     xp = _fits(x, "x", dt, shape, device)
     wp = None if w is None else _fits(w, "w", dt, (d,), device)
-    out, op = _out(out, "out", shape, x, device)
+    out, op = _out(out, "out", shape, x, device, stream)
     _check(load_library().brownout_moe_pre_norm(dtype, T, d, eps, xp, wp, op, _stream_ptr(stream, device)), "brownout_moe_pre_norm")
     return out
 
@@ -745,11 +754,11 @@ def post_norm(y: torch.Tensor, x: torch.Tensor, norm: bool = True, *, w_post: Op
         raise ValueError("w_next and out_next belong to next_norm")
     wp = None if w_post is None else _fits(w_post, "w_post", dt, (d,), device)
     mode, gp = (GATE_NONE, None) if gate is None else _gate_mode(gate, T, d, dt, device)
-    out, rp = _out(out, "out", shape, y, device)
+    out, rp = _out(out, "out", shape, y, device, stream)
     np_, ap = None, None
     if next_norm:
         np_ = None if w_next is None else _fits(w_next, "w_next", dt, (d,), device)
-        out_next, ap = _out(out_next, "out_next", shape, y, device)
+        out_next, ap = _out(out_next, "out_next", shape, y, device, stream)
     _check(load_library().brownout_moe_post_norm(dtype, T, d, eps, 1 if norm else 0, res_scale, mode, yp, xp, wp, gp,
                                                  rp, np_, ap, _stream_ptr(stream, device)), "brownout_moe_post_norm")
     return out, out_next

@@ -407,3 +407,25 @@ def test_hidden_values_whose_sums_leave_fp32(n, rows, f, d, group, zeros):
             tol = _sum_error(f, group) * np.abs(hs[fin]) @ R.w4_magnitude(*td, f, group)[s].T
             tol = R.HALF["bf16"] * (np.abs(wanty[fin]) + tol) + tol
             assert (np.abs(y64[sl][fin] - wanty[fin]) <= tol).all()
+
+
+def test_outputs_are_memory_of_the_calls_stream():
+    """A call on another stream than the current one writes no memory that the current stream may still read."""
+    rng = np.random.default_rng(12)
+    w = _w4(R.w4_random(rng, 2, 64, 64, 32, False), 64, 32)
+    a, off = R.rand(rng, (8, 64), 1.0, "bf16").cuda(), torch.tensor([0, 5, 8], dtype=torch.int32, device="cuda")
+    calls = {"matmul": lambda s: (B.w4_matmul(off, a, w, stream=s),), "gate_up": lambda s: (B.w4_gate_up(off, a, w, w, stream=s),),
+             "ffn": lambda s: B.w4_ffn(off, a, w, w, w, stream=s), "pre": lambda s: (B.pre_norm(a, stream=s),),
+             "post": lambda s: B.post_norm(a, a, next_norm=True, stream=s),
+             "quantize": lambda s: (lambda q: (q.codes, q.scales, q.zeros))(B.w4_quantize(a[None], 32, True, stream=s))}
+    for name, call in calls.items():
+        torch.cuda.synchronize()
+        s = torch.cuda.Stream()
+        outs = call(s)
+        torch.cuda.synchronize()
+        want = call(None)
+        for got, w0 in zip(outs, want):
+            assert torch.equal(got, w0), name
+            seg, = (g for g in torch.cuda.memory_snapshot()
+                    if g["address"] <= got.data_ptr() < g["address"] + g["total_size"])
+            assert seg["stream"] == s.cuda_stream, name
