@@ -567,6 +567,12 @@ def _dtype_of(t) -> int:
     return dtype
 
 
+def _int32(*sizes):
+    """The calls take sizes as 32-bit integers; a larger one would arrive as another."""
+    if max(sizes) > 0x7fffffff:
+        raise ValueError(f"a size of {max(sizes)} is past 2^31 - 1")
+
+
 def w4_row_bytes(K: int) -> int:
     """Bytes of a row of K codes."""
     return 16 * ((K + 31) // 32)
@@ -590,6 +596,7 @@ class W4:
         if not isinstance(codes, torch.Tensor) or codes.dim() != 3:
             raise ValueError("codes must be [n, N, row bytes]")
         n, N, _ = codes.shape
+        _int32(n, N, K)
         self.device = _device_of(codes, "codes")
         ng = -(-K // group)
         _fits(codes, "codes", torch.uint8, (n, N, w4_row_bytes(K)), self.device)
@@ -619,6 +626,7 @@ def w4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, *, strea
     if w.dim() != 3:
         raise ValueError("w must be [n, N, K]")
     n, N, K = w.shape
+    _int32(n, N, K)
     dtype = _dtype_of(w)
     wp = _fits(w, "w", w.dtype, (n, N, K), device)
     if group not in (32, 64, 128) or K < 8 or K % 8:
@@ -638,11 +646,13 @@ def _w4_rows(offsets, a, a_rows, n: int, K: int, device: int):
     if not isinstance(a, torch.Tensor) or a.dim() != 2:
         raise ValueError("a must be [rows, K]")
     m = a.shape[0]
+    _int32(m)
     ap = _fits(a, "a", torch.bfloat16, (m, K), device)
     op = _fits(offsets, "offsets", torch.int32, (n + 1,), device)
     if a_rows is None:
         return m, op, None, 0, ap
     rows = a_rows.numel()
+    _int32(rows)
     if rows and not m:
         raise ValueError("a_rows names rows of an empty a")
     return rows, op, _fits(a_rows, "a_rows", torch.int32, (rows,), device), m, ap
@@ -714,6 +724,7 @@ def pre_norm(x: torch.Tensor, w: Optional[torch.Tensor] = None, eps: float = 1e-
     if x.dim() != 2:
         raise ValueError("x must be [T, d]")
     T, d = shape = x.shape
+    _int32(T, d)
     dt, dtype = x.dtype, _dtype_of(x)
     xp = _fits(x, "x", dt, shape, device)
     wp = None if w is None else _fits(w, "w", dt, (d,), device)
@@ -746,6 +757,7 @@ def post_norm(y: torch.Tensor, x: torch.Tensor, norm: bool = True, *, w_post: Op
     if y.dim() != 2:
         raise ValueError("y must be [T, d]")
     T, d = shape = y.shape
+    _int32(T, d)
     dt, dtype = y.dtype, _dtype_of(y)
     yp, xp = _fits(y, "y", dt, shape, device), _fits(x, "x", dt, shape, device)
     if w_post is not None and not norm:

@@ -175,3 +175,31 @@ def test_reference_unpacks_known_codes():
     v = R.w4_values(codes, scales, zeros, 40, 32)[0, 0]
     assert v[0] == 18.0 and v[1] == 4.0 and v[2] == -2.0 and v[38] == -2.0 and v[39] == 5.5 and v[37] == -2.0
     assert np.array_equal(R.w4_values(codes, scales, None, 40, 32)[0, 0, :2], [4.0, -10.0])
+
+
+class Far(torch.Tensor):
+    """A tensor of GPU 0 with a size and no memory."""
+
+    @staticmethod
+    def __new__(cls, *shape, dtype=torch.bfloat16):
+        return torch.Tensor._make_wrapper_subclass(cls, shape, dtype=dtype, device="cuda:0")
+
+    @classmethod
+    def __torch_dispatch__(cls, func, types, args=(), kwargs=None):
+        raise AssertionError(f"{func} on a tensor without memory")
+
+
+def test_sizes_past_32_bits_are_refused(monkeypatch):
+    """The C calls take int32: 2^32 + 5 rows would arrive as 5."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    n = 2 ** 32 + 5
+    x = Far(n, 8)
+    w = B.W4(Far(1, 8, 16, dtype=torch.uint8), Far(1, 8, 1), K=8, group=32)
+    off, rows, u8 = Far(2, dtype=torch.int32), Far(n, dtype=torch.int32), torch.uint8
+    calls = (lambda: B.pre_norm(x, out=x), lambda: B.post_norm(x, x, out=x), lambda: B.w4_quantize(Far(1, n, 8)),
+             lambda: B.w4_matmul(off, x, w, y=x), lambda: B.w4_matmul(off, Far(3, 8), w, a_rows=rows, y=x),
+             lambda: B.w4_gate_up(off, x, w, w, h=x), lambda: B.w4_ffn(off, x, w, w, w, h=x, y=x),
+             lambda: B.W4(Far(1, n, 16, dtype=u8), Far(1, n, 1), K=8, group=32))
+    for call in calls:
+        with pytest.raises(ValueError, match=f"size of {n}"):
+            call()
