@@ -40,6 +40,13 @@ void recorder_device(int device, int device_status, int cus, int cus_status) {
     g_cus_status = cus_status;
     launches.clear();
 }
+// the kernels that the library holds, whether launched or not
+int recorder_kernels() { return (int)names().size(); }
+const char* recorder_kernel(int i) {
+    auto it = names().begin();
+    while (i--) ++it;
+    return it->second.c_str();
+}
 int recorder_count() { return (int)launches.size(); }
 const char* recorder_name(int i) { return launches[i].name.c_str(); }
 void recorder_grid(int i, uint32_t* g) {

@@ -25,6 +25,17 @@ def ffn_part(part, n_seg, rows_cap, d, d_ff, dtype=1, workspace=False, **device)
             "args": [["i", v] for v in (dtype, n_seg, rows_cap, d, d_ff)] + [["p", PTR]] * ptrs + ws, **device}
 
 
+def struct(s):
+    """An argument that points to a ctypes structure (its own pointers are never followed)."""
+    return ["s", bytes(s).hex()]
+
+
+def kernels(tmp_path):
+    """The names of all kernels in the library."""
+    (_, launches), = record([{"fn": None}], tmp_path)
+    return {n for n, _ in launches}
+
+
 def record(calls, tmp_path):
     """For each call (status, [(kernel, grid), ...]); a call may name the
     device's answers: device, device_status, cus, cus_status."""
@@ -42,10 +53,16 @@ def _main(recorder, lib):
     rec = ctypes.CDLL(recorder, mode=ctypes.RTLD_GLOBAL)
     rec.recorder_name.restype = ctypes.c_char_p
     bmoe = ctypes.CDLL(lib)
+    rec.recorder_kernel.restype = ctypes.c_char_p
     kinds = {"i": ctypes.c_int32, "p": ctypes.c_void_p, "z": ctypes.c_size_t}
+    kinds.update(f=ctypes.c_float, s=lambda v: ctypes.create_string_buffer(bytes.fromhex(v), len(v) // 2))
     res = []
     for c in json.load(sys.stdin):
         rec.recorder_device(c.get("device", 0), c.get("device_status", 0), c.get("cus", 256), c.get("cus_status", 0))
+        if c["fn"] is None:
+            res.append({"status": 0, "launches": [[rec.recorder_kernel(i).decode(), [0, 0, 0]]
+                                                  for i in range(rec.recorder_kernels())]})
+            continue
         status = getattr(bmoe, c["fn"])(*[kinds[k](v) for k, v in c["args"]])
         grid = (ctypes.c_uint32 * 3)()
         launches = []

@@ -27,6 +27,9 @@ CASES = {
     "many-items-odd": dict(T=5, d=200, E=64, top_k=8, G=40, f=296, fs=24),
     "wider-than-lds": dict(T=16, d=2056, E=8, top_k=1, G=4, f=40),
     "few-columns": dict(T=13, d=40, E=33, top_k=7, G=11, f=16),
+    # d and d_ff in whole units, and more tokens than their LDS copies hold
+    "whole-units-past-lds-9": dict(T=9, d=4096, E=8, top_k=2, G=4, f=512, norm=1),
+    "whole-units-past-lds-16": dict(T=16, d=4096, E=8, top_k=2, G=4, f=512, fs=256),
 }
 FORMATS = [("bf16", 0, False), ("f32", 0, False), ("bf16", 32, False), ("bf16", 64, True), ("bf16", 128, False),
            ("bf16", 128, True)]

@@ -111,3 +111,34 @@ def test_norm_stream_and_graph():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(r1, want[0]) and torch.equal(a1, want[1]), f"replay {k}"
+
+
+# (T, d) for the splits of a row that SIZES has not
+PRE_SPLITS = [(1030, 1024), (2, 12296), (2, 24584)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d", PRE_SPLITS)
+def test_pre_norm_row_splits(T, d, dtype):
+    rng = np.random.default_rng(T + d)
+    x, w = R.rand(rng, (T, d), 1.5, dtype), R.rand(rng, (d,), 1.0, dtype)
+    want = R.np64(x) * R.inv_rms(R.np64(x), EPS) * R.np64(w)
+    R.assert_rounded(B.pre_norm(x.cuda(), w.cuda(), EPS), want, R.SUM * np.abs(want), dtype, f"T={T} d={d} {dtype}")
+
+
+# (T, d) for every number of threads a row and chunks a thread that a post_norm can take
+POST_SPLITS = [(5, 200), (1030, 256), (1030, 1032), (1024, 512), (3, 1032), (4, 2056), (5, 4104), (3, 8200), (2, 12296), (3, 24584), (2, 32768)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d", POST_SPLITS)
+def test_post_norm_row_splits(T, d, dtype):
+    rng = np.random.default_rng(T + d)
+    x, y, g = (R.rand(rng, (T, d), s, dtype) for s in (2.0, 0.4, 1.0))
+    wp, wn = R.rand(rng, (d,), 1.0, dtype), R.rand(rng, (d,), 1.0, dtype)
+    r, a = B.post_norm(y.cuda(), x.cuda(), True, w_post=wp.cuda(), gate=g.cuda(), res_scale=0.75, next_norm=True,
+                       w_next=wn.cuda(), eps=EPS)
+    n64 = R.np64
+    want, er, wa, ea = R.post_ref(n64(y), n64(x), True, n64(wp), n64(g), 0.75, n64(wn), EPS)
+    R.assert_rounded(r, want, er, dtype, "r")
+    R.assert_rounded(a, wa, ea, dtype, "a")

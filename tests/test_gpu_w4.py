@@ -429,3 +429,64 @@ def test_outputs_are_memory_of_the_calls_stream():
             seg, = (g for g in torch.cuda.memory_snapshot()
                     if g["address"] <= got.data_ptr() < g["address"] + g["total_size"])
             assert seg["stream"] == s.cuda_stream, name
+
+
+# (n, rows, N, K): at least 256 blocks of four tiles a wave; rows that end a tile of 16 and a pass of 32, K in whole
+# units and not, units that the eight waves do not share evenly, the last tile of columns cut
+FOUR_TILES = [(8, 250, 4096, 2048), (4, 100, 4096, 4360), (6, 96, 2808, 4096), (1, 16, 16384, 264), (1, 32, 8200, 512),
+              (1, 64, 5464, 40), (3, 7, 8192, 264)]
+# the same rows for one tile a wave
+ONE_TILE = [(1, 16, 264, 2048), (1, 32, 136, 8200), (1, 64, 40, 4360), (1, 33, 64, 4096)]
+
+
+@pytest.mark.parametrize("group,zeros", [(32, True), (32, False), (64, True), (64, False), (128, True), (128, False)])
+@pytest.mark.parametrize("n,rows,N,K", FOUR_TILES + ONE_TILE)
+def test_w4_matmul_by_tiles(n, rows, N, K, group, zeros):
+    rng = np.random.default_rng(rows + N + K)
+    t = R.w4_random(rng, n, N, K, group, zeros)
+    offs = _segments(rng, rows, n) if n > 1 else np.array([0, rows], np.int32)
+    a = R.rand(rng, (rows, K), 1.0, "bf16")
+    y = B.w4_matmul(torch.from_numpy(offs).cuda(), a.cuda(), _w4(t, K, group))
+    # (some of the columns: the first and last tiles, and every 37th)
+    cols = np.unique(np.concatenate([np.arange(min(N, 80)), np.arange(0, N, 37), np.arange(max(N - 80, 0), N)]))
+    part = y[:, torch.from_numpy(cols).cuda()]
+    tc = t[0][:, cols], t[1][:, cols], None if t[2] is None else t[2][:, cols]
+    w64, mag, a64 = R.w4_values(*tc, K, group), R.w4_magnitude(*tc, K, group), R.np64(a)
+    for s in range(n):
+        sl = slice(offs[s], offs[s + 1])
+        _check(part, a64[sl] @ w64[s].T, _sum_error(K, group) * np.abs(a64[sl]) @ mag[s].T, sl, f"segment {s}")
+
+
+# (n, rows, f, d): gate_up with four tiles a wave
+FFN_FOUR_TILES = [(8, 250, 1408, 2048), (8, 200, 1400, 2312), (4, 130, 1408, 4096), (6, 60, 1416, 264), (1, 64, 5464, 264)]
+
+
+@pytest.mark.parametrize("group,zeros", [(32, True), (32, False), (64, True), (64, False), (128, True), (128, False)])
+@pytest.mark.parametrize("n,rows,f,d", FFN_FOUR_TILES)
+def test_w4_ffn_by_tiles(n, rows, f, d, group, zeros):
+    rng = np.random.default_rng(rows + f + d)
+    tg, tu = (R.w4_random(rng, n, f, d, group, zeros) for _ in range(2))
+    td = R.w4_random(rng, n, d, f, group, zeros)
+    offs = _segments(rng, rows, n) if n > 1 else np.array([0, rows], np.int32)
+    m = rows // 4 + 1
+    a = R.rand(rng, (m, d), 1.0, "bf16")
+    src = rng.integers(0, m, rows).astype(np.int32)
+    y, h = B.w4_ffn(torch.from_numpy(offs).cuda(), a.cuda(), _w4(tg, d, group), _w4(tu, d, group), _w4(td, f, group),
+                    a_rows=torch.from_numpy(src).cuda())
+    a64, h64 = R.np64(a)[src], R.np64(h)
+    hc = np.unique(np.concatenate([np.arange(min(f, 70)), np.arange(0, f, 29), np.arange(max(f - 70, 0), f)]))
+    yc = np.unique(np.concatenate([np.arange(min(d, 70)), np.arange(0, d, 29), np.arange(max(d - 70, 0), d)]))
+    pick = lambda t, c: (t[0][:, c], t[1][:, c], None if t[2] is None else t[2][:, c])  # noqa: E731
+    wg, mg = R.w4_values(*pick(tg, hc), d, group), R.w4_magnitude(*pick(tg, hc), d, group)
+    wu, mu = R.w4_values(*pick(tu, hc), d, group), R.w4_magnitude(*pick(tu, hc), d, group)
+    wd, md = R.w4_values(*pick(td, yc), f, group), R.w4_magnitude(*pick(td, yc), f, group)
+    hp, yp = h[:, torch.from_numpy(hc).cuda()], y[:, torch.from_numpy(yc).cuda()]
+    e = _sum_error(d, group)
+    for s in range(n):
+        sl = slice(offs[s], offs[s + 1])
+        g, u = a64[sl] @ wg[s].T, a64[sl] @ wu[s].T
+        eg, eu = e * np.abs(a64[sl]) @ mg[s].T, e * np.abs(a64[sl]) @ mu[s].T
+        want = R.silu(g) * u
+        err = 1.1 * np.abs(u) * eg + (np.abs(R.silu(g)) + 1.1 * eg) * eu + 2.0 ** -20 * np.abs(want)
+        _check(hp, want, err, sl, f"h of segment {s}")
+        _check(yp, h64[sl] @ wd[s].T, _sum_error(f, group) * np.abs(h64[sl]) @ md[s].T, sl, f"y of segment {s}")
