@@ -143,25 +143,27 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void post_norm_kernel(PostPara
 template <int V>
 using Int = std::integral_constant<int, V>;
 
+// f(NT, CH) with the least CH of LEAST, 2 LEAST, .. MOST that holds a thread's chunks
+template <int NT, int LEAST, int MOST, typename F>
+void with_chunks(int nch, F f) {
+    if constexpr (LEAST < MOST) {
+        if (nch > NT * LEAST) return with_chunks<NT, 2 * LEAST, MOST>(nch, f);
+    }
+    f(Int<NT>{}, Int<LEAST>{});
+}
+
 // runs f(NT, CH) with the row split that fits: a wave a row where there are rows for
-// every wave of the chip and a lane's share of the row is at most wave_chunks, else four
-// waves; sixteen where a row needs them. wave_chunks: 4 for pre_norm, 2 for post_norm,
+// every wave of the chip and a lane's share of the row is at most WAVE_CHUNKS, else four
+// waves; sixteen where a row needs them. WAVE_CHUNKS: 4 for pre_norm, 2 for post_norm,
 // which holds three rows; with more, too few waves fit a SIMD to keep its loads going
 // (8192 bf16 rows, a wave and four waves a row: pre_norm 6.8 and 10.0 us of 1024
 // columns, 11.7 and 13.2 of 2048, 22.7 and 20.5 of 4096; post_norm 17.4 and 24.8, 39.7
 // and 34.0, 116.7 and 70.4).
-template <typename F>
-hipError_t with_split(int64_t T, int nch, int wave_chunks, F f) {
-    auto with_ch = [&](auto nt) {
-        const int per = ceil_div(nch, decltype(nt)::value);
-        if (per <= 1) f(nt, Int<1>{});
-        else if (per <= 2) f(nt, Int<2>{});
-        else if (per <= 4) f(nt, Int<4>{});
-        else f(nt, Int<8>{});
-    };
-    if (nch <= 64 || (nch <= 64 * wave_chunks && T >= 1024)) with_ch(Int<64>{});
-    else if (nch <= 2048) with_ch(Int<256>{});
-    else with_ch(Int<1024>{});
+template <int WAVE_CHUNKS, int MAX_NCH, typename F>
+hipError_t with_split(int64_t T, int nch, F f) {
+    if (nch <= 64 || (nch <= 64 * WAVE_CHUNKS && T >= 1024)) with_chunks<64, 1, WAVE_CHUNKS>(nch, f);
+    else if (nch <= 2048) with_chunks<256, 1, 8>(nch, f);
+    else with_chunks<1024, 4, MAX_NCH / 1024>(nch, f);
     return hipGetLastError();
 }
 
@@ -172,32 +174,37 @@ unsigned grid_of(int64_t T) {
     return (unsigned)(wgs < (1 << 20) ? wgs : (1 << 20));
 }
 
-}  // namespace
-
-hipError_t launch_pre_norm(const PreNormArgs& a, hipStream_t s) {
-    const int nch = a.d / (a.dtype == BMOE_BF16 ? 8 : 4);
-    return with_split(a.T, nch, 4, [&](auto nt, auto ch) {
+template <typename E>
+hipError_t launch_pre_norm_t(const PreNormArgs& a, hipStream_t s) {
+    constexpr int N = Vec<E>::N;
+    const int nch = a.d / N;
+    return with_split<4, BMOE_NORM_MAX_D / N>(a.T, nch, [&](auto nt, auto ch) {
         constexpr int NT = decltype(nt)::value, CH = decltype(ch)::value;
-        const dim3 grid(grid_of<NT>(a.T)), block(NT > 256 ? NT : 256);
-        if (a.dtype == BMOE_BF16)
-            hipLaunchKernelGGL((pre_norm_kernel<uint16_t, NT, CH>), grid, block, 0, s, (const uint4*)a.x,
-                               (const uint4*)a.w, (uint4*)a.out, a.T, nch, a.eps);
-        else
-            hipLaunchKernelGGL((pre_norm_kernel<float, NT, CH>), grid, block, 0, s, (const uint4*)a.x,
-                               (const uint4*)a.w, (uint4*)a.out, a.T, nch, a.eps);
+        hipLaunchKernelGGL((pre_norm_kernel<E, NT, CH>), dim3(grid_of<NT>(a.T)), dim3(NT > 256 ? NT : 256), 0, s,
+                           (const uint4*)a.x, (const uint4*)a.w, (uint4*)a.out, a.T, nch, a.eps);
     });
 }
 
-hipError_t launch_post_norm(const PostNormArgs& a, hipStream_t s) {
-    const int nch = a.d / (a.dtype == BMOE_BF16 ? 8 : 4);
+template <typename E>
+hipError_t launch_post_norm_t(const PostNormArgs& a, hipStream_t s) {
+    constexpr int N = Vec<E>::N;
+    const int nch = a.d / N;
     const PostParams p{(const uint4*)a.y, (const uint4*)a.x, (const uint4*)a.w_post, (const uint4*)a.w_next, a.gate,
                        (uint4*)a.r, (uint4*)a.a, a.T, nch, a.norm_y, a.gate_mode, a.eps, a.res_scale};
-    return with_split(a.T, nch, 2, [&](auto nt, auto ch) {
+    return with_split<2, BMOE_NORM_MAX_D / N>(a.T, nch, [&](auto nt, auto ch) {
         constexpr int NT = decltype(nt)::value, CH = decltype(ch)::value;
-        const dim3 grid(grid_of<NT>(a.T)), block(NT > 256 ? NT : 256);
-        if (a.dtype == BMOE_BF16) hipLaunchKernelGGL((post_norm_kernel<uint16_t, NT, CH>), grid, block, 0, s, p);
-        else hipLaunchKernelGGL((post_norm_kernel<float, NT, CH>), grid, block, 0, s, p);
+        hipLaunchKernelGGL((post_norm_kernel<E, NT, CH>), dim3(grid_of<NT>(a.T)), dim3(NT > 256 ? NT : 256), 0, s, p);
     });
+}
+
+}  // namespace
+
+hipError_t launch_pre_norm(const PreNormArgs& a, hipStream_t s) {
+    return a.dtype == BMOE_BF16 ? launch_pre_norm_t<uint16_t>(a, s) : launch_pre_norm_t<float>(a, s);
+}
+
+hipError_t launch_post_norm(const PostNormArgs& a, hipStream_t s) {
+    return a.dtype == BMOE_BF16 ? launch_post_norm_t<uint16_t>(a, s) : launch_post_norm_t<float>(a, s);
 }
 
 }  // namespace bmoe

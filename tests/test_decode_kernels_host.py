@@ -1,11 +1,14 @@
-"""Which kernels the decode-side calls launch, seen without a GPU: test cases that are meant for a kernel reach it."""
+"""Which kernels the decode-side calls launch, seen without a GPU: every one that is built is run by the cases of the
+GPU tests, and cases that are meant for a kernel reach it."""
+import re
 import shutil
 
 import pytest
 
 import test_gpu_few as F
+import test_gpu_norm as N
 import test_gpu_w4 as Q
-from launch_record import PTR, record, struct
+from launch_record import PTR, kernels, record, struct
 from paper_2607_04164_amd import binding as B
 
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="needs a host compiler for the recording runtime")
@@ -43,10 +46,40 @@ def gate_up_call(n, rows, f, d, group, **device):
                      ["p", 2 * PTR], ["p", 0]], **device}
 
 
+def quantize_call(dtype, group):
+    return {"fn": "brownout_moe_w4_quantize", "args": [*ints(dtype, 1, 8, 64, group), *ptrs(4), ["p", 0]]}
+
+
+def pre_call(T, d, dtype):
+    return {"fn": "brownout_moe_pre_norm", "args": [*ints(dtype, T, d), ["f", 1e-6], *ptrs(3), ["p", 0]]}
+
+
+def post_call(T, d, dtype):
+    return {"fn": "brownout_moe_post_norm",
+            "args": [*ints(dtype, T, d), ["f", 1e-6], ["i", 1], ["f", 1.0], ["i", 3], *ptrs(6), ["p", 2 * PTR], ["p", 0]]}
+
+
 def launched(calls, tmp_path):
     res = record(calls, tmp_path)
     assert all(status == 0 for status, _ in res)
     return [ls for _, ls in res]
+
+
+def test_every_kernel_is_run_by_a_test_case(tmp_path):
+    calls = [few_call(c, *fmt) for c in F.CASES.values() for fmt in F.FORMATS]
+    calls += [few_call(dict(T=T, d=96, E=10, top_k=3, G=5, f=48, fs=24), *fmt) for T in range(1, 17) for fmt in F.FORMATS[:3]]
+    calls += [matmul_call(*c, g) for c in Q.CASES + Q.FOUR_TILES + Q.ONE_TILE for g in GROUPS]
+    calls += [gate_up_call(*c, g) for c in Q.FFN_FOUR_TILES for g in GROUPS]
+    # test_w4_ffn, test_w4_layer_of_any_size
+    calls += [gate_up_call(*c) for c in ((1, 1, 1408, 2048, 32), (1, 1, 24, 40, 32), (1, 1, 1408, 2048, 64),
+                                         (1, 1, 24, 40, 64), (1, 1, 1408, 2048, 128), (1, 1, 24, 40, 128))]
+    calls += [quantize_call(t, g) for t in (0, 1) for g in GROUPS]
+    calls += [pre_call(T, d, t) for T, d in N.SIZES + N.PRE_SPLITS for t in (0, 1)]
+    calls += [post_call(T, d, t) for T, d in N.POST_SPLITS + [(1, 2048), (5, 264), (1030, 520), (3, 16392)] for t in (0, 1)]
+    ran = {name for ls in launched(calls, tmp_path) for name, _ in ls}
+    built = {k for k in kernels(tmp_path) if re.search(r"few_|w4_|_norm_kernel", k)}
+    assert len(built) > 70
+    assert not built - ran, "\n".join(sorted(built - ran))
 
 
 @pytest.mark.parametrize("group", GROUPS)
