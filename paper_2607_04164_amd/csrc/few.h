@@ -853,8 +853,9 @@ __global__ __launch_bounds__(kDownThreads, F::DOWN_WAVES) void few_down_kernel(F
 
 // Workgroups that share `cols` output columns: as many as two or three a CU, where the
 // columns are fewer
-inline int most_splits(int d, int cols, int per_cu) {
-    const int tiles = ceil_div(d, cols), n = per_cu * 256 / tiles;
+constexpr int kMostCus = 256;  // that the workspace is for; a launch counts no more of them
+inline int most_splits(int d, int cols, int per_cu, int cus) {
+    const int tiles = ceil_div(d, cols), n = per_cu * (cus < kMostCus ? cus : kMostCus) / tiles;
     return n < 1 ? 1 : n > kSplitMax ? kSplitMax : n;
 }
 
@@ -865,7 +866,7 @@ inline size_t done_bytes(int d) { return round256((size_t)ceil_div(d, kFewCols) 
 inline size_t partial_bytes(int d) {
     size_t most = 0;
     for (int tiles = 1; tiles <= 4; tiles *= 2) {
-        const int split = most_splits(d, tiles * kFewCols, 3);
+        const int split = most_splits(d, tiles * kFewCols, 3, kMostCus);
         const size_t n = split == 1 ? 0 : (size_t)ceil_div(d, tiles * kFewCols) * split * tiles * kTile * sizeof(float);
         most = n > most ? n : most;
     }
@@ -908,7 +909,8 @@ hipError_t launch_few_t(const FewArgs& a, ToStack st, hipStream_t s) {
     const int64_t units = most * ceil_div(a.f, F::UK) + ceil_div(a.fs, F::UK);
     const bool pack = F::PARTS == 2 && a.T <= 8;
     const int down_cols = (pack ? F::PACK_TILES : F::DOWN_TILES) * kFewCols;
-    p.split = most_splits(a.d, down_cols, F::DOWN_WAVES);
+    const int cus = persistent_workgroups();
+    p.split = most_splits(a.d, down_cols, F::DOWN_WAVES, cus);
     if (units < (int64_t)p.split * (kDownThreads / 64)) p.split = (int)ceil_div64(units, kDownThreads / 64);  // a unit a wave
     hipError_t e = launch_few_logits(a, p.done, s);
     if (e != hipSuccess) return e;
@@ -920,9 +922,9 @@ hipError_t launch_few_t(const FewArgs& a, ToStack st, hipStream_t s) {
         const int cols = tiles * kFewCols;
         return most * ceil_div(a.f, cols) + ceil_div(a.fs, cols);
     };
-    const int up_tiles = F::PAIRS && a.T <= 8 && items_of(F::UP_TILES) > 256 ? 1 : F::UP_TILES;
+    const int up_tiles = F::PAIRS && a.T <= 8 && items_of(F::UP_TILES) > cus ? 1 : F::UP_TILES;
     const int64_t items = items_of(up_tiles);
-    const int64_t room = (int64_t)F::UP_WAVES * 256 / kUpThreads * persistent_workgroups();
+    const int64_t room = (int64_t)F::UP_WAVES * 256 / kUpThreads * cus;
     const dim3 up((unsigned)(items < room ? items : room)), down((unsigned)(ceil_div(a.d, down_cols) * p.split));
     const bool up_ragged = a.d % (F::UK * (2 / up_tiles) * (kUpThreads / 64)) != 0;
     const bool down_ragged = a.f % F::UK != 0 || a.fs % F::UK != 0;

@@ -330,7 +330,7 @@ hipError_t launch_w4(const W4Params& p, int group, hipStream_t s) {
     const int64_t passes = (int64_t)p.rows_cap / kW4Rows + (p.n_seg < p.rows_cap ? p.n_seg : p.rows_cap);
     // fewer workgroups than CUs: one tile of each matrix a wave (one row of 4096 x 4096, groups of
     // 128: 7.0 us, with four tiles 9.5; where there are more, the FFN above takes 24.8 + 16.1 with two)
-    if (passes * ceil_div(p.N, 64 / NR) < 256) return launch_w4_tiles<NR, NR>(p, group, passes, s);
+    if (passes * ceil_div(p.N, 64 / NR) < persistent_workgroups()) return launch_w4_tiles<NR, NR>(p, group, passes, s);
     return launch_w4_tiles<NR, 4>(p, group, passes, s);
 }
 

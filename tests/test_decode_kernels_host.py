@@ -99,3 +99,18 @@ def test_cases_of_four_tiles_reach_them(group, tmp_path):
     for ls in launched(hidden, tmp_path):
         assert [n for n, _ in ls if f"few_up_kernel<bmoe::(anonymous namespace)::FmtW4<{group}>, 2, false, false>" in n]
         assert [n for n, _ in ls if f"few_down_kernel<bmoe::(anonymous namespace)::FmtW4<{group}>, false, false>" in n]
+
+
+def test_choices_follow_the_cu_count(tmp_path):
+    """On half of the chip (128 CUs) the splits and tiles are chosen for half as many workgroups, and more CUs than the
+    workspace is for change nothing."""
+    case = dict(T=1, d=2048, E=60, top_k=4, G=15, f=1408)
+    up, down = "few_up_kernel<bmoe::(anonymous namespace)::FmtPlain<unsigned short>, {}, false", "few_down_kernel"
+    for i, (cus, tiles, ups, downs) in enumerate(((256, 2, 176, 768), (128, 1, 256, 384), (304, 2, 176, 768))):
+        ls, = launched([few_call(case, "bf16", 0, False, cus=cus, device=20 + i)], tmp_path)
+        (_, (u, g)), (_, (dn, h)) = [(n, x) for n, x in enumerate(ls) if "few_logits" not in x[0]]
+        assert up.format(tiles) in u and g[0] == ups and down in dn and h[0] == downs
+    # 200 blocks of four tiles
+    one, four = (launched([matmul_call(1, 5, 12800, 512, 64, cus=c, device=30 + i)], tmp_path)[0][0][0]
+                 for i, c in enumerate((256, 128)))
+    assert "w4_gemm_kernel<1, 1, 64" in one and "w4_gemm_kernel<1, 4, 64" in four
