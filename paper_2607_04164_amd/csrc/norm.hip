@@ -40,20 +40,24 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
     return v;
 }
 
-// 1 / sqrt(mean of f^2 + eps) of a row
+// 1 / sqrt(mean of f^2 + eps) of a row. A row whose squares overflow is summed at 2^-100 of
+// its values, and left at 2^-4 of them with 2^4 times the result (which would lose bits
+// where it is below 2^-126).
 template <int NT, int M>
-__device__ __forceinline__ float inv_rms(const float (&f)[M], int d, float eps, float* part) {
+__device__ __forceinline__ float inv_rms(float (&f)[M], int d, float eps, float* part) {
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < M; ++i) s = fmaf(f[i], f[i], s);
     s = row_sum<NT>(s, part);
     if (!(s <= 3.0e38f)) {  // (the same for every thread of the row)
-        constexpr float kDown = 0x1p-100f;
         s = 0.f;
 #pragma unroll
-        for (int i = 0; i < M; ++i) s = fmaf(f[i] * kDown, f[i] * kDown, s);
+        for (int i = 0; i < M; ++i) {
+            s = fmaf(f[i] * 0x1p-100f, f[i] * 0x1p-100f, s);
+            f[i] *= 0x1p-4f;
+        }
         s = row_sum<NT>(s, part);
-        return kDown / sqrtf(s / (float)d);
+        return 0x1p-96f / sqrtf(s / (float)d);
     }
     return 1.f / sqrtf(s / (float)d + eps);
 }

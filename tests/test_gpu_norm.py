@@ -142,3 +142,25 @@ def test_post_norm_row_splits(T, d, dtype):
     want, er, wa, ea = R.post_ref(n64(y), n64(x), True, n64(wp), n64(g), 0.75, n64(wn), EPS)
     R.assert_rounded(r, want, er, dtype, "r")
     R.assert_rounded(a, wa, ea, dtype, "a")
+
+
+def test_rows_near_the_largest_value_in_fp32():
+    """A row of +-c: every step is exact but the reciprocal of the root and the product with it (the sum of squares
+    has 14 + 8 bits), so the result is +-1 within two roundings, however large c is."""
+    for c in [m * e for m in (103 / 64, 108 / 64, 111 / 64, 115 / 64) for e in (2.0 ** 127, 2.0 ** 100, 1.0)]:
+        sign = 1.0 - 2.0 * (torch.arange(256, device="cuda") % 3 == 0)
+        x = (sign * c).float()[None].expand(3, -1).contiguous()
+        zero = torch.zeros_like(x)
+        outs = [B.pre_norm(x, None, 1e-12), B.post_norm(x, zero, True, eps=1e-12)[0],
+                B.post_norm(zero, x, False, next_norm=True, eps=1e-12)[1]]
+        for out in outs:
+            assert bool(((out * sign - 1).abs() <= 2 * 2.0 ** -24).all()), f"{c}: {(out * sign - 1).abs().max()}"
+    # small values beside a large one, which is most of the sum: its square, the quotient, the root, the reciprocal and
+    # the product, half a step each (the sum's other terms are below 2^-24 of it)
+    x = torch.full((2, 256), 1e-12, device="cuda")
+    x[:, 7] = 3.1e38
+    x[:, 8:40] = torch.logspace(-14, 30, 32, device="cuda")
+    want = R.np64(x) * R.inv_rms(R.np64(x), 0.0)
+    for out in (B.pre_norm(x, None, 1e-12), B.post_norm(torch.zeros_like(x), x, False, next_norm=True, eps=1e-12)[1]):
+        # (results below 2^-126 keep fewer bits)
+        assert (np.abs(R.np64(out) - want) <= 4 * 2.0 ** -24 * np.abs(want) + 2.0 ** -149).all()
