@@ -485,3 +485,27 @@ def test_calls_from_another_device_are_refused(few, monkeypatch):
             with pytest.raises(ValueError, match="the layer on GPU"):
                 call()
     assert torch.equal(layer(x), want)
+
+
+@pytest.mark.parametrize("group,zeros", [(32, True), (128, False)])
+def test_w4_layer_graph(group, zeros):
+    """The four calls of a 4-bit layer with shared experts on their own stream, captured: replays give the eager bits."""
+    case = dict(T=24, d=256, E=12, top_k=3, G=5, f=200, fs=72)
+    c, _ = R.make_case(61, group=group, zeros=zeros, **case)
+    w, x = to_gpu(c, case, group)
+    layer, other = (B.LayerForward(desc_of(case, "bf16"), w) for _ in range(2))
+    xs = [R.rand(np.random.default_rng(i), (24, 256), 1.0, "bf16").cuda() for i in range(3)]
+    want = [other(v).clone() for v in xs]
+    layer(x)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = layer(x)
+    for k in range(4):
+        x.copy_(xs[k % 3])
+        out.zero_()
+        other(xs[(k + 1) % 3])
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[k % 3]), f"replay {k}"
