@@ -479,6 +479,11 @@ BMOE_API bmoe_status brownout_moe_w4_quantize(int32_t dtype, int32_t n, int32_t 
  *   brownout_moe_w4_gate_up  h[row,:] = silu(a[row,:] Wg[s]^T) * (a[row,:] Wu[s]^T)
  *                            Wg, Wu [n_seg, d_ff, d], the same group and both with or without zeros
  *   brownout_moe_w4_ffn      gate_up, then y[row,:] = h[row,:] Wd[s]^T   Wd [n_seg, d, d_ff]
+ *                            (from the stored h: rounded to dtype, as in brownout_moe_ffn)
+ * A result that leaves fp32 on the way though it is finite itself (activations near the
+ * largest value), or that an infinite h makes infinite, is what the definition gives.
+ * Long segments are multiplied right but not fast: bf16 weights and brownout_moe_ffn are
+ * faster from about 70 rows a segment on.
  */
 BMOE_API bmoe_status brownout_moe_w4_matmul(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t N, int32_t K,
                                    const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,

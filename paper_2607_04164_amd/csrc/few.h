@@ -28,13 +28,18 @@
 // Hidden values of bf16 layers are kept as the sum of two bf16 (16 bits of
 // significand) and multiplied as such, since the matrix cores idle here anyway;
 // so the layer's output is rounded once. Up to eight tokens have their high parts
-// in rows 0..7 of the A operand and their low parts in rows 8..15.
+// in rows 0..7 of the A operand and their low parts in rows 8..15. In 4-bit layers
+// hidden values and outputs that are not finite are formed again as they are
+// defined (see w4.h).
 //
-// d 2048, 60 experts, top-4, 15 segments, d_ff 1408, kernel by kernel: one token 2.9 +
-// 14.4 + 9 us (63 MB; of the second 3.5 before its first weights), 16 tokens 4.6 + 30 +
-// 19 (177 MB), one token in 4 bits 2.8 + 10 + 7.8 (17 MB: latency). Two tokens of d 4096,
-// d_ff 14336: 4.6 + 121 + 65 (914 MB, 4.9 TB/s); six of them in 4 bits 4.8 + 63 + 42
-// (331 MB: two waves a SIMD by registers, each with one unit on its way).
+// d 2048, 60 experts, top-4, 15 segments, d_ff 1408, kernel by kernel (medians over
+// three sets of weights in turn, part of which stays in the last-level cache): one token
+// 3.0 + 14.4 + 8.9 us (63 MB on average; of the second 3.5 before its first weights), 16
+// tokens 4.6 + 29.4 + 18.7 (177 MB), one token in 4 bits 2.8 + 10.4 + 7.8 (17 MB: latency).
+// Two tokens of d 4096, d_ff 14336 that reach three or four segments: 4.6 + 122 + 64 (1060
+// to 1410 MB); six of them in 4 bits 4.8 + 63 + 42 (331 MB: two waves a SIMD by registers,
+// each with one unit on its way). Down of more than eight tokens is short of registers: at
+// three waves a SIMD bf16 spills 8 bytes a lane, at two 4-bit groups of 32 spill 44.
 #pragma once
 
 #include <math.h>

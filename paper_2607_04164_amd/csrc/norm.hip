@@ -162,7 +162,10 @@ void with_chunks(int nch, F f) {
 // which holds three rows; with more, too few waves fit a SIMD to keep its loads going
 // (8192 bf16 rows, a wave and four waves a row: pre_norm 6.8 and 10.0 us of 1024
 // columns, 11.7 and 13.2 of 2048, 22.7 and 20.5 of 4096; post_norm 17.4 and 24.8, 39.7
-// and 34.0, 116.7 and 70.4).
+// and 34.0, 116.7 and 70.4). Wider rows have no split that keeps both: with four waves
+// bf16 post_norm of 8192 columns holds 234 registers (4096 rows with a full gate: 75 us, 4.5
+// TB/s, against 5.0 at 4096 columns), of 16384 256 (2048 rows: 114 us, 2.9), and with sixteen
+// waves it spills (32768 columns: 385 us, 1.7). pre_norm stays at 5.2 TB/s and more.
 template <int WAVE_CHUNKS, int MAX_NCH, typename F>
 hipError_t with_split(int64_t T, int nch, F f) {
     if (nch <= 64 || (nch <= 64 * WAVE_CHUNKS && T >= 1024)) with_chunks<64, 1, WAVE_CHUNKS>(nch, f);

@@ -43,7 +43,7 @@ def _check(y, want, err, rows, what):
         assert np.linalg.norm(got - want) <= R.HALF["bf16"] * np.linalg.norm(want), what
 
 
-# rows a tile and a pass of 64 end in, K that ends inside a chunk, a group and 32 columns, N inside a tile
+# rows that end inside a tile of 16 and a pass of 32, K that ends inside a chunk, a group and 32 columns, N inside a tile
 CASES = [(1, 1, 8, 8), (1, 1, 4096, 1408), (1, 17, 24, 264), (1, 65, 72, 136), (3, 7, 40, 128), (5, 130, 16, 1408),
          (8, 64, 256, 2048), (4, 300, 56, 40), (60, 48, 176, 352),
          (1, 3, 24, 4096), (2, 150, 40, 2048), (1, 33, 16, 8192)]
