@@ -679,7 +679,7 @@ template <class F>
 __device__ __forceinline__ float defined_output(const FewParams<F>& p, int t, int c) {
     double sum = 0.0;
 #pragma clang loop unroll(disable)
-    for (int i = 0; i <= p.k; ++i) {  // (the last one: the shared experts)
+    for (int i = 0; i <= p.k && !isnan(sum); ++i) {  // (the last one: the shared experts)
         const bool sh = i == p.k;
         const int slot = t * p.k + min(i, p.k - 1), g = sh ? 0 : p.slot_group[slot], width = pick(sh, p.fs, p.f);
         if (sh ? p.fs == 0 : (unsigned)g >= (unsigned)p.G) continue;
