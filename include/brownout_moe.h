@@ -415,7 +415,8 @@ BMOE_API bmoe_status brownout_moe_combine(const bmoe_desc* desc, const int32_t* 
  * Sums in fp32 over the whole row, one rounding at each output. Every tensor
  * except the per-token gate is 16-byte aligned. d is at most 32768; eps in
  * [1e-12, 1]; res_scale finite. An output may be one of the input tensors of
- * its shape (the residual stream updated in place); r and a differ. No workspace.
+ * its shape (the residual stream updated in place); any other memory shared with
+ * an input, or by r and a, is BMOE_ERR_UNSUPPORTED. No workspace.
  */
 typedef enum bmoe_gate_mode {
     BMOE_GATE_NONE = 0,
@@ -474,7 +475,7 @@ BMOE_API bmoe_status brownout_moe_w4_quantize(int32_t dtype, int32_t n, int32_t 
  * brownout_moe_ffn: segment s covers rows offsets[s] .. offsets[s+1]-1; rows of
  * no segment are left as they are. a_rows as in brownout_moe_ffn_gather, or NULL
  * (row r reads a[r]; a then has rows_cap rows and a_count is not used). A product's output
- * is not its input (BMOE_ERR_UNSUPPORTED). No workspace.
+ * shares no memory with its input (BMOE_ERR_UNSUPPORTED; w4_ffn's y may with a). No workspace.
  *   brownout_moe_w4_matmul   y[row,:] = a[row,:] W[s]^T                 W [n_seg, N, K]
  *   brownout_moe_w4_gate_up  h[row,:] = silu(a[row,:] Wg[s]^T) * (a[row,:] Wu[s]^T)
  *                            Wg, Wu [n_seg, d_ff, d], the same group and both with or without zeros

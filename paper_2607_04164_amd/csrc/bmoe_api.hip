@@ -13,6 +13,11 @@ inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 inline int elem_bytes(int dtype) { return dtype == BMOE_BF16 ? 2 : 4; }
 
+// whether an output of n bytes shares memory with an input of m bytes
+inline bool shares(const void* out, size_t n, const void* in, size_t m) {
+    return out && in && (uintptr_t)out < (uintptr_t)in + m && (uintptr_t)in < (uintptr_t)out + n;
+}
+
 bmoe_status norm_check(int32_t dtype, int32_t T, int32_t d, float eps) {
     if (dtype != BMOE_F32 && dtype != BMOE_BF16) return BMOE_ERR_UNSUPPORTED;
     if (T < 0 || d < 8 || d % 8 != 0 || d > BMOE_NORM_MAX_D) return BMOE_ERR_SHAPE;
@@ -327,6 +332,10 @@ bmoe_status brownout_moe_pre_norm(int32_t dtype, int32_t T, int32_t d, float eps
     if (st != BMOE_OK || T == 0) return st;
     if (!x || !out) return BMOE_ERR_NULL;
     if (!aligned16(x) || !aligned16(out) || !aligned16(w)) return BMOE_ERR_ALIGN;
+    const size_t row = (size_t)d * elem_bytes(dtype), all = (size_t)T * row;
+    // (a row is read before it is written, but no other row, nor the weights once there are more)
+    if ((out != x && shares(out, all, x, all)) || ((out != w || T > 1) && shares(out, all, w, row)))
+        return BMOE_ERR_UNSUPPORTED;
     return hip_status(bmoe::launch_pre_norm(bmoe::PreNormArgs{x, w, out, T, d, dtype, eps}, (hipStream_t)stream));
 }
 
@@ -340,12 +349,21 @@ bmoe_status brownout_moe_post_norm(int32_t dtype, int32_t T, int32_t d, float ep
     if (!isfinite(res_scale)) return BMOE_ERR_SHAPE;
     if (T == 0) return BMOE_OK;
     if (!y || !x || !r || (gate_mode != BMOE_GATE_NONE && !gate)) return BMOE_ERR_NULL;
-    // what would not be read is not taken; r and a would overwrite each other
-    if ((gate_mode == BMOE_GATE_NONE && gate) || (!norm_y && w_post) || (!a && w_next) || a == r)
+    // what would not be read is not taken
+    if ((gate_mode == BMOE_GATE_NONE && gate) || (!norm_y && w_post) || (!a && w_next))
         return BMOE_ERR_UNSUPPORTED;
     for (const void* p : {y, x, w_post, (const void*)r, w_next, (const void*)a})
         if (!aligned16(p)) return BMOE_ERR_ALIGN;
     if (gate && ((uintptr_t)gate & (gate_mode == BMOE_GATE_TOKEN ? 3u : 15u))) return BMOE_ERR_ALIGN;
+    const size_t row = (size_t)d * elem_bytes(dtype), all = (size_t)T * row;
+    const size_t gates = gate_mode == BMOE_GATE_FULL ? all : gate_mode == BMOE_GATE_CHANNEL ? row : (size_t)T * 4;
+    if (shares(r, all, a, all)) return BMOE_ERR_UNSUPPORTED;
+    for (const void* out : {(const void*)r, (const void*)a}) {
+        if ((out != y && shares(out, all, y, all)) || (out != x && shares(out, all, x, all)) ||
+            (!(out == gate && gate_mode == BMOE_GATE_FULL) && shares(out, all, gate, gates)) ||
+            shares(out, all, w_post, row) || shares(out, all, w_next, row))
+            return BMOE_ERR_UNSUPPORTED;
+    }
     return hip_status(bmoe::launch_post_norm(
         bmoe::PostNormArgs{y, x, w_post, gate, w_next, r, a, T, d, dtype, norm_y, gate_mode, eps, res_scale},
         (hipStream_t)stream));
@@ -368,7 +386,8 @@ bmoe_status brownout_moe_w4_matmul(int32_t dtype, int32_t n_seg, int32_t rows_ca
                                    const bmoe_w4* w, void* y, void* stream) {
     bmoe_status st = w4_check(dtype, n_seg, rows_cap, N, K, offsets, a_rows, a_count, a, w, nullptr, y);
     if (st != BMOE_OK || rows_cap == 0) return st;
-    if (y == a) return BMOE_ERR_UNSUPPORTED;  // (other workgroups still read a)
+    // (other workgroups still read a)
+    if (shares(y, (size_t)rows_cap * N * 2, a, (size_t)(a_rows ? a_count : rows_cap) * K * 2)) return BMOE_ERR_UNSUPPORTED;
     return hip_status(bmoe::launch_w4_gemm(
         bmoe::W4GemmArgs{offsets, a_rows, a_count, a, w, nullptr, y, n_seg, rows_cap, N, K}, (hipStream_t)stream));
 }
@@ -379,7 +398,7 @@ bmoe_status brownout_moe_w4_gate_up(int32_t dtype, int32_t n_seg, int32_t rows_c
     if (rows_cap > 0 && !w_up) return BMOE_ERR_NULL;
     bmoe_status st = w4_check(dtype, n_seg, rows_cap, d_ff, d, offsets, a_rows, a_count, a, w_gate, w_up, h);
     if (st != BMOE_OK || rows_cap == 0) return st;
-    if (h == a) return BMOE_ERR_UNSUPPORTED;
+    if (shares(h, (size_t)rows_cap * d_ff * 2, a, (size_t)(a_rows ? a_count : rows_cap) * d * 2)) return BMOE_ERR_UNSUPPORTED;
     return hip_status(bmoe::launch_w4_gemm(
         bmoe::W4GemmArgs{offsets, a_rows, a_count, a, w_gate, w_up, h, n_seg, rows_cap, d_ff, d},
         (hipStream_t)stream));
@@ -393,7 +412,9 @@ bmoe_status brownout_moe_w4_ffn(int32_t dtype, int32_t n_seg, int32_t rows_cap, 
     bmoe_status st = w4_check(dtype, n_seg, rows_cap, d_ff, d, offsets, a_rows, a_count, a, w_gate, w_up, h);
     if (st == BMOE_OK) st = w4_check(dtype, n_seg, rows_cap, d, d_ff, offsets, nullptr, 0, h, w_down, nullptr, y);
     if (st != BMOE_OK || rows_cap == 0) return st;
-    if (h == a || y == h) return BMOE_ERR_UNSUPPORTED;  // (y may be a: it is read before)
+    const size_t h_bytes = (size_t)rows_cap * d_ff * 2;  // (y may be a: it is read before)
+    if (shares(h, h_bytes, a, (size_t)(a_rows ? a_count : rows_cap) * d * 2) || shares(y, (size_t)rows_cap * d * 2, h, h_bytes))
+        return BMOE_ERR_UNSUPPORTED;
     const hipError_t e = bmoe::launch_w4_gemm(
         bmoe::W4GemmArgs{offsets, a_rows, a_count, a, w_gate, w_up, h, n_seg, rows_cap, d_ff, d}, (hipStream_t)stream);
     if (e != hipSuccess) return BMOE_ERR_HIP;

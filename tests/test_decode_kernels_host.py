@@ -13,6 +13,7 @@ from paper_2607_04164_amd import binding as B
 
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="needs a host compiler for the recording runtime")
 GROUPS = (32, 64, 128)
+FAR = 1 << 40  # outputs
 
 
 def ptrs(n):
@@ -36,14 +37,14 @@ def w4(group, zeros=False):
 
 def matmul_call(n, rows, N_, K, group, **device):
     return {"fn": "brownout_moe_w4_matmul",
-            "args": [*ints(1, n, rows, N_, K), ["p", PTR], ["p", 0], ["i", 0], ["p", PTR], w4(group), ["p", 2 * PTR], ["p", 0]],
+            "args": [*ints(1, n, rows, N_, K), ["p", PTR], ["p", 0], ["i", 0], ["p", PTR], w4(group), ["p", FAR], ["p", 0]],
             **device}
 
 
 def gate_up_call(n, rows, f, d, group, **device):
     return {"fn": "brownout_moe_w4_gate_up",
             "args": [*ints(1, n, rows, d, f), ["p", PTR], ["p", 0], ["i", 0], ["p", PTR], w4(group), w4(group),
-                     ["p", 2 * PTR], ["p", 0]], **device}
+                     ["p", FAR], ["p", 0]], **device}
 
 
 def quantize_call(dtype, group):
@@ -51,12 +52,13 @@ def quantize_call(dtype, group):
 
 
 def pre_call(T, d, dtype):
-    return {"fn": "brownout_moe_pre_norm", "args": [*ints(dtype, T, d), ["f", 1e-6], *ptrs(3), ["p", 0]]}
+    return {"fn": "brownout_moe_pre_norm", "args": [*ints(dtype, T, d), ["f", 1e-6], *ptrs(2), ["p", FAR], ["p", 0]]}
 
 
 def post_call(T, d, dtype):
     return {"fn": "brownout_moe_post_norm",
-            "args": [*ints(dtype, T, d), ["f", 1e-6], ["i", 1], ["f", 1.0], ["i", 3], *ptrs(6), ["p", 2 * PTR], ["p", 0]]}
+            "args": [*ints(dtype, T, d), ["f", 1e-6], ["i", 1], ["f", 1.0], ["i", 3], *ptrs(4), ["p", FAR], ["p", PTR],
+                     ["p", 2 * FAR], ["p", 0]]}
 
 
 def launched(calls, tmp_path):

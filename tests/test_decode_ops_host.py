@@ -203,3 +203,34 @@ def test_sizes_past_32_bits_are_refused(monkeypatch):
     for call in calls:
         with pytest.raises(ValueError, match=f"size of {n}"):
             call()
+
+
+ELSEWHERE = 1 << 40
+
+
+@pytest.mark.parametrize("T,kw", [(4, dict(out=A + 128)), (4, dict(x=A + 384)), (4, dict(x=ELSEWHERE, w=A + 512 - 16)),
+                                  (2, dict(x=ELSEWHERE, w=A)), (1, dict(x=ELSEWHERE, w=A + 64))])
+def test_pre_norm_refuses_shared_memory(lib, T, kw):
+    """T rows of 64 bf16 at A: an output that begins inside its input or reaches the weights."""
+    assert pre(lib, T=T, **{"w": None, **kw}) == UNSUP
+
+
+@pytest.mark.parametrize("kw", [
+    dict(r=A + 256), dict(x=A + 256), dict(y=A + 16), dict(wp=A), dict(wp=A + 256), dict(mode=1, gate=A + 256),
+    dict(mode=2, gate=A + 1020), dict(mode=3, gate=A + 16), dict(a=A + 768), dict(a=ELSEWHERE, wn=A + 512),
+    dict(a=ELSEWHERE, wn=ELSEWHERE + 256), dict(r=ELSEWHERE, a=A + 16), dict(r=ELSEWHERE, a=A, mode=2, gate=A)])
+def test_post_norm_refuses_shared_memory(lib, kw):
+    """Four rows of 64 fp32 at A."""
+    assert post(lib, **{"wp": None, **kw}) == UNSUP
+
+
+def test_w4_products_refuse_shared_memory(lib):
+    """Five rows of 64 and 16 bf16: outputs that begin inside the input, or end there."""
+    for a, y in ((A, A + 512), (A + 144, A), (A + 16, A)):
+        assert matmul(lib, a=a, y=y) == UNSUP
+    # gathered rows: a has m of them
+    assert matmul(lib, a=A, y=A + 8 * 128 - 16, a_rows=ELSEWHERE, m=8) == UNSUP
+    ref = ctypes.byref(w4s())
+    ffn = lambda a, h, y: lib.brownout_moe_w4_ffn(1, 2, 5, 64, 64, A, None, 0, a, ref, ref, ref, h, y, None)  # noqa: E731
+    assert lib.brownout_moe_w4_gate_up(1, 2, 5, 64, 64, A, None, 0, A, ref, ref, A + 624, None) == UNSUP
+    assert ffn(A, A + 16, ELSEWHERE) == UNSUP and ffn(ELSEWHERE, A, A + 624) == UNSUP
