@@ -21,7 +21,9 @@
  *   brownout_moe_ffn       grouped SwiGLU FFN over the united experts
  *   brownout_moe_combine   gate-weighted sum back into token order
  * For up to 16 tokens one call does the same (brownout_moe_few). The experts may be held
- * in 4 bits (bmoe_w4; brownout_moe_w4_ffn in place of brownout_moe_ffn, or brownout_moe_few).
+ * in 4 bits (bmoe_w4; brownout_moe_w4_ffn in place of brownout_moe_ffn, or brownout_moe_few),
+ * or in 8 bits with the activations rounded to 8 bits by token (bmoe_w8; brownout_moe_w8_ffn).
+ * brownout_moe_balance measures how evenly the router's picks fall, with its gradient by the logits.
  * brownout_moe_pre_norm and brownout_moe_post_norm are the layer's two ends in a residual block.
  *
  * Conventions for every call:
@@ -532,6 +534,97 @@ typedef struct bmoe_few_weights {
 BMOE_API bmoe_status brownout_moe_few(const bmoe_desc* desc, const bmoe_few_weights* weights, const void* x,
                              int32_t* topk_idx, float* topk_w, int32_t* slot_group, float* slot_gate, void* out,
                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rows held in 8 bits with one scale each: weights [n, N, K] by output channel, activations
+ * [rows, K] by token. A stack of rows of K values (K a multiple of 8, at most BMOE_W8_MAX_K) is
+ *   codes  [rows, P] int8, P = 128 * ceil(K/128): the codes of a row, then zeros
+ *   scales [rows] float
+ * and stands for x = scale * code. Both 16-byte aligned.
+ *
+ * brownout_moe_w8_quantize -- rounds x [rows, K] (dtype) to that format: scale = max|x| / 127 in
+ * fp32, code = round(x / scale) to nearest even, of the true quotient. A row whose scale would be
+ * below 2^-120 (zeros, say) has scale 0 and codes 0. A row with a value that is not finite has
+ * scale NaN and codes 0: all of it reads NaN, and so does every product with it. rows at most
+ * 2^30; outputs share no memory with x (BMOE_ERR_UNSUPPORTED).
+ */
+#define BMOE_W8_MAX_K 131072
+#define BMOE_W8_ROW_BYTES(K) (((K) + 127) / 128 * 128)
+typedef struct bmoe_w8 {
+    const int8_t* codes;
+    const float* scales;
+} bmoe_w8;
+BMOE_API bmoe_status brownout_moe_w8_quantize(int32_t dtype, int32_t rows, int32_t K, const void* x, int8_t* codes,
+                                     float* scales, void* stream);
+
+/*
+ * Grouped products in 8-bit integers. dtype: BMOE_BF16 (the activations' and outputs'; others are
+ * BMOE_ERR_UNSUPPORTED). Segments as in brownout_moe_ffn: segment s covers rows offsets[s] ..
+ * offsets[s+1]-1; rows of no segment are left as they are. Row r reads a[a_rows[r]] (entries
+ * clamped into [0, a_count), the codes below 2^32 bytes), or a[r] with a_rows NULL (a then has
+ * rows_cap rows and a_count is not used). The activations are given as a (dtype; the call rounds
+ * them to 8 bits, each row once however many rows read it) or as a8 (rounded already); the other
+ * is NULL.
+ *   brownout_moe_w8_matmul   y[row, n] = sa[row] * sw[s, n] * sum_k qa[row, k] * qw[s, n, k]    W [n_seg, N, K]
+ *   brownout_moe_w8_gate_up  h[row, :] = silu(gate[row, :]) * up[row, :], two such products      [n_seg, d_ff, d]
+ *   brownout_moe_w8_ffn      gate_up, then y from the stored h (rounded to dtype, as in
+ *                            brownout_moe_ffn, then to 8 bits by row) and w_down                 [n_seg, d, d_ff]
+ * The sums are exact (int32); a product is rounded to fp32 three times and once to dtype. N and d
+ * are multiples of 8. An output shares no memory with the input of its product
+ * (BMOE_ERR_UNSUPPORTED; w8_ffn's y may with a).
+ * workspace (256-byte aligned, no initialisation, not preserved; calls that can overlap in time must
+ * not share one): at least bmoe_w8_workspace_bytes(a_count, K, rows_cap, d_ff, 0) bytes, a_count 0
+ * where a8 is given (rows_cap where a_rows is NULL), K the columns of a, d_ff 0 but for w8_ffn.
+ * With the size for split 1, which depends on the current device, the K loops of the last large
+ * tiles may be split, as in brownout_moe_ffn; the results are the same bits.
+ */
+BMOE_API size_t bmoe_w8_workspace_bytes(int32_t a_count, int32_t K, int32_t rows_cap, int32_t d_ff, int32_t split);
+BMOE_API bmoe_status brownout_moe_w8_matmul(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t N, int32_t K,
+                                   const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,
+                                   const bmoe_w8* a8, const bmoe_w8* w, void* y, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+BMOE_API bmoe_status brownout_moe_w8_gate_up(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t d, int32_t d_ff,
+                                    const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,
+                                    const bmoe_w8* a8, const bmoe_w8* w_gate, const bmoe_w8* w_up, void* h,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+BMOE_API bmoe_status brownout_moe_w8_ffn(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t d, int32_t d_ff,
+                                const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,
+                                const bmoe_w8* a8, const bmoe_w8* w_gate, const bmoe_w8* w_up, const bmoe_w8* w_down,
+                                void* h, void* y, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * brownout_moe_balance -- how evenly the router's picks fall on the experts, or on the groups that
+ * a map makes of them. Over the tokens that count (valid[t] != 0; all of them with valid NULL), V
+ * in number:
+ *   p_t = softmax(logits_t),  lse_t = log(sum over e of exp(logits_te))
+ *   counts[e] = picks of expert e among topk_idx,  counts[E] = V
+ *   prob[e]   = mean of p_te
+ *   F_r       = (sum of counts[e] over the experts of group r) / (k V)
+ *   losses[0] = G * sum over e of F_{e2g[e]} * prob[e]     (1 where picks and probabilities are even)
+ *   losses[1] = mean of lse_t^2                            (the z loss)
+ * brownout_moe_balance_grad -- the gradient of d_losses[0] losses[0] + d_losses[1] losses[1] by the
+ * logits, the counts held constant:
+ *   d_logits[t,e] = (d_losses[0] G / V) p_te (F_{e2g[e]} - sum over j of F_{e2g[j]} p_tj)
+ *                   + d_losses[1] (2 / V) lse_t p_te,   0 for tokens that do not count
+ * logits [T,E] float (as brownout_moe_route writes them), topk_idx [T,k] int32 (entries outside
+ * [0, E) pick nothing; a repeated one counts each time), valid [T] uint8 or NULL, e2g [E] int32
+ * (entries outside [0, G) belong to no group and add nothing) or NULL (groups are the experts: G
+ * must be E). All in DEVICE memory. Outputs: losses [2], prob [E] float, counts [E+1] int32;
+ * d_logits [T,E] float, which may be logits itself (other shared memory is BMOE_ERR_UNSUPPORTED).
+ * Logits of tokens that do not count are not read. -infinity is an expert of probability 0; a
+ * token of nothing else has no probabilities, adds nothing to the losses and gets gradient 0,
+ * though it counts in V. With V == 0 losses and prob are 0. Sums in a fixed order: results are
+ * deterministic. E in 1..256, k in 1..16, G in 1..256.
+ * workspace: bmoe_balance_workspace_bytes(T, E) bytes (0 for few tokens), 8-byte aligned, no
+ * initialisation; calls that can overlap in time must not share one.
+ */
+BMOE_API size_t bmoe_balance_workspace_bytes(int32_t T, int32_t E);
+BMOE_API bmoe_status brownout_moe_balance(int32_t T, int32_t E, int32_t k, int32_t G, const float* logits,
+                                 const int32_t* topk_idx, const uint8_t* valid, const int32_t* e2g, float* losses,
+                                 int32_t* counts, float* prob, void* workspace, size_t workspace_bytes, void* stream);
+BMOE_API bmoe_status brownout_moe_balance_grad(int32_t T, int32_t E, int32_t k, int32_t G, const float* logits,
+                                      const uint8_t* valid, const int32_t* e2g, const int32_t* counts,
+                                      const float* d_losses, float* d_logits, void* stream);
 
 #ifdef __cplusplus
 }

@@ -31,11 +31,14 @@ EXPORTED = ("bmoe_validate", "bmoe_validate_map", "bmoe_workspace_bytes", "bmoe_
             "brownout_moe_ffn_gather", "brownout_moe_ffn_gate_up_gather", "brownout_moe_united_init",
             "brownout_moe_distill_mse", "brownout_moe_ffn_ex", "bmoe_partial_segment_map", "brownout_moe_dispatch_noalloc", "brownout_moe_ffn_down_combine",
             "brownout_moe_pre_norm", "brownout_moe_post_norm", "brownout_moe_w4_quantize", "brownout_moe_w4_matmul",
-            "brownout_moe_w4_gate_up", "brownout_moe_w4_ffn", "brownout_moe_few")
+            "brownout_moe_w4_gate_up", "brownout_moe_w4_ffn", "brownout_moe_few", "brownout_moe_w8_quantize",
+            "bmoe_w8_workspace_bytes", "brownout_moe_w8_matmul", "brownout_moe_w8_gate_up", "brownout_moe_w8_ffn",
+            "bmoe_balance_workspace_bytes", "brownout_moe_balance", "brownout_moe_balance_grad")
 STATUS_CODES = {v: k for k, v in STATUS.items()}
 DISTILL_WS_BYTES = 32768
 FEW_MAX_TOKENS = 16
 NORM_MAX_D = 32768
+W8_MAX_K = 131072
 GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_FULL = 0, 1, 2, 3
 DISPATCH_SCRATCH_BYTES = 1048576  # the array behind brownout_moe_dispatch_noalloc
 
@@ -71,6 +74,10 @@ def make_desc(T, d, E, top_k, G, d_ff, d_ff_shared=0, norm_topk=0, dtype="bf16")
 class _W4Struct(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p),
                 ("group", ctypes.c_int32)]
+
+
+class _W8Struct(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
 
 
 class _Matrix(ctypes.Structure):
@@ -148,6 +155,23 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.brownout_moe_w4_ffn.restype = I32
     lib.brownout_moe_few.argtypes = [DP, ctypes.POINTER(_FewWeights)] + [P] * 7 + [SZ, P]
     lib.brownout_moe_few.restype = I32
+    W8P = ctypes.POINTER(_W8Struct)
+    lib.brownout_moe_w8_quantize.argtypes = [I32] * 3 + [P] * 4
+    lib.brownout_moe_w8_quantize.restype = I32
+    lib.bmoe_w8_workspace_bytes.argtypes = [I32] * 5
+    lib.bmoe_w8_workspace_bytes.restype = SZ
+    lib.brownout_moe_w8_matmul.argtypes = [I32] * 5 + [P, P, I32, P, W8P, W8P, P, P, SZ, P]
+    lib.brownout_moe_w8_matmul.restype = I32
+    lib.brownout_moe_w8_gate_up.argtypes = [I32] * 5 + [P, P, I32, P, W8P, W8P, W8P, P, P, SZ, P]
+    lib.brownout_moe_w8_gate_up.restype = I32
+    lib.brownout_moe_w8_ffn.argtypes = [I32] * 5 + [P, P, I32, P, W8P, W8P, W8P, W8P, P, P, P, SZ, P]
+    lib.brownout_moe_w8_ffn.restype = I32
+    lib.bmoe_balance_workspace_bytes.argtypes = [I32, I32]
+    lib.bmoe_balance_workspace_bytes.restype = SZ
+    lib.brownout_moe_balance.argtypes = [I32] * 4 + [P] * 8 + [SZ, P]
+    lib.brownout_moe_balance.restype = I32
+    lib.brownout_moe_balance_grad.argtypes = [I32] * 4 + [P] * 7
+    lib.brownout_moe_balance_grad.restype = I32
     _lib = lib
     return lib
 
@@ -685,7 +709,7 @@ def w4_matmul(offsets: torch.Tensor, a: torch.Tensor, w: W4, *, a_rows: Optional
     return y
 
 
-def _w4_gated(w_gate: W4, w_up: W4):
+def _gated(w_gate, w_up):
     if w_gate.shape != w_up.shape:
         raise ValueError(f"w_gate {w_gate.shape} and w_up {w_up.shape} differ")
     return w_gate.shape
@@ -694,7 +718,7 @@ def _w4_gated(w_gate: W4, w_up: W4):
 def w4_gate_up(offsets: torch.Tensor, a: torch.Tensor, w_gate: W4, w_up: W4, *, a_rows=None, h=None, stream=None):
     """h[row] = silu(a[row] Wg[s]^T) * (a[row] Wu[s]^T); arguments as w4_matmul."""
     device = _device_of(a, "a")
-    n, f, d = _w4_gated(w_gate, w_up)
+    n, f, d = _gated(w_gate, w_up)
     rows, op, rp, m, ap = _w4_rows(offsets, a, a_rows, n, d, device)
     h, hp = _out(h, "h", (rows, f), a, device, stream)
     _check(load_library().brownout_moe_w4_gate_up(BMOE_BF16, n, rows, d, f, op, rp, m, ap, w_gate._on(device),
@@ -706,7 +730,7 @@ def w4_ffn(offsets: torch.Tensor, a: torch.Tensor, w_gate: W4, w_up: W4, w_down:
            stream=None):
     """The grouped SwiGLU FFN with 4-bit weights: (y, h); arguments as w4_matmul."""
     device = _device_of(a, "a")
-    n, f, d = _w4_gated(w_gate, w_up)
+    n, f, d = _gated(w_gate, w_up)
     if w_down.shape != (n, d, f):
         raise ValueError(f"w_down must be {(n, d, f)}, got {w_down.shape}")
     rows, op, rp, m, ap = _w4_rows(offsets, a, a_rows, n, d, device)
@@ -716,6 +740,298 @@ def w4_ffn(offsets: torch.Tensor, a: torch.Tensor, w_gate: W4, w_up: W4, w_down:
                                               w_down._on(device), hp, yp, _stream_ptr(stream, device)), "brownout_moe_w4_ffn")
     return y, h
 
+
+# ---------------------------------------------------------------------------
+# rows in 8 bits, and the products with them
+
+def w8_row_bytes(K: int) -> int:
+    """Bytes of a row of K codes."""
+    return 128 * ((K + 127) // 128)
+
+
+class _Rows8:
+    """Rows of K values in 8 bits with a scale each: codes [.., w8_row_bytes(K)] int8 (zeros past K), scales [..]
+    float. The tensors are checked once here; they are kept, not copied."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, K: int, dims: int):
+        if K < 8 or K % 8 or K > W8_MAX_K:
+            raise ValueError(f"K must be a multiple of 8 from 8 to {W8_MAX_K}")
+        if not isinstance(codes, torch.Tensor) or codes.dim() != dims:
+            raise ValueError(f"codes must have {dims} dimensions, the last one row bytes")
+        rows = tuple(codes.shape[:-1])
+        _int32(*rows, K)
+        self.device = _device_of(codes, "codes")
+        _fits(codes, "codes", torch.int8, (*rows, w8_row_bytes(K)), self.device)
+        _fits(scales, "scales", torch.float32, rows, self.device)
+        self.codes, self.scales, self.shape = codes, scales, (*rows, int(K))
+        self._struct = _W8Struct(codes.data_ptr(), scales.data_ptr())
+        self._ref = ctypes.byref(self._struct)
+
+    def _on(self, device: int):
+        """The call's argument, for a call on GPU `device`."""
+        if self.device != device:
+            raise ValueError(f"8-bit rows are on GPU {self.device}, the call is on GPU {device}")
+        return self._ref
+
+
+class W8(_Rows8):
+    """A matrix stack [n, N, K] in 8 bits with a scale for each output channel: w = scale * code."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, *, K: int):
+        super().__init__(codes, scales, K, 3)
+
+
+class A8(_Rows8):
+    """Activations [rows, K] in 8 bits with a scale for each token: a = scale * code."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, *, K: int):
+        super().__init__(codes, scales, K, 2)
+
+
+def _quantize8(x, dims, kind, out, stream):
+    device = _device_of(x, "x")
+    if x.dim() != dims:
+        raise ValueError(f"x must have {dims} dimensions")
+    *rows, K = shape = tuple(x.shape)
+    n = 1
+    for r in rows:
+        n *= r
+    _int32(n, K)
+    dtype, xp = _dtype_of(x), _fits(x, "x", x.dtype, shape, device)
+    if K < 8 or K % 8 or K > W8_MAX_K:
+        raise ValueError(f"the last dimension must be a multiple of 8 from 8 to {W8_MAX_K}")
+    if out is None:
+        out = kind(_new((*rows, w8_row_bytes(K)), torch.int8, x.device, stream),
+                   _new(tuple(rows), torch.float32, x.device, stream), K=K)
+    elif not isinstance(out, kind) or out.shape != shape:
+        raise ValueError(f"out must be {kind.__name__} rows of shape {shape}")
+    out._on(device)
+    _check(load_library().brownout_moe_w8_quantize(dtype, n, K, xp, out._struct.codes, out._struct.scales,
+                                                   _stream_ptr(stream, device)), "brownout_moe_w8_quantize")
+    return out
+
+
+def w8_quantize(w: torch.Tensor, *, out: Optional[W8] = None, stream=None) -> W8:
+    """w [n, N, K] (bf16 or fp32) rounded to 8 bits by output channel. A channel with a value that is not finite
+    reads NaN throughout."""
+    return _quantize8(w, 3, W8, out, stream)
+
+
+def a8_quantize(a: torch.Tensor, *, out: Optional[A8] = None, stream=None) -> A8:
+    """Activations [rows, K] (bf16 or fp32) rounded to 8 bits by token, for several products with the same input
+    (the products round a tensor themselves)."""
+    return _quantize8(a, 2, A8, out, stream)
+
+
+def w8_workspace_bytes(a_count: int, K: int, rows_cap: int = 0, d_ff: int = 0, split: bool = True) -> int:
+    return int(load_library().bmoe_w8_workspace_bytes(a_count, K, rows_cap, d_ff, 1 if split else 0))
+
+
+def new_w8_workspace(a_count: int, K: int, device, *, rows_cap: int = 0, d_ff: int = 0,
+                     split: bool = True) -> torch.Tensor:
+    """A workspace for 8-bit products of activations [a_count, K] (0: given as A8); rows_cap and d_ff for w8_ffn;
+    split: with the room that lets the K loops of large tiles be split."""
+    n = w8_workspace_bytes(a_count, K, rows_cap, d_ff, split)
+    return torch.empty((max(n, 1) + 255) // 256 * 256, dtype=torch.uint8, device=device)
+
+
+def _w8_rows(offsets, a, a_rows, n: int, K: int, device: int):
+    """Checks the row arguments of an 8-bit product: (rows_cap, offsets, a_rows, a_count, a, a8) as the call takes
+    them, and the rows it rounds itself."""
+    if isinstance(a, A8):
+        if a.shape[1] != K:
+            raise ValueError(f"a must have {K} columns, got {a.shape[1]}")
+        m, ap, a8 = a.shape[0], None, a._on(device)
+    else:
+        if not isinstance(a, torch.Tensor) or a.dim() != 2:
+            raise ValueError("a must be [rows, K], or an A8")
+        m, a8 = a.shape[0], None
+        _int32(m)
+        ap = _fits(a, "a", torch.bfloat16, (m, K), device)
+    op = _fits(offsets, "offsets", torch.int32, (n + 1,), device)
+    own = 0 if a8 is not None else m
+    if a_rows is None:
+        return (m, op, None, 0, ap, a8), own
+    rows = a_rows.numel()
+    _int32(rows)
+    if rows and not m:
+        raise ValueError("a_rows names rows of an empty a")
+    return (rows, op, _fits(a_rows, "a_rows", torch.int32, (rows,), device), m, ap, a8), own
+
+
+def _w8_out(t, name, shape, device, stream):
+    t = _new(shape, torch.bfloat16, torch.device("cuda", device), stream) if t is None else t
+    return t, _fits(t, name, torch.bfloat16, shape, device)
+
+
+def _w8_ws(ws, a_count, K, rows_cap, d_ff, device, stream):
+    """(the workspace, kept alive by the caller; pointer; bytes): a call's own one where none is given"""
+    if ws is None:
+        n = w8_workspace_bytes(a_count, K, rows_cap, d_ff, False)
+        if not n:
+            return None, None, 0
+        ws = _new((n,), torch.uint8, torch.device("cuda", device), stream)
+    return ws, _fits(ws, "workspace", torch.uint8, (ws.numel(),), device), ws.numel()
+
+
+def _device_of_rows(a) -> int:
+    return _device_of(a.codes if isinstance(a, A8) else a, "a")
+
+
+def w8_matmul(offsets: torch.Tensor, a, w: W8, *, a_rows: Optional[torch.Tensor] = None,
+              y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """y[row] = a[row] W[s]^T in 8-bit integers for the rows of segment s (offsets [n+1], as in ffn); a_rows as in
+    ffn_gather. a: bf16 [rows, K], which the call rounds to 8 bits by token, or an A8. Rows of no segment are left as
+    they are (unspecified in a new y). workspace: new_w8_workspace's, or None (memory of the call's own stream, and no
+    split)."""
+    device = _device_of_rows(a)
+    n, N, K = w.shape
+    (rows, op, rp, m, ap, a8), own = _w8_rows(offsets, a, a_rows, n, K, device)
+    y, yp = _w8_out(y, "y", (rows, N), device, stream)
+    ws, wp, wn = _w8_ws(workspace, own, K, 0, 0, device, stream)
+    _check(load_library().brownout_moe_w8_matmul(BMOE_BF16, n, rows, N, K, op, rp, m, ap, a8, w._on(device), yp, wp, wn,
+                                                 _stream_ptr(stream, device)), "brownout_moe_w8_matmul")
+    return y
+
+
+def w8_gate_up(offsets: torch.Tensor, a, w_gate: W8, w_up: W8, *, a_rows=None, h=None, workspace=None, stream=None):
+    """h[row] = silu(a[row] Wg[s]^T) * (a[row] Wu[s]^T); arguments as w8_matmul."""
+    device = _device_of_rows(a)
+    n, f, d = _gated(w_gate, w_up)
+    (rows, op, rp, m, ap, a8), own = _w8_rows(offsets, a, a_rows, n, d, device)
+    h, hp = _w8_out(h, "h", (rows, f), device, stream)
+    ws, wp, wn = _w8_ws(workspace, own, d, 0, 0, device, stream)
+    _check(load_library().brownout_moe_w8_gate_up(BMOE_BF16, n, rows, d, f, op, rp, m, ap, a8, w_gate._on(device),
+                                                  w_up._on(device), hp, wp, wn, _stream_ptr(stream, device)),
+           "brownout_moe_w8_gate_up")
+    return h
+
+
+def w8_ffn(offsets: torch.Tensor, a, w_gate: W8, w_up: W8, w_down: W8, *, a_rows=None, h=None, y=None, workspace=None,
+           stream=None):
+    """The grouped SwiGLU FFN in 8-bit integers: (y, h); arguments as w8_matmul (the workspace made with rows_cap and
+    d_ff)."""
+    device = _device_of_rows(a)
+    n, f, d = _gated(w_gate, w_up)
+    if w_down.shape != (n, d, f):
+        raise ValueError(f"w_down must be {(n, d, f)}, got {w_down.shape}")
+    (rows, op, rp, m, ap, a8), own = _w8_rows(offsets, a, a_rows, n, d, device)
+    h, hp = _w8_out(h, "h", (rows, f), device, stream)
+    y, yp = _w8_out(y, "y", (rows, d), device, stream)
+    ws, wp, wn = _w8_ws(workspace, own, d, rows, f, device, stream)
+    _check(load_library().brownout_moe_w8_ffn(BMOE_BF16, n, rows, d, f, op, rp, m, ap, a8, w_gate._on(device),
+                                              w_up._on(device), w_down._on(device), hp, yp, wp, wn,
+                                              _stream_ptr(stream, device)), "brownout_moe_w8_ffn")
+    return y, h
+
+
+# ---------------------------------------------------------------------------
+# how evenly the router's picks fall
+
+def new_balance_workspace(T: int, E: int, device) -> torch.Tensor:
+    """balance's workspace for up to T tokens of E experts."""
+    n = int(load_library().bmoe_balance_workspace_bytes(T, E))
+    return torch.empty((max(n, 1) + 255) // 256 * 256, dtype=torch.uint8, device=device)
+
+
+def new_balance_buffers(E: int, device) -> Dict[str, torch.Tensor]:
+    """balance's outputs: losses [2], counts [E + 1] (the last: tokens that count), prob [E]."""
+    return {"losses": _empty((2,), torch.float32, device), "counts": _empty((E + 1,), torch.int32, device),
+            "prob": _empty((E,), torch.float32, device)}
+
+
+def _balance_args(logits, valid, e2g, G):
+    """(T, E, G, device, logits, valid, e2g) as the calls take them."""
+    device = _device_of(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError("logits must be [T, E]")
+    T, E = logits.shape
+    _int32(T, E)
+    lp = _fits(logits, "logits", torch.float32, (T, E), device)
+    vp = None if valid is None else _fits(valid, "valid", torch.uint8, (T,), device)
+    if e2g is None:
+        if G not in (None, E):
+            raise ValueError("G without e2g")
+        return T, E, E, device, lp, vp, None
+    if G is None:
+        raise ValueError("e2g without G")
+    return T, E, int(G), device, lp, vp, _fits(e2g, "e2g", torch.int32, (E,), device)
+
+
+def balance(logits: torch.Tensor, topk_idx: torch.Tensor, *, valid: Optional[torch.Tensor] = None,
+            e2g: Optional[torch.Tensor] = None, G: Optional[int] = None, out: Optional[Dict[str, torch.Tensor]] = None,
+            workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """How evenly route's picks fall on the experts, or on the G groups of e2g: losses (balance loss, z loss),
+    counts (picks per expert, then the number of tokens that count) and prob (mean probabilities). logits [T, E] and
+    topk_idx [T, k] as route writes them; valid [T] uint8: the tokens that count (None: all)."""
+    T, E, G, device, lp, vp, gp = _balance_args(logits, valid, e2g, G)
+    if not isinstance(topk_idx, torch.Tensor) or topk_idx.dim() != 2:
+        raise ValueError("topk_idx must be [T, k]")
+    k = topk_idx.shape[1]
+    ip = _fits(topk_idx, "topk_idx", torch.int32, (T, k), device)
+    o = dict(out) if out else {}
+    for name, dt, shape in (("losses", torch.float32, (2,)), ("counts", torch.int32, (E + 1,)),
+                            ("prob", torch.float32, (E,))):
+        if name not in o:
+            o[name] = _new(shape, dt, logits.device, stream)
+    ptrs = (_fits(o["losses"], "losses", torch.float32, (2,), device),
+            _fits(o["counts"], "counts", torch.int32, (E + 1,), device),
+            _fits(o["prob"], "prob", torch.float32, (E,), device))
+    if workspace is None:
+        n = int(load_library().bmoe_balance_workspace_bytes(T, E))
+        workspace = _new((n,), torch.uint8, logits.device, stream) if n else None
+    wp = None if workspace is None else _fits(workspace, "workspace", torch.uint8, (workspace.numel(),), device)
+    _check(load_library().brownout_moe_balance(T, E, k, G, lp, ip, vp, gp, *ptrs, wp,
+                                               0 if workspace is None else workspace.numel(),
+                                               _stream_ptr(stream, device)), "brownout_moe_balance")
+    return o
+
+
+def balance_grad(logits: torch.Tensor, counts: torch.Tensor, k: int, d_losses: torch.Tensor, *,
+                 valid: Optional[torch.Tensor] = None, e2g: Optional[torch.Tensor] = None, G: Optional[int] = None,
+                 out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The gradient of d_losses [2] times balance's losses by the logits: counts as balance wrote them (held
+    constant), the other arguments as it took them. out may be logits."""
+    T, E, G, device, lp, vp, gp = _balance_args(logits, valid, e2g, G)
+    cp = _fits(counts, "counts", torch.int32, (E + 1,), device)
+    dp = _fits(d_losses, "d_losses", torch.float32, (2,), device)
+    if out is None:
+        out = _new((T, E), torch.float32, logits.device, stream)
+    op = _fits(out, "out", torch.float32, (T, E), device)
+    _check(load_library().brownout_moe_balance_grad(T, E, int(k), G, lp, vp, gp, cp, dp, op,
+                                                    _stream_ptr(stream, device)), "brownout_moe_balance_grad")
+    return out
+
+
+class _BalanceLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, topk_idx, valid, e2g, G):
+        if logits.shape[0]:
+            o = balance(logits, topk_idx, valid=valid, e2g=e2g, G=G)
+        else:  # (the call writes nothing)
+            o = {n: t.zero_() for n, t in new_balance_buffers(logits.shape[1], logits.device).items()}
+        ctx.save_for_backward(logits, o["counts"], valid, e2g)
+        ctx.k, ctx.G = topk_idx.shape[1], G
+        ctx.mark_non_differentiable(o["counts"], o["prob"])
+        return o["losses"], o["counts"], o["prob"]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_losses, *_):
+        logits, counts, valid, e2g = ctx.saved_tensors
+        d = balance_grad(logits, counts, ctx.k, d_losses.contiguous(), valid=valid, e2g=e2g, G=ctx.G)
+        return d, None, None, None, None
+
+
+def balance_loss(logits: torch.Tensor, topk_idx: torch.Tensor, *, valid: Optional[torch.Tensor] = None,
+                 e2g: Optional[torch.Tensor] = None, G: Optional[int] = None):
+    """balance for training: (losses, counts, prob), where losses [2] can be differentiated by the logits, once. On
+    the current stream."""
+    return _BalanceLoss.apply(logits, topk_idx, valid, e2g, G)
+
+
+# ---------------------------------------------------------------------------
+# the norms around the layer
 
 def pre_norm(x: torch.Tensor, w: Optional[torch.Tensor] = None, eps: float = 1e-6, *,
              out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -834,25 +1150,35 @@ class LayerForward:
     segment, and bf16 weights are faster from about 70 rows a segment on (the layer
     above: 64 tokens 57 us against 68, 256 tokens 116 against 114, 4096 tokens 1162
     against 324). The layer's device is its weights': `device` must name it.
+
+    8-bit weights: the FFN matrices (the shared ones too) given as W8 objects, bf16 layers, any number of tokens. The
+    products run in 8-bit integers on the activations rounded token by token (brownout_moe_w8_ffn); the routed FFN
+    gathers its rows (fused_gather), stream_k lets the tiles be split (the same bits either way). fold_combine and
+    few_tokens do not go with them; `device` as for 4-bit weights.
+
+    balance=True: route keeps its logits (bufs["route"]["logits"]), and the method balance() gives the picks per
+    expert and the balance and z losses of the last forward (bufs["balance"]). Not with few_tokens.
     """
 
     def __init__(self, desc: Desc, weights: Dict[str, torch.Tensor], device="cuda", stream_k: bool = True,
                  fused_gather: Optional[bool] = None, fold_combine: bool = False, concurrent_shared: bool = True,
-                 few_tokens: bool = False):
+                 few_tokens: bool = False, balance: bool = False):
         self.desc = desc
         self.w = weights
         self.few_tokens = bool(few_tokens)
-        self.w4 = isinstance(weights["w_gate"], W4)
-        self._few_device = None  # the GPU of a few_tokens or 4-bit layer
-        if self.w4 or self.few_tokens:
-            if fold_combine or (self.w4 and fused_gather is False):
-                raise ValueError("fold_combine and fused_gather=False do not go with few_tokens or 4-bit weights")
-            self._check_few_and_w4(device)
+        self.w4, self.w8 = isinstance(weights["w_gate"], W4), isinstance(weights["w_gate"], W8)
+        self._few_device = None  # the GPU of a few_tokens, 4-bit or 8-bit layer
+        if self.few_tokens and (self.w8 or balance):
+            raise ValueError("few_tokens does not go with 8-bit weights or balance")
+        if self.w4 or self.w8 or self.few_tokens:
+            if fold_combine or ((self.w4 or self.w8) and fused_gather is False):
+                raise ValueError("fold_combine and fused_gather=False do not go with few_tokens, 4-bit or 8-bit weights")
+            self._check_few_and_packed(device)
         if self.few_tokens:
             self._plan_few(device)
             return
-        if self.w4:
-            fused_gather, stream_k = True, False
+        if self.w4 or self.w8:
+            fused_gather = True
         if fused_gather is None:
             # (the gathered copies address x with 32-bit byte offsets)
             x_bytes = desc.T * desc.d * (2 if desc.dtype == BMOE_BF16 else 4)
@@ -878,7 +1204,16 @@ class LayerForward:
         if not fused_gather:
             self.bufs["dispatch"]["x_perm"] = _empty((rows, d), dt, device)
         self.ws = new_dispatch_workspace(desc, device)
-        self.ffn_ws = new_ffn_workspace(desc, device) if stream_k else None
+        if balance:
+            self.bufs["route"]["logits"] = _empty((T, E), torch.float32, device)
+            self.bufs["balance"] = new_balance_buffers(E, device)
+            self._balance_ws = new_balance_workspace(T, E, device)
+        if self.w8:  # (the shared experts' rounded rows beside the routed ones')
+            self.ffn_ws = new_w8_workspace(T, d, device, rows_cap=rows, d_ff=desc.d_ff, split=stream_k)
+            self.shared_ws = new_w8_workspace(T, d, device, rows_cap=T, d_ff=desc.d_ff_shared,
+                                              split=False) if desc.d_ff_shared else None
+        else:
+            self.ffn_ws = new_ffn_workspace(desc, device) if stream_k and not self.w4 else None
         self.fold_ws = new_down_combine_workspace(desc, device) if fold_combine else None
         self._side = None
         if desc.d_ff_shared:
@@ -890,13 +1225,14 @@ class LayerForward:
                 self._side = torch.cuda.Stream(device=device)
         self._plan()
 
-    def _check_few_and_w4(self, buffers):
-        """Checks the weights of a few_tokens or 4-bit layer, and that its buffers will be beside them."""
+    def _check_few_and_packed(self, buffers):
+        """Checks the weights of a few_tokens, 4-bit or 8-bit layer, and that its buffers will be beside them."""
         desc, w = self.desc, self.w
         _check(validate(desc), "bmoe_validate")
         dt, d, E, G = desc.torch_dtype, desc.d, desc.E, desc.G
-        if self.w4 and desc.dtype != BMOE_BF16:
-            raise ValueError("4-bit weights need a bf16 layer")
+        packed = W4 if self.w4 else W8
+        if (self.w4 or self.w8) and desc.dtype != BMOE_BF16:
+            raise ValueError(f"{4 if self.w4 else 8}-bit weights need a bf16 layer")
         device = _device_of(w["e2g"], "e2g")
         buffers = torch.device(buffers)
         if buffers.type != "cuda" or buffers.index not in (None, device):
@@ -910,16 +1246,16 @@ class LayerForward:
             fs = desc.d_ff_shared
             shapes.update(w_gate_sh=(1, fs, d), w_up_sh=(1, fs, d), w_down_sh=(1, d, fs))
         for name, shape in shapes.items():
-            if not self.w4:
+            if not (self.w4 or self.w8):
                 _fits(w[name], name, dt, shape, device)
                 continue
             m, first = w[name], w["w_gate"]
-            if not isinstance(m, W4):
-                raise ValueError(f"{name} must be a W4, as w_gate is")
+            if not isinstance(m, packed):
+                raise ValueError(f"{name} must be a {packed.__name__}, as w_gate is")
             m._on(device)
             if m.shape != shape:
                 raise ValueError(f"{name} must have shape {shape}, got {m.shape}")
-            if m.group != first.group or (m.zeros is None) != (first.zeros is None):
+            if self.w4 and (m.group != first.group or (m.zeros is None) != (first.zeros is None)):
                 raise ValueError(f"{name} must have w_gate's group size, and zero points as it has")
         self._few_names, self._few_device = tuple(shapes), device
 
@@ -972,18 +1308,18 @@ class LayerForward:
         _dev(w["e2g"], "e2g", torch.int32, (E,))
         if w.get("bias") is not None:
             _dev(w["bias"], "bias", torch.float32, (E,))
-        if not self.w4:
+        if not (self.w4 or self.w8):
             _dev(w["w_gate"], "w_gate", dt, (G, f, d))
             _dev(w["w_up"], "w_up", dt, (G, f, d))
             _dev(w["w_down"], "w_down", dt, (G, d, f))
-        ptr = lambda t: None if t is None else t._ref if isinstance(t, W4) else t.data_ptr()
+        ptr = lambda t: None if t is None else t._ref if isinstance(t, (W4, W8)) else t.data_ptr()
         wsp, wsn = (ptr(self.ffn_ws), self.ffn_ws.numel()) if self.ffn_ws is not None else (None, 0)
         self._lib = load_library()
         self._desc_ref = ctypes.byref(desc)
         self._xshape, self._dt = (T, d), dt
         r, dp = b["route"], b["dispatch"]
         self._route_args = (ptr(w["w_router"]), ptr(w.get("bias")), None, ptr(w["e2g"]), ptr(r["topk_idx"]),
-                            ptr(r["topk_w"]), ptr(r["slot_group"]), ptr(r["slot_gate"]), None)
+                            ptr(r["topk_w"]), ptr(r["slot_group"]), ptr(r["slot_gate"]), ptr(r.get("logits")))
         fused = self.fused_gather
         self._dispatch_args = (ptr(dp["counts"]), ptr(dp["offsets"]), ptr(dp["perm_token"]), ptr(dp["slot_row"]),
                                None if fused else ptr(dp["x_perm"]), ptr(self.ws), self.ws.numel())
@@ -1005,6 +1341,12 @@ class LayerForward:
             self._ffn_args, self._gate_up_args = self._ffn_args[:-2], self._gate_up_args[:-2]
             self._down_args = (dtype, G, rows, d, f, ptr(dp["offsets"]), None, 0, ptr(b["h"]), ptr(w["w_down"]),
                                ptr(b["y"]))
+        if self.w8:  # (.., a, a8, ..)
+            names = ["brownout_moe_w8_ffn", "brownout_moe_w8_gate_up", "brownout_moe_w8_matmul"]
+            self._ffn_args = (*self._ffn_args[:8], None, *self._ffn_args[8:])
+            self._gate_up_args = (*self._gate_up_args[:8], None, *self._gate_up_args[8:])
+            self._down_args = (dtype, G, rows, d, f, ptr(dp["offsets"]), None, 0, ptr(b["h"]), None, ptr(w["w_down"]),
+                               ptr(b["y"]), wsp, wsn)
         self._ffn_names = names
         self._ffn_calls = [getattr(lib, n) for n in names]
         self._a_at = 8 if fused else None  # where x's pointer goes in the fused argument lists
@@ -1020,6 +1362,13 @@ class LayerForward:
             self._shared_name, self._shared_at = "brownout_moe_w4_ffn", 8
             self._shared_args = (dtype, 1, T, d, fs, ptr(self.sh_offsets), None, 0, ptr(w["w_gate_sh"]),
                                  ptr(w["w_up_sh"]), ptr(w["w_down_sh"]), ptr(b["h_sh"]), ptr(b["y_sh"]))
+            self._shared_side_args = self._shared_args
+        elif desc.d_ff_shared and self.w8:
+            fs = desc.d_ff_shared
+            self._shared_name, self._shared_at = "brownout_moe_w8_ffn", 8
+            self._shared_args = (dtype, 1, T, d, fs, ptr(self.sh_offsets), None, 0, None, ptr(w["w_gate_sh"]),
+                                 ptr(w["w_up_sh"]), ptr(w["w_down_sh"]), ptr(b["h_sh"]), ptr(b["y_sh"]),
+                                 ptr(self.shared_ws), self.shared_ws.numel())
             self._shared_side_args = self._shared_args
         elif desc.d_ff_shared:
             fs = desc.d_ff_shared
@@ -1057,6 +1406,15 @@ class LayerForward:
                                                self._x(x), *self._dispatch_args, self._s(stream)),
                "brownout_moe_dispatch")
         return self.bufs["dispatch"]
+
+    def balance(self, valid: Optional[torch.Tensor] = None, *, groups: bool = False, stream=None):
+        """How evenly the last forward's picks fall on the experts, or (groups) on the layer's united experts: the
+        module's balance over the layer's own logits and picks, into bufs["balance"]."""
+        if "balance" not in self.bufs:
+            raise ValueError("balance needs a layer made with balance=True")
+        r, over = self.bufs["route"], {"e2g": self.w["e2g"], "G": self.desc.G} if groups else {}
+        return balance(r["logits"], r["topk_idx"], valid=valid, out=self.bufs["balance"], workspace=self._balance_ws,
+                       stream=stream, **over)
 
     def _fused_args(self, args, x):
         if x is None:

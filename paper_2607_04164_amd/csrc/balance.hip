@@ -1,0 +1,350 @@
+// How evenly the router's picks fall on the experts (or on their groups), and what to change in the logits:
+//   p_t = softmax(z_t), lse_t = log sum exp z_t;  over the V tokens that count:
+//   c_e = picks of expert e,  P_e = mean of p_te,  F_r = (sum of c_e over group r) / (k V)
+//   balance = G sum_e F_g(e) P_e,   z loss = mean of lse_t^2
+//   dz_te = b G / V p_te (F_g(e) - sum_j F_g(j) p_tj) + a 2 / V lse_t p_te      (the counts are constants)
+//
+// S lanes of a wave hold a token's row (lane s: experts s, s + S, ..), so a wave takes 64 / S neighbouring rows at a
+// time and a row's maximum and sums are register permutations. A lane keeps the sums of p of its experts over its
+// tokens; a workgroup's sums meet in LDS in wave order, the workgroups' in a second launch in 64 bits: no float
+// atomics, so results do not depend on the order of anything. Up to kOneGroup tokens one workgroup does it all.
+#include "bmoe_common.h"
+
+namespace bmoe {
+namespace {
+
+constexpr int kThreads = 1024;  // of the forward's workgroups
+constexpr int kWaves = kThreads / 64;
+constexpr int kMaxGroups = 256;  // workgroups of the forward, at most
+constexpr int kOneGroup = 512;   // tokens one workgroup takes by itself
+constexpr int kGradThreads = 256;
+
+// sum / maximum over the S lanes of a token, the same bits in each of them
+template <int CTRL>
+__device__ __forceinline__ float permuted(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int S, typename OP>
+__device__ __forceinline__ float over_lanes(float v, OP op) {
+    static_assert(S == 4 || S == 16, "lanes of a token");
+    v = op(v, permuted<0xb1>(v));  // xor 1
+    v = op(v, permuted<0x4e>(v));  // xor 2
+    if constexpr (S == 16) {
+        v = op(v, permuted<0x141>(v));  // half-row mirror
+        v = op(v, permuted<0x140>(v));  // row mirror
+    }
+    return v;
+}
+
+// e^x for x <= 0: exp2 of the rounded product, corrected by what the rounding left out
+__device__ __forceinline__ float exp_neg(float x) {
+    x = x < -104.f ? -104.f : x;  // (0 in fp32; a comparison, so that NaN stays)
+    constexpr float L = 1.44269504f, L2 = 1.92596303e-8f;  // log2(e), and the rest of it
+    const float t = x * L, r = fmaf(x, L2, fmaf(x, L, -t));
+    const float e = __builtin_amdgcn_exp2f(t);
+    return fmaf(e, r * 0.693147182f, e);
+}
+
+// A row's logits to its probabilities; the row's log sum exp. Rows of nothing but -infinity: zeros.
+template <int S, int V>
+__device__ __forceinline__ float softmax_row(float (&z)[V]) {
+    float m = z[0];
+#pragma unroll
+    for (int v = 1; v < V; ++v) m = fmaxf(m, z[v]);
+    m = over_lanes<S>(m, [](float a, float b) { return fmaxf(a, b); });
+    const float top = m == -__builtin_inff() ? 0.f : m;
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        z[v] = exp_neg(z[v] - top);
+        sum += z[v];
+    }
+    sum = over_lanes<S>(sum, [](float a, float b) { return a + b; });
+    if (sum == 0.f) return 0.f;
+    const float inv = 1.f / sum;
+#pragma unroll
+    for (int v = 0; v < V; ++v) z[v] *= inv;
+    return top + logf(sum);
+}
+
+// the logits of token t that lane s holds; past E, and for tokens that do not count, -infinity
+template <int S, int V>
+__device__ __forceinline__ void load_logits(float (&z)[V], const float* logits, int64_t t, int s, int E, bool on) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int e = s + S * v;
+        z[v] = on && e < E ? logits[t * E + e] : -__builtin_inff();
+    }
+}
+
+// ---- the losses from the sums over all tokens
+
+struct Sums {
+    double p[BMOE_MAX_EXPERTS];  // of p_te
+    int c[BMOE_MAX_EXPERTS + 1]; // picks; the last: tokens that count
+    double z;                    // of lse^2
+    // work of finish()
+    int group[BMOE_MAX_EXPERTS];
+    double part[kWaves];
+};
+
+// Ends a call: every thread of one workgroup of kThreads, s complete (a barrier behind it).
+__device__ __forceinline__ void finish(const BalanceArgs& a, Sums& s) {
+    const int tid = threadIdx.x, E = a.E;
+    for (int r = tid; r < BMOE_MAX_EXPERTS; r += kThreads) s.group[r] = 0;
+    __syncthreads();
+    const int n = s.c[E];
+    const double V = n > 0 ? (double)n : 1.0;
+    int g = -1;
+    if (tid < E) {
+        g = a.e2g ? a.e2g[tid] : tid;
+        if (g < 0 || g >= a.G) g = -1;  // of no group
+        else atomicAdd(&s.group[g], s.c[tid]);
+        a.counts[tid] = s.c[tid];
+        a.prob[tid] = (float)(s.p[tid] / V);
+    }
+    __syncthreads();
+    double sum = g >= 0 ? (double)s.group[g] / ((double)a.k * V) * (s.p[tid] / V) : 0.0;
+#pragma unroll
+    for (int off = 32; off; off >>= 1) sum += __shfl_xor(sum, off);
+    if ((tid & 63) == 0) s.part[tid >> 6] = sum;
+    __syncthreads();
+    if (tid == 0) {
+        sum = 0.0;
+        for (int w = 0; w < BMOE_MAX_EXPERTS / 64; ++w) sum += s.part[w];
+        a.losses[0] = (float)((double)a.G * sum);
+        a.losses[1] = (float)(s.z / V);
+        a.counts[E] = n;
+    }
+}
+
+// A workgroup's sums in the workspace: z [groups] double, p [groups, E] float, c [groups, E + 1] int32
+struct Parts {
+    double* z;
+    float* p;
+    int* c;
+};
+__host__ __device__ inline Parts parts_of(void* ws, int groups, int E) {
+    Parts q;
+    q.z = (double*)ws;
+    q.p = (float*)(q.z + groups);
+    q.c = (int*)(q.p + (size_t)groups * E);
+    return q;
+}
+
+template <int S, int V>
+__global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
+    constexpr int PER = 64 / S;  // tokens of a wave at a time
+    __shared__ float s_p[kWaves][S * V];
+    __shared__ float s_z[kWaves];
+    __shared__ Sums sums;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int E = a.E, k = a.k, s = lane % S;
+    for (int e = tid; e <= E; e += kThreads) sums.c[e] = 0;
+    __syncthreads();
+    float p[V], z2 = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) p[v] = 0.f;
+    const int64_t step = (int64_t)gridDim.x * kWaves * PER;
+    int64_t t = ((int64_t)blockIdx.x * kWaves + wave) * PER + lane / S;
+    auto counts_token = [&](int64_t i) { return i < a.T && (!a.valid || a.valid[i] != 0); };
+    float next[V];
+    bool on = counts_token(t);
+    load_logits<S, V>(next, a.logits, t, s, E, on);
+    // (the lanes of a wave stay together: the permutations read their neighbours)
+    for (; __any(t < a.T); t += step) {
+        float z[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) z[v] = next[v];
+        const bool now = on;
+        if (now) {
+            for (int i = s; i < k; i += S) {
+                const int e = a.topk_idx[t * k + i];
+                if (e >= 0 && e < E) atomicAdd(&sums.c[e], 1);
+            }
+            if (s == 0) atomicAdd(&sums.c[E], 1);
+        }
+        on = counts_token(t + step);
+        load_logits<S, V>(next, a.logits, t + step, s, E, on);
+        const float lse = softmax_row<S, V>(z);
+        if (now) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) p[v] += z[v];
+            z2 = fmaf(lse, lse, z2);
+        }
+    }
+    // the wave's tokens, then the waves in order
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+#pragma unroll
+        for (int off = S; off < 64; off *= 2) p[v] += __shfl_xor(p[v], off);
+        if (lane < S) s_p[wave][s + S * v] = p[v];
+    }
+#pragma unroll
+    for (int off = S; off < 64; off *= 2) z2 += __shfl_xor(z2, off);
+    if (lane == 0) s_z[wave] = z2;
+    __syncthreads();
+    const int groups = gridDim.x;
+    const Parts q = parts_of(a.ws, groups, E);
+    if (tid < E) {
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) sum += s_p[w][tid];
+        if (groups == 1) sums.p[tid] = (double)sum;
+        else q.p[(size_t)blockIdx.x * E + tid] = sum;
+    }
+    if (groups > 1 && tid <= E) q.c[(size_t)blockIdx.x * (E + 1) + tid] = sums.c[tid];
+    if (tid == 0) {
+        double sum = 0.0;
+        for (int w = 0; w < kWaves; ++w) sum += (double)s_z[w];
+        if (groups == 1) sums.z = sum;
+        else q.z[blockIdx.x] = sum;
+    }
+    if (groups > 1) return;
+    __syncthreads();
+    finish(a, sums);
+}
+
+// The workgroups' sums, in order. ep: a power of two, E or more.
+__global__ __launch_bounds__(kThreads) void balance_join_kernel(BalanceArgs a, int groups, int ep) {
+    __shared__ Sums sums;
+    __shared__ double s_p[kThreads];
+    __shared__ int s_c[kThreads];
+    const int tid = threadIdx.x, E = a.E, e = tid % ep, j = tid / ep, J = kThreads / ep;
+    const Parts q = parts_of(a.ws, groups, E);
+    double p = 0.0;
+    int c = 0;
+    if (e < E)
+#pragma unroll 8
+        for (int g = j; g < groups; g += J) {
+            p += (double)q.p[(size_t)g * E + e];
+            c += q.c[(size_t)g * (E + 1) + e];
+        }
+    s_p[tid] = p;
+    s_c[tid] = c;
+    // tokens that count, and the z loss: the first wave
+    int n = 0;
+    double z = 0.0;
+    if (tid < 64) {
+        for (int g = tid; g < groups; g += 64) {
+            n += q.c[(size_t)g * (E + 1) + E];
+            z += q.z[g];
+        }
+#pragma unroll
+        for (int off = 32; off; off >>= 1) {
+            n += __shfl_xor(n, off);
+            z += __shfl_xor(z, off);
+        }
+    }
+    __syncthreads();
+    if (tid < E) {  // (e == tid)
+        for (int i = 1; i < J; ++i) {
+            p += s_p[i * ep + tid];
+            c += s_c[i * ep + tid];
+        }
+        sums.p[tid] = p;
+        sums.c[tid] = c;
+    }
+    if (tid == 0) {
+        sums.c[E] = n;
+        sums.z = z;
+    }
+    __syncthreads();
+    finish(a, sums);
+}
+
+template <int S, int V>
+__global__ __launch_bounds__(kGradThreads) void balance_grad_kernel(BalanceGradArgs a) {
+    constexpr int PER = 64 / S;
+    __shared__ int s_group[BMOE_MAX_EXPERTS];
+    __shared__ float s_f[S * V];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, s = lane % S, E = a.E;
+    const int n = a.counts[E];
+    const double V_ = n > 0 ? (double)n : 1.0;
+    // the losses' slopes by p (balance) and by lse^2, of every expert
+    const double b = (double)a.d_losses[0] / V_;
+    const float zc = (float)(2.0 * (double)a.d_losses[1] / V_);
+    for (int r = tid; r < BMOE_MAX_EXPERTS; r += kGradThreads) s_group[r] = 0;
+    __syncthreads();
+    int g = -1;
+    if (tid < E) {
+        g = a.e2g ? a.e2g[tid] : tid;
+        if (g < 0 || g >= a.G) g = -1;
+        else atomicAdd(&s_group[g], a.counts[tid]);
+    }
+    __syncthreads();
+    if (tid < S * V)
+        s_f[tid] = g >= 0 ? (float)(b * (double)a.G * (double)s_group[g] / ((double)a.k * V_)) : 0.f;
+    __syncthreads();
+    float f[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) f[v] = s_f[s + S * v];
+    const int64_t step = (int64_t)gridDim.x * (kGradThreads / 64) * PER;
+    for (int64_t t = ((int64_t)blockIdx.x * (kGradThreads / 64) + wave) * PER + lane / S; __any(t < a.T); t += step) {
+        const bool in = t < a.T, on = in && (!a.valid || a.valid[t] != 0);
+        float z[V];
+        load_logits<S, V>(z, a.logits, t, s, E, on);
+        const float lse = softmax_row<S, V>(z);
+        float dot = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) dot = fmaf(f[v], z[v], dot);
+        dot = over_lanes<S>(dot, [](float x, float y) { return x + y; });
+        const float c = fmaf(zc, lse, -dot);
+        if (in) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int e = s + S * v;
+                if (e < E) a.d_logits[t * E + e] = on ? z[v] * (f[v] + c) : 0.f;
+            }
+        }
+    }
+}
+
+int forward_groups(int T, int E) {
+    if (T <= kOneGroup) return 1;
+    const int per = kWaves * (E <= 16 ? 16 : 4);  // tokens of a workgroup at a time
+    return (int)min((int64_t)kMaxGroups, ceil_div64(T, per));
+}
+
+template <int S, int V>
+hipError_t forward(const BalanceArgs& a, hipStream_t s) {
+    const int groups = forward_groups(a.T, a.E);
+    hipLaunchKernelGGL((balance_kernel<S, V>), dim3(groups), dim3(kThreads), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || groups == 1) return e;
+    int ep = 64;  // (fewer would leave one thread many sums to add)
+    while (ep < a.E) ep *= 2;
+    hipLaunchKernelGGL(balance_join_kernel, dim3(1), dim3(kThreads), 0, s, a, groups, ep);
+    return hipGetLastError();
+}
+
+template <int S, int V>
+hipError_t gradient(const BalanceGradArgs& a, hipStream_t s) {
+    const int64_t per = (kGradThreads / 64) * (64 / S);
+    const int blocks = (int)min((int64_t)2048, ceil_div64(a.T, per));
+    hipLaunchKernelGGL((balance_grad_kernel<S, V>), dim3(blocks), dim3(kGradThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t balance_ws_bytes(int T, int E) {
+    const size_t g = forward_groups(T, E);
+    return g == 1 ? 0 : g * (8 + 4 * (size_t)E + 4 * (size_t)(E + 1));
+}
+
+hipError_t launch_balance(const BalanceArgs& a, hipStream_t s) {
+    if (a.E <= 16) return forward<4, 4>(a, s);
+    if (a.E <= 64) return forward<16, 4>(a, s);
+    if (a.E <= 128) return forward<16, 8>(a, s);
+    return forward<16, 16>(a, s);
+}
+
+hipError_t launch_balance_grad(const BalanceGradArgs& a, hipStream_t s) {
+    if (a.E <= 16) return gradient<4, 4>(a, s);
+    if (a.E <= 64) return gradient<16, 4>(a, s);
+    if (a.E <= 128) return gradient<16, 8>(a, s);
+    return gradient<16, 16>(a, s);
+}
+
+}  // namespace bmoe

@@ -48,6 +48,93 @@ bmoe_status w4_check(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t N, 
     return BMOE_OK;
 }
 
+constexpr int32_t kW8MaxRows = 1 << 30;
+
+inline size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+// rows of K values in 8 bits: the codes, then the scales
+inline size_t w8_codes_bytes(int64_t rows, int K) { return up256((size_t)rows * w8_pitch(K)); }
+inline size_t w8_rows_bytes(int64_t rows, int K) { return w8_codes_bytes(rows, K) + up256((size_t)rows * 4); }
+
+// One grouped product in 8 bits (w1: the second matrix of a gated one, or nullptr). a, a8: its input, one of them.
+bmoe_status w8_check(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t N, int32_t K, const int32_t* offsets,
+                     const int32_t* a_rows, int32_t a_count, const void* a, const bmoe_w8* a8, const bmoe_w8* w0,
+                     const bmoe_w8* w1, const void* c) {
+    if (dtype != BMOE_BF16) return BMOE_ERR_UNSUPPORTED;
+    if (n_seg < 1 || n_seg > BMOE_MAX_EXPERTS || rows_cap < 0 || rows_cap > kW8MaxRows) return BMOE_ERR_SHAPE;
+    if (N < 8 || N % 8 != 0 || N > (1 << 20) || K < 8 || K % 8 != 0 || K > BMOE_W8_MAX_K) return BMOE_ERR_SHAPE;
+    if (rows_cap == 0) return BMOE_OK;
+    if (!offsets || (!a && !a8) || !w0 || !c) return BMOE_ERR_NULL;
+    if (a && a8) return BMOE_ERR_UNSUPPORTED;
+    // (the copies address a gathered source with 32-bit byte offsets)
+    if (a_rows && (a_count < 1 || a_count > kW8MaxRows || a_count * w8_pitch(K) >= ((int64_t)1 << 32)))
+        return BMOE_ERR_SHAPE;
+    for (const bmoe_w8* w : {a8, w0, w1}) {
+        if (!w) continue;
+        if (!w->codes || !w->scales) return BMOE_ERR_NULL;
+        if (!aligned16(w->codes) || !aligned16(w->scales)) return BMOE_ERR_ALIGN;
+    }
+    if (!aligned16(a) || !aligned16(c)) return BMOE_ERR_ALIGN;
+    const size_t out = (size_t)rows_cap * N * 2;
+    const int64_t rows = a_rows ? a_count : rows_cap;
+    if (a8 ? shares(c, out, a8->codes, (size_t)rows * w8_pitch(K)) || shares(c, out, a8->scales, (size_t)rows * 4)
+           : shares(c, out, a, (size_t)rows * K * 2))
+        return BMOE_ERR_UNSUPPORTED;
+    return BMOE_OK;
+}
+
+// a [rows, K] rounded into the workspace
+hipError_t w8_rounded(const void* a, int64_t rows, int K, void* ws, bmoe_w8& out, hipStream_t s,
+                      const int32_t* offsets = nullptr, int n_seg = 0) {
+    int8_t* codes = (int8_t*)ws;
+    float* scales = (float*)(codes + w8_codes_bytes(rows, K));
+    out = bmoe_w8{codes, scales};
+    W8QuantizeArgs q{a, codes, scales, rows, K, BMOE_BF16};
+    q.offsets = offsets;
+    q.n_seg = n_seg;
+    return launch_w8_quantize(q, s);
+}
+
+// The products of a checked call: part 1 up (or the only one), 2 down, 3 both
+struct W8Call {
+    int32_t n_seg, rows_cap, d, d_ff;
+    const int32_t* offsets;
+    const int32_t* a_rows;
+    int32_t a_count;
+    const void* a;
+    const bmoe_w8 *a8, *w_gate, *w_up, *w_down;
+    void *h, *y, *ws;
+    size_t ws_bytes;
+    hipStream_t s;
+};
+
+bmoe_status w8_run(const W8Call& c) {
+    const int64_t rows = c.a_rows ? c.a_count : c.rows_cap;
+    const size_t need = bmoe_w8_workspace_bytes(c.a8 ? 0 : (int32_t)rows, c.d, c.rows_cap, c.w_down ? c.d_ff : 0, 0);
+    if (need > 0 && !c.ws) return BMOE_ERR_WORKSPACE;
+    if (c.ws_bytes < need) return BMOE_ERR_WORKSPACE;
+    if ((uintptr_t)c.ws & 255u) return BMOE_ERR_ALIGN;
+    char* ws = (char*)c.ws;
+    const bool split = c.ws && c.ws_bytes - need >= ffn_workspace_bytes();
+    W8GemmArgs g{c.offsets, c.a_rows, c.a_count, {}, *c.w_gate, c.w_up ? *c.w_up : bmoe_w8{nullptr, nullptr}, c.h,
+                 split ? ws + need : nullptr, split ? c.ws_bytes - need : 0, c.n_seg, c.rows_cap, c.d_ff, c.d};
+    hipError_t e = hipSuccess;
+    if (c.a8) g.a = *c.a8;
+    else e = w8_rounded(c.a, rows, c.d, ws, g.a, c.s);
+    if (e == hipSuccess) e = launch_w8_gemm(g, c.s);
+    if (e != hipSuccess || !c.w_down) return e == hipSuccess ? BMOE_OK : BMOE_ERR_HIP;
+    // (in the place of a's rows, which the product before has read)
+    e = w8_rounded(c.h, c.rows_cap, c.d_ff, ws, g.a, c.s, c.offsets, c.n_seg);
+    g.a_rows = nullptr;
+    g.a_count = 0;
+    g.w0 = *c.w_down;
+    g.w1 = bmoe_w8{nullptr, nullptr};
+    g.c = c.y;
+    g.N = c.d;
+    g.K = c.d_ff;
+    if (e == hipSuccess) e = launch_w8_gemm(g, c.s);
+    return e == hipSuccess ? BMOE_OK : BMOE_ERR_HIP;
+}
+
 inline bmoe_status hip_status(hipError_t e) { return e == hipSuccess ? BMOE_OK : BMOE_ERR_HIP; }
 
 }  // namespace
@@ -420,6 +507,123 @@ bmoe_status brownout_moe_w4_ffn(int32_t dtype, int32_t n_seg, int32_t rows_cap, 
     if (e != hipSuccess) return BMOE_ERR_HIP;
     return hip_status(bmoe::launch_w4_gemm(
         bmoe::W4GemmArgs{offsets, nullptr, 0, h, w_down, nullptr, y, n_seg, rows_cap, d, d_ff}, (hipStream_t)stream));
+}
+
+bmoe_status brownout_moe_w8_quantize(int32_t dtype, int32_t rows, int32_t K, const void* x, int8_t* codes,
+                                     float* scales, void* stream) {
+    if (dtype != BMOE_F32 && dtype != BMOE_BF16) return BMOE_ERR_UNSUPPORTED;
+    if (rows < 0 || rows > kW8MaxRows || K < 8 || K % 8 != 0 || K > BMOE_W8_MAX_K) return BMOE_ERR_SHAPE;
+    if (rows == 0) return BMOE_OK;
+    if (!x || !codes || !scales) return BMOE_ERR_NULL;
+    if (!aligned16(x) || !aligned16(codes) || !aligned16(scales)) return BMOE_ERR_ALIGN;
+    const size_t in = (size_t)rows * K * elem_bytes(dtype), out = (size_t)rows * w8_pitch(K);
+    if (shares(codes, out, x, in) || shares(scales, (size_t)rows * 4, x, in) ||
+        shares(scales, (size_t)rows * 4, codes, out))
+        return BMOE_ERR_UNSUPPORTED;
+    return hip_status(bmoe::launch_w8_quantize(bmoe::W8QuantizeArgs{x, codes, scales, rows, K, dtype},
+                                               (hipStream_t)stream));
+}
+
+size_t bmoe_w8_workspace_bytes(int32_t a_count, int32_t K, int32_t rows_cap, int32_t d_ff, int32_t split) {
+    if (a_count < 0 || a_count > kW8MaxRows || rows_cap < 0 || rows_cap > kW8MaxRows || K < 8 || K > BMOE_W8_MAX_K ||
+        d_ff < 0 || d_ff > BMOE_W8_MAX_K)
+        return 0;
+    const size_t a = a_count ? w8_rows_bytes(a_count, K) : 0, h = d_ff && rows_cap ? w8_rows_bytes(rows_cap, d_ff) : 0;
+    return (a > h ? a : h) + (split ? ffn_workspace_bytes() : 0);
+}
+
+bmoe_status brownout_moe_w8_matmul(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t N, int32_t K,
+                                   const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,
+                                   const bmoe_w8* a8, const bmoe_w8* w, void* y, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+    const bmoe_status st = w8_check(dtype, n_seg, rows_cap, N, K, offsets, a_rows, a_count, a, a8, w, nullptr, y);
+    if (st != BMOE_OK || rows_cap == 0) return st;
+    return w8_run(W8Call{n_seg, rows_cap, K, N, offsets, a_rows, a_count, a, a8, w, nullptr, nullptr, y, nullptr,
+                         workspace, workspace_bytes, (hipStream_t)stream});
+}
+
+bmoe_status brownout_moe_w8_gate_up(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t d, int32_t d_ff,
+                                    const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,
+                                    const bmoe_w8* a8, const bmoe_w8* w_gate, const bmoe_w8* w_up, void* h,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+    if (rows_cap > 0 && !w_up) return BMOE_ERR_NULL;
+    const bmoe_status st = w8_check(dtype, n_seg, rows_cap, d_ff, d, offsets, a_rows, a_count, a, a8, w_gate, w_up, h);
+    if (st != BMOE_OK || rows_cap == 0) return st;
+    return w8_run(W8Call{n_seg, rows_cap, d, d_ff, offsets, a_rows, a_count, a, a8, w_gate, w_up, nullptr, h, nullptr,
+                         workspace, workspace_bytes, (hipStream_t)stream});
+}
+
+bmoe_status brownout_moe_w8_ffn(int32_t dtype, int32_t n_seg, int32_t rows_cap, int32_t d, int32_t d_ff,
+                                const int32_t* offsets, const int32_t* a_rows, int32_t a_count, const void* a,
+                                const bmoe_w8* a8, const bmoe_w8* w_gate, const bmoe_w8* w_up, const bmoe_w8* w_down,
+                                void* h, void* y, void* workspace, size_t workspace_bytes, void* stream) {
+    if (rows_cap > 0 && (!w_up || !w_down)) return BMOE_ERR_NULL;
+    bmoe_status st = w8_check(dtype, n_seg, rows_cap, d_ff, d, offsets, a_rows, a_count, a, a8, w_gate, w_up, h);
+    // (the down product's input is h)
+    if (st == BMOE_OK) st = w8_check(dtype, n_seg, rows_cap, d, d_ff, offsets, nullptr, 0, h, nullptr, w_down, nullptr, y);
+    if (st != BMOE_OK || rows_cap == 0) return st;
+    return w8_run(W8Call{n_seg, rows_cap, d, d_ff, offsets, a_rows, a_count, a, a8, w_gate, w_up, w_down, h, y,
+                         workspace, workspace_bytes, (hipStream_t)stream});
+}
+
+size_t bmoe_balance_workspace_bytes(int32_t T, int32_t E) {
+    return T < 1 || E < 1 || E > BMOE_MAX_EXPERTS ? 0 : balance_ws_bytes(T, E);
+}
+
+}  // extern "C"
+
+namespace {
+bmoe_status balance_check(int32_t T, int32_t E, int32_t k, int32_t G, const int32_t* e2g) {
+    if (T < 0 || E < 1 || E > BMOE_MAX_EXPERTS || k < 1 || k > BMOE_MAX_TOPK || G < 1 || G > BMOE_MAX_EXPERTS)
+        return BMOE_ERR_SHAPE;
+    if ((int64_t)T * k > INT_MAX / 2 || (!e2g && G != E)) return BMOE_ERR_SHAPE;
+    return BMOE_OK;
+}
+inline bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+}  // namespace
+
+extern "C" {
+
+bmoe_status brownout_moe_balance(int32_t T, int32_t E, int32_t k, int32_t G, const float* logits,
+                                 const int32_t* topk_idx, const uint8_t* valid, const int32_t* e2g, float* losses,
+                                 int32_t* counts, float* prob, void* workspace, size_t workspace_bytes, void* stream) {
+    const bmoe_status st = balance_check(T, E, k, G, e2g);
+    if (st != BMOE_OK || T == 0) return st;
+    if (!logits || !topk_idx || !losses || !counts || !prob) return BMOE_ERR_NULL;
+    for (const void* p : {(const void*)logits, (const void*)topk_idx, (const void*)e2g, (const void*)losses,
+                          (const void*)counts, (const void*)prob})
+        if (!aligned4(p)) return BMOE_ERR_ALIGN;
+    const size_t need = balance_ws_bytes(T, E), sizes[3] = {8, 4 * (size_t)E + 4, 4 * (size_t)E};
+    if (need > 0 && (!workspace || workspace_bytes < need)) return BMOE_ERR_WORKSPACE;
+    if (need > 0 && ((uintptr_t)workspace & 7u)) return BMOE_ERR_ALIGN;
+    const void* outs[3] = {losses, counts, prob};
+    for (int i = 0; i < 3; ++i) {  // (other workgroups still read the inputs)
+        if (shares(outs[i], sizes[i], logits, (size_t)T * E * 4) || shares(outs[i], sizes[i], topk_idx, (size_t)T * k * 4) ||
+            shares(outs[i], sizes[i], valid, (size_t)T) || shares(outs[i], sizes[i], e2g, (size_t)E * 4))
+            return BMOE_ERR_UNSUPPORTED;
+        for (int j = 0; j < i; ++j)
+            if (shares(outs[i], sizes[i], outs[j], sizes[j])) return BMOE_ERR_UNSUPPORTED;
+    }
+    return hip_status(bmoe::launch_balance(
+        bmoe::BalanceArgs{logits, topk_idx, valid, e2g, losses, counts, prob, workspace, T, E, k, G}, (hipStream_t)stream));
+}
+
+bmoe_status brownout_moe_balance_grad(int32_t T, int32_t E, int32_t k, int32_t G, const float* logits,
+                                      const uint8_t* valid, const int32_t* e2g, const int32_t* counts,
+                                      const float* d_losses, float* d_logits, void* stream) {
+    const bmoe_status st = balance_check(T, E, k, G, e2g);
+    if (st != BMOE_OK || T == 0) return st;
+    if (!logits || !counts || !d_losses || !d_logits) return BMOE_ERR_NULL;
+    for (const void* p : {(const void*)logits, (const void*)e2g, (const void*)counts, (const void*)d_losses,
+                          (const void*)d_logits})
+        if (!aligned4(p)) return BMOE_ERR_ALIGN;
+    const size_t all = (size_t)T * E * 4;
+    if ((d_logits != logits && shares(d_logits, all, logits, all)) || shares(d_logits, all, valid, (size_t)T) ||
+        shares(d_logits, all, e2g, (size_t)E * 4) || shares(d_logits, all, counts, (size_t)E * 4 + 4) ||
+        shares(d_logits, all, d_losses, 8))
+        return BMOE_ERR_UNSUPPORTED;
+    return hip_status(bmoe::launch_balance_grad(
+        bmoe::BalanceGradArgs{logits, valid, e2g, counts, d_losses, d_logits, T, E, k, G}, (hipStream_t)stream));
 }
 
 bmoe_status brownout_moe_few(const bmoe_desc* d, const bmoe_few_weights* w, const void* x, int32_t* topk_idx,

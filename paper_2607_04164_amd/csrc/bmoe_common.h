@@ -61,6 +61,49 @@ __device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, f32x16 
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
 }
 
+// 16x16x64 and 32x32x32 int8 MFMA: a lane's 16 bytes of an operand are 16 k-values, elsewhere the
+// layout is that of the bf16 ones above; sums in int32.
+typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
+typedef __attribute__((__vector_size__(16 * sizeof(int)))) int i32x16;
+
+// What the grouped GEMMs multiply: operand rows are rows of 16-bit units (a bf16 value, or two int8
+// values), and K counts those units, so copies, LDS and fragments are the same bytes for both.
+struct OpBf16 {
+    static constexpr bool kScales = false;
+    using acc = float;
+    using acc4 = f32x4;
+    using acc16 = f32x16;
+    template <typename V>
+    static __device__ __forceinline__ f32x4 mma16(const V& a, const V& b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                       0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mma32(const uint4& a, const uint4& b, f32x16 c) { return mfma32(a, b, c); }
+};
+// int8 values, a scale for each row of either operand
+struct OpI8 {
+    static constexpr bool kScales = true;
+    using acc = int;
+    using acc4 = i32x4;
+    using acc16 = i32x16;
+    template <typename V>
+    static __device__ __forceinline__ i32x4 mma16(const V& a, const V& b, i32x4 c) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0,
+                                                     0);
+    }
+    static __device__ __forceinline__ i32x16 mma32(const uint4& a, const uint4& b, i32x16 c) {
+        return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0,
+                                                     0);
+    }
+};
+
+// sum * a * b, the smaller scale first: |sum| >= 1 then neither under- nor overflows on the way to a
+// result that does not. A scale that is not a number makes the result one (fminf would drop it).
+__device__ __forceinline__ float scaled(int sum, float a, float b) {
+    const bool less = a < b;
+    return (float)sum * (less ? a : b) * (less ? b : a);
+}
+
 __host__ __device__ constexpr int ceil_div(int a, int b) { return (a + b - 1) / b; }
 __host__ __device__ constexpr int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -83,6 +126,15 @@ __device__ __forceinline__ void dma16s(const void* base, uint32_t voff, uint32_t
     const uint64_t ub = ((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32) |
                         (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
     asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(ub),
+                 "s"(__builtin_amdgcn_readfirstlane(lds_addr))
+                 : "memory", "m0");
+}
+// 4 bytes a lane, to LDS at M0 + 4 * lane
+__device__ __forceinline__ void dma4s(const void* base, uint32_t voff, uint32_t lds_addr) {
+    const uint64_t b = (uint64_t)(uintptr_t)base;
+    const uint64_t ub = ((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32) |
+                        (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
+    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1" ::"v"(voff), "s"(ub),
                  "s"(__builtin_amdgcn_readfirstlane(lds_addr))
                  : "memory", "m0");
 }
@@ -291,6 +343,61 @@ struct W4GemmArgs {
     int n_seg, rows_cap, N, K;
 };
 hipError_t launch_w4_gemm(const W4GemmArgs& a, hipStream_t s);
+
+// rows of codes [rows, w8_pitch(K)] and scales [rows] of x [rows, K]
+__host__ __device__ constexpr int64_t w8_pitch(int K) { return (int64_t)ceil_div(K, 128) * 128; }
+struct W8QuantizeArgs {
+    const void* x;
+    int8_t* codes;
+    float* scales;
+    int64_t rows;
+    int K, dtype;
+    // rows [offsets[0], offsets[n_seg]) only (device memory; nullptr: all)
+    const int32_t* offsets = nullptr;
+    int n_seg = 0;
+};
+hipError_t launch_w8_quantize(const W8QuantizeArgs& a, hipStream_t s);
+
+// c[row] = a[row] W^T, or silu(a Wg^T) * (a Wu^T) with w1; bf16 c
+struct W8GemmArgs {
+    const int32_t* offsets;
+    const int32_t* a_rows;  // or nullptr
+    int a_count;
+    bmoe_w8 a, w0, w1;  // w1.codes nullptr: one matrix
+    void* c;
+    void* ws;  // stream-K workspace, or nullptr
+    size_t ws_bytes;
+    int n_seg, rows_cap, N, K;
+};
+hipError_t launch_w8_gemm(const W8GemmArgs& a, hipStream_t s);
+// rows_cap of at most 64 rows a segment; false: the sizes are the large kernel's
+bool w8_skinny_fits(const W8GemmArgs& a);
+hipError_t launch_w8_skinny(const W8GemmArgs& a, hipStream_t s);
+
+struct BalanceArgs {
+    const float* logits;
+    const int32_t* topk_idx;
+    const uint8_t* valid;  // or nullptr
+    const int32_t* e2g;    // or nullptr (G == E)
+    float* losses;
+    int32_t* counts;
+    float* prob;
+    void* ws;
+    int T, E, k, G;
+};
+size_t balance_ws_bytes(int T, int E);
+hipError_t launch_balance(const BalanceArgs& a, hipStream_t s);
+
+struct BalanceGradArgs {
+    const float* logits;
+    const uint8_t* valid;
+    const int32_t* e2g;
+    const int32_t* counts;
+    const float* d_losses;
+    float* d_logits;
+    int T, E, k, G;
+};
+hipError_t launch_balance_grad(const BalanceGradArgs& a, hipStream_t s);
 
 struct FewArgs {
     bmoe_few_weights w;

@@ -42,6 +42,10 @@ struct GemmParams {
     const int32_t* a_rows = nullptr;  // gathered A: row r is A[a_rows[r]] (A has a_count rows)
     int a_count = 0;
     FoldArgs fold;  // combine folded into the down projection's epilogue (out == nullptr: not folded)
+    // int8 operands (K then counts pairs of values): scales of A's rows, and of the rows of B0 and B1 [n_seg, N]
+    const float* sa = nullptr;
+    const float* sb0 = nullptr;
+    const float* sb1 = nullptr;
 };
 
 // Register-staged tiles: BM 128 or 256 rows, 128 output columns of each of
@@ -341,8 +345,11 @@ constexpr int kSkSlotBytes = kSkPartBytes + 1280;
 
 // VAR: the kernel that also takes half tiles and a ragged last K-step (see
 // gemm_var_pays); the other one has neither.
-template <bool GATED, bool VAR = false>
+template <bool GATED, bool VAR = false, class OP_ = OpBf16>
 struct DmaCfg {
+    using OP = OP_;
+    using acc16 = typename OP::acc16;
+    using acc4 = typename OP::acc4;
     static constexpr bool kVar = VAR;
     static constexpr int BM = 256, BK = kDmaBK, KC = BK / 8;  // KC: 16-byte chunks per row
     static constexpr int SUB = BK / 16;                       // MFMA sub-steps per K-step
@@ -366,7 +373,9 @@ struct DmaCfg {
     static constexpr int STG_OFF = RING;
     static constexpr int SCHED_OFF = STG_OFF + 4 * HSTG;                 // schedule arrays after them
     static constexpr int SCHED = 2 * 4 * 8 + (4 * BMOE_MAX_EXPERTS + 1) * 4;
-    static constexpr int SMEM = SCHED_OFF + SCHED;
+    // int8: the scales of a tile's A rows and B rows, for this work item and the next
+    static constexpr int SCL_OFF = (SCHED_OFF + SCHED + 15) / 16 * 16, SCL = (BM + RB) * 4;
+    static constexpr int SMEM = OP::kScales ? SCL_OFF + 2 * SCL : SCHED_OFF + SCHED;
     static constexpr int CPR = WTN / 8;                                   // 16-byte chunks per output row
     static constexpr int NACC4 = NMAT * MB * NB * 4;                      // float4 accumulators per lane
     static_assert(KC == 8 && BM == 256 && RB == 256, "tile shape");
@@ -469,7 +478,7 @@ __device__ __forceinline__ void frag_read(uint4 (&ga)[C::MB], uint4 (&gb)[C::NMA
 // copies and the B copies). (Issuing a sub-step's copies after each of its
 // first MFMAs instead measured 1-3 % slower: the copies must be spread.)
 template <class C, int MB, int RD, int ND, int NA>
-__device__ __forceinline__ void mfmas_ops(f32x16 (&acc)[C::NMAT][C::MB][C::NB], const uint4 (&af)[C::MB],
+__device__ __forceinline__ void mfmas_ops(typename C::acc16 (&acc)[C::NMAT][C::MB][C::NB], const uint4 (&af)[C::MB],
                                           const uint4 (&bf)[C::NMAT][C::NB], uint4 (&ga1)[C::MB],
                                           uint4 (&gb1)[C::NMAT][C::NB], const char* st1, int kk1,
                                           uint4 (&ga2)[C::MB], uint4 (&gb2)[C::NMAT][C::NB], const char* st2,
@@ -480,7 +489,7 @@ __device__ __forceinline__ void mfmas_ops(f32x16 (&acc)[C::NMAT][C::MB][C::NB], 
 #pragma unroll
     for (int q = 0; q < NM; ++q) {
         const int mb = q / (C::NMAT * C::NB), mat = (q / C::NB) % C::NMAT, nb = q % C::NB;
-        acc[mat][mb][nb] = mfma32(af[mb], bf[mat][nb], acc[mat][mb][nb]);
+        acc[mat][mb][nb] = C::OP::mma32(af[mb], bf[mat][nb], acc[mat][mb][nb]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int r = q * RD * NR / NM; r < (q + 1) * RD * NR / NM; ++r) {
@@ -713,6 +722,19 @@ __device__ __forceinline__ void dma_sources(DmaSrc<C>& src, const GemmParams& p,
     }
 }
 
+// int8: the scales of the tile's A rows (wave w: rows 64 w ..) and B rows into lds (the next item's go there during
+// this one's last K-steps, so they cost the epilogue no load). A copy issued beside those of the K-steps only makes
+// their counted waits wait for more.
+template <class C, bool GATED>
+__device__ __forceinline__ void dma_scales(const GemmParams& p, const TileCoord& tc, uint32_t lds, int wave, int lane) {
+    const int r = wave * 64 + lane;
+    const int row = gathered_row(p.a_rows, p.a_count, min(tc.m0 + r, tc.m_end - 1));
+    dma4s(p.sa, (uint32_t)row * 4, lds + wave * 256);
+    const int bmat = GATED ? wave * 64 / C::BN : 0;
+    const int n = min(tc.n0 + r % C::BN, p.N - 1);
+    dma4s((bmat ? p.sb1 : p.sb0) + (size_t)tc.s * p.N, (uint32_t)n * 4, lds + C::BM * 4 + wave * 256);
+}
+
 // Columns of the last K-step when K is not whole K-steps (else 0). The copies
 // of that K-step repeat its first chunk in place of the chunks past the row's
 // end (which may be past the tensor's), and once they have landed the
@@ -781,9 +803,10 @@ enum { kAfterNone = 0, kAfterStores = 1 };
 // K-steps: items are whole tiles of at least three K-steps (launch_gemm_dma),
 // so the copies of the last one are issued here, not by the previous item.
 template <class C, bool GATED, int MB>
-__device__ __forceinline__ void tile_ksteps(f32x16 (&acc)[C::NMAT][C::MB][C::NB], DmaSrc<C>& src, char* smem,
+__device__ __forceinline__ void tile_ksteps(typename C::acc16 (&acc)[C::NMAT][C::MB][C::NB], DmaSrc<C>& src, char* smem,
                                             int ka, int kb, int wave, int lane, int after, int s0,
-                                            const GemmParams& p, const TileCoord& tc2, int nka, int nkb) {
+                                            const GemmParams& p, const TileCoord& tc2, int nka, int nkb,
+                                            uint32_t scl2) {
     const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
     const int wm = wave >> 1, wn = wave & 1;
     const int n = kb - ka, nn = nkb - nka;
@@ -852,7 +875,10 @@ __device__ __forceinline__ void tile_ksteps(f32x16 (&acc)[C::NMAT][C::MB][C::NB]
     // j = kt + 2 - n of the next item; where it has no such K-step (or there
     // is no next item) they copy one it (or this item) has into the free
     // slot, which nothing reads (one code path, no branch between K-steps)
-    if (nn > 0) dma_sources<C, GATED>(src, p, tc2, wave, lane);
+    if (nn > 0) {
+        dma_sources<C, GATED>(src, p, tc2, wave, lane);
+        if constexpr (C::OP::kScales) dma_scales<C, GATED>(p, tc2, scl2, wave, lane);
+    }
     for (; kt < n; ++kt) {
         const int j = kt + 2 - n;
         const int kj = nn > 0 ? nka + min(j, nn - 1) : ka;
@@ -868,7 +894,7 @@ __device__ __forceinline__ void tile_ksteps(f32x16 (&acc)[C::NMAT][C::MB][C::NB]
 }
 
 template <class C, int MB>
-__device__ __forceinline__ void zero_acc(f32x16 (&acc)[C::NMAT][C::MB][C::NB]) {
+__device__ __forceinline__ void zero_acc(typename C::acc16 (&acc)[C::NMAT][C::MB][C::NB]) {
 #pragma unroll
     for (int mat = 0; mat < C::NMAT; ++mat)
 #pragma unroll
@@ -876,14 +902,15 @@ __device__ __forceinline__ void zero_acc(f32x16 (&acc)[C::NMAT][C::MB][C::NB]) {
 #pragma unroll
             for (int nb = 0; nb < C::NB; ++nb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[mat][mb][nb][i] = 0.f;
+                for (int i = 0; i < 16; ++i) acc[mat][mb][nb][i] = 0;
 }
 
 // An accumulator moved out of its AGPR at the point of use (the compiler
 // otherwise copies every accumulator to VGPRs at once after the K loop and,
 // inside the persistent loop, spills to scratch).
-__device__ __forceinline__ float acc_read(float a) {
-    float v;
+template <typename A>
+__device__ __forceinline__ A acc_read(A a) {
+    A v;
     asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(a));
     return v;
 }
@@ -991,15 +1018,15 @@ __device__ __forceinline__ void fold_rows(const GemmParams& p, const TileCoord& 
 }
 
 template <class C, bool GATED, int MB, bool FOLD = false>
-__device__ __forceinline__ void store_tile(const f32x16 (&acc)[C::NMAT][C::MB][C::NB], const GemmParams& p,
-                                           const TileCoord& tc, char* smem, int wave, int lane,
+__device__ __forceinline__ void store_tile(const typename C::acc16 (&acc)[C::NMAT][C::MB][C::NB], const GemmParams& p,
+                                           const TileCoord& tc, char* smem, int wave, int lane, const char* scl,
                                            char* piece = nullptr) {
     const int wm = wave >> 1, wn = wave & 1;
     uint16_t* st = (uint16_t*)(smem + C::STG_OFF + wave * C::HSTG);
     const int l32 = lane & 31;
     const int row0 = tc.m0, col0 = tc.n0 + wn * C::WTN;
     if (MB == C::MB && piece) {  // (split tiles are whole)
-        float4* d = (float4*)piece;
+        typename C::acc4* d = (typename C::acc4*)piece;
 #pragma unroll
         for (int mb = 0; mb < C::MB; ++mb)
 #pragma unroll
@@ -1010,13 +1037,20 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[C::NMAT][C::MB][C
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
                         const int q = ((mat * C::MB + mb) * C::NB + nb) * 4 + i / 4;
-                        d[q * kGemmThreads + threadIdx.x] =
-                            make_float4(acc_read(acc[mat][mb][nb][i]), acc_read(acc[mat][mb][nb][i + 1]),
-                                        acc_read(acc[mat][mb][nb][i + 2]),
-                                        acc_read(acc[mat][mb][nb][i + 3]));
+                        d[q * kGemmThreads + threadIdx.x] = typename C::acc4{
+                            acc_read(acc[mat][mb][nb][i]), acc_read(acc[mat][mb][nb][i + 1]),
+                            acc_read(acc[mat][mb][nb][i + 2]), acc_read(acc[mat][mb][nb][i + 3])};
                     }
             }
         return;
+    }
+    float cs[C::NMAT][C::NB];  // int8: the scales of the lane's columns
+    if constexpr (C::OP::kScales) {
+#pragma unroll
+        for (int mat = 0; mat < C::NMAT; ++mat)
+#pragma unroll
+            for (int nb = 0; nb < C::NB; ++nb)
+                cs[mat][nb] = ((const float*)scl)[C::BM + mat * C::BN + wn * C::WTN + nb * 32 + l32];
     }
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
@@ -1029,16 +1063,27 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[C::NMAT][C::MB][C
             // the SiLU chains (exp, add, reciprocal, products) of different
             // elements overlap instead of running one after another
             float v[C::NB][8];
+            float4 rs[2];  // int8: the scales of the lane's eight rows
+            if constexpr (C::OP::kScales) {
+                const float* at = (const float*)scl + dma_arow(wm, mb, MB) + 16 * h + 4 * (lane >> 5);
+                rs[0] = *(const float4*)at;
+                rs[1] = *(const float4*)(at + 8);
+            }
+            auto value = [&](int mat, int nb, int e) -> float {
+                const auto a = acc_read(acc[mat][mb][nb][8 * h + e]);
+                if constexpr (C::OP::kScales) return scaled(a, ((const float*)&rs[e >> 2])[e & 3], cs[mat][nb]);
+                else return a;
+            };
 #pragma unroll
             for (int nb = 0; nb < C::NB; ++nb)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[nb][e] = acc_read(acc[0][mb][nb][8 * h + e]);
+                for (int e = 0; e < 8; ++e) v[nb][e] = value(0, nb, e);
             if constexpr (GATED) {
                 float u[C::NB][8], t[C::NB][8];
 #pragma unroll
                 for (int nb = 0; nb < C::NB; ++nb)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) u[nb][e] = acc_read(acc[1][mb][nb][8 * h + e]);
+                    for (int e = 0; e < 8; ++e) u[nb][e] = value(1, nb, e);
 #pragma unroll
                 for (int nb = 0; nb < C::NB; ++nb)
 #pragma unroll
@@ -1088,9 +1133,9 @@ __device__ __forceinline__ void store_tile(const f32x16 (&acc)[C::NMAT][C::MB][C
 
 // P = gridDim.x persistent workgroups (a multiple of 8); ws: the stream-K
 // workspace, or nullptr (tiles stay whole).
-template <bool GATED, bool VAR, bool FOLD = false>
+template <bool GATED, bool VAR, bool FOLD = false, class OP = OpBf16>
 __global__ __launch_bounds__(kGemmThreads, 1) void grouped_gemm_dma_kernel(GemmParams p, char* ws) {
-    using C = DmaCfg<GATED, VAR>;
+    using C = DmaCfg<GATED, VAR, OP>;
     __shared__ __align__(16) char smem[C::SMEM];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int P = gridDim.x;
@@ -1142,9 +1187,11 @@ __global__ __launch_bounds__(kGemmThreads, 1) void grouped_gemm_dma_kernel(GemmP
     next_item(L, ka, kb, slot);
     TileCoord tc;
     tc.half = 0;
+    int sb = 0;  // which half of the scales' area holds this item's
     if (L >= 0) {
         tc = tile_coord<C>(ts, p.n_seg, L);
         dma_sources<C, GATED>(src, p, tc, wave, lane);
+        if constexpr (OP::kScales) dma_scales<C, GATED>(p, tc, (uint32_t)(uintptr_t)smem + C::SCL_OFF, wave, lane);
         ksteps_prologue<C>(src, smem, ka, kb, wave);
     }
     int after = kAfterNone, s0 = 0;
@@ -1152,14 +1199,15 @@ __global__ __launch_bounds__(kGemmThreads, 1) void grouped_gemm_dma_kernel(GemmP
     auto items = [&](auto blocks) {
         constexpr int MB = decltype(blocks)::value;
         while (L >= 0 && (!VAR || (tc.half != 0) == (MB != C::MB))) {
-            f32x16 acc[C::NMAT][C::MB][C::NB];
+            typename C::acc16 acc[C::NMAT][C::MB][C::NB];
             zero_acc<C, MB>(acc);
             int L2, ka2, kb2, slot2;
             next_item(L2, ka2, kb2, slot2);
             TileCoord tc2 = tc;
             if (L2 >= 0) tc2 = tile_coord<C>(ts, p.n_seg, L2);
-            tile_ksteps<C, GATED, MB>(acc, src, smem, ka, kb, wave, lane, after, s0, p, tc2, ka2, L2 >= 0 ? kb2 : ka2);
-            store_tile<C, GATED, MB, FOLD>(acc, p, tc, smem, wave, lane,
+            tile_ksteps<C, GATED, MB>(acc, src, smem, ka, kb, wave, lane, after, s0, p, tc2, ka2, L2 >= 0 ? kb2 : ka2,
+                                      (uint32_t)(uintptr_t)smem + C::SCL_OFF + (sb ^ 1) * C::SCL);
+            store_tile<C, GATED, MB, FOLD>(acc, p, tc, smem, wave, lane, smem + C::SCL_OFF + sb * C::SCL,
                                            slot < 0 ? nullptr : ws + ((size_t)2 * pw + slot) * kSkSlotBytes);
             after = kAfterStores;
             s0 = (s0 + kb - ka) & 1;
@@ -1168,6 +1216,7 @@ __global__ __launch_bounds__(kGemmThreads, 1) void grouped_gemm_dma_kernel(GemmP
             kb = kb2;
             slot = slot2;
             tc = tc2;
+            sb ^= 1;
         }
     };
     if constexpr (VAR) {
@@ -1192,9 +1241,10 @@ __global__ __launch_bounds__(kGemmThreads, 1) void grouped_gemm_dma_kernel(GemmP
 constexpr int kFixSplit = 32;
 constexpr int kFixInflight = 8;
 
-template <bool GATED>
+template <bool GATED, class OP = OpBf16>
 __global__ __launch_bounds__(kGemmThreads) void gemm_fixup_kernel(GemmParams p, const char* ws, int P) {
-    using C = DmaCfg<GATED>;
+    using C = DmaCfg<GATED, false, OP>;
+    using acc4 = typename C::acc4;
     __shared__ __align__(16) char sched[C::SCHED];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     // the tile count first, by a plain sum: with nothing split every
@@ -1228,27 +1278,22 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_fixup_kernel(GemmParams p, 
         if (q >= (t + 1) * nk) continue;  // no boundary inside: computed whole
         const int p0 = t * nk / sk.share, p1 = ((t + 1) * nk - 1) / sk.share;
         const TileCoord tc = tile_coord<C>(ts, p.n_seg, sk.F * P + t);
-        float4 sum[QPER][C::NMAT];
+        acc4 sum[QPER][C::NMAT];
 #pragma unroll
         for (int k = 0; k < QPER; ++k)
 #pragma unroll
-            for (int mat = 0; mat < C::NMAT; ++mat) sum[k][mat] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int mat = 0; mat < C::NMAT; ++mat) sum[k][mat] = acc4{0, 0, 0, 0};
         auto piece = [&](int pw) {
             const int slot = pw * sk.share >= t * nk ? 0 : 1;  // share starts inside tile t, or ends in it
-            return (const float4*)(ws + ((size_t)2 * pw + slot) * kSkSlotBytes);
+            return (const acc4*)(ws + ((size_t)2 * pw + slot) * kSkSlotBytes);
         };
-        auto add = [&](float4& a, const float4& v) {
-            a.x += v.x;
-            a.y += v.y;
-            a.z += v.z;
-            a.w += v.w;
-        };
+        auto add = [&](acc4& a, const acc4& v) { a += v; };
         int pw = p0;
         for (; pw + kFixInflight - 1 <= p1; pw += kFixInflight) {
-            float4 v[kFixInflight][QPER][C::NMAT];
+            acc4 v[kFixInflight][QPER][C::NMAT];
 #pragma unroll
             for (int j = 0; j < kFixInflight; ++j) {
-                const float4* d = piece(pw + j);
+                const acc4* d = piece(pw + j);
 #pragma unroll
                 for (int k = 0; k < QPER; ++k)
 #pragma unroll
@@ -1263,7 +1308,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_fixup_kernel(GemmParams p, 
                     for (int mat = 0; mat < C::NMAT; ++mat) add(sum[k][mat], v[j][k][mat]);
         }
         for (; pw <= p1; ++pw) {
-            const float4* d = piece(pw);
+            const acc4* d = piece(pw);
 #pragma unroll
             for (int k = 0; k < QPER; ++k)
 #pragma unroll
@@ -1276,13 +1321,26 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_fixup_kernel(GemmParams p, 
             const int i4 = qq & 3, nb = (qq >> 2) % C::NB, mb = (qq >> 2) / C::NB;
             const int r0 = dma_arow(wm, mb, C::MB) + 8 * i4 + 4 * (lane >> 5);  // (split tiles are whole)
             const int gn = tc.n0 + wn * C::WTN + nb * 32 + (lane & 31);
-            const float g4[4] = {sum[k][0].x, sum[k][0].y, sum[k][0].z, sum[k][0].w};
-            const float4 u = sum[k][C::NMAT - 1];
-            const float u4[4] = {u.x, u.y, u.z, u.w};
+            const acc4 g4 = sum[k][0], u4 = sum[k][C::NMAT - 1];
+            float cs[2] = {1.f, 1.f};
+            if constexpr (OP::kScales) {
+                const size_t col = (size_t)tc.s * p.N + min(gn, p.N - 1);
+                cs[0] = p.sb0[col];
+                if (GATED) cs[1] = p.sb1[col];
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float v = GATED ? silu_mul(g4[j], u4[j]) : g4[j];
                 const int gm = tc.m0 + r0 + j;
+                float g, u;
+                if constexpr (OP::kScales) {
+                    const float rs = p.sa[gathered_row(p.a_rows, p.a_count, min(gm, tc.m_end - 1))];
+                    g = scaled(g4[j], rs, cs[0]);
+                    u = scaled(u4[j], rs, cs[1]);
+                } else {
+                    g = g4[j];
+                    u = u4[j];
+                }
+                const float v = GATED ? silu_mul(g, u) : g;
                 if (gm < tc.m_end && gn < p.N) p.C[(size_t)gm * p.N + gn] = (uint16_t)pack_bf16x2_hw(v, 0.f);
             }
         }
@@ -1326,7 +1384,7 @@ static bool gemm_var_pays(const GemmParams& g) {
     return g.K % kDmaBK != 0 || (int64_t)g.rows_cap < (int64_t)g.n_seg * kVarRows;
 }
 
-template <bool GATED>
+template <bool GATED, class OP = OpBf16>
 hipError_t launch_gemm_dma(const GemmParams& g0, void* ws, size_t ws_bytes, hipStream_t s) {
     using C = DmaCfg<GATED>;
     GemmParams g = g0;
@@ -1336,7 +1394,7 @@ hipError_t launch_gemm_dma(const GemmParams& g0, void* ws, size_t ws_bytes, hipS
     // the chip's, without the split (whose workspace has the device's size).
     const int cus = stream_k_workgroups();
     const int P = persistent_workgroups();
-    if constexpr (!GATED) {
+    if constexpr (!GATED && !OP::kScales) {
         if (g.fold.out != nullptr) {
             // the fold needs every tile whole (no stream-K pieces)
             if (g.K % C::BK != 0 || cus <= 0) return hipErrorInvalidValue;  // (ffn_can_fold)
@@ -1354,14 +1412,14 @@ hipError_t launch_gemm_dma(const GemmParams& g0, void* ws, size_t ws_bytes, hipS
     const bool can = g.K % C::BK == 0 && (int64_t)(P - 1) * (g.K / C::BK) > (int64_t)g.sk_min_idle * P;
     const bool split = can && cus > 0 && ws != nullptr && ws_bytes >= (size_t)2 * P * kSkSlotBytes;
     if (gemm_var_pays(g))
-        hipLaunchKernelGGL((grouped_gemm_dma_kernel<GATED, true>), dim3(P), dim3(kGemmThreads), 0, s, g,
+        hipLaunchKernelGGL((grouped_gemm_dma_kernel<GATED, true, false, OP>), dim3(P), dim3(kGemmThreads), 0, s, g,
                            split ? (char*)ws : (char*)nullptr);
     else
-        hipLaunchKernelGGL((grouped_gemm_dma_kernel<GATED, false>), dim3(P), dim3(kGemmThreads), 0, s, g,
+        hipLaunchKernelGGL((grouped_gemm_dma_kernel<GATED, false, false, OP>), dim3(P), dim3(kGemmThreads), 0, s, g,
                            split ? (char*)ws : (char*)nullptr);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !split) return e;
-    hipLaunchKernelGGL((gemm_fixup_kernel<GATED>), dim3(P), dim3(kGemmThreads), 0, s, g, (const char*)ws, P);
+    hipLaunchKernelGGL((gemm_fixup_kernel<GATED, OP>), dim3(P), dim3(kGemmThreads), 0, s, g, (const char*)ws, P);
     return hipGetLastError();
 }
 
@@ -1459,6 +1517,23 @@ hipError_t launch_ffn(const FfnArgs& a, hipStream_t s, int part) {
                                         : launch_gemm_staged<false>(g2, s);
     }
     return hipSuccess;
+}
+
+// Grouped products of rows held in int8 (w8.hip): the same kernels, whose K-steps then hold twice the columns
+// (the pitch of the codes makes them whole).
+hipError_t launch_w8_gemm(const W8GemmArgs& a, hipStream_t s) {
+    if (a.rows_cap == 0) return hipSuccess;
+    if (w8_skinny_fits(a)) return launch_w8_skinny(a, s);
+    GemmParams g{(const uint16_t*)a.a.codes, (const uint16_t*)a.w0.codes, (const uint16_t*)a.w1.codes, (uint16_t*)a.c,
+                 a.offsets, a.n_seg, a.rows_cap, a.N, (int)(w8_pitch(a.K) / 2)};
+    g.a_rows = a.a_rows;
+    g.a_count = a.a_count;
+    g.sk_min_idle = -1;
+    g.sa = a.a.scales;
+    g.sb0 = a.w0.scales;
+    g.sb1 = a.w1.scales;
+    return a.w1.codes ? launch_gemm_dma<true, OpI8>(g, a.ws, a.ws_bytes, s)
+                      : launch_gemm_dma<false, OpI8>(g, a.ws, a.ws_bytes, s);
 }
 
 }  // namespace bmoe

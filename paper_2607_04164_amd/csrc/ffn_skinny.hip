@@ -48,7 +48,32 @@ struct SkinnyParams {
     int n_seg, rows_cap, N, K;
     const int32_t* a_rows = nullptr;  // gathered A: row r is A[a_rows[r]] (A has a_count rows)
     int a_count = 0;
+    // int8 operands (K then counts pairs of values): scales of A's rows, and of the rows of B0 and B1 [n_seg, N]
+    const float* sa = nullptr;
+    const float* sb0 = nullptr;
+    const float* sb1 = nullptr;
 };
+
+// Output values of columns col .. col+3 and row `row` of segment s from their sums.
+template <bool GATED, class OP, typename S>
+__device__ __forceinline__ void sk_values(float (&v)[4], const S& g, const S& u, const SkinnyParams& p, int s, int row,
+                                          int col) {
+    if constexpr (OP::kScales) {
+        const float rs = p.sa[gathered_row(p.a_rows, p.a_count, row)];
+        // (N is a multiple of 8, so that is one quarter of a row of scales; columns past N are not stored)
+        const size_t at = (size_t)s * p.N + min(col, p.N - 4);
+        const float4 c0 = *(const float4*)(p.sb0 + at);
+        const float4 c1 = GATED ? *(const float4*)(p.sb1 + at) : c0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = scaled(g[i], rs, ((const float*)&c0)[i]);
+            v[i] = GATED ? silu_mul(x, scaled(u[i], rs, ((const float*)&c1)[i])) : x;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = GATED ? silu_mul(g[i], u[i]) : g[i];
+    }
+}
 
 // LDS byte offset of logical 16-byte chunk c of activation row r
 __device__ __forceinline__ int sk_off(int r, int c) { return r * kSkRowBytes + ((c ^ (r & 15)) << 4); }
@@ -228,7 +253,7 @@ struct S2Cfg {
 
 __device__ __forceinline__ int s2_off(int row, int chunk) { return row * kS2RowB + ((chunk ^ (row & 7)) << 4); }
 
-template <bool GATED>
+template <bool GATED, class OP = OpBf16>
 __global__ __launch_bounds__(kSkThreads, 1) void skinny_dma_kernel(SkinnyParams p) {
     constexpr int NMAT = GATED ? 2 : 1;
     using C = S2Cfg<NMAT>;
@@ -287,11 +312,11 @@ __global__ __launch_bounds__(kSkThreads, 1) void skinny_dma_kernel(SkinnyParams 
                 off[i] = (uint32_t)((size_t)arow * K * 2 + ((lchk ^ (row & 7)) << 4));
             }
         }
-        f32x4 acc[NMAT][4];
+        typename OP::acc4 acc[NMAT][4];
 #pragma unroll
         for (int mat = 0; mat < NMAT; ++mat)
 #pragma unroll
-            for (int nt = 0; nt < 4; ++nt) acc[mat][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int nt = 0; nt < 4; ++nt) acc[mat][nt] = typename OP::acc4{0, 0, 0, 0};
         // The MFMAs of chunk c (the A operand: the weights, the B operand: the
         // activation rows), from its ring slot.
         auto chunk_mfmas = [&](int c) {
@@ -310,9 +335,7 @@ __global__ __launch_bounds__(kSkThreads, 1) void skinny_dma_kernel(SkinnyParams 
                 for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
                     for (int mat = 0; mat < NMAT; ++mat)
-                        acc[mat][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv[mat]),
-                                                                               __builtin_bit_cast(bf16x8, xv[nt]),
-                                                                               acc[mat][nt], 0, 0, 0);
+                        acc[mat][nt] = OP::mma16(wv[mat], xv[nt], acc[mat][nt]);
             }
         };
         // Prologue: the first NSL - CPB chunks. Each step then waits for its
@@ -353,11 +376,7 @@ __global__ __launch_bounds__(kSkThreads, 1) void skinny_dma_kernel(SkinnyParams 
             const int row = m0 + nt * 16 + r16;
             if (row >= end) continue;
             float v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (GATED) v[i] = silu_mul(acc[0][nt][i], acc[NMAT - 1][nt][i]);
-                else v[i] = acc[0][nt][i];
-            }
+            sk_values<GATED, OP>(v, acc[0][nt], acc[NMAT - 1][nt], p, s, row, col);
             uint16_t* dst = p.C + (size_t)row * N + col;
             if (col + 3 < N) {
                 *(uint2*)dst = make_uint2(pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3]));
@@ -400,12 +419,13 @@ constexpr int kRgCols = 16;  // output columns per workgroup
 // not (d_ff = 1408, 1 token: 9.0 -> 8.0 us).
 // Row tiles per pass: four for gate/up; two for down, whose accumulators of
 // four measured slower at every size.
-template <bool GATED, int PAIRS>
+template <bool GATED, int PAIRS, class OP = OpBf16>
 __global__ __launch_bounds__(kSkThreads, 2) void skinny_reg_kernel(SkinnyParams p) {
     constexpr int NMAT = GATED ? 2 : 1;
     constexpr int U = 2 * PAIRS;  // MFMA steps of 32 columns
     constexpr int TILES = GATED ? 4 : 2;
-    __shared__ __align__(16) f32x4 part[4][NMAT * TILES][64];
+    using acc4 = typename OP::acc4;
+    __shared__ __align__(16) acc4 part[4][NMAT * TILES][64];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int K = p.K, N = p.N;
     const int ncb = ceil_div(N, kRgCols);
@@ -428,16 +448,14 @@ __global__ __launch_bounds__(kSkThreads, 2) void skinny_reg_kernel(SkinnyParams 
 #pragma unroll
         for (int nt = 0; nt < TILES; ++nt)
             xp[nt] = p.A + (size_t)gathered_row(p.a_rows, p.a_count, min(m0 + nt * 16 + r16, end - 1)) * K + q * 8;
-        f32x4 acc[NMAT][TILES];
+        acc4 acc[NMAT][TILES];
 #pragma unroll
         for (int mat = 0; mat < NMAT; ++mat)
 #pragma unroll
-            for (int nt = 0; nt < TILES; ++nt) acc[mat][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int nt = 0; nt < TILES; ++nt) acc[mat][nt] = acc4{0, 0, 0, 0};
         auto mfmas = [&](int nt, const v4u(&w)[NMAT], v4u x) {
 #pragma unroll
-            for (int mat = 0; mat < NMAT; ++mat)
-                acc[mat][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                    __builtin_bit_cast(bf16x8, w[mat]), __builtin_bit_cast(bf16x8, x), acc[mat][nt], 0, 0, 0);
+            for (int mat = 0; mat < NMAT; ++mat) acc[mat][nt] = OP::mma16(w[mat], x, acc[mat][nt]);
         };
         // step u of the batch from pair p0: columns 32 (u & 1) .. of pair p0 + 4 (u / 2)
         for (int p0 = wave; p0 < npairs; p0 += 4 * PAIRS) {
@@ -492,7 +510,7 @@ __global__ __launch_bounds__(kSkThreads, 2) void skinny_reg_kernel(SkinnyParams 
         // wave nt < TILES finishes row tile nt: the lane holds D[weight row 4q+i][segment row r16]
         const int row = m0 + wave * 16 + r16, col = n0 + 4 * q;
         if (wave < TILES && row < end) {
-            f32x4 sum[NMAT];
+            acc4 sum[NMAT];
 #pragma unroll
             for (int mat = 0; mat < NMAT; ++mat) {
                 sum[mat] = part[0][mat * TILES + wave][lane];
@@ -500,11 +518,7 @@ __global__ __launch_bounds__(kSkThreads, 2) void skinny_reg_kernel(SkinnyParams 
                 for (int w = 1; w < 4; ++w) sum[mat] += part[w][mat * TILES + wave][lane];
             }
             float v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (GATED) v[i] = silu_mul(sum[0][i], sum[NMAT - 1][i]);
-                else v[i] = sum[0][i];
-            }
+            sk_values<GATED, OP>(v, sum[0], sum[NMAT - 1], p, s, row, col);
             uint16_t* dst = p.C + (size_t)row * N + col;
             if (col + 3 < N) {
                 *(uint2*)dst = make_uint2(pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3]));
@@ -587,30 +601,45 @@ bool takes_reg(const SkinnyParams& p) {
     return rows <= 96 && rows <= (in_flight ? 7 : 4) * n;
 }
 
-template <bool GATED, int PAIRS>
-void launch_reg(const SkinnyParams& sp, int64_t blocks, hipStream_t s) {
-    hipLaunchKernelGGL((skinny_reg_kernel<GATED, PAIRS>), dim3((unsigned)blocks), dim3(kSkThreads), 0, s, sp);
+// the copies address A rows by 32-bit byte offsets from A
+bool skinny_dma_fits(const SkinnyParams& sp) {
+    const int64_t a_rows = sp.a_rows ? sp.a_count : sp.rows_cap;
+    return sp.K % kS2KC == 0 && a_rows * sp.K * 2 < ((int64_t)1 << 31) && (int64_t)kSkCols * sp.K * 2 < ((int64_t)1 << 31);
 }
 
-template <bool GATED>
+template <bool GATED, int PAIRS, class OP>
+void launch_reg(const SkinnyParams& sp, int64_t blocks, hipStream_t s) {
+    hipLaunchKernelGGL((skinny_reg_kernel<GATED, PAIRS, OP>), dim3((unsigned)blocks), dim3(kSkThreads), 0, s, sp);
+}
+
+template <bool GATED, class OP = OpBf16>
 hipError_t launch_skinny(const SkinnyParams& sp, hipStream_t s) {
     const int64_t blocks = (int64_t)sp.n_seg * ceil_div(sp.N, kSkCols);
     if (blocks <= 0) return hipSuccess;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     const int64_t narrow = (int64_t)sp.n_seg * ceil_div(sp.N, kRgCols);
     if (takes_reg<GATED>(sp) && narrow <= 0x7fffffff) {
-        if constexpr (GATED) launch_reg<GATED, 8>(sp, narrow, s);
-        else if (sp.K > 4 * 4 * 64 && sp.K <= 6 * 4 * 64) launch_reg<GATED, 6>(sp, narrow, s);
-        else launch_reg<GATED, 4>(sp, narrow, s);
+        if constexpr (GATED) launch_reg<GATED, 8, OP>(sp, narrow, s);
+        else if (sp.K > 4 * 4 * 64 && sp.K <= 6 * 4 * 64) launch_reg<GATED, 6, OP>(sp, narrow, s);
+        else launch_reg<GATED, 4, OP>(sp, narrow, s);
         return hipGetLastError();
     }
-    // the copies address A rows by 32-bit byte offsets from A
-    const int64_t a_rows = sp.a_rows ? sp.a_count : sp.rows_cap;
-    if (sp.K % kS2KC == 0 && a_rows * sp.K * 2 < ((int64_t)1 << 31) && (int64_t)kSkCols * sp.K * 2 < ((int64_t)1 << 31))
-        hipLaunchKernelGGL((skinny_dma_kernel<GATED>), dim3((unsigned)blocks), dim3(kSkThreads), 0, s, sp);
+    if (OP::kScales || skinny_dma_fits(sp))
+        hipLaunchKernelGGL((skinny_dma_kernel<GATED, OP>), dim3((unsigned)blocks), dim3(kSkThreads), 0, s, sp);
     else
         hipLaunchKernelGGL((skinny_gemm_kernel<GATED>), dim3((unsigned)blocks), dim3(kSkThreads), 0, s, sp);
     return hipGetLastError();
+}
+
+SkinnyParams w8_params(const W8GemmArgs& a) {
+    SkinnyParams g{(const uint16_t*)a.a.codes, (const uint16_t*)a.w0.codes, (const uint16_t*)a.w1.codes,
+                   (uint16_t*)a.c, a.offsets, a.n_seg, a.rows_cap, a.N, (int)(w8_pitch(a.K) / 2)};
+    g.a_rows = a.a_rows;
+    g.a_count = a.a_count;
+    g.sa = a.a.scales;
+    g.sb0 = a.w0.scales;
+    g.sb1 = a.w1.scales;
+    return g;
 }
 
 }  // namespace
@@ -635,6 +664,14 @@ hipError_t launch_ffn_skinny(const FfnArgs& a, hipStream_t s, int part) {
         return launch_skinny<false>(g2, s);
     }
     return hipSuccess;
+}
+
+bool w8_skinny_fits(const W8GemmArgs& a) {
+    return (int64_t)a.rows_cap <= (int64_t)kSkRows * a.n_seg && skinny_dma_fits(w8_params(a));
+}
+
+hipError_t launch_w8_skinny(const W8GemmArgs& a, hipStream_t s) {
+    return a.w1.codes ? launch_skinny<true, OpI8>(w8_params(a), s) : launch_skinny<false, OpI8>(w8_params(a), s);
 }
 
 }  // namespace bmoe

@@ -1,0 +1,161 @@
+"""8-bit layers and the router's balance as they are used: a layer whose forward is the calls it is made of, in a
+residual block, captured; its counts as the frequencies of partial brownout."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import desc_of, dev_tensor, device_weights
+from paper_2607_04164_amd import binding as B
+from paper_2607_04164_amd import brownout as BO
+from paper_2607_04164_amd import workload as W
+
+pytestmark = pytest.mark.gpu
+
+CASES = {
+    "one-token": W.CONFIGS["fine"].with_(name="w8-one", T=1, d=512, d_ff=264),
+    "decode": W.CONFIGS["decode"].with_(name="w8-decode", T=48, d=520, d_ff=200),
+    "prefill": W.CONFIGS["mixtral"].with_(name="w8-prefill", T=2100, d=256, d_ff=384),
+    "shared": W.CONFIGS["heavy"].with_(name="w8-shared", T=700, d=512, d_ff=192, d_ff_shared_each=192),
+}
+MATRICES = ("w_gate", "w_up", "w_down", "w_gate_sh", "w_up_sh", "w_down_sh")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.load_library()
+
+
+def made(name, seed=0):
+    cfg = CASES[name]
+    L = W.make_layer(cfg, seed)
+    plain = device_weights(L)
+    return cfg, desc_of(cfg), dev_tensor(L.x, cfg.dtype), plain, {
+        n: B.w8_quantize(t) if n in MATRICES else t for n, t in plain.items()}
+
+
+def by_calls(desc, x, w):
+    """The layer's output from the free functions, each tested by itself."""
+    r = B.route(desc, x, w["w_router"], w["bias"], w["e2g"], want_logits=True)
+    d = B.dispatch(desc, r["slot_group"], None, B.new_dispatch_workspace(desc, "cuda"), copy_rows=False)
+    y, h = B.w8_ffn(d["offsets"], x, w["w_gate"], w["w_up"], w["w_down"], a_rows=d["perm_token"])
+    sh = None
+    if desc.d_ff_shared:
+        sh, _ = B.w8_ffn(torch.tensor([0, desc.T], dtype=torch.int32, device="cuda"), x, w["w_gate_sh"], w["w_up_sh"],
+                         w["w_down_sh"])
+    return B.combine(desc, d["slot_row"], r["slot_gate"], y, sh), r, d, h
+
+
+@pytest.mark.parametrize("name", list(CASES))
+def test_layer_is_its_calls(name):
+    cfg, desc, x, plain, w = made(name)
+    want, r, d, h = by_calls(desc, x, w)
+    layers = [B.LayerForward(desc, w, balance=True)]
+    layers += [B.LayerForward(desc, w, stream_k=False), B.LayerForward(desc, w, concurrent_shared=False)]
+    for layer in layers:
+        assert layer.w8 and layer.fused_gather
+        assert torch.equal(layer(x), want)
+    # stage by stage, as the benchmark times them
+    layer = layers[0]
+    layer.route(x), layer.dispatch(x), layer.ffn_gate_up(x=x), layer.ffn_down()
+    if desc.d_ff_shared:
+        layer.shared(x)
+    assert torch.equal(layer.combine(), want)
+    assert torch.equal(layer.bufs["route"]["logits"], r["logits"])
+    # the same layer with the weights in bf16 is near: 8 bits of a row's largest, on three products
+    ref = B.LayerForward(desc, plain)(x).double()
+    assert float((want.double() - ref).norm() / ref.norm()) < 0.05
+
+
+@pytest.mark.parametrize("name", list(CASES))
+def test_layer_balance(name):
+    cfg, desc, x, _, w = made(name)
+    layer = B.LayerForward(desc, w, balance=True)
+    layer(x)
+    r = layer.bufs["route"]
+    valid = (torch.arange(desc.T, device="cuda") % 3 != 1).to(torch.uint8)
+    for kw, over in (({}, {}), ({"groups": True}, {"e2g": w["e2g"], "G": desc.G})):
+        o = layer.balance(valid, **kw)
+        assert o["counts"] is layer.bufs["balance"]["counts"]
+        want = B.balance(r["logits"], r["topk_idx"], valid=valid, **over)
+        assert all(torch.equal(o[n], want[n]) for n in want)
+    picks = np.bincount(r["topk_idx"][valid != 0].cpu().numpy().ravel(), minlength=desc.E)
+    assert o["counts"].tolist() == picks.tolist() + [int(valid.sum())]
+    with pytest.raises(ValueError, match="balance=True"):
+        B.LayerForward(desc, w).balance()
+
+
+def test_counts_are_the_frequencies_of_partial_brownout():
+    cfg, desc, x, plain, w = made("decode")
+    layer = B.LayerForward(desc, w, balance=True)
+    layer(x)
+    counts = layer.balance()["counts"].cpu().numpy()
+    e2g = w["e2g"].cpu().numpy()
+    e2s, segments = BO.segment_map(counts[:-1], e2g, desc.G, 0.4)
+    S = len(segments)
+    # every expert's own matrices are its group's here, so the layer over the segments is the layer itself
+    pick = torch.tensor([e2g[i] if kind == "expert" else i for kind, i in segments], device="cuda")
+    seg = {n: B.W8(m.codes[pick].contiguous(), m.scales[pick].contiguous(), K=m.shape[2]) if n in MATRICES else m
+           for n, m in w.items()}
+    seg["e2g"] = torch.from_numpy(e2s.astype(np.int32)).cuda()
+    partial = B.LayerForward(desc.replace(G=S), seg, balance=True)
+    out = partial(x)
+    # (a token whose picks share a group calls it once per segment: the sums round apart)
+    torch.testing.assert_close(out.float(), layer(x).float(), rtol=2.0 ** -6, atol=2.0 ** -6 * float(out.abs().max()))
+    assert partial.balance()["counts"].tolist() == counts.tolist()
+
+
+@pytest.mark.parametrize("name", ["one-token", "shared"])
+def test_block_captured(name):
+    """Norm, 8-bit layer, balance, norm in one graph, replayed beside eager work."""
+    cfg, desc, x, _, w = made(name)
+    layer = B.LayerForward(desc, w, balance=True)
+    block = B.ResidualBlock(layer, res_scale=0.5, next_norm=True)
+    x1 = x.flip(0).contiguous() * 0.5
+    want = []
+    for src in (x, x1):
+        r, a = block(src)
+        want.append((r.clone(), a.clone(), {n: t.clone() for n, t in layer.balance(groups=True).items()}))
+    xin = x.clone()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        block(xin)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r, a = block(xin)
+        o = layer.balance(groups=True)
+    for rep in range(4):
+        xin.copy_((x, x1)[rep % 2])
+        for t in (r, a, *o.values(), layer.bufs["out"]):
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        wr, wa, wo = want[rep % 2]
+        assert torch.equal(r, wr) and torch.equal(a, wa) and all(torch.equal(o[n], wo[n]) for n in wo), f"replay {rep}"
+
+
+def test_layer_refusals():
+    cfg, desc, x, plain, w = made("shared")
+    first = B.W8(w["w_gate"].codes[:1].contiguous(), w["w_gate"].scales[:1].contiguous(), K=w["w_gate"].shape[2])
+    for kw in ({"few_tokens": True}, {"fold_combine": True}, {"fused_gather": False}):
+        with pytest.raises(ValueError):
+            B.LayerForward(desc.replace(T=2), w, **kw)
+    for bad in ({"w_up": plain["w_up"]}, {"w_down_sh": plain["w_down_sh"]}, {"w_up": first}, {"w_gate": plain["w_gate"]}):
+        with pytest.raises((ValueError, AttributeError)):
+            B.LayerForward(desc, {**w, **bad})
+    with pytest.raises(ValueError, match="bf16"):
+        B.LayerForward(desc.replace(dtype=B.BMOE_F32), w)
+    with pytest.raises(ValueError, match="few_tokens"):
+        B.LayerForward(desc.replace(T=2), plain, few_tokens=True, balance=True)
+    layer = B.LayerForward(desc, w)
+    with pytest.raises(ValueError, match="pass x"):
+        layer.ffn()
+    with pytest.raises(ValueError):
+        layer(x.float())

@@ -1,0 +1,217 @@
+"""Refusals of the 8-bit and balance calls on the host: every call here fails validation or is an empty no-op, so
+nothing is enqueued. And the kernels that the cases of the GPU tests reach."""
+import ctypes
+import os
+import re
+import shutil
+
+import pytest
+
+from launch_record import PTR, kernels, record, struct
+from paper_2607_04164_amd import binding as B
+
+OK, NULL, SHAPE, ALIGN, UNSUP, WS = 0, 1, 2, 3, 5, 6
+A = 0x10000  # aligned, never read
+Y = 0x40000000  # outputs, apart from the inputs
+ODD = 0x10008
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return B.load_library()
+
+
+def test_header_constants():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = open(os.path.join(root, "include", "brownout_moe.h")).read()
+    assert int(re.search(r"#define BMOE_W8_MAX_K (\d+)", text).group(1)) == B.W8_MAX_K
+    assert [B.w8_row_bytes(K) for K in (8, 128, 136, 4096)] == [128, 128, 256, 4096]
+
+
+def rows8(codes=A, scales=A):
+    return ctypes.byref(B._W8Struct(codes, scales))
+
+
+def quantize(lib, **kw):
+    a = dict(dtype=1, rows=4, K=64, x=A, codes=Y, scales=2 * Y)
+    a.update(kw)
+    return lib.brownout_moe_w8_quantize(*(a[n] for n in ("dtype", "rows", "K", "x", "codes", "scales")), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    ({"dtype": 2}, UNSUP), ({"rows": -1}, SHAPE), ({"rows": (1 << 30) + 1}, SHAPE), ({"K": 0}, SHAPE), ({"K": 12}, SHAPE),
+    ({"K": 131080}, SHAPE), ({"x": None}, NULL), ({"codes": None}, NULL), ({"scales": None}, NULL), ({"x": ODD}, ALIGN),
+    ({"codes": ODD}, ALIGN), ({"scales": ODD}, ALIGN), ({"codes": A}, UNSUP), ({"codes": A + 496}, UNSUP),
+    ({"scales": A + 16}, UNSUP), ({"scales": Y + 496}, UNSUP), ({"rows": 0, "x": None}, OK)])
+def test_quantize_refusals(lib, kw, code):
+    assert quantize(lib, **kw) == code
+
+
+MATMUL = ("dtype", "n", "rows", "N", "K", "off", "src", "m", "a", "a8", "w", "y", "ws", "bytes")
+
+
+def matmul(lib, **kw):
+    a = dict(dtype=1, n=2, rows=8, N=32, K=64, off=A, src=None, m=0, a=A, a8=None, w=rows8(), y=Y, ws=2 * Y,
+             bytes=1 << 20)
+    a.update(kw)
+    return lib.brownout_moe_w8_matmul(*(a[n] for n in MATMUL), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    ({"dtype": 0}, UNSUP), ({"dtype": 7}, UNSUP), ({"n": 0}, SHAPE), ({"n": 257}, SHAPE), ({"rows": -1}, SHAPE),
+    ({"rows": (1 << 30) + 1}, SHAPE), ({"N": 0}, SHAPE), ({"N": 20}, SHAPE), ({"N": (1 << 20) + 8}, SHAPE),
+    ({"K": 4}, SHAPE), ({"K": 131080}, SHAPE), ({"off": None}, NULL), ({"a": None}, NULL), ({"w": None}, NULL),
+    ({"y": None}, NULL), ({"w": rows8(codes=None)}, NULL), ({"w": rows8(scales=None)}, NULL),
+    ({"a": None, "a8": rows8(scales=None)}, NULL), ({"a8": rows8()}, UNSUP), ({"a": ODD}, ALIGN), ({"y": Y + 8}, ALIGN),
+    ({"w": rows8(codes=ODD)}, ALIGN), ({"w": rows8(scales=ODD)}, ALIGN), ({"a": None, "a8": rows8(codes=ODD)}, ALIGN),
+    ({"src": A, "m": 0}, SHAPE), ({"src": A, "m": 1 << 25, "K": 128}, SHAPE), ({"src": A, "m": (1 << 30) + 1}, SHAPE),
+    ({"y": A}, UNSUP), ({"y": A + 1008}, UNSUP), ({"a": None, "a8": rows8(), "y": A}, UNSUP),
+    ({"a": None, "a8": rows8(codes=4 * Y, scales=Y + 496)}, UNSUP), ({"ws": None}, WS), ({"bytes": 1279}, WS),
+    ({"ws": 2 * Y + 128}, ALIGN), ({"rows": 0, "a": None, "off": None, "w": None, "y": None, "ws": None}, OK)])
+def test_matmul_refusals(lib, kw, code):
+    assert matmul(lib, **kw) == code
+
+
+def ffn(lib, **kw):
+    a = dict(dtype=1, n=2, rows=8, d=64, f=32, off=A, src=None, m=0, a=A, a8=None, wg=rows8(), wu=rows8(), wd=rows8(),
+             h=Y, y=2 * Y, ws=3 * Y, bytes=1 << 20)
+    a.update(kw)
+    return lib.brownout_moe_w8_ffn(*(a[n] for n in ("dtype", "n", "rows", "d", "f", "off", "src", "m", "a", "a8", "wg",
+                                                    "wu", "wd", "h", "y", "ws", "bytes")), None)
+
+
+def gate_up(lib, **kw):
+    a = dict(dtype=1, n=2, rows=8, d=64, f=32, off=A, src=None, m=0, a=A, a8=None, wg=rows8(), wu=rows8(), h=Y,
+             ws=3 * Y, bytes=1 << 20)
+    a.update(kw)
+    return lib.brownout_moe_w8_gate_up(*(a[n] for n in ("dtype", "n", "rows", "d", "f", "off", "src", "m", "a", "a8",
+                                                        "wg", "wu", "h", "ws", "bytes")), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    ({"dtype": 0}, UNSUP), ({"f": 131080}, SHAPE), ({"d": 131080}, SHAPE), ({"f": 12}, SHAPE), ({"wg": None}, NULL),
+    ({"wu": None}, NULL), ({"h": None}, NULL), ({"wu": rows8(codes=ODD)}, ALIGN), ({"h": Y + 8}, ALIGN), ({"h": A}, UNSUP),
+    ({"bytes": 255}, WS), ({"ws": None}, WS)])
+def test_ffn_refusals(lib, kw, code):
+    # (as a hidden size of 131080 is only a product's width)
+    if kw != {"f": 131080}:
+        assert gate_up(lib, **kw) == code
+    assert ffn(lib, **kw) == code
+
+
+@pytest.mark.parametrize("kw,code", [
+    ({"wd": None}, NULL), ({"y": None}, NULL), ({"wd": rows8(scales=None)}, NULL), ({"y": Y}, UNSUP), ({"y": ODD}, ALIGN),
+    ({"a": None, "a8": rows8(), "ws": None}, WS), ({"rows": 0, "a": None, "y": None, "h": None, "ws": None, "wu": None}, OK)])
+def test_ffn_down_refusals(lib, kw, code):
+    assert ffn(lib, **kw) == code
+
+
+def test_workspace_sizes(lib):
+    size = lambda *a: lib.bmoe_w8_workspace_bytes(*a, 0)  # noqa: E731
+    assert size(0, 64, 100, 0) == 0
+    assert size(3, 64, 100, 0) == 512 + 256
+    assert size(3, 64, 100, 264) == 100 * 384 + 512  # (the hidden rows take the place of the input's)
+    assert size(1 << 20, 14336, 8, 264) == (1 << 20) * (14336 + 4)
+    assert size(-1, 64, 1, 1) == 0 and size(1, 64, 1, 131080) == 0 and size(1, 4, 1, 8) == 0
+
+
+def bal(lib, **kw):
+    a = dict(T=100, E=12, k=2, G=12, z=A, idx=A, valid=None, e2g=None, losses=Y, counts=2 * Y, prob=3 * Y, ws=4 * Y,
+             bytes=1 << 30)
+    a.update(kw)
+    return lib.brownout_moe_balance(*(a[n] for n in ("T", "E", "k", "G", "z", "idx", "valid", "e2g", "losses", "counts",
+                                                     "prob", "ws", "bytes")), None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    ({"T": -1}, SHAPE), ({"E": 0}, SHAPE), ({"E": 257, "G": 257}, SHAPE), ({"k": 0}, SHAPE), ({"k": 17}, SHAPE),
+    ({"G": 3}, SHAPE), ({"G": 0, "e2g": A}, SHAPE), ({"G": 257, "e2g": A}, SHAPE), ({"T": 1 << 30, "k": 4}, SHAPE),
+    ({"z": None}, NULL), ({"idx": None}, NULL), ({"losses": None}, NULL), ({"counts": None}, NULL), ({"prob": None}, NULL),
+    ({"z": A + 2}, ALIGN), ({"losses": Y + 1}, ALIGN), ({"e2g": A + 2}, ALIGN), ({"prob": A}, UNSUP),
+    ({"losses": A + 4796}, UNSUP), ({"counts": 3 * Y + 44}, UNSUP), ({"valid": 3 * Y + 40}, UNSUP),
+    ({"T": 5000, "ws": None}, WS), ({"T": 5000, "bytes": 100}, WS), ({"T": 5000, "ws": 4 * Y + 4}, ALIGN),
+    ({"T": 0, "z": None, "losses": None}, OK)])
+def test_balance_refusals(lib, kw, code):
+    assert bal(lib, **kw) == code
+
+
+def grad(lib, **kw):
+    a = dict(T=100, E=12, k=2, G=12, z=A, valid=None, e2g=None, counts=2 * Y, d=3 * Y, dz=Y)
+    a.update(kw)
+    return lib.brownout_moe_balance_grad(*(a[n] for n in ("T", "E", "k", "G", "z", "valid", "e2g", "counts", "d", "dz")),
+                                         None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    ({"T": -1}, SHAPE), ({"E": 300}, SHAPE), ({"k": 0}, SHAPE), ({"G": 5}, SHAPE), ({"z": None}, NULL),
+    ({"counts": None}, NULL), ({"d": None}, NULL), ({"dz": None}, NULL), ({"dz": Y + 2}, ALIGN), ({"dz": A + 4}, UNSUP),
+    ({"dz": 2 * Y + 48}, UNSUP), ({"dz": 3 * Y + 4}, UNSUP), ({"valid": Y + 4799}, UNSUP),
+    ({"T": 0, "z": None, "dz": None}, OK)])
+def test_balance_grad_refusals(lib, kw, code):
+    assert grad(lib, **kw) == code
+
+
+# ---------------------------------------------------------------------------
+# the kernels that the calls reach
+
+needs_recorder = pytest.mark.skipif(shutil.which("g++") is None, reason="needs a host compiler for the recording runtime")
+
+
+def ints(*v):
+    return [["i", i] for i in v]
+
+
+def w8(codes=PTR):
+    return struct(B._W8Struct(codes, PTR))
+
+
+def product(n, rows, N, K, gated=False, ws=1 << 33, **device):
+    far = ["p", 1 << 40]
+    args = [*ints(1, n, rows, *((K, N) if gated else (N, K))), ["p", PTR], ["p", 0], ["i", 0], ["p", 0], w8(), w8()]
+    args += ([w8()] if gated else []) + [far, ["p", 1 << 41], ["z", ws], ["p", 0]]
+    return {"fn": f"brownout_moe_w8_{'gate_up' if gated else 'matmul'}", "args": args, **device}
+
+
+def launched(calls, tmp_path):
+    res = record(calls, tmp_path)
+    assert all(status == 0 for status, _ in res)
+    return [ls for _, ls in res]
+
+
+@needs_recorder
+def test_every_kernel_is_run_by_a_test_case(tmp_path):
+    import test_gpu_balance as TB
+    import test_gpu_w8 as T8
+    calls = [product(*c) for c in T8.CASES] + [product(n, rows, f, d, True) for n, rows, f, d in
+                                               [(1, 1, 1408, 2048), (8, 250, 72, 1408), (2, 2000, 392, 264),
+                                                (5, 900, 520, 72), (1, 1300, 1032, 8192), (1, 1, 24, 40)]]
+    calls += [product(1, 1300, 1032, 8192)]  # test_split_tiles_have_the_same_bits
+    calls += [{"fn": "brownout_moe_w8_quantize", "args": [*ints(t, 2, K), ["p", PTR], ["p", 1 << 40], ["p", 1 << 41],
+                                                          ["p", 0]]} for t in (0, 1) for K in (8, 1048, 4096, 8192, 20008)]
+    for T, E, k in TB.SIZES:
+        calls += [{"fn": "brownout_moe_balance", "args": [*ints(T, E, k, E), ["p", PTR], ["p", PTR], ["p", 0], ["p", 0],
+                                                          ["p", 1 << 40], ["p", 1 << 41], ["p", 1 << 42], ["p", 1 << 43],
+                                                          ["z", 1 << 30], ["p", 0]]},
+                  {"fn": "brownout_moe_balance_grad", "args": [*ints(T, E, k, E), ["p", PTR], ["p", 0], ["p", 0], ["p", PTR],
+                                                               ["p", PTR], ["p", 1 << 40], ["p", 0]]}]
+    ran = {name for ls in launched(calls, tmp_path) for name, _ in ls}
+    built = {k for k in kernels(tmp_path) if re.search(r"OpI8|q8_|balance_", k)}
+    assert len(built) >= 30
+    assert not built - ran, "\n".join(sorted(built - ran))
+
+
+@needs_recorder
+def test_product_choice(tmp_path):
+    """Few rows on the weight-streaming kernels, more on the large tiles (half ones where segments are short); the
+    fixup only with the room for it and where K can be split."""
+    cases = [((1, 64, 512, 4096), ["skinny"]), ((1, 65, 512, 4096), ["dma_kernel<false, true"]),
+             ((4, 4 * 768, 512, 4096), ["dma_kernel<false, false"]),
+             ((1, 1300, 1032, 8192), ["dma_kernel<false, false", "fixup"]), ((1, 1300, 1032, 6144), ["dma_kernel<false, false"])]
+    for case, want in cases:
+        ls, = launched([product(*case)], tmp_path)
+        assert len(ls) == len(want) and all(w in name and "OpI8" in name for w, (name, _) in zip(want, ls)), (case, ls)
+    ls, = launched([product(1, 1300, 1032, 8192, ws=0)], tmp_path)
+    assert len(ls) == 1
+    # a source too large for the few-row copies' 32-bit offsets
+    ls, = launched([product(256, 256 * 64, 64, 131072)], tmp_path)
+    assert "grouped_gemm_dma_kernel" in ls[0][0]
