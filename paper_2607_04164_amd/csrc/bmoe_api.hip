@@ -94,7 +94,7 @@ hipError_t w8_rounded(const void* a, int64_t rows, int K, void* ws, bmoe_w8& out
     return launch_w8_quantize(q, s);
 }
 
-// The products of a checked call: part 1 up (or the only one), 2 down, 3 both
+// The products of a checked call (w_down: the second one, from h)
 struct W8Call {
     int32_t n_seg, rows_cap, d, d_ff;
     const int32_t* offsets;
@@ -117,13 +117,16 @@ bmoe_status w8_run(const W8Call& c) {
     const bool split = c.ws && c.ws_bytes - need >= ffn_workspace_bytes();
     W8GemmArgs g{c.offsets, c.a_rows, c.a_count, {}, *c.w_gate, c.w_up ? *c.w_up : bmoe_w8{nullptr, nullptr}, c.h,
                  split ? ws + need : nullptr, split ? c.ws_bytes - need : 0, c.n_seg, c.rows_cap, c.d_ff, c.d};
-    hipError_t e = hipSuccess;
-    if (c.a8) g.a = *c.a8;
-    else e = w8_rounded(c.a, rows, c.d, ws, g.a, c.s);
-    if (e == hipSuccess) e = launch_w8_gemm(g, c.s);
+    // x (or a8) times g's weights
+    auto product = [&](const void* x, int64_t x_rows, const bmoe_w8* a8, const int32_t* offsets) {
+        if (!a8 && w8_few_fits(g)) return launch_w8_few(g, x, c.s);
+        hipError_t e = hipSuccess;
+        if (a8) g.a = *a8;
+        else e = w8_rounded(x, x_rows, g.K, ws, g.a, c.s, offsets, c.n_seg);
+        return e == hipSuccess ? launch_w8_gemm(g, c.s) : e;
+    };
+    hipError_t e = product(c.a, rows, c.a8, nullptr);
     if (e != hipSuccess || !c.w_down) return e == hipSuccess ? BMOE_OK : BMOE_ERR_HIP;
-    // (in the place of a's rows, which the product before has read)
-    e = w8_rounded(c.h, c.rows_cap, c.d_ff, ws, g.a, c.s, c.offsets, c.n_seg);
     g.a_rows = nullptr;
     g.a_count = 0;
     g.w0 = *c.w_down;
@@ -131,7 +134,8 @@ bmoe_status w8_run(const W8Call& c) {
     g.c = c.y;
     g.N = c.d;
     g.K = c.d_ff;
-    if (e == hipSuccess) e = launch_w8_gemm(g, c.s);
+    // (the rounded rows of h in the place of a's, which the product before has read; only rows of segments are there)
+    e = product(c.h, c.rows_cap, nullptr, c.offsets);
     return e == hipSuccess ? BMOE_OK : BMOE_ERR_HIP;
 }
 

@@ -97,11 +97,13 @@ struct OpI8 {
     }
 };
 
-// sum * a * b, the smaller scale first: |sum| >= 1 then neither under- nor overflows on the way to a
+// a scale with which sum * a * b cannot leave fp32 on the way
+__device__ __forceinline__ bool plain_scale(float s) { return s == 0.f || (s >= 0x1p-60f && s <= 0x1p60f); }
+// sum * a * b. Scales far from 1: the smaller first, so that |sum| >= 1 neither under- nor overflows on the way to a
 // result that does not. A scale that is not a number makes the result one (fminf would drop it).
 __device__ __forceinline__ float scaled(int sum, float a, float b) {
-    const bool less = a < b;
-    return (float)sum * (less ? a : b) * (less ? b : a);
+    const bool swap = !(plain_scale(a) && plain_scale(b)) && !(a < b);
+    return (float)sum * (swap ? b : a) * (swap ? a : b);
 }
 
 __host__ __device__ constexpr int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -370,6 +372,9 @@ struct W8GemmArgs {
     int n_seg, rows_cap, N, K;
 };
 hipError_t launch_w8_gemm(const W8GemmArgs& a, hipStream_t s);
+// the same from activations x in bf16 (a.a not used), rounded by the product itself, where rows_cap * K is small
+bool w8_few_fits(const W8GemmArgs& a);
+hipError_t launch_w8_few(const W8GemmArgs& a, const void* x, hipStream_t s);
 // rows_cap of at most 64 rows a segment; false: the sizes are the large kernel's
 bool w8_skinny_fits(const W8GemmArgs& a);
 hipError_t launch_w8_skinny(const W8GemmArgs& a, hipStream_t s);

@@ -251,6 +251,34 @@ struct S2Cfg {
     static_assert(NSL * SLOT <= 160 * 1024, "LDS of one workgroup");
 };
 
+// Pass m of all segments' passes of kSkRows rows, in order: its segment and rows; false past the last one. (int8: the
+// passes of a segment run side by side. In one workgroup, one after the other, a segment of more than a pass made the
+// kernel's time: 250 rows of 8 random segments, d = 2048, d_ff = 1408, gate/up 21 us, down 12.)
+__device__ __forceinline__ bool sk_pass(const SkinnyParams& p, int m, int& s, int& beg, int& end) {
+    const int lane = threadIdx.x & 63;
+    for (int s0 = 0; s0 < p.n_seg; s0 += kWave) {
+        const int i = min(s0 + lane, p.n_seg - 1);
+        const int b = min(max(p.offsets[i], 0), p.rows_cap), e = min(max(p.offsets[i + 1], b), p.rows_cap);
+        const int mine = s0 + lane < p.n_seg ? ceil_div(e - b, kSkRows) : 0;
+        int incl = mine;
+#pragma unroll
+        for (int off = 1; off < kWave; off <<= 1) {
+            const int o = __shfl_up(incl, off);
+            if (lane >= off) incl += o;
+        }
+        const uint64_t past = __ballot(incl > m);
+        if (past) {
+            const int at = __ffsll((unsigned long long)past) - 1;
+            s = __builtin_amdgcn_readfirstlane(s0 + at);
+            beg = __builtin_amdgcn_readfirstlane(__shfl(b + (m - (incl - mine)) * kSkRows, at));
+            end = __builtin_amdgcn_readfirstlane(min(__shfl(e, at), beg + kSkRows));
+            return true;
+        }
+        m -= __builtin_amdgcn_readfirstlane(__shfl(incl, kWave - 1));
+    }
+    return false;
+}
+
 __device__ __forceinline__ int s2_off(int row, int chunk) { return row * kS2RowB + ((chunk ^ (row & 7)) << 4); }
 
 template <bool GATED, class OP = OpBf16>
@@ -261,11 +289,16 @@ __global__ __launch_bounds__(kSkThreads, 1) void skinny_dma_kernel(SkinnyParams 
     // the wave index in an SGPR: the copy bases below stay scalar
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int ncb = ceil_div(p.N, kSkCols);
-    const int s = blockIdx.x / ncb, cb = blockIdx.x % ncb;
-    if (s >= p.n_seg) return;
-    const int beg = min(max(p.offsets[s], 0), p.rows_cap);
-    const int end = min(max(p.offsets[s + 1], beg), p.rows_cap);
-    if (end <= beg) return;
+    int s = blockIdx.x / ncb, beg, end;
+    const int cb = blockIdx.x % ncb;
+    if constexpr (OP::kScales) {
+        if (!sk_pass(p, s, s, beg, end)) return;
+    } else {
+        if (s >= p.n_seg) return;
+        beg = min(max(p.offsets[s], 0), p.rows_cap);
+        end = min(max(p.offsets[s + 1], beg), p.rows_cap);
+        if (end <= beg) return;
+    }
     const int K = p.K, N = p.N;
     const int nch = K / kS2KC;
     const int n0 = cb * kSkCols;
@@ -624,7 +657,12 @@ hipError_t launch_skinny(const SkinnyParams& sp, hipStream_t s) {
         else launch_reg<GATED, 4, OP>(sp, narrow, s);
         return hipGetLastError();
     }
-    if (OP::kScales || skinny_dma_fits(sp))
+    if (OP::kScales) {
+        // a segment's passes: one for its rows up to kSkRows, and at most one for every kSkRows more
+        const int64_t passes = ((int64_t)sp.n_seg + sp.rows_cap / kSkRows) * ceil_div(sp.N, kSkCols);
+        if (passes > 0x7fffffff) return hipErrorInvalidValue;
+        hipLaunchKernelGGL((skinny_dma_kernel<GATED, OP>), dim3((unsigned)passes), dim3(kSkThreads), 0, s, sp);
+    } else if (skinny_dma_fits(sp))
         hipLaunchKernelGGL((skinny_dma_kernel<GATED, OP>), dim3((unsigned)blocks), dim3(kSkThreads), 0, s, sp);
     else
         hipLaunchKernelGGL((skinny_gemm_kernel<GATED>), dim3((unsigned)blocks), dim3(kSkThreads), 0, s, sp);

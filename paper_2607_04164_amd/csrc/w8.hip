@@ -50,6 +50,14 @@ __device__ __forceinline__ uint4 codes_of(const float (&f)[16], float s, float i
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// the scale of a row whose largest magnitude bits are m, and its reciprocal (0: the codes are 0)
+__device__ __forceinline__ float row_scale(uint32_t m, float& inv) {
+    const float s = __uint_as_float(m) / 127.f;
+    const bool finite = m < 0x7f800000u, live = finite && s >= kMinScale;
+    inv = live ? 1.f / s : 0.f;
+    return live ? s : finite ? 0.f : __builtin_nanf("");
+}
+
 template <typename E, int NT, int CH>
 __global__ __launch_bounds__(NT > 256 ? NT : 256) void q8_rows_kernel(W8QuantizeArgs a) {
     constexpr int R = NT > 256 ? 1 : 256 / NT;  // rows of a workgroup
@@ -84,10 +92,8 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void q8_rows_kernel(W8Quantize
 #pragma unroll
         for (int w = 0; w < W; ++w) m = max(m, part[w]);
     }
-    float s = __uint_as_float(m) / 127.f, inv = 0.f;
-    const bool finite = m < 0x7f800000u;
-    if (finite && s >= kMinScale) inv = 1.f / s;
-    else s = finite ? 0.f : __builtin_nanf("");
+    float inv;
+    const float s = row_scale(m, inv);
     uint4* out = (uint4*)(a.codes + (size_t)r * w8_pitch(K));
     const uint4 none = make_uint4(0, 0, 0, 0);
 #pragma unroll
@@ -122,7 +128,165 @@ hipError_t pick_q8(const W8QuantizeArgs& a, hipStream_t s) {
     return launch_q8<E, 256, 4>(a, s);
 }
 
+// ---- products of a few rows that round their activations themselves
+//
+// One launch instead of two where rows_cap * K is small: every workgroup rounds its segment's rows (at most
+// kFewValues values, from the L2 cache) into LDS while its first weights are on their way, and then multiplies as
+// skinny_reg_kernel does: 16 output columns, K split over the four waves (128-column pairs of MFMA steps, PAIRS of
+// them in flight a wave), the waves' sums added in LDS.
+constexpr int kFewThreads = 256;
+constexpr int kFewRows = 16;
+constexpr int kFewValues = 16384;                              // rows_cap * pitch, at most
+constexpr int kFewUnits = kFewValues / 16 / kFewThreads;       // units of 16 values a thread
+constexpr int kFewPad = 16;                                    // bytes between rows in LDS: rows on other banks
+
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
+struct Few8Params {
+    const uint16_t* A;
+    const int8_t* B0;
+    const int8_t* B1;
+    const float* sb0;
+    const float* sb1;
+    uint16_t* C;
+    const int32_t* offsets;
+    const int32_t* a_rows;
+    int a_count, n_seg, rows_cap, N, K;
+};
+
+template <bool GATED, int PAIRS>
+__global__ __launch_bounds__(kFewThreads, 2) void few8_kernel(Few8Params p) {
+    constexpr int NMAT = GATED ? 2 : 1;
+    __shared__ __align__(16) char s_x[kFewValues + kFewRows * kFewPad];
+    __shared__ __align__(16) i32x4 s_part[4][NMAT][64];
+    __shared__ uint32_t s_max[kFewRows];
+    __shared__ float s_scale[kFewRows];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int N = p.N, K = p.K, P = (int)w8_pitch(K);
+    const int ncb = ceil_div(N, 16), s = blockIdx.x / ncb, n0 = (blockIdx.x % ncb) * 16;
+    const int beg = min(max(p.offsets[s], 0), p.rows_cap);
+    const int end = min(max(p.offsets[s + 1], beg), p.rows_cap);
+    const int rows = end - beg;  // (rows_cap of them at most, so kFewRows, and rows * P <= kFewValues)
+    if (rows <= 0) return;
+    const int r16 = lane & 15, q = lane >> 4;
+    const size_t wrow = (size_t)s * N + min(n0 + r16, N - 1);
+    const char* wp[NMAT];
+    wp[0] = (const char*)p.B0 + wrow * P + q * 16;
+    if constexpr (GATED) wp[NMAT - 1] = (const char*)p.B1 + wrow * P + q * 16;
+    const int npairs = P / 128;
+    // step u of the batch from pair p0: bytes 64 (u & 1) .. of pair p0 + 4 (u / 2)
+    v4u w[2 * PAIRS][NMAT];
+    auto load_weights = [&](int p0) {
+#pragma unroll
+        for (int u = 0; u < 2 * PAIRS; ++u)
+            if (p0 + 4 * (u >> 1) < npairs) {
+#pragma unroll
+                for (int mat = 0; mat < NMAT; ++mat)
+                    w[u][mat] = *(const v4u*)(wp[mat] + (p0 + 4 * (u >> 1)) * 128 + (u & 1) * 64);
+            }
+    };
+    // the rows' values, a unit of 16 a thread and round
+    const int upr = P / 16, units = rows * upr;
+    uint4 x[kFewUnits][2];
+#pragma unroll
+    for (int i = 0; i < kFewUnits; ++i) {
+        const int j = tid + kFewThreads * i, r = j / upr, u = j - r * upr;
+        x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
+        if (j < units) {
+            const uint4* row = (const uint4*)(p.A + (size_t)gathered_row(p.a_rows, p.a_count, beg + r) * K);
+            if (u * 16 < K) x[i][0] = row[2 * u];
+            if (u * 16 + 8 < K) x[i][1] = row[2 * u + 1];
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_weights(wave);
+    __builtin_amdgcn_sched_barrier(0);
+    if (tid < kFewRows) s_max[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kFewUnits; ++i) {
+        const int j = tid + kFewThreads * i;
+        if (j >= units) break;
+        uint32_t m = 0;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const uint32_t v[4] = {x[i][c].x, x[i][c].y, x[i][c].z, x[i][c].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m = max(m, max(v[e] << 16 & 0x7fff0000u, v[e] & 0x7fff0000u));
+        }
+        atomicMax(&s_max[j / upr], m);  // (whatever the order)
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kFewUnits; ++i) {
+        const int j = tid + kFewThreads * i, r = j / upr, u = j - r * upr;
+        if (j >= units) break;
+        float inv;
+        const float sc = row_scale(s_max[r], inv);
+        float f[16];
+        Vec<uint16_t>::load(x[i][0], f);
+        Vec<uint16_t>::load(x[i][1], f + 8);
+        *(uint4*)(s_x + r * (P + kFewPad) + u * 16) = inv > 0.f ? codes_of(f, sc, inv) : make_uint4(0, 0, 0, 0);
+        if (u == 0) s_scale[r] = sc;
+    }
+    __syncthreads();
+    i32x4 acc[NMAT];
+#pragma unroll
+    for (int mat = 0; mat < NMAT; ++mat) acc[mat] = i32x4{0, 0, 0, 0};
+    // (lanes past the last row repeat it: their results are not stored)
+    const char* xp = s_x + min(r16, rows - 1) * (P + kFewPad) + q * 16;
+    for (int p0 = wave; p0 < npairs; p0 += 4 * PAIRS) {
+        if (p0 != wave) load_weights(p0);
+#pragma unroll
+        for (int u = 0; u < 2 * PAIRS; ++u)
+            if (p0 + 4 * (u >> 1) < npairs) {
+                const v4u xv = *(const v4u*)(xp + (p0 + 4 * (u >> 1)) * 128 + (u & 1) * 64);
+#pragma unroll
+                for (int mat = 0; mat < NMAT; ++mat) acc[mat] = OpI8::mma16(w[u][mat], xv, acc[mat]);
+            }
+    }
+#pragma unroll
+    for (int mat = 0; mat < NMAT; ++mat) s_part[wave][mat][lane] = acc[mat];
+    __syncthreads();
+    // the lane holds columns n0 + 4 q .. + 3 of row r16
+    if (wave != 0 || r16 >= rows) return;
+    const int col = n0 + 4 * q;
+    if (col >= N) return;  // (N is a multiple of 8)
+    i32x4 sum[NMAT];
+#pragma unroll
+    for (int mat = 0; mat < NMAT; ++mat)
+        sum[mat] = s_part[0][mat][lane] + s_part[1][mat][lane] + s_part[2][mat][lane] + s_part[3][mat][lane];
+    const float rs = s_scale[r16];
+    const float4 c0 = *(const float4*)(p.sb0 + (size_t)s * N + col);
+    const float4 c1 = GATED ? *(const float4*)(p.sb1 + (size_t)s * N + col) : c0;
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = scaled(sum[0][i], rs, ((const float*)&c0)[i]);
+        if (GATED) v[i] = silu_mul(v[i], scaled(sum[NMAT - 1][i], rs, ((const float*)&c1)[i]));
+    }
+    *(uint2*)(p.C + (size_t)(beg + r16) * N + col) =
+        make_uint2(pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3]));
+}
+
+template <bool GATED, int PAIRS>
+hipError_t launch_few8(const Few8Params& p, hipStream_t s) {
+    hipLaunchKernelGGL((few8_kernel<GATED, PAIRS>), dim3((unsigned)(p.n_seg * ceil_div(p.N, 16))), dim3(kFewThreads), 0, s,
+                       p);
+    return hipGetLastError();
+}
+
 }  // namespace
+
+bool w8_few_fits(const W8GemmArgs& a) {
+    return a.rows_cap <= kFewRows && a.rows_cap * w8_pitch(a.K) <= kFewValues;
+}
+
+hipError_t launch_w8_few(const W8GemmArgs& a, const void* x, hipStream_t s) {
+    const Few8Params p{(const uint16_t*)x, a.w0.codes, a.w1.codes, a.w0.scales, a.w1.scales, (uint16_t*)a.c,
+                       a.offsets, a.a_rows, a.a_count, a.n_seg, a.rows_cap, a.N, a.K};
+    return a.w1.codes ? launch_few8<true, 4>(p, s) : launch_few8<false, 8>(p, s);
+}
 
 hipError_t launch_w8_quantize(const W8QuantizeArgs& a, hipStream_t s) {
     if (a.rows == 0) return hipSuccess;
