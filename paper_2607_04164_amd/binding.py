@@ -969,20 +969,19 @@ def balance(logits: torch.Tensor, topk_idx: torch.Tensor, *, valid: Optional[tor
         raise ValueError("topk_idx must be [T, k]")
     k = topk_idx.shape[1]
     ip = _fits(topk_idx, "topk_idx", torch.int32, (T, k), device)
-    o = dict(out) if out else {}
-    for name, dt, shape in (("losses", torch.float32, (2,)), ("counts", torch.int32, (E + 1,)),
-                            ("prob", torch.float32, (E,))):
-        if name not in o:
-            o[name] = _new(shape, dt, logits.device, stream)
-    ptrs = (_fits(o["losses"], "losses", torch.float32, (2,), device),
-            _fits(o["counts"], "counts", torch.int32, (E + 1,), device),
-            _fits(o["prob"], "prob", torch.float32, (E,), device))
+    new = lambda n, dt: _new((n,), dt, logits.device, stream)  # noqa: E731
+    o = {} if out is None else dict(out)
+    losses = o["losses"] if "losses" in o else o.setdefault("losses", new(2, torch.float32))
+    counts = o["counts"] if "counts" in o else o.setdefault("counts", new(E + 1, torch.int32))
+    prob = o["prob"] if "prob" in o else o.setdefault("prob", new(E, torch.float32))
     if workspace is None:
         n = int(load_library().bmoe_balance_workspace_bytes(T, E))
-        workspace = _new((n,), torch.uint8, logits.device, stream) if n else None
-    wp = None if workspace is None else _fits(workspace, "workspace", torch.uint8, (workspace.numel(),), device)
-    _check(load_library().brownout_moe_balance(T, E, k, G, lp, ip, vp, gp, *ptrs, wp,
-                                               0 if workspace is None else workspace.numel(),
+        workspace = new(n, torch.uint8) if n else None
+    wp, wn = (None, 0) if workspace is None else (_fits(workspace, "workspace", torch.uint8, workspace.shape, device),
+                                                  workspace.numel())
+    _check(load_library().brownout_moe_balance(T, E, k, G, lp, ip, vp, gp, _fits(losses, "losses", torch.float32, (2,), device),
+                                               _fits(counts, "counts", torch.int32, (E + 1,), device),
+                                               _fits(prob, "prob", torch.float32, (E,), device), wp, wn,
                                                _stream_ptr(stream, device)), "brownout_moe_balance")
     return o
 

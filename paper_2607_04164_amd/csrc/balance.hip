@@ -4,10 +4,11 @@
 //   balance = G sum_e F_g(e) P_e,   z loss = mean of lse_t^2
 //   dz_te = b G / V p_te (F_g(e) - sum_j F_g(j) p_tj) + a 2 / V lse_t p_te      (the counts are constants)
 //
-// S lanes of a wave hold a token's row (lane s: experts s, s + S, ..), so a wave takes 64 / S neighbouring rows at a
-// time and a row's maximum and sums are register permutations. A lane keeps the sums of p of its experts over its
+// S lanes of a wave hold a token's row (lane s: experts s, s + S, .., or four neighbours at a time where rows are whole
+// 16-byte chunks), so a wave takes 64 / S neighbouring rows at a time and a row's maximum and sums are register
+// permutations. A lane keeps the sums of p of its experts over its
 // tokens; a workgroup's sums meet in LDS in wave order, the workgroups' in a second launch in 64 bits: no float
-// atomics, so results do not depend on the order of anything. Up to kOneGroup tokens one workgroup does it all.
+// atomics, so results do not depend on the order of anything. Up to kOneGroup rounds one workgroup does it all.
 #include "bmoe_common.h"
 
 namespace bmoe {
@@ -16,7 +17,7 @@ namespace {
 constexpr int kThreads = 1024;  // of the forward's workgroups
 constexpr int kWaves = kThreads / 64;
 constexpr int kMaxGroups = 256;  // workgroups of the forward, at most
-constexpr int kOneGroup = 512;   // tokens one workgroup takes by itself
+constexpr int kOneGroup = 8;     // rounds of tokens that one workgroup takes by itself
 constexpr int kGradThreads = 256;
 
 // sum / maximum over the S lanes of a token, the same bits in each of them
@@ -67,13 +68,23 @@ __device__ __forceinline__ float softmax_row(float (&z)[V]) {
     return top + logf(sum);
 }
 
+// the expert of lane s's value v; B: neighbours at a time (1, or 4 with E a multiple of 4 and rows 16-byte aligned)
+template <int S, int B>
+__device__ __forceinline__ int expert_of(int s, int v) { return B * (s + S * (v / B)) + v % B; }
+
 // the logits of token t that lane s holds; past E, and for tokens that do not count, -infinity
-template <int S, int V>
+template <int S, int V, int B>
 __device__ __forceinline__ void load_logits(float (&z)[V], const float* logits, int64_t t, int s, int E, bool on) {
+    const float none = -__builtin_inff();
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int e = s + S * v;
-        z[v] = on && e < E ? logits[t * E + e] : -__builtin_inff();
+    for (int v = 0; v < V; v += B) {
+        const int e = expert_of<S, B>(s, v);
+        if constexpr (B == 4) {
+            const float4 q = on && e < E ? *(const float4*)(logits + t * E + e) : make_float4(none, none, none, none);
+            z[v] = q.x, z[v + 1] = q.y, z[v + 2] = q.z, z[v + 3] = q.w;
+        } else {
+            z[v] = on && e < E ? logits[t * E + e] : none;
+        }
     }
 }
 
@@ -132,7 +143,7 @@ __host__ __device__ inline Parts parts_of(void* ws, int groups, int E) {
     return q;
 }
 
-template <int S, int V>
+template <int S, int V, int B>
 __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     constexpr int PER = 64 / S;  // tokens of a wave at a time
     __shared__ float s_p[kWaves][S * V];
@@ -150,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     auto counts_token = [&](int64_t i) { return i < a.T && (!a.valid || a.valid[i] != 0); };
     float next[V];
     bool on = counts_token(t);
-    load_logits<S, V>(next, a.logits, t, s, E, on);
+    load_logits<S, V, B>(next, a.logits, t, s, E, on);
     // (the lanes of a wave stay together: the permutations read their neighbours)
     for (; __any(t < a.T); t += step) {
         float z[V];
@@ -165,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
             if (s == 0) atomicAdd(&sums.c[E], 1);
         }
         on = counts_token(t + step);
-        load_logits<S, V>(next, a.logits, t + step, s, E, on);
+        load_logits<S, V, B>(next, a.logits, t + step, s, E, on);
         const float lse = softmax_row<S, V>(z);
         if (now) {
 #pragma unroll
@@ -178,7 +189,7 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     for (int v = 0; v < V; ++v) {
 #pragma unroll
         for (int off = S; off < 64; off *= 2) p[v] += __shfl_xor(p[v], off);
-        if (lane < S) s_p[wave][s + S * v] = p[v];
+        if (lane < S) s_p[wave][expert_of<S, B>(s, v)] = p[v];
     }
 #pragma unroll
     for (int off = S; off < 64; off *= 2) z2 += __shfl_xor(z2, off);
@@ -214,11 +225,25 @@ __global__ __launch_bounds__(kThreads) void balance_join_kernel(BalanceArgs a, i
     const Parts q = parts_of(a.ws, groups, E);
     double p = 0.0;
     int c = 0;
+    // (one workgroup's latency: kAhead loads of each in flight, those past the end of the last row instead of branches)
+    constexpr int kAhead = 16;
     if (e < E)
-#pragma unroll 8
-        for (int g = j; g < groups; g += J) {
-            p += (double)q.p[(size_t)g * E + e];
-            c += q.c[(size_t)g * (E + 1) + e];
+        for (int g0 = j; g0 < groups; g0 += J * kAhead) {
+            float pv[kAhead];
+            int cv[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int g = min(g0 + J * i, groups - 1);
+                pv[i] = q.p[(size_t)g * E + e];
+                cv[i] = q.c[(size_t)g * (E + 1) + e];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const bool in = g0 + J * i < groups;
+                p += in ? (double)pv[i] : 0.0;
+                c += in ? cv[i] : 0;
+            }
         }
     s_p[tid] = p;
     s_c[tid] = c;
@@ -253,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void balance_join_kernel(BalanceArgs a, i
     finish(a, sums);
 }
 
-template <int S, int V>
+template <int S, int V, int B>
 __global__ __launch_bounds__(kGradThreads) void balance_grad_kernel(BalanceGradArgs a) {
     constexpr int PER = 64 / S;
     __shared__ int s_group[BMOE_MAX_EXPERTS];
@@ -278,12 +303,12 @@ __global__ __launch_bounds__(kGradThreads) void balance_grad_kernel(BalanceGradA
     __syncthreads();
     float f[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) f[v] = s_f[s + S * v];
+    for (int v = 0; v < V; ++v) f[v] = s_f[expert_of<S, B>(s, v)];
     const int64_t step = (int64_t)gridDim.x * (kGradThreads / 64) * PER;
     for (int64_t t = ((int64_t)blockIdx.x * (kGradThreads / 64) + wave) * PER + lane / S; __any(t < a.T); t += step) {
         const bool in = t < a.T, on = in && (!a.valid || a.valid[t] != 0);
         float z[V];
-        load_logits<S, V>(z, a.logits, t, s, E, on);
+        load_logits<S, V, B>(z, a.logits, t, s, E, on);
         const float lse = softmax_row<S, V>(z);
         float dot = 0.f;
 #pragma unroll
@@ -292,24 +317,32 @@ __global__ __launch_bounds__(kGradThreads) void balance_grad_kernel(BalanceGradA
         const float c = fmaf(zc, lse, -dot);
         if (in) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int e = s + S * v;
-                if (e < E) a.d_logits[t * E + e] = on ? z[v] * (f[v] + c) : 0.f;
+            for (int v = 0; v < V; ++v) z[v] = on ? z[v] * (f[v] + c) : 0.f;
+#pragma unroll
+            for (int v = 0; v < V; v += B) {
+                const int e = expert_of<S, B>(s, v);
+                if (e >= E) continue;
+                if constexpr (B == 4) *(float4*)(a.d_logits + t * E + e) = make_float4(z[v], z[v + 1], z[v + 2], z[v + 3]);
+                else a.d_logits[t * E + e] = z[v];
             }
         }
     }
 }
 
 int forward_groups(int T, int E) {
-    if (T <= kOneGroup) return 1;
     const int per = kWaves * (E <= 16 ? 16 : 4);  // tokens of a workgroup at a time
+    if (T <= kOneGroup * per) return 1;
     return (int)min((int64_t)kMaxGroups, ceil_div64(T, per));
 }
 
-template <int S, int V>
+bool whole_chunks(int E, const void* a, const void* b) {
+    return E % 4 == 0 && (((uintptr_t)a | (uintptr_t)b) & 15u) == 0;
+}
+
+template <int S, int V, int B>
 hipError_t forward(const BalanceArgs& a, hipStream_t s) {
     const int groups = forward_groups(a.T, a.E);
-    hipLaunchKernelGGL((balance_kernel<S, V>), dim3(groups), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((balance_kernel<S, V, B>), dim3(groups), dim3(kThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || groups == 1) return e;
     int ep = 64;  // (fewer would leave one thread many sums to add)
@@ -318,12 +351,28 @@ hipError_t forward(const BalanceArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <int S, int V>
+template <int S, int V, int B>
 hipError_t gradient(const BalanceGradArgs& a, hipStream_t s) {
     const int64_t per = (kGradThreads / 64) * (64 / S);
     const int blocks = (int)min((int64_t)2048, ceil_div64(a.T, per));
-    hipLaunchKernelGGL((balance_grad_kernel<S, V>), dim3(blocks), dim3(kGradThreads), 0, s, a);
+    hipLaunchKernelGGL((balance_grad_kernel<S, V, B>), dim3(blocks), dim3(kGradThreads), 0, s, a);
     return hipGetLastError();
+}
+
+template <int B>
+hipError_t pick(const BalanceArgs& a, hipStream_t s) {
+    if (a.E <= 16) return forward<4, 4, B>(a, s);
+    if (a.E <= 64) return forward<16, 4, B>(a, s);
+    if (a.E <= 128) return forward<16, 8, B>(a, s);
+    return forward<16, 16, B>(a, s);
+}
+
+template <int B>
+hipError_t pick(const BalanceGradArgs& a, hipStream_t s) {
+    if (a.E <= 16) return gradient<4, 4, B>(a, s);
+    if (a.E <= 64) return gradient<16, 4, B>(a, s);
+    if (a.E <= 128) return gradient<16, 8, B>(a, s);
+    return gradient<16, 16, B>(a, s);
 }
 
 }  // namespace
@@ -334,17 +383,11 @@ size_t balance_ws_bytes(int T, int E) {
 }
 
 hipError_t launch_balance(const BalanceArgs& a, hipStream_t s) {
-    if (a.E <= 16) return forward<4, 4>(a, s);
-    if (a.E <= 64) return forward<16, 4>(a, s);
-    if (a.E <= 128) return forward<16, 8>(a, s);
-    return forward<16, 16>(a, s);
+    return whole_chunks(a.E, a.logits, nullptr) ? pick<4>(a, s) : pick<1>(a, s);
 }
 
 hipError_t launch_balance_grad(const BalanceGradArgs& a, hipStream_t s) {
-    if (a.E <= 16) return gradient<4, 4>(a, s);
-    if (a.E <= 64) return gradient<16, 4>(a, s);
-    if (a.E <= 128) return gradient<16, 8>(a, s);
-    return gradient<16, 16>(a, s);
+    return whole_chunks(a.E, a.logits, a.d_logits) ? pick<4>(a, s) : pick<1>(a, s);
 }
 
 }  // namespace bmoe

@@ -375,7 +375,7 @@ hipError_t launch_w8_gemm(const W8GemmArgs& a, hipStream_t s);
 // the same from activations x in bf16 (a.a not used), rounded by the product itself, where rows_cap * K is small
 bool w8_few_fits(const W8GemmArgs& a);
 hipError_t launch_w8_few(const W8GemmArgs& a, const void* x, hipStream_t s);
-// rows_cap of at most 64 rows a segment; false: the sizes are the large kernel's
+// whether the kernels for few rows take it (false: the large one)
 bool w8_skinny_fits(const W8GemmArgs& a);
 hipError_t launch_w8_skinny(const W8GemmArgs& a, hipStream_t s);
 

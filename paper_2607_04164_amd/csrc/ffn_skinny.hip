@@ -704,8 +704,33 @@ hipError_t launch_ffn_skinny(const FfnArgs& a, hipStream_t s, int part) {
     return hipSuccess;
 }
 
+// Up to 64 rows a segment on average, and above where the estimate below says so: the large kernel's 256-row tiles
+// often leave most of the CUs idle, and a round of its tiles takes as long as two to three of these. Rounds by the
+// number of workgroups with rows (half a pass, half a tile more a segment than its rows fill; one segment exactly); a
+// round's time by its 128-byte K-chunks, us: here 4 + 0.31 a chunk (gate/up 0.55), there 8 + 1.4, or where its K loops
+// are split 30 and its tiles' chunks over all CUs at 1.6 of that rate. us, here / the large kernel:
+//   gate/up, d = 2048, d_ff = 1408: 1 segment, 384 rows 13.4 / 29.1, 768 rows 25.7 / 31.9, 1536 rows 38.1 / 37.5; 4
+//     segments, 1200 rows 28.9 / 35.1, 2400 rows 52.9 / 37.5; 15 segments, 1200 rows 40.8 / 30.8; d_ff = 176, 15
+//     segments, 4500 rows 19.1 / 31.1
+//   down, d_ff = 1408: 4 segments, 1200 rows 22.3 / 27.6, 2400 rows 38.0 / 30.6; 15 segments, 960 rows 21.3 / 23.8, 1200
+//     rows 27.7 / 24.2; N = K = 4096: 4 segments, 600 rows 40.3 / 55.7, 1200 rows 67.0 / 61.0; N = 1000, K = 1048: 15
+//     segments, 1920 rows 18.5 / 21.5, 3000 rows 27.9 / 26.0; N = 4096, K = 14336 (split): 1 segment, 192 rows 36.1 /
+//     42.6, 384 rows 70.0 / 53.9; 4 segments, 300 rows 70.4 / 96.9, 600 rows 103.7 / 105.3
 bool w8_skinny_fits(const W8GemmArgs& a) {
-    return (int64_t)a.rows_cap <= (int64_t)kSkRows * a.n_seg && skinny_dma_fits(w8_params(a));
+    if (!skinny_dma_fits(w8_params(a))) return false;
+    const int64_t rows = a.rows_cap, n = a.n_seg;
+    if (rows <= kSkRows * n) return true;
+    const bool gated = a.w1.codes != nullptr;
+    const double cus = persistent_workgroups(), chunks = (double)(w8_pitch(a.K) / 128);
+    auto tiles = [&](int bm, int bn) {
+        const double m = n == 1 ? (double)ceil_div64(rows, bm) : (double)rows / bm + 0.5 * (double)n;
+        return m * ceil_div(a.N, bn);
+    };
+    const double here = ceil(tiles(kSkRows, kSkCols) / cus) * (4.0 + (gated ? 0.55 : 0.31) * chunks);
+    const double large = tiles(256, gated ? 128 : 256);
+    double there = ceil(large / cus) * (8.0 + 1.4 * chunks);
+    if (a.ws) there = fmin(there, 30.0 + large / cus * 1.6 * 1.4 * chunks);
+    return here <= there;
 }
 
 hipError_t launch_w8_skinny(const W8GemmArgs& a, hipStream_t s) {

@@ -118,11 +118,14 @@ hipError_t launch_q8(const W8QuantizeArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+constexpr int kShortRows = 512;
+
 template <typename E>
 hipError_t pick_q8(const W8QuantizeArgs& a, hipStream_t s) {
     const int units = (int)(w8_pitch(a.K) / 16);
+    // (few rows: a workgroup each, for their latency)
     if (units <= 64) return launch_q8<E, 64, 1>(a, s);
-    if (units <= 128) return launch_q8<E, 64, 2>(a, s);
+    if (units <= 128 && a.rows > kShortRows) return launch_q8<E, 64, 2>(a, s);
     if (units <= 256) return launch_q8<E, 256, 1>(a, s);
     if (units <= 512) return launch_q8<E, 256, 2>(a, s);
     return launch_q8<E, 256, 4>(a, s);

@@ -151,7 +151,7 @@ def test_even_picks_and_probabilities_give_one():
     assert float(B.balance_grad(z, o["counts"], k, torch.tensor([1.0, 0.0], device="cuda")).abs().max()) <= 4 * F32 / T
 
 
-@pytest.mark.parametrize("T", [40, 900])
+@pytest.mark.parametrize("T", [40, 900, 3000])
 def test_masks_and_infinities(T):
     """Tokens that do not count may hold anything; -inf is an expert of probability 0; a row of nothing else adds
     nothing; picks outside the experts pick nothing."""
@@ -219,6 +219,26 @@ def test_large_logits():
         with np.errstate(over="ignore"):
             z2 = np.float32(want[0][1])
         assert float(o["losses"][1]) == z2 or abs(float(o["losses"][1]) / z2 - 1) <= 1e-6
+
+
+@pytest.mark.parametrize("T,E,k", [(70, 8, 2), (900, 60, 4), (300, 128, 2), (700, 256, 8)])
+def test_rows_off_16_byte_chunks(T, E, k):
+    """E a multiple of four, the logits (or the gradient) a view that starts between 16-byte chunks: another path, the
+    same definition."""
+    z, idx, valid = make(T, T, E, k)
+    zd, id_, vd = device(z, idx, valid)
+    off = torch.empty(T * E + 1, device="cuda")[1:].view(T, E).copy_(zd)
+    d = torch.tensor([0.3, 0.2], device="cuda")
+    a, b = B.balance(zd, id_, valid=vd), B.balance(off, id_, valid=vd)
+    assert torch.equal(a["counts"], b["counts"])
+    # (either is off by what test_losses_and_gradient allows)
+    tol = 2 * (row_error(z).max() + (T / 64 + 34) * F32)
+    torch.testing.assert_close(a["prob"], b["prob"], rtol=tol, atol=0)
+    torch.testing.assert_close(a["losses"], b["losses"], rtol=4 * tol, atol=0)
+    g = B.balance_grad(zd, a["counts"], k, d, valid=vd)
+    size = float(g.abs().max())
+    for src, dst in ((off, None), (zd, torch.empty(T * E + 1, device="cuda")[1:].view(T, E))):
+        torch.testing.assert_close(B.balance_grad(src, a["counts"], k, d, valid=vd, out=dst), g, rtol=0, atol=8 * tol * size)
 
 
 def test_results_do_not_depend_on_the_run():

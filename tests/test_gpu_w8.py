@@ -90,7 +90,7 @@ def check_hidden(h, gate, up, what):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("rows,K", [(1, 8), (3, 40), (5, 128), (7, 136), (64, 1024), (33, 1048), (6, 2048), (9, 4096),
-                                    (4, 8192), (5, 8200), (3, 16384), (2, 20008), (2, 131072), (3001, 264)])
+                                    (4, 8192), (5, 8200), (3, 16384), (2, 20008), (2, 131072), (3001, 264), (600, 2048)])
 def test_quantize(rows, K, dtype):
     g = gen(rows * 7 + K)
     x = randn(g, rows, K, dtype=dtype) * torch.exp(2 * torch.randn((rows, 1), generator=g, device="cuda")).to(dtype)
@@ -175,7 +175,9 @@ CASES = [(1, 1, 8, 8), (1, 1, 4096, 1408), (1, 17, 24, 264), (3, 7, 40, 128), (5
          (60, 48, 176, 352), (60, 300, 1408, 256), (1, 64, 2816, 2048), (4, 12, 4096, 14336), (15, 40, 1408, 2048),
          (1, 9, 136, 2816),
          (1, 65, 72, 136), (5, 777, 1000, 1048), (3, 700, 264, 64), (2, 3000, 264, 520), (1, 1000, 8, 8),
-         (7, 2000, 136, 384), (1, 800, 1032, 128)]
+         (7, 2000, 136, 384), (1, 800, 1032, 128),
+         # large tiles: whole ones, and half ones for short segments; K of one K-step, N and rows inside a tile
+         (1, 9000, 1032, 136), (15, 6000, 520, 264), (40, 20000, 136, 40), (3, 40000, 72, 8), (2, 9000, 264, 1400)]
 
 
 @pytest.mark.parametrize("n,rows,N,K", CASES)
@@ -199,7 +201,8 @@ def test_w8_matmul(n, rows, N, K):
 
 
 @pytest.mark.parametrize("n,rows,f,d", [(1, 1, 24, 40), (1, 1, 1408, 2048), (4, 33, 200, 264), (8, 250, 72, 1408),
-                                        (15, 4, 1408, 2048), (3, 500, 136, 128), (2, 2000, 392, 264), (5, 900, 520, 72)])
+                                        (15, 4, 1408, 2048), (3, 500, 136, 128), (2, 2000, 392, 264), (5, 900, 520, 72),
+                                        (2, 9000, 392, 264), (15, 9000, 520, 72)])
 def test_w8_ffn(n, rows, f, d):
     g = gen(rows + f)
     wg, wu, wd = weights(g, n, f, d), weights(g, n, f, d), weights(g, n, d, f)
@@ -224,7 +227,8 @@ def test_w8_ffn(n, rows, f, d):
         assert torch.equal(y1, y) and torch.equal(h1, h)
 
 
-@pytest.mark.parametrize("n,rows,N,K", [(1, 1300, 1032, 8192), (4, 700, 520, 14336), (2, 257, 264, 20000)])
+@pytest.mark.parametrize("n,rows,N,K", [(1, 4000, 1032, 8192), (4, 9000, 520, 14336), (15, 9000, 520, 14336),
+                                        (2, 257, 264, 20000)])
 def test_split_tiles_have_the_same_bits(n, rows, N, K):
     """K long enough that the last tiles' K loops are split over the workgroups."""
     g = gen(K)
@@ -243,7 +247,7 @@ def test_split_tiles_have_the_same_bits(n, rows, N, K):
     check_hidden(h, products64(q, s, offs, w), products64(q, s, offs, w1), "gated")
 
 
-@pytest.mark.parametrize("rows,first,last", [(90, 5, 61), (2000, 300, 1500)])
+@pytest.mark.parametrize("rows,first,last", [(90, 5, 61), (2000, 300, 1500), (20000, 300, 15000)])
 def test_rows_of_no_segment_stay_as_they_are(rows, first, last):
     g = gen(rows)
     n, d, f = 3, 160, 136
@@ -270,7 +274,7 @@ def test_rows_of_no_segment_stay_as_they_are(rows, first, last):
     assert bool((y == 7).all())
 
 
-@pytest.mark.parametrize("rows", [4, 300])
+@pytest.mark.parametrize("rows", [4, 300, 60000])
 def test_source_rows_out_of_range_are_clamped(rows):
     g = gen(rows)
     w = weights(g, 1, 32, 64)
@@ -280,7 +284,7 @@ def test_source_rows_out_of_range_are_clamped(rows):
     assert torch.equal(B.w8_matmul(off, a, w, a_rows=src), B.w8_matmul(off, a, w, a_rows=src.clamp(0, 3)))
 
 
-@pytest.mark.parametrize("rows", [5, 400])
+@pytest.mark.parametrize("rows", [5, 400, 40000])
 def test_values_that_are_not_finite_stay_in_their_rows_and_channels(rows):
     g = gen(rows)
     n, d, f = 2, 264, 72
@@ -298,7 +302,7 @@ def test_values_that_are_not_finite_stay_in_their_rows_and_channels(rows):
     assert bool(torch.isnan(y[bad].float()).all()) and torch.equal(y[~bad], clean[~bad])
 
 
-@pytest.mark.parametrize("rows", [3, 300])
+@pytest.mark.parametrize("rows", [3, 300, 60000])
 def test_scales_far_apart(rows):
     """Scales near both ends of fp32 whose products, or whose products with the sum, would leave it on the way."""
     K, N = 128, 8
@@ -321,7 +325,7 @@ def test_scales_far_apart(rows):
     assert bool(((y.double() - want).abs() <= tol)[fits].all())
 
 
-@pytest.mark.parametrize("n,rows", [(65, 64), (200, 300), (256, 20000)])
+@pytest.mark.parametrize("n,rows", [(65, 64), (200, 300), (256, 20000), (256, 90000)])
 def test_more_segments_than_lanes(n, rows):
     g = gen(n)
     N, K = 24, 72
@@ -348,7 +352,7 @@ def test_largest_sums():
         check_product(y, products64(*rounded64(a), [0, rows], w), f"{rows} rows")
 
 
-@pytest.mark.parametrize("n,rows,f,d", [(4, 40, 96, 256), (3, 900, 264, 392)])
+@pytest.mark.parametrize("n,rows,f,d", [(3, 9, 96, 256), (4, 40, 96, 256), (3, 9000, 520, 136)])
 def test_stream_and_graph(n, rows, f, d):
     g = gen(9)
     ws = weights(g, n, f, d), weights(g, n, f, d), weights(g, n, d, f)

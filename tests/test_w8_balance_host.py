@@ -165,9 +165,10 @@ def w8(codes=PTR):
     return struct(B._W8Struct(codes, PTR))
 
 
-def product(n, rows, N, K, gated=False, ws=1 << 33, **device):
+def product(n, rows, N, K, gated=False, ws=1 << 36, a8=False, **device):
     far = ["p", 1 << 40]
-    args = [*ints(1, n, rows, *((K, N) if gated else (N, K))), ["p", PTR], ["p", 0], ["i", 0], ["p", 0], w8(), w8()]
+    a = [["p", 0], w8()] if a8 else [["p", PTR], ["p", 0]]
+    args = [*ints(1, n, rows, *((K, N) if gated else (N, K))), ["p", PTR], ["p", 0], ["i", 0], *a, w8()]
     args += ([w8()] if gated else []) + [far, ["p", 1 << 41], ["z", ws], ["p", 0]]
     return {"fn": f"brownout_moe_w8_{'gate_up' if gated else 'matmul'}", "args": args, **device}
 
@@ -182,14 +183,20 @@ def launched(calls, tmp_path):
 def test_every_kernel_is_run_by_a_test_case(tmp_path):
     import test_gpu_balance as TB
     import test_gpu_w8 as T8
-    calls = [product(*c) for c in T8.CASES] + [product(n, rows, f, d, True) for n, rows, f, d in
-                                               [(1, 1, 1408, 2048), (8, 250, 72, 1408), (2, 2000, 392, 264),
-                                                (5, 900, 520, 72), (1, 1300, 1032, 8192), (1, 1, 24, 40)]]
-    calls += [product(1, 1300, 1032, 8192)]  # test_split_tiles_have_the_same_bits
-    calls += [{"fn": "brownout_moe_w8_quantize", "args": [*ints(t, 2, K), ["p", PTR], ["p", 1 << 40], ["p", 1 << 41],
-                                                          ["p", 0]]} for t in (0, 1) for K in (8, 1048, 4096, 8192, 20008)]
+    calls = [product(*c, a8=a8) for c in T8.CASES for a8 in (False, True)]
+    # test_w8_ffn, test_split_tiles_have_the_same_bits
+    calls += [product(n, rows, f, d, True) for n, rows, f, d in [
+        (1, 1, 1408, 2048), (8, 250, 72, 1408), (1, 1, 24, 40), (2, 9000, 392, 264), (15, 9000, 520, 72), (4, 33, 200, 264),
+        (4, 9000, 520, 14336)]]
+    calls += [product(1, 1, 1408, 2048, True, a8=True), product(4, 9000, 520, 14336)]
+    calls += [{"fn": "brownout_moe_w8_quantize", "args": [*ints(t, rows, K), ["p", PTR], ["p", 1 << 40], ["p", 1 << 41],
+                                                          ["p", 0]]}
+              for t in (0, 1) for rows, K in ((1, 8), (600, 2048), (9, 4096), (4, 8192), (2, 20008))]
     for T, E, k in TB.SIZES:
-        calls += [{"fn": "brownout_moe_balance", "args": [*ints(T, E, k, E), ["p", PTR], ["p", PTR], ["p", 0], ["p", 0],
+        calls += [{"fn": "brownout_moe_balance", "args": [*ints(T, E, k, E), ["p", PTR + 4], ["p", PTR], ["p", 0], ["p", 0],
+                                                          ["p", 1 << 40], ["p", 1 << 41], ["p", 1 << 42], ["p", 1 << 43],
+                                                          ["z", 1 << 30], ["p", 0]]},  # (test_rows_off_16_byte_chunks)
+                  {"fn": "brownout_moe_balance", "args": [*ints(T, E, k, E), ["p", PTR], ["p", PTR], ["p", 0], ["p", 0],
                                                           ["p", 1 << 40], ["p", 1 << 41], ["p", 1 << 42], ["p", 1 << 43],
                                                           ["z", 1 << 30], ["p", 0]]},
                   {"fn": "brownout_moe_balance_grad", "args": [*ints(T, E, k, E), ["p", PTR], ["p", 0], ["p", 0], ["p", PTR],
@@ -202,16 +209,32 @@ def test_every_kernel_is_run_by_a_test_case(tmp_path):
 
 @needs_recorder
 def test_product_choice(tmp_path):
-    """Few rows on the weight-streaming kernels, more on the large tiles (half ones where segments are short); the
-    fixup only with the room for it and where K can be split."""
-    cases = [((1, 64, 512, 4096), ["skinny"]), ((1, 65, 512, 4096), ["dma_kernel<false, true"]),
-             ((4, 4 * 768, 512, 4096), ["dma_kernel<false, false"]),
-             ((1, 1300, 1032, 8192), ["dma_kernel<false, false", "fixup"]), ((1, 1300, 1032, 6144), ["dma_kernel<false, false"])]
+    """Very few rows round their activations themselves; few rows, and more where the large tiles would leave the CUs
+    idle, take the weight-streaming kernels; else the large tiles (half ones where segments are short), with the
+    fixup where there is room for it and K is long."""
+    few, skinny, whole, half = "few8_kernel", "skinny_", "grouped_gemm_dma_kernel<false, false", "grouped_gemm_dma_kernel<false, true"
+    cases = [((15, 4, 2048, 1408), [few]), ((1, 4, 512, 4096), [few]), ((1, 5, 512, 4096), ["q8_", skinny]),
+             ((1, 17, 512, 128), ["q8_", skinny]), ((4, 256, 4096, 4096), ["q8_", skinny]),
+             # both sides of the estimate
+             ((1, 1536, 2048, 1408), ["q8_", skinny]), ((4, 1200, 2048, 1408), ["q8_", skinny]),
+             ((15, 1200, 2048, 1408), ["q8_", half]), ((4, 2400, 2048, 1408), ["q8_", half]),
+             ((4, 600, 4096, 4096), ["q8_", skinny]), ((4, 4800, 4096, 4096), ["q8_", whole]),
+             ((1, 192, 4096, 14336), ["q8_", skinny]), ((1, 384, 4096, 14336), ["q8_", half, "fixup"]),
+             ((1, 4000, 1032, 8192), ["q8_", whole, "fixup"]), ((1, 40000, 1032, 6144), ["q8_", whole])]
     for case, want in cases:
         ls, = launched([product(*case)], tmp_path)
-        assert len(ls) == len(want) and all(w in name and "OpI8" in name for w, (name, _) in zip(want, ls)), (case, ls)
-    ls, = launched([product(1, 1300, 1032, 8192, ws=0)], tmp_path)
-    assert len(ls) == 1
+        assert [w for w, (name, _) in zip(want, ls) if w in name] == want and len(ls) == len(want), (case, ls)
+    # activations that are rounded already, no room for a split
+    assert len(launched([product(15, 4, 2048, 1408, a8=True)], tmp_path)[0]) == 1
+    assert len(launched([product(1, 4000, 1032, 8192, a8=True, ws=0)], tmp_path)[0]) == 1
     # a source too large for the few-row copies' 32-bit offsets
-    ls, = launched([product(256, 256 * 64, 64, 131072)], tmp_path)
+    ls, = launched([product(256, 256 * 64, 64, 131072, a8=True)], tmp_path)
     assert "grouped_gemm_dma_kernel" in ls[0][0]
+
+
+@needs_recorder
+def test_choice_follows_the_cu_count(tmp_path):
+    """On half of the chip the few-row tiles take twice the rounds."""
+    names = [launched([product(4, 1200, 2048, 1408, cus=c, device=40 + i)], tmp_path)[0][1][0]
+             for i, c in enumerate((256, 128))]
+    assert "skinny_dma" in names[0] and "grouped_gemm" in names[1]
