@@ -135,6 +135,9 @@ struct Parts {
     float* p;
     int* c;
 };
+__host__ __device__ inline size_t parts_bytes(int groups, int E) {
+    return ((size_t)groups * (8 + 4 * (size_t)E + 4 * (size_t)(E + 1)) + 7) / 8 * 8;
+}
 __host__ __device__ inline Parts parts_of(void* ws, int groups, int E) {
     Parts q;
     q.z = (double*)ws;
@@ -216,13 +219,60 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     finish(a, sums);
 }
 
+// Many workgroups' sums of many experts, kFold at a time, by several workgroups first: one workgroup alone reads them
+// at its CU's rate (256 workgroups' of 256 experts 11 us; 4 here, and 4 for the join of what is left).
+constexpr int kFold = 32;
+constexpr int kFoldThreads = 256;
+__global__ __launch_bounds__(kFoldThreads) void balance_fold_kernel(void* from, int groups, void* to, int E) {
+    constexpr int J = kFoldThreads / 64, PER = kFold / J;
+    __shared__ double s_p[J][64];
+    __shared__ int s_c[J][64];
+    const int lane = threadIdx.x & 63, j = threadIdx.x >> 6, e = blockIdx.y * 64 + lane;
+    const int g0 = blockIdx.x * kFold + j * PER;
+    const Parts a = parts_of(from, groups, E), b = parts_of(to, gridDim.x, E);
+    float pv[PER];
+    int cv[PER];
+    double p = 0.0;
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const size_t g = min(g0 + i, groups - 1);
+        pv[i] = a.p[g * E + min(e, E - 1)];
+        cv[i] = a.c[g * (E + 1) + min(e, E)];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const bool in = g0 + i < groups;
+        p += in ? (double)pv[i] : 0.0;
+        c += in ? cv[i] : 0;
+    }
+    s_p[j][lane] = p;
+    s_c[j][lane] = c;
+    __syncthreads();
+    if (j == 0) {
+#pragma unroll
+        for (int i = 1; i < J; ++i) {
+            p += s_p[i][lane];
+            c += s_c[i][lane];
+        }
+        if (e < E) b.p[(size_t)blockIdx.x * E + e] = (float)p;
+        if (e <= E) b.c[(size_t)blockIdx.x * (E + 1) + e] = c;
+        if (e == 0) {
+            double z = 0.0;
+            for (int g = blockIdx.x * kFold; g < min((int)(blockIdx.x + 1) * kFold, groups); ++g) z += a.z[g];
+            b.z[blockIdx.x] = z;
+        }
+    }
+}
+
 // The workgroups' sums, in order. ep: a power of two, E or more.
-__global__ __launch_bounds__(kThreads) void balance_join_kernel(BalanceArgs a, int groups, int ep) {
+__global__ __launch_bounds__(kThreads) void balance_join_kernel(BalanceArgs a, void* parts, int groups, int ep) {
     __shared__ Sums sums;
     __shared__ double s_p[kThreads];
     __shared__ int s_c[kThreads];
     const int tid = threadIdx.x, E = a.E, e = tid % ep, j = tid / ep, J = kThreads / ep;
-    const Parts q = parts_of(a.ws, groups, E);
+    const Parts q = parts_of(parts, groups, E);
     double p = 0.0;
     int c = 0;
     // (one workgroup's latency: kAhead loads of each in flight, those past the end of the last row instead of branches)
@@ -335,6 +385,8 @@ int forward_groups(int T, int E) {
     return (int)min((int64_t)kMaxGroups, ceil_div64(T, per));
 }
 
+bool folds(int groups, int E) { return groups * E > 40960; }
+
 bool whole_chunks(int E, const void* a, const void* b) {
     return E % 4 == 0 && (((uintptr_t)a | (uintptr_t)b) & 15u) == 0;
 }
@@ -347,7 +399,15 @@ hipError_t forward(const BalanceArgs& a, hipStream_t s) {
     if (e != hipSuccess || groups == 1) return e;
     int ep = 64;  // (fewer would leave one thread many sums to add)
     while (ep < a.E) ep *= 2;
-    hipLaunchKernelGGL(balance_join_kernel, dim3(1), dim3(kThreads), 0, s, a, groups, ep);
+    if (!folds(groups, a.E)) {
+        hipLaunchKernelGGL(balance_join_kernel, dim3(1), dim3(kThreads), 0, s, a, a.ws, groups, ep);
+        return hipGetLastError();
+    }
+    void* folded = (char*)a.ws + parts_bytes(groups, a.E);
+    const int left = ceil_div(groups, kFold);
+    hipLaunchKernelGGL(balance_fold_kernel, dim3(left, ceil_div(a.E + 1, 64)), dim3(kFoldThreads), 0, s, a.ws, groups, folded,
+                       a.E);
+    hipLaunchKernelGGL(balance_join_kernel, dim3(1), dim3(kThreads), 0, s, a, folded, left, ep);
     return hipGetLastError();
 }
 
@@ -378,8 +438,8 @@ hipError_t pick(const BalanceGradArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t balance_ws_bytes(int T, int E) {
-    const size_t g = forward_groups(T, E);
-    return g == 1 ? 0 : g * (8 + 4 * (size_t)E + 4 * (size_t)(E + 1));
+    const int g = forward_groups(T, E);
+    return g == 1 ? 0 : parts_bytes(g, E) + (folds(g, E) ? parts_bytes(ceil_div(g, kFold), E) : 0);
 }
 
 hipError_t launch_balance(const BalanceArgs& a, hipStream_t s) {

@@ -74,7 +74,7 @@ def device(*arrays):
 
 # one workgroup and several, each lane layout and its edges, more tokens than a round
 SIZES = [(1, 1, 1), (1, 2, 1), (3, 7, 2), (64, 8, 2), (17, 16, 4), (65, 17, 3), (64, 64, 6), (513, 60, 4), (600, 65, 1),
-         (1001, 128, 8), (777, 129, 16), (2049, 256, 8), (20000, 4, 2), (40000, 64, 6)]
+         (1001, 128, 8), (777, 129, 16), (2049, 256, 8), (20000, 4, 2), (40000, 64, 6), (9001, 131, 5), (20011, 256, 3)]
 
 
 @pytest.mark.parametrize("grouped", [False, True], ids=["experts", "groups"])
