@@ -365,18 +365,18 @@ struct DmaCfg {
     static constexpr int DMA_PER_STAGE = A_DMA + B_DMA;
     static constexpr int A_STAGE = BM * ROW_BYTES, B_STAGE = RB * ROW_BYTES;
     static constexpr int STAGE = A_STAGE + B_STAGE;
-    static constexpr int SROW = WTN + 8;
+    static constexpr int SCOLS = 64, SROW = SCOLS + 8;
     static constexpr int RING = 2 * STAGE;
-    // epilogue staging: each wave its own 16 rows x WTN, outside the ring, so
+    // epilogue staging: each wave its own 32 rows x SCOLS, outside the ring, so
     // the next tile's first copies can land while a tile's results go out
-    static constexpr int HSTG = 16 * SROW * 2;
+    static constexpr int HSTG = 32 * SROW * 2;
     static constexpr int STG_OFF = RING;
     static constexpr int SCHED_OFF = STG_OFF + 4 * HSTG;                 // schedule arrays after them
     static constexpr int SCHED = 2 * 4 * 8 + (4 * BMOE_MAX_EXPERTS + 1) * 4;
     // int8: the scales of a tile's A rows and B rows, for this work item and the next
     static constexpr int SCL_OFF = (SCHED_OFF + SCHED + 15) / 16 * 16, SCL = (BM + RB) * 4;
     static constexpr int SMEM = OP::kScales ? SCL_OFF + 2 * SCL : SCHED_OFF + SCHED;
-    static constexpr int CPR = WTN / 8;                                   // 16-byte chunks per output row
+    static constexpr int CPR = SCOLS / 8;                                 // 16-byte chunks per staged row
     static constexpr int NACC4 = NMAT * MB * NB * 4;                      // float4 accumulators per lane
     static_assert(KC == 8 && BM == 256 && RB == 256, "tile shape");
     static_assert(SUB % 2 == 0, "fragment double buffer alternates within a K-step");
@@ -489,7 +489,8 @@ __device__ __forceinline__ void mfmas_ops(typename C::acc16 (&acc)[C::NMAT][C::M
 #pragma unroll
     for (int q = 0; q < NM; ++q) {
         const int mb = q / (C::NMAT * C::NB), mat = (q / C::NB) % C::NMAT, nb = q % C::NB;
-        acc[mat][mb][nb] = C::OP::mma32(af[mb], bf[mat][nb], acc[mat][mb][nb]);
+        // (B's rows as the result's rows: a lane then holds four neighbouring columns of one row)
+        acc[mat][mb][nb] = C::OP::mma32(bf[mat][nb], af[mb], acc[mat][mb][nb]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int r = q * RD * NR / NM; r < (q + 1) * RD * NR / NM; ++r) {
@@ -1027,7 +1028,8 @@ __device__ __forceinline__ void store_tile(const typename C::acc16 (&acc)[C::NMA
                                            char* piece = nullptr) {
     const int wm = wave >> 1, wn = wave & 1;
     uint16_t* st = (uint16_t*)(smem + C::STG_OFF + wave * C::HSTG);
-    const int l32 = lane & 31;
+    // accumulator element i of block (mb, nb): row l32, column 8 (i / 4) + 4 hi + i % 4
+    const int l32 = lane & 31, hi = lane >> 5;
     const int row0 = tc.m0, col0 = tc.n0 + wn * C::WTN;
     wait_vmcnt<0>();  // the copies of the next item's first two K-steps have landed (kAfterStores)
     if (MB == C::MB && piece) {  // (split tiles are whole)
@@ -1049,94 +1051,87 @@ __device__ __forceinline__ void store_tile(const typename C::acc16 (&acc)[C::NMA
             }
         return;
     }
-    float cs[C::NMAT][C::NB];  // int8: the scales of the lane's columns
+    // int8: the scales of the wave's rows and columns
+    const float* row_scales = (const float*)scl + dma_arow(wm, 0, MB);
+    const float* col_scales = (const float*)scl + C::BM + wn * C::WTN;
+    // whether they are all such that the products below stay in fp32's range on the way: else the values are formed
+    // and stored again at the end (the test by value, in scaled, costs three operations more for each: gate/up of 4096
+    // rows, d = 2048 126.3 -> 133.8 us)
+    bool plain = true;
+    if constexpr (C::OP::kScales) {
+#pragma unroll
+        for (int i = 0; i < MB / 2; ++i) plain = plain && plain_scale(row_scales[i * 64 + lane]);
+#pragma unroll
+        for (int mat = 0; mat < C::NMAT; ++mat)
+#pragma unroll
+            for (int i = 0; i < C::WTN; i += 64) plain = plain && plain_scale(col_scales[mat * C::BN + i + lane]);
+        plain = __all(plain);
+    }
+    float4 cs[C::NMAT][C::NB][4];  // the lane's columns' scales
     if constexpr (C::OP::kScales) {
 #pragma unroll
         for (int mat = 0; mat < C::NMAT; ++mat)
 #pragma unroll
             for (int nb = 0; nb < C::NB; ++nb)
-                cs[mat][nb] = ((const float*)scl)[C::BM + mat * C::BN + wn * C::WTN + nb * 32 + l32];
-    }
-    // whether the wave's scales are all such that the products below stay in fp32's range on the way: else the values
-    // are formed and stored again at the end (the test by value, in scaled, costs three operations more for each:
-    // gate/up of 4096 rows, d = 2048 126.3 -> 133.8 us)
-    bool plain = true;
-    if constexpr (C::OP::kScales) {
 #pragma unroll
-        for (int mat = 0; mat < C::NMAT; ++mat)
-#pragma unroll
-            for (int nb = 0; nb < C::NB; ++nb) plain = plain && plain_scale(cs[mat][nb]);
-#pragma unroll
-        for (int i = 0; i < MB / 2; ++i) plain = plain && plain_scale(((const float*)scl)[dma_arow(wm, 0, MB) + i * 64 + lane]);
-        plain = __all(plain);
+                for (int g = 0; g < 4; ++g)
+                    cs[mat][nb][g] = *(const float4*)(col_scales + mat * C::BN + nb * 32 + 8 * g + 4 * hi);
     }
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
         if (row0 + dma_arow(wm, mb, MB) >= tc.m_end) continue;  // a block wholly past the segment
+        float rs = 1.f;
+        if constexpr (C::OP::kScales) rs = row_scales[mb * 32 + l32];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            // rows 16h .. 16h+15 of the 32-row block: accumulator elements 8h .. 8h+7
+        for (int n2 = 0; n2 < C::NB; n2 += 2) {
+            // SCOLS columns of the block: all values first, each step over all of them, so the SiLU chains (exp, add,
+            // reciprocal, products) of different elements overlap instead of running one after another
             __builtin_amdgcn_sched_barrier(0);
-            // the half block's values first, each step over all of them, so
-            // the SiLU chains (exp, add, reciprocal, products) of different
-            // elements overlap instead of running one after another
-            float v[C::NB][8];
-            float4 rs[2];  // int8: the scales of the lane's eight rows
-            if constexpr (C::OP::kScales) {
-                const float* at = (const float*)scl + dma_arow(wm, mb, MB) + 16 * h + 4 * (lane >> 5);
-                rs[0] = *(const float4*)at;
-                rs[1] = *(const float4*)(at + 8);
-            }
-            auto values = [&](float (&to)[C::NB][8], int mat) {
+            auto values = [&](float (&to)[2][16], int mat) {
 #pragma unroll
-                for (int nb = 0; nb < C::NB; ++nb)
+                for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const auto x = acc_read(acc[mat][mb][nb][8 * h + e]);
+                    for (int i = 0; i < 16; ++i) {
+                        const auto x = acc_read(acc[mat][mb][n2 + nb][i]);
                         if constexpr (C::OP::kScales)
-                            to[nb][e] = (float)x * ((const float*)&rs[e >> 2])[e & 3] * cs[mat][nb];
-                        else to[nb][e] = x;
+                            to[nb][i] = (float)x * rs * ((const float*)&cs[mat][n2 + nb][i / 4])[i % 4];
+                        else to[nb][i] = x;
                     }
             };
+            float v[2][16];
             values(v, 0);
             if constexpr (GATED) {
-                float u[C::NB][8], t[C::NB][8];
+                float u[2][16], s[2][16];
                 values(u, 1);
 #pragma unroll
-                for (int nb = 0; nb < C::NB; ++nb)
+                for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) t[nb][e] = __expf(-v[nb][e]);
+                    for (int i = 0; i < 16; ++i) s[nb][i] = __expf(-v[nb][i]);
 #pragma unroll
-                for (int nb = 0; nb < C::NB; ++nb)
+                for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) t[nb][e] = __builtin_amdgcn_rcpf(1.f + t[nb][e]);
+                    for (int i = 0; i < 16; ++i) s[nb][i] = __builtin_amdgcn_rcpf(1.f + s[nb][i]);
 #pragma unroll
-                for (int nb = 0; nb < C::NB; ++nb)
+                for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[nb][e] = v[nb][e] * t[nb][e] * u[nb][e];
+                    for (int i = 0; i < 16; ++i) v[nb][i] = v[nb][i] * s[nb][i] * u[nb][i];
             }
 #pragma unroll
-            for (int nb = 0; nb < C::NB; ++nb)
+            for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
-                for (int i = 8 * h; i < 8 * h + 8; i += 2) {
-                    const float v0 = v[nb][i - 8 * h], v1 = v[nb][i + 1 - 8 * h];
-                    const uint32_t pk = pack_bf16x2_hw(v0, v1);
-                    const int r = 8 * ((i >> 2) - 2 * h) + 4 * (lane >> 5) + (i & 3);
-                    const int c = nb * 32 + l32;
-                    st[r * C::SROW + c] = (uint16_t)pk;
-                    st[(r + 1) * C::SROW + c] = (uint16_t)(pk >> 16);
-                }
+                for (int i = 0; i < 16; i += 4)
+                    *(uint2*)(st + l32 * C::SROW + nb * 32 + 2 * i + 4 * hi) =
+                        make_uint2(pack_bf16x2_hw(v[nb][i], v[nb][i + 1]), pack_bf16x2_hw(v[nb][i + 2], v[nb][i + 3]));
             // the wave reads back only what it wrote (LDS operations of a wave
-            // complete in order), then the next half block reuses the area
+            // complete in order), then the next columns reuse the area
 #pragma unroll
-            for (int k = 0; k < 16 * C::CPR / 64; ++k) {
-                const int c = lane + 64 * k;
-                const int rr = c / C::CPR, cc = c % C::CPR;
-                const int gm = row0 + dma_arow(wm, mb, MB) + 16 * h + rr, gn = col0 + cc * 8;
-                const uint4 v = *(const uint4*)(st + rr * C::SROW + cc * 8);
+            for (int k = 0; k < 32 * C::CPR / 64; ++k) {
+                const int rr = lane / C::CPR + k * (64 / C::CPR), cc = lane % C::CPR;
+                const int gm = row0 + dma_arow(wm, mb, MB) + rr, gn = col0 + n2 * 32 + cc * 8;
+                const uint4 o = *(const uint4*)(st + rr * C::SROW + cc * 8);
                 if (gm < tc.m_end && gn < p.N) {
-                    if constexpr (FOLD) store_coherent(p.C + (size_t)gm * p.N + gn, v);
-                    else *(uint4*)(p.C + (size_t)gm * p.N + gn) = v;
+                    if constexpr (FOLD) store_coherent(p.C + (size_t)gm * p.N + gn, o);
+                    else *(uint4*)(p.C + (size_t)gm * p.N + gn) = o;
                 }
             }
         }
@@ -1144,18 +1139,21 @@ __device__ __forceinline__ void store_tile(const typename C::acc16 (&acc)[C::NMA
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (C::OP::kScales) {
         if (!plain) {
+            int lane2 = lane;  // (nothing of this is to be formed ahead and kept)
+            asm volatile("" : "+v"(lane2));
+            const int l32 = lane2 & 31, hi = lane2 >> 5;
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     __builtin_amdgcn_sched_barrier(0);
-                    const int r = dma_arow(wm, mb, MB) + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
-                    const float rs = ((const float*)scl)[r];
+                    const int r = mb * 32 + l32, gm = row0 + dma_arow(wm, 0, MB) + r;
+                    const float rs = row_scales[r];
 #pragma unroll
                     for (int nb = 0; nb < C::NB; ++nb) {
-                        float v = scaled(acc_read(acc[0][mb][nb][i]), rs, cs[0][nb]);
-                        if (GATED) v = silu_mul(v, scaled(acc_read(acc[C::NMAT - 1][mb][nb][i]), rs, cs[C::NMAT - 1][nb]));
-                        const int gm = row0 + r, gn = col0 + nb * 32 + l32;
+                        const int c = nb * 32 + 8 * (i / 4) + 4 * hi + i % 4, gn = col0 + c;
+                        float v = scaled(acc_read(acc[0][mb][nb][i]), rs, col_scales[c]);
+                        if (GATED) v = silu_mul(v, scaled(acc_read(acc[C::NMAT - 1][mb][nb][i]), rs, col_scales[C::BN + c]));
                         if (gm < tc.m_end && gn < p.N) p.C[(size_t)gm * p.N + gn] = (uint16_t)pack_bf16x2_hw(v, 0.f);
                     }
                 }
@@ -1274,7 +1272,7 @@ __global__ __launch_bounds__(kGemmThreads, 1) void grouped_gemm_dma_kernel(GemmP
 // parts of the tile's accumulator slots, so a split tile is finished by
 // kFixSplit workgroups at once. Each thread adds its float4 slots of the
 // pieces in the order of the pieces, as the unsplit path would (eight
-// pieces' loads in flight), and writes its four rows of one column straight
+// pieces' loads in flight), and writes its four columns of one row straight
 // to the output.
 constexpr int kFixSplit = 32;
 constexpr int kFixInflight = 8;
@@ -1357,30 +1355,25 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_fixup_kernel(GemmParams p, 
         for (int k = 0; k < QPER; ++k) {
             const int qq = qs * QPER + k;  // slot (mb, nb, i4) in the order of store_tile's pieces
             const int i4 = qq & 3, nb = (qq >> 2) % C::NB, mb = (qq >> 2) / C::NB;
-            const int r0 = dma_arow(wm, mb, C::MB) + 8 * i4 + 4 * (lane >> 5);  // (split tiles are whole)
-            const int gn = tc.n0 + wn * C::WTN + nb * 32 + (lane & 31);
+            const int gm = tc.m0 + dma_arow(wm, mb, C::MB) + (lane & 31);  // (split tiles are whole)
+            const int gn = tc.n0 + wn * C::WTN + nb * 32 + 8 * i4 + 4 * (lane >> 5);
+            if (gm >= tc.m_end || gn >= p.N) continue;  // (N is a multiple of 8)
             const acc4 g4 = sum[k][0], u4 = sum[k][C::NMAT - 1];
-            float cs[2] = {1.f, 1.f};
+            float v[4];
             if constexpr (OP::kScales) {
-                const size_t col = (size_t)tc.s * p.N + min(gn, p.N - 1);
-                cs[0] = p.sb0[col];
-                if (GATED) cs[1] = p.sb1[col];
-            }
+                const float rs = p.sa[gathered_row(p.a_rows, p.a_count, gm)];
+                const float4 c0 = *(const float4*)(p.sb0 + (size_t)tc.s * p.N + gn);
+                const float4 c1 = GATED ? *(const float4*)(p.sb1 + (size_t)tc.s * p.N + gn) : c0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int gm = tc.m0 + r0 + j;
-                float g, u;
-                if constexpr (OP::kScales) {
-                    const float rs = p.sa[gathered_row(p.a_rows, p.a_count, min(gm, tc.m_end - 1))];
-                    g = scaled(g4[j], rs, cs[0]);
-                    u = scaled(u4[j], rs, cs[1]);
-                } else {
-                    g = g4[j];
-                    u = u4[j];
+                for (int j = 0; j < 4; ++j) {
+                    v[j] = scaled(g4[j], rs, ((const float*)&c0)[j]);
+                    if (GATED) v[j] = silu_mul(v[j], scaled(u4[j], rs, ((const float*)&c1)[j]));
                 }
-                const float v = GATED ? silu_mul(g, u) : g;
-                if (gm < tc.m_end && gn < p.N) p.C[(size_t)gm * p.N + gn] = (uint16_t)pack_bf16x2_hw(v, 0.f);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = GATED ? silu_mul(g4[j], u4[j]) : g4[j];
             }
+            *(uint2*)(p.C + (size_t)gm * p.N + gn) = make_uint2(pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3]));
         }
     }
 }

@@ -54,20 +54,35 @@ struct SkinnyParams {
     const float* sb1 = nullptr;
 };
 
-// Output values of columns col .. col+3 and row `row` of segment s from their sums.
-template <bool GATED, class OP, typename S>
-__device__ __forceinline__ void sk_values(float (&v)[4], const S& g, const S& u, const SkinnyParams& p, int s, int row,
-                                          int col) {
+// int8: the scales of columns col .. col+3 of segment s (N is a multiple of 8, so they are a quarter of a row's; columns
+// past N are not stored) and of row `row`. Loaded ahead of the sums, so the epilogue waits for nothing.
+struct SkScales {
+    float4 c0, c1;
+};
+template <bool GATED, class OP>
+__device__ __forceinline__ SkScales sk_col_scales(const SkinnyParams& p, int s, int col) {
+    SkScales r;
     if constexpr (OP::kScales) {
-        const float rs = p.sa[gathered_row(p.a_rows, p.a_count, row)];
-        // (N is a multiple of 8, so that is one quarter of a row of scales; columns past N are not stored)
         const size_t at = (size_t)s * p.N + min(col, p.N - 4);
-        const float4 c0 = *(const float4*)(p.sb0 + at);
-        const float4 c1 = GATED ? *(const float4*)(p.sb1 + at) : c0;
+        r.c0 = *(const float4*)(p.sb0 + at);
+        r.c1 = GATED ? *(const float4*)(p.sb1 + at) : r.c0;
+    }
+    return r;
+}
+template <class OP>
+__device__ __forceinline__ float sk_row_scale(const SkinnyParams& p, int row) {
+    if constexpr (OP::kScales) return p.sa[gathered_row(p.a_rows, p.a_count, row)];
+    return 1.f;
+}
+
+// Output values of four columns of a row from their sums.
+template <bool GATED, class OP, typename S>
+__device__ __forceinline__ void sk_values(float (&v)[4], const S& g, const S& u, const SkScales& c, float rs) {
+    if constexpr (OP::kScales) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float x = scaled(g[i], rs, ((const float*)&c0)[i]);
-            v[i] = GATED ? silu_mul(x, scaled(u[i], rs, ((const float*)&c1)[i])) : x;
+            const float x = scaled(g[i], rs, ((const float*)&c.c0)[i]);
+            v[i] = GATED ? silu_mul(x, scaled(u[i], rs, ((const float*)&c.c1)[i])) : x;
         }
     } else {
 #pragma unroll
@@ -345,6 +360,11 @@ __global__ __launch_bounds__(kSkThreads, 1) void skinny_dma_kernel(SkinnyParams 
                 off[i] = (uint32_t)((size_t)arow * K * 2 + ((lchk ^ (row & 7)) << 4));
             }
         }
+        const int col = n0 + wave * 16 + 4 * q;
+        const SkScales cs = sk_col_scales<GATED, OP>(p, s, col);
+        float rs[4];
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) rs[nt] = sk_row_scale<OP>(p, min(m0 + nt * 16 + r16, end - 1));
         typename OP::acc4 acc[NMAT][4];
 #pragma unroll
         for (int mat = 0; mat < NMAT; ++mat)
@@ -403,13 +423,12 @@ __global__ __launch_bounds__(kSkThreads, 1) void skinny_dma_kernel(SkinnyParams 
 
         // epilogue: lane holds D[weight row 4q+i][segment row r16] of every
         // row tile nt, i.e. output columns col .. col+3 of row m0+16nt+r16
-        const int col = n0 + wave * 16 + 4 * q;
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt) {
             const int row = m0 + nt * 16 + r16;
             if (row >= end) continue;
             float v[4];
-            sk_values<GATED, OP>(v, acc[0][nt], acc[NMAT - 1][nt], p, s, row, col);
+            sk_values<GATED, OP>(v, acc[0][nt], acc[NMAT - 1][nt], cs, rs[nt]);
             uint16_t* dst = p.C + (size_t)row * N + col;
             if (col + 3 < N) {
                 *(uint2*)dst = make_uint2(pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3]));
@@ -533,6 +552,8 @@ __global__ __launch_bounds__(kSkThreads, 2) void skinny_reg_kernel(SkinnyParams 
                     if (nt < tiles) mfmas(nt, wt, in ? *(const v4u*)(xp[nt] + col) : v4u{0, 0, 0, 0});
             }
         }
+        const SkScales cs = sk_col_scales<GATED, OP>(p, s, n0 + 4 * q);
+        const float rs = sk_row_scale<OP>(p, min(m0 + min(wave, TILES - 1) * 16 + r16, end - 1));
 #pragma unroll
         for (int nt = 0; nt < TILES; ++nt)
             if (nt < tiles) {
@@ -551,7 +572,7 @@ __global__ __launch_bounds__(kSkThreads, 2) void skinny_reg_kernel(SkinnyParams 
                 for (int w = 1; w < 4; ++w) sum[mat] += part[w][mat * TILES + wave][lane];
             }
             float v[4];
-            sk_values<GATED, OP>(v, sum[0], sum[NMAT - 1], p, s, row, col);
+            sk_values<GATED, OP>(v, sum[0], sum[NMAT - 1], cs, rs);
             uint16_t* dst = p.C + (size_t)row * N + col;
             if (col + 3 < N) {
                 *(uint2*)dst = make_uint2(pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3]));

@@ -167,10 +167,6 @@ __global__ __launch_bounds__(kFewThreads, 2) void few8_kernel(Few8Params p) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int N = p.N, K = p.K, P = (int)w8_pitch(K);
     const int ncb = ceil_div(N, 16), s = blockIdx.x / ncb, n0 = (blockIdx.x % ncb) * 16;
-    const int beg = min(max(p.offsets[s], 0), p.rows_cap);
-    const int end = min(max(p.offsets[s + 1], beg), p.rows_cap);
-    const int rows = end - beg;  // (rows_cap of them at most, so kFewRows, and rows * P <= kFewValues)
-    if (rows <= 0) return;
     const int r16 = lane & 15, q = lane >> 4;
     const size_t wrow = (size_t)s * N + min(n0 + r16, N - 1);
     const char* wp[NMAT];
@@ -188,6 +184,15 @@ __global__ __launch_bounds__(kFewThreads, 2) void few8_kernel(Few8Params p) {
                     w[u][mat] = *(const v4u*)(wp[mat] + (p0 + 4 * (u >> 1)) * 128 + (u & 1) * 64);
             }
     };
+    // (one segment has rows, whatever its offsets: its weights need not wait for them)
+    const bool early = p.n_seg == 1;
+    if (early) load_weights(wave);
+    // the source of row `lane` (rows_cap <= kFewRows), loaded beside the offsets
+    const int source = gathered_row(p.a_rows, p.a_count, min(lane, p.rows_cap - 1));
+    const int beg = min(max(p.offsets[s], 0), p.rows_cap);
+    const int end = min(max(p.offsets[s + 1], beg), p.rows_cap);
+    const int rows = end - beg;  // (rows_cap of them at most, so kFewRows, and rows * P <= kFewValues)
+    if (rows <= 0) return;
     // the rows' values, a unit of 16 a thread and round
     const int upr = P / 16, units = rows * upr;
     uint4 x[kFewUnits][2];
@@ -195,14 +200,18 @@ __global__ __launch_bounds__(kFewThreads, 2) void few8_kernel(Few8Params p) {
     for (int i = 0; i < kFewUnits; ++i) {
         const int j = tid + kFewThreads * i, r = j / upr, u = j - r * upr;
         x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
+        const int from = __shfl(source, min(beg + r, kFewRows - 1));
         if (j < units) {
-            const uint4* row = (const uint4*)(p.A + (size_t)gathered_row(p.a_rows, p.a_count, beg + r) * K);
+            const uint4* row = (const uint4*)(p.A + (size_t)from * K);
             if (u * 16 < K) x[i][0] = row[2 * u];
             if (u * 16 + 8 < K) x[i][1] = row[2 * u + 1];
         }
     }
     __builtin_amdgcn_sched_barrier(0);
-    load_weights(wave);
+    if (!early) load_weights(wave);
+    const int col = n0 + 4 * q;  // (N is a multiple of 8: the scales are a quarter of a row's)
+    const size_t at = (size_t)s * N + min(col, N - 4);
+    const float4 c0 = *(const float4*)(p.sb0 + at), c1 = GATED ? *(const float4*)(p.sb1 + at) : c0;
     __builtin_amdgcn_sched_barrier(0);
     if (tid < kFewRows) s_max[tid] = 0;
     __syncthreads();
@@ -253,15 +262,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void few8_kernel(Few8Params p) {
     __syncthreads();
     // the lane holds columns n0 + 4 q .. + 3 of row r16
     if (wave != 0 || r16 >= rows) return;
-    const int col = n0 + 4 * q;
-    if (col >= N) return;  // (N is a multiple of 8)
+    if (col >= N) return;
     i32x4 sum[NMAT];
 #pragma unroll
     for (int mat = 0; mat < NMAT; ++mat)
         sum[mat] = s_part[0][mat][lane] + s_part[1][mat][lane] + s_part[2][mat][lane] + s_part[3][mat][lane];
     const float rs = s_scale[r16];
-    const float4 c0 = *(const float4*)(p.sb0 + (size_t)s * N + col);
-    const float4 c1 = GATED ? *(const float4*)(p.sb1 + (size_t)s * N + col) : c0;
     float v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
