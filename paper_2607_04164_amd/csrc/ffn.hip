@@ -819,6 +819,7 @@ __device__ __forceinline__ void tile_ksteps(typename C::acc16 (&acc)[C::NMAT][C:
         if (n > 1) wait_vmcnt<C::DMA_PER_STAGE>();
         else wait_vmcnt<0>();
     }
+    if constexpr (C::OP::kScales) lds_reads_done();  // (scales that a wave past the segment's end did not use)
     wg_barrier();
     // Fragments two sub-steps ahead, in four register sets (set j holds
     // sub-step j of a K-step). Sub-step 0 reads sub-steps 2 and 3, so a barrier
@@ -857,6 +858,7 @@ __device__ __forceinline__ void tile_ksteps(typename C::acc16 (&acc)[C::NMAT][C:
                                     dma_lds, wave, kb, D1);
         __builtin_amdgcn_sched_barrier(0);
         if (kt > 0 || after == kAfterNone) wait_vmcnt<D1 + D2>();  // (else the second K-step's are there)
+        lds_reads_done();  // (none is outstanding: no sub-step since the last barrier reads)
         wg_barrier();  // the next K-step is resident
         if (C::kVar && before_tail) tail_zero<C>(nxt, tv);
         __builtin_amdgcn_sched_barrier(0);
@@ -1139,6 +1141,7 @@ __device__ __forceinline__ void store_tile(const typename C::acc16 (&acc)[C::NMA
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (C::OP::kScales) {
         if (!plain) {
+            wait_vmcnt<0>();  // (other lanes stored these values above)
             int lane2 = lane;  // (nothing of this is to be formed ahead and kept)
             asm volatile("" : "+v"(lane2));
             const int l32 = lane2 & 31, hi = lane2 >> 5;

@@ -1,10 +1,12 @@
 // Rows in 8 bits with a scale for each row: activations by token, weights by output channel.
 //   scale = max|x| / 127,   code = round(x / scale)   (to nearest even, of the true quotient)
-// The grouped products with them are those of ffn.hip and ffn_skinny.hip on int8 MFMA.
+// The grouped products with them are those of ffn.hip and ffn_skinny.hip on int8 MFMA (their sums are exact in int32:
+// 131072 * 127^2 < 2^31), but for very few rows (few8_kernel).
 //
-// Bound by memory: a row is read once into registers (NT threads a row, CH units of 16 values a thread; longer
-// rows are read again for what does not fit), its largest magnitude is reduced over the row's threads, and the
-// codes go out 16 bytes a thread.
+// The quantizer is bound by memory: a row is read once into registers (NT threads a row, CH units of 16 values a
+// thread; longer rows are read again for what does not fit), its largest magnitude is reduced over the row's threads,
+// and the codes go out 16 bytes a thread. 30000 bf16 rows of 1408 (127 MB) 28 to 32 us, 4.0 to 4.5 TB/s; 8192 rows of
+// 14336, which the last-level cache holds in part, 59 us (5.9 TB/s); up to 512 rows 2.5 to 4 us of latency.
 #include "bmoe_common.h"
 #include "chunk16.h"
 #include "stream_io.h"
@@ -136,7 +138,10 @@ hipError_t pick_q8(const W8QuantizeArgs& a, hipStream_t s) {
 // One launch instead of two where rows_cap * K is small: every workgroup rounds its segment's rows (at most
 // kFewValues values, from the L2 cache) into LDS while its first weights are on their way, and then multiplies as
 // skinny_reg_kernel does: 16 output columns, K split over the four waves (128-column pairs of MFMA steps, PAIRS of
-// them in flight a wave), the waves' sums added in LDS.
+// them in flight a wave), the waves' sums added in LDS. Bound by a chain of latencies (offsets, rows, their maximum,
+// codes, sums) beside the weights' load: a row through 4096 x 4096 6.9 us, 2.4 TB/s; one token's four rows on four of 15
+// segments, d = 2048, d_ff = 1408, gate/up 10, down 6 us. Every load whose address the kernel's arguments give is issued
+// before the offsets are there (source rows, the scales, one segment's weights).
 constexpr int kFewThreads = 256;
 constexpr int kFewRows = 16;
 constexpr int kFewValues = 16384;                              // rows_cap * pitch, at most
@@ -287,8 +292,13 @@ hipError_t launch_few8(const Few8Params& p, hipStream_t s) {
 
 }  // namespace
 
+// Half as many values where all rows are one segment's (every workgroup then rounds all of them). us, this kernel / the
+// quantizer and the product, weights of three sets in turn: 1 segment, d = 2048, d_ff = 1408 gate/up 4 rows 7.5 / 8.5, 8
+// rows 9.2 / 9.0; N = K = 4096, 2 rows 8.7 / 10.0, 4 rows 10.5 / 10.2; N = K = 1024, 8 rows 5.7 / 6.6, 16 rows 7.6 / 6.8;
+// 15 segments, gate/up 4 rows 9.9 / 12.2, 8 rows 11.5 / 17.2, down 8 rows 8.8 / 11.1; 4 segments, N = K = 4096, 4 rows
+// 13.8 / 14.7. (Room for 32768 values costs the smaller calls 0.3 to 1 us by its registers.)
 bool w8_few_fits(const W8GemmArgs& a) {
-    return a.rows_cap <= kFewRows && a.rows_cap * w8_pitch(a.K) <= kFewValues;
+    return a.rows_cap <= kFewRows && a.rows_cap * w8_pitch(a.K) <= (a.n_seg == 1 ? kFewValues / 2 : kFewValues);
 }
 
 hipError_t launch_w8_few(const W8GemmArgs& a, const void* x, hipStream_t s) {

@@ -325,6 +325,41 @@ def test_scales_far_apart(rows):
     assert bool(((y.double() - want).abs() <= tol)[fits].all())
 
 
+@pytest.mark.parametrize("rows", [3, 300, 60000])
+def test_gated_scales_far_apart(rows):
+    """Activations of 2^70 and of 2^-60 beside ordinary ones, weights that bring them back."""
+    K, N = 128, 16
+    g = gen(rows)
+    a = randn(g, rows, K)
+    a[0] *= 2.0 ** 70
+    a[1] *= 2.0 ** -60
+    wg, wu = weights(g, 1, N, K), weights(g, 1, N, K)
+    wg.scales[0, :4] *= 2.0 ** -72
+    wu.scales[0, :4] *= 2.0 ** -66
+    wg.scales[0, 4:8] *= 2.0 ** 58
+    wu.scales[0, 4:8] *= 2.0 ** 62
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    h = B.w8_gate_up(off, a, wg, wu)
+    q, s = rounded64(a)
+    gate, up = products64(q, s, [0, rows], wg), products64(q, s, [0, rows], wu)
+    inside = (gate.abs() < 2.0 ** 120) & (up.abs() < 2.0 ** 120) & ((gate * up).abs() < 2.0 ** 120)
+    assert bool(inside[0, :4].all()) and bool(inside[1, :8].all()) and not bool(inside[0].all())
+    big = torch.where(inside, gate, torch.zeros_like(gate)), torch.where(inside, up, torch.zeros_like(up))
+    check_hidden(torch.where(inside, h, torch.zeros_like(h)), *big, "h")
+
+
+@pytest.mark.parametrize("n,rows,d", [(2, 5, 256), (3, 60, 264), (2, 9000, 392)])
+def test_the_output_in_place_of_the_activations(n, rows, d):
+    g = gen(d)
+    f = 136
+    ws = weights(g, n, f, d), weights(g, n, f, d), weights(g, n, d, f)
+    o = torch.from_numpy(segments(rows, rows, n)).cuda()
+    a = randn(g, rows, d)
+    y, h = B.w8_ffn(o, a, *ws)
+    y1, h1 = B.w8_ffn(o, a, *ws, y=a)
+    assert y1 is a and torch.equal(a, y) and torch.equal(h, h1)
+
+
 @pytest.mark.parametrize("n,rows", [(65, 64), (200, 300), (256, 20000), (256, 90000)])
 def test_more_segments_than_lanes(n, rows):
     g = gen(n)

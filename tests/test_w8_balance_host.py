@@ -213,7 +213,8 @@ def test_product_choice(tmp_path):
     idle, take the weight-streaming kernels; else the large tiles (half ones where segments are short), with the
     fixup where there is room for it and K is long."""
     few, skinny, whole, half = "few8_kernel", "skinny_", "grouped_gemm_dma_kernel<false, false", "grouped_gemm_dma_kernel<false, true"
-    cases = [((15, 4, 2048, 1408), [few]), ((1, 4, 512, 4096), [few]), ((1, 5, 512, 4096), ["q8_", skinny]),
+    cases = [((15, 4, 2048, 1408), [few]), ((1, 2, 512, 4096), [few]), ((1, 3, 512, 4096), ["q8_", skinny]),
+             ((2, 4, 512, 4096), [few]), ((2, 5, 512, 4096), ["q8_", skinny]), ((4, 16, 512, 1024), [few]),
              ((1, 17, 512, 128), ["q8_", skinny]), ((4, 256, 4096, 4096), ["q8_", skinny]),
              # both sides of the estimate
              ((1, 1536, 2048, 1408), ["q8_", skinny]), ((4, 1200, 2048, 1408), ["q8_", skinny]),
