@@ -611,7 +611,7 @@ BMOE_API bmoe_status brownout_moe_w8_ffn(int32_t dtype, int32_t n_seg, int32_t r
  * (entries outside [0, G) belong to no group and add nothing) or NULL (groups are the experts: G
  * must be E). All in DEVICE memory. Outputs: losses [2], prob [E] float, counts [E+1] int32;
  * d_logits [T,E] float, which may be logits itself (other shared memory is BMOE_ERR_UNSUPPORTED).
- * Logits of tokens that do not count are not read. -infinity is an expert of probability 0; a
+ * Logits of tokens that do not count may hold anything. -infinity is an expert of probability 0; a
  * token of nothing else has no probabilities, adds nothing to the losses and gets gradient 0,
  * though it counts in V. With V == 0 losses and prob are 0. Sums in a fixed order: results are
  * deterministic. E in 1..256, k in 1..16, G in 1..256.

@@ -72,21 +72,42 @@ __device__ __forceinline__ float softmax_row(float (&z)[V]) {
 template <int S, int B>
 __device__ __forceinline__ int expert_of(int s, int v) { return B * (s + S * (v / B)) + v % B; }
 
-// the logits of token t that lane s holds; past E, and for tokens that do not count, -infinity
+// the logits of token t that lane s holds; past E and T, -infinity
 template <int S, int V, int B>
-__device__ __forceinline__ void load_logits(float (&z)[V], const float* logits, int64_t t, int s, int E, bool on) {
+__device__ __forceinline__ void load_logits(float (&z)[V], const float* logits, int64_t t, int64_t T, int s, int E) {
     const float none = -__builtin_inff();
 #pragma unroll
     for (int v = 0; v < V; v += B) {
         const int e = expert_of<S, B>(s, v);
         if constexpr (B == 4) {
-            const float4 q = on && e < E ? *(const float4*)(logits + t * E + e) : make_float4(none, none, none, none);
+            const float4 q = t < T && e < E ? *(const float4*)(logits + t * E + e) : make_float4(none, none, none, none);
             z[v] = q.x, z[v + 1] = q.y, z[v + 2] = q.z, z[v + 3] = q.w;
         } else {
-            z[v] = on && e < E ? logits[t * E + e] : none;
+            z[v] = t < T && e < E ? logits[t * E + e] : none;
         }
     }
 }
+
+// A token's loads, issued together and ahead of their use: its logits, whether it counts, and its picks (the lane's
+// i-th is slot s + S i).
+template <int S, int V, int B, int PK>
+struct Token {
+    float z[V];
+    int pick[PK > 0 ? PK : 1];
+    int valid;
+    __device__ __forceinline__ void load(const float* logits, const int32_t* picks, const uint8_t* mask, int64_t t,
+                                         int64_t T, int s, int E, int k) {
+        load_logits<S, V, B>(z, logits, t, T, s, E);
+        valid = t < T ? (mask ? mask[t] : 1) : 0;
+#pragma unroll
+        for (int i = 0; i < PK; ++i) pick[i] = t < T && s + S * i < k ? picks[t * k + s + S * i] : -1;
+    }
+    // the logits of a token that does not count: -infinity, whatever they hold
+    __device__ __forceinline__ void mask() {
+#pragma unroll
+        for (int v = 0; v < V; ++v) z[v] = valid ? z[v] : -__builtin_inff();
+    }
+};
 
 // ---- the losses from the sums over all tokens
 
@@ -99,23 +120,27 @@ struct Sums {
     double part[kWaves];
 };
 
-// Ends a call: every thread of one workgroup of kThreads, s complete (a barrier behind it).
-__device__ __forceinline__ void finish(const BalanceArgs& a, Sums& s) {
+// the group of expert `tid` (loaded before a kernel's other work), or -1
+__device__ __forceinline__ int group_of(const int32_t* e2g, int E, int G, int tid) {
+    if (tid >= E) return -1;
+    const int g = e2g ? e2g[tid] : tid;
+    return g < G ? g : -1;
+}
+
+// Ends a call: every thread of one workgroup of kThreads, s complete (a barrier behind it). g: group_of this thread.
+__device__ __forceinline__ void finish(const BalanceArgs& a, Sums& s, int g) {
     const int tid = threadIdx.x, E = a.E;
     for (int r = tid; r < BMOE_MAX_EXPERTS; r += kThreads) s.group[r] = 0;
     __syncthreads();
     const int n = s.c[E];
-    const double V = n > 0 ? (double)n : 1.0;
-    int g = -1;
+    const double per = 1.0 / (n > 0 ? (double)n : 1.0);
     if (tid < E) {
-        g = a.e2g ? a.e2g[tid] : tid;
-        if (g < 0 || g >= a.G) g = -1;  // of no group
-        else atomicAdd(&s.group[g], s.c[tid]);
+        if (g >= 0) atomicAdd(&s.group[g], s.c[tid]);
         a.counts[tid] = s.c[tid];
-        a.prob[tid] = (float)(s.p[tid] / V);
+        a.prob[tid] = (float)(s.p[tid] * per);
     }
     __syncthreads();
-    double sum = g >= 0 ? (double)s.group[g] / ((double)a.k * V) * (s.p[tid] / V) : 0.0;
+    double sum = g >= 0 ? (double)s.group[g] * s.p[tid] : 0.0;
 #pragma unroll
     for (int off = 32; off; off >>= 1) sum += __shfl_xor(sum, off);
     if ((tid & 63) == 0) s.part[tid >> 6] = sum;
@@ -123,8 +148,8 @@ __device__ __forceinline__ void finish(const BalanceArgs& a, Sums& s) {
     if (tid == 0) {
         sum = 0.0;
         for (int w = 0; w < BMOE_MAX_EXPERTS / 64; ++w) sum += s.part[w];
-        a.losses[0] = (float)((double)a.G * sum);
-        a.losses[1] = (float)(s.z / V);
+        a.losses[0] = (float)((double)a.G * sum * per * per / (double)a.k);
+        a.losses[1] = (float)(s.z * per);
         a.counts[E] = n;
     }
 }
@@ -154,37 +179,30 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     __shared__ Sums sums;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int E = a.E, k = a.k, s = lane % S;
+    const int64_t step = (int64_t)gridDim.x * kWaves * PER;
+    int64_t t = ((int64_t)blockIdx.x * kWaves + wave) * PER + lane / S;
+    Token<S, V, B, BMOE_MAX_TOPK / S> next;
+    next.load(a.logits, a.topk_idx, a.valid, t, a.T, s, E, k);
+    const int g = gridDim.x == 1 ? group_of(a.e2g, E, a.G, tid) : -1;
     for (int e = tid; e <= E; e += kThreads) sums.c[e] = 0;
     __syncthreads();
     float p[V], z2 = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = 0.f;
-    const int64_t step = (int64_t)gridDim.x * kWaves * PER;
-    int64_t t = ((int64_t)blockIdx.x * kWaves + wave) * PER + lane / S;
-    auto counts_token = [&](int64_t i) { return i < a.T && (!a.valid || a.valid[i] != 0); };
-    float next[V];
-    bool on = counts_token(t);
-    load_logits<S, V, B>(next, a.logits, t, s, E, on);
     // (the lanes of a wave stay together: the permutations read their neighbours)
     for (; __any(t < a.T); t += step) {
-        float z[V];
+        Token<S, V, B, BMOE_MAX_TOPK / S> now = next;
+        next.load(a.logits, a.topk_idx, a.valid, t + step, a.T, s, E, k);
+        now.mask();
+        const float lse = softmax_row<S, V>(now.z);
+        if (now.valid) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) z[v] = next[v];
-        const bool now = on;
-        if (now) {
-            for (int i = s; i < k; i += S) {
-                const int e = a.topk_idx[t * k + i];
-                if (e >= 0 && e < E) atomicAdd(&sums.c[e], 1);
-            }
-            if (s == 0) atomicAdd(&sums.c[E], 1);
-        }
-        on = counts_token(t + step);
-        load_logits<S, V, B>(next, a.logits, t + step, s, E, on);
-        const float lse = softmax_row<S, V>(z);
-        if (now) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) p[v] += z[v];
+            for (int v = 0; v < V; ++v) p[v] += now.z[v];
             z2 = fmaf(lse, lse, z2);
+#pragma unroll
+            for (int i = 0; i < BMOE_MAX_TOPK / S; ++i)
+                if (now.pick[i] >= 0 && now.pick[i] < E) atomicAdd(&sums.c[now.pick[i]], 1);
+            if (s == 0) atomicAdd(&sums.c[E], 1);
         }
     }
     // the wave's tokens, then the waves in order
@@ -216,7 +234,7 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     }
     if (groups > 1) return;
     __syncthreads();
-    finish(a, sums);
+    finish(a, sums, g);
 }
 
 // Many workgroups' sums of many experts, kFold at a time, by several workgroups first: one workgroup alone reads them
@@ -273,6 +291,7 @@ __global__ __launch_bounds__(kThreads) void balance_join_kernel(BalanceArgs a, v
     __shared__ int s_c[kThreads];
     const int tid = threadIdx.x, E = a.E, e = tid % ep, j = tid / ep, J = kThreads / ep;
     const Parts q = parts_of(parts, groups, E);
+    const int group = group_of(a.e2g, E, a.G, tid);
     double p = 0.0;
     int c = 0;
     // (one workgroup's latency: kAhead loads of each in flight, those past the end of the last row instead of branches)
@@ -325,7 +344,7 @@ __global__ __launch_bounds__(kThreads) void balance_join_kernel(BalanceArgs a, v
         sums.z = z;
     }
     __syncthreads();
-    finish(a, sums);
+    finish(a, sums, group);
 }
 
 template <int S, int V, int B>
@@ -334,40 +353,39 @@ __global__ __launch_bounds__(kGradThreads) void balance_grad_kernel(BalanceGradA
     __shared__ int s_group[BMOE_MAX_EXPERTS];
     __shared__ float s_f[S * V];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, s = lane % S, E = a.E;
-    const int n = a.counts[E];
-    const double V_ = n > 0 ? (double)n : 1.0;
-    // the losses' slopes by p (balance) and by lse^2, of every expert
-    const double b = (double)a.d_losses[0] / V_;
-    const float zc = (float)(2.0 * (double)a.d_losses[1] / V_);
+    const int64_t step = (int64_t)gridDim.x * (kGradThreads / 64) * PER;
+    int64_t t = ((int64_t)blockIdx.x * (kGradThreads / 64) + wave) * PER + lane / S;
+    Token<S, V, B, 0> next;
+    next.load(a.logits, nullptr, a.valid, t, a.T, s, E, 0);
+    const int g = group_of(a.e2g, E, a.G, tid);
+    const int count = tid < E ? a.counts[tid] : 0, n = a.counts[E];
+    const double per = 1.0 / (n > 0 ? (double)n : 1.0);
+    // the losses' slopes by p (balance; every expert's) and by lse^2
+    const double b = (double)a.d_losses[0] * per * per * (double)a.G / (double)a.k;
+    const float zc = (float)(2.0 * (double)a.d_losses[1] * per);
     for (int r = tid; r < BMOE_MAX_EXPERTS; r += kGradThreads) s_group[r] = 0;
     __syncthreads();
-    int g = -1;
-    if (tid < E) {
-        g = a.e2g ? a.e2g[tid] : tid;
-        if (g < 0 || g >= a.G) g = -1;
-        else atomicAdd(&s_group[g], a.counts[tid]);
-    }
+    if (g >= 0) atomicAdd(&s_group[g], count);
     __syncthreads();
-    if (tid < S * V)
-        s_f[tid] = g >= 0 ? (float)(b * (double)a.G * (double)s_group[g] / ((double)a.k * V_)) : 0.f;
+    if (tid < S * V) s_f[tid] = g >= 0 ? (float)(b * (double)s_group[g]) : 0.f;
     __syncthreads();
     float f[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) f[v] = s_f[expert_of<S, B>(s, v)];
-    const int64_t step = (int64_t)gridDim.x * (kGradThreads / 64) * PER;
-    for (int64_t t = ((int64_t)blockIdx.x * (kGradThreads / 64) + wave) * PER + lane / S; __any(t < a.T); t += step) {
-        const bool in = t < a.T, on = in && (!a.valid || a.valid[t] != 0);
-        float z[V];
-        load_logits<S, V, B>(z, a.logits, t, s, E, on);
+    for (; __any(t < a.T); t += step) {
+        Token<S, V, B, 0> now = next;
+        next.load(a.logits, nullptr, a.valid, t + step, a.T, s, E, 0);
+        now.mask();
+        float (&z)[V] = now.z;
         const float lse = softmax_row<S, V>(z);
         float dot = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) dot = fmaf(f[v], z[v], dot);
         dot = over_lanes<S>(dot, [](float x, float y) { return x + y; });
         const float c = fmaf(zc, lse, -dot);
-        if (in) {
+        if (t < a.T) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) z[v] = on ? z[v] * (f[v] + c) : 0.f;
+            for (int v = 0; v < V; ++v) z[v] = now.valid ? z[v] * (f[v] + c) : 0.f;
 #pragma unroll
             for (int v = 0; v < V; v += B) {
                 const int e = expert_of<S, B>(s, v);

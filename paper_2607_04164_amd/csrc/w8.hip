@@ -68,7 +68,6 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void q8_rows_kernel(W8Quantize
     int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / NT;
     // (one row of a workgroup where its threads have a barrier: they leave together)
     if (r >= a.rows) return;
-    if (a.offsets && (r < a.offsets[0] || r >= a.offsets[a.n_seg])) return;
     const int K = a.K, t = threadIdx.x % NT;
     const int units = (int)(w8_pitch(K) / 16);
     const uint4* row = (const uint4*)((const E*)a.x + (size_t)r * K);
@@ -86,6 +85,8 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void q8_rows_kernel(W8Quantize
 #pragma unroll
         for (int i = 0; i < 16; ++i) m = max(m, magnitude(g[i]));
     }
+    // (rows of no segment: their loads do not wait for the offsets)
+    if (a.offsets && (r < a.offsets[0] || r >= a.offsets[a.n_seg])) return;
 #pragma unroll
     for (int off = 32; off; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
     if constexpr (W > 1) {
