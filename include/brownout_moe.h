@@ -615,9 +615,12 @@ BMOE_API bmoe_status brownout_moe_w8_ffn(int32_t dtype, int32_t n_seg, int32_t r
  * token of nothing else has no probabilities, adds nothing to the losses and gets gradient 0,
  * though it counts in V. With V == 0 losses and prob are 0. Sums in a fixed order: results are
  * deterministic. E in 1..256, k in 1..16, G in 1..256.
- * workspace: bmoe_balance_workspace_bytes(T, E) bytes (0 for few tokens), 8-byte aligned, no
- * initialisation; calls that can overlap in time must not share one.
+ * workspace: bmoe_balance_workspace_bytes(T, E) bytes (0 for few tokens), 8-byte aligned. Its
+ * first BMOE_BALANCE_ZERO_BYTES bytes (arrival counters) are zero before the first call that uses
+ * it; every call leaves them zero; the rest needs no initialisation. Calls that can overlap in
+ * time must not share one.
  */
+#define BMOE_BALANCE_ZERO_BYTES 64
 BMOE_API size_t bmoe_balance_workspace_bytes(int32_t T, int32_t E);
 BMOE_API bmoe_status brownout_moe_balance(int32_t T, int32_t E, int32_t k, int32_t G, const float* logits,
                                  const int32_t* topk_idx, const uint8_t* valid, const int32_t* e2g, float* losses,

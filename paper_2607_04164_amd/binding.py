@@ -8,6 +8,7 @@ streams. There is no fallback: without the built library every call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, Optional, Tuple
@@ -39,6 +40,7 @@ DISTILL_WS_BYTES = 32768
 FEW_MAX_TOKENS = 16
 NORM_MAX_D = 32768
 W8_MAX_K = 131072
+BALANCE_ZERO_BYTES = 64
 GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_FULL = 0, 1, 2, 3
 DISPATCH_SCRATCH_BYTES = 1048576  # the array behind brownout_moe_dispatch_noalloc
 
@@ -929,9 +931,9 @@ def w8_ffn(offsets: torch.Tensor, a, w_gate: W8, w_up: W8, w_down: W8, *, a_rows
 # how evenly the router's picks fall
 
 def new_balance_workspace(T: int, E: int, device) -> torch.Tensor:
-    """balance's workspace for up to T tokens of E experts."""
+    """balance's workspace for T tokens of E experts (its counters zero, as every call leaves them)."""
     n = int(load_library().bmoe_balance_workspace_bytes(T, E))
-    return torch.empty((max(n, 1) + 255) // 256 * 256, dtype=torch.uint8, device=device)
+    return torch.zeros((max(n, 1) + 255) // 256 * 256, dtype=torch.uint8, device=device)
 
 
 def new_balance_buffers(E: int, device) -> Dict[str, torch.Tensor]:
@@ -958,12 +960,21 @@ def _balance_args(logits, valid, e2g, G):
     return T, E, int(G), device, lp, vp, _fits(e2g, "e2g", torch.int32, (E,), device)
 
 
+def _counters(ws, stream):
+    """A new workspace of a call on `stream`, its counters cleared there."""
+    with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+        ws[:BALANCE_ZERO_BYTES].zero_()
+    return ws
+
+
 def balance(logits: torch.Tensor, topk_idx: torch.Tensor, *, valid: Optional[torch.Tensor] = None,
             e2g: Optional[torch.Tensor] = None, G: Optional[int] = None, out: Optional[Dict[str, torch.Tensor]] = None,
             workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
     """How evenly route's picks fall on the experts, or on the G groups of e2g: losses (balance loss, z loss),
     counts (picks per expert, then the number of tokens that count) and prob (mean probabilities). logits [T, E] and
-    topk_idx [T, k] as route writes them; valid [T] uint8: the tokens that count (None: all)."""
+    topk_idx [T, k] as route writes them; valid [T] uint8: the tokens that count (None: all). workspace:
+    new_balance_workspace's for these T and E (or more tokens), or None (memory of the call's own stream, cleared by a
+    launch of its own)."""
     T, E, G, device, lp, vp, gp = _balance_args(logits, valid, e2g, G)
     if not isinstance(topk_idx, torch.Tensor) or topk_idx.dim() != 2:
         raise ValueError("topk_idx must be [T, k]")
@@ -976,7 +987,7 @@ def balance(logits: torch.Tensor, topk_idx: torch.Tensor, *, valid: Optional[tor
     prob = o["prob"] if "prob" in o else o.setdefault("prob", new(E, torch.float32))
     if workspace is None:
         n = int(load_library().bmoe_balance_workspace_bytes(T, E))
-        workspace = new(n, torch.uint8) if n else None
+        workspace = _counters(new(n, torch.uint8), stream) if n else None
     wp, wn = (None, 0) if workspace is None else (_fits(workspace, "workspace", torch.uint8, workspace.shape, device),
                                                   workspace.numel())
     _check(load_library().brownout_moe_balance(T, E, k, G, lp, ip, vp, gp, _fits(losses, "losses", torch.float32, (2,), device),

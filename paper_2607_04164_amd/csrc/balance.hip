@@ -6,9 +6,15 @@
 //
 // S lanes of a wave hold a token's row (lane s: experts s, s + S, .., or four neighbours at a time where rows are whole
 // 16-byte chunks), so a wave takes 64 / S neighbouring rows at a time and a row's maximum and sums are register
-// permutations. A lane keeps the sums of p of its experts over its
-// tokens; a workgroup's sums meet in LDS in wave order, the workgroups' in a second launch in 64 bits: no float
-// atomics, so results do not depend on the order of anything. Up to kOneGroup rounds one workgroup does it all.
+// permutations. A lane keeps the sums of p of its experts over its tokens; a workgroup's sums meet in LDS in wave order.
+// The last of every fold_of(E) workgroups to finish adds their sums, the last of those the rest, in 64 bits and by
+// workgroup (arrival counters say who is last, the sums' order does not depend on it; no float atomics). That is one
+// launch: a second one for these sums takes the host longer than them (8192 tokens of 60 experts 12.2 -> 10.5 us a call,
+// though 9.2 and 9.0 in a graph). Up to kOneGroup rounds of tokens one workgroup does it all.
+//
+// Bound by memory where there are many tokens (131072 of 256 experts: 36 us, 3.9 TB/s of 4.9; the read of the logits
+// alone 29), by the host's call for few (64 tokens: kernel 4.5 us, call 8), and between them by two or three round trips
+// past the caches for the sums.
 #include "bmoe_common.h"
 
 namespace bmoe {
@@ -154,21 +160,113 @@ __device__ __forceinline__ void finish(const BalanceArgs& a, Sums& s, int g) {
     }
 }
 
-// A workgroup's sums in the workspace: z [groups] double, p [groups, E] float, c [groups, E + 1] int32
+// ---- the sums of several workgroups
+//
+// Rows of sums in the workspace: z [rows] double, p [rows, E] float, c [rows, E + 1] int32. They are written and read
+// past the XCDs' own L2 caches (relaxed atomics of device scope: sc1 stores and loads); a row is complete before its
+// workgroup counts itself in.
+// Rows a workgroup adds at a time. More make fewer levels (3 us each) but longer ones: up to 64 experts 4096 tokens in 64
+// workgroups 7.8 us, in two levels of 32 9.9; 256 workgroups of 256 experts by 32 36 us, by 64 40.
+__host__ __device__ constexpr int fold_of(int E) { return E <= 64 ? 64 : 32; }
+constexpr int kTickets = 16;  // arrival counters: of all folds, and of each; zero between calls
+static_assert(kMaxGroups / 32 < kTickets, "a counter for each fold");
 struct Parts {
     double* z;
     float* p;
     int* c;
 };
-__host__ __device__ inline size_t parts_bytes(int groups, int E) {
-    return ((size_t)groups * (8 + 4 * (size_t)E + 4 * (size_t)(E + 1)) + 7) / 8 * 8;
+__host__ __device__ inline size_t parts_bytes(int rows, int E) {
+    return ((size_t)rows * (8 + 4 * (size_t)E + 4 * (size_t)(E + 1)) + 7) / 8 * 8;
 }
-__host__ __device__ inline Parts parts_of(void* ws, int groups, int E) {
+__host__ __device__ inline Parts parts_of(void* at, int rows, int E) {
     Parts q;
-    q.z = (double*)ws;
-    q.p = (float*)(q.z + groups);
-    q.c = (int*)(q.p + (size_t)groups * E);
+    q.z = (double*)at;
+    q.p = (float*)(q.z + rows);
+    q.c = (int*)(q.p + (size_t)rows * E);
     return q;
+}
+template <typename T>
+__device__ __forceinline__ T load_far(const T* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename T>
+__device__ __forceinline__ void store_far(T* p, T v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// s to row `row`, by a workgroup whose threads see it complete
+__device__ __forceinline__ void put_row(const Parts& q, int row, int E, const Sums& s) {
+    const int tid = threadIdx.x;
+    if (tid < E) store_far(q.p + (size_t)row * E + tid, (float)s.p[tid]);
+    if (tid <= E) store_far(q.c + (size_t)row * (E + 1) + tid, s.c[tid]);
+    if (tid == 0) store_far(q.z + row, s.z);
+}
+
+// Counts a workgroup in, after its row; whether it is the last of n (which leaves the counter zero).
+__device__ __forceinline__ bool last_of(int* ticket, int n, int* flag) {
+    wait_vmcnt<0>();  // this thread's part of the row is there
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const bool last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n - 1;
+        if (last) store_far(ticket, 0);
+        *flag = last ? 1 : 0;
+    }
+    __syncthreads();
+    return *flag != 0;
+}
+
+// The sum of rows row0 .. row0 + n - 1 (n <= fold_of(EP)) in s, in their order. J = kThreads / ep threads an expert, ep a power
+// of two, E or more.
+struct Scratch {
+    double p[kThreads];
+    int c[kThreads];
+};
+template <int EP>
+__device__ __forceinline__ void add_rows(const Parts& q, int row0, int n, int E, Sums& s, Scratch& w) {
+    constexpr int J = kThreads / EP, PER = fold_of(EP) / J;
+    static_assert(PER > 0, "a thread's rows");
+    const int tid = threadIdx.x, e = tid % EP, j = tid / EP;
+    float pv[PER];
+    int cv[PER];
+    // (those past the last row repeat it instead of branching)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const size_t row = row0 + min(j * PER + i, n - 1);
+        pv[i] = load_far(q.p + row * E + min(e, E - 1));
+        cv[i] = load_far(q.c + row * (E + 1) + min(e, E - 1));
+    }
+    // tokens that count, and the z loss: a thread a row
+    int m = 0;
+    double z = 0.0;
+    if (tid < n) {
+        m = load_far(q.c + (size_t)(row0 + tid) * (E + 1) + E);
+        z = load_far(q.z + row0 + tid);
+    }
+    double p = 0.0;
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        p += j * PER + i < n ? (double)pv[i] : 0.0;
+        c += j * PER + i < n ? cv[i] : 0;
+    }
+    w.p[tid] = p;
+    w.c[tid] = c;
+#pragma unroll
+    for (int off = 32; off; off >>= 1) {
+        m += __shfl_xor(m, off);
+        z += __shfl_xor(z, off);
+    }
+    __syncthreads();
+    if (tid < E) {  // (e == tid)
+#pragma unroll
+        for (int i = 1; i < J; ++i) {
+            p += w.p[i * EP + tid];
+            c += w.c[i * EP + tid];
+        }
+        s.p[tid] = p;
+        s.c[tid] = c;
+    }
+    if (tid == 0) {
+        s.c[E] = m;
+        s.z = z;
+    }
+    __syncthreads();
 }
 
 template <int S, int V, int B>
@@ -177,13 +275,15 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     __shared__ float s_p[kWaves][S * V];
     __shared__ float s_z[kWaves];
     __shared__ Sums sums;
+    __shared__ Scratch scratch;
+    __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int E = a.E, k = a.k, s = lane % S;
     const int64_t step = (int64_t)gridDim.x * kWaves * PER;
     int64_t t = ((int64_t)blockIdx.x * kWaves + wave) * PER + lane / S;
     Token<S, V, B, BMOE_MAX_TOPK / S> next;
     next.load(a.logits, a.topk_idx, a.valid, t, a.T, s, E, k);
-    const int g = gridDim.x == 1 ? group_of(a.e2g, E, a.G, tid) : -1;
+    const int g = group_of(a.e2g, E, a.G, tid);
     for (int e = tid; e <= E; e += kThreads) sums.c[e] = 0;
     __syncthreads();
     float p[V], z2 = 0.f;
@@ -216,135 +316,35 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     for (int off = S; off < 64; off *= 2) z2 += __shfl_xor(z2, off);
     if (lane == 0) s_z[wave] = z2;
     __syncthreads();
-    const int groups = gridDim.x;
-    const Parts q = parts_of(a.ws, groups, E);
     if (tid < E) {
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) sum += s_p[w][tid];
-        if (groups == 1) sums.p[tid] = (double)sum;
-        else q.p[(size_t)blockIdx.x * E + tid] = sum;
+        sums.p[tid] = (double)sum;
     }
-    if (groups > 1 && tid <= E) q.c[(size_t)blockIdx.x * (E + 1) + tid] = sums.c[tid];
     if (tid == 0) {
         double sum = 0.0;
         for (int w = 0; w < kWaves; ++w) sum += (double)s_z[w];
-        if (groups == 1) sums.z = sum;
-        else q.z[blockIdx.x] = sum;
+        sums.z = sum;
     }
-    if (groups > 1) return;
     __syncthreads();
+    const int groups = gridDim.x;
+    if (groups > 1) {
+        constexpr int EP = S * V < 64 ? 64 : S * V, kFold = fold_of(EP);
+        int* tickets = (int*)a.ws;
+        const Parts q = parts_of(tickets + kTickets, groups, E);
+        const int fold = blockIdx.x / kFold, folds = ceil_div(groups, kFold), row0 = fold * kFold;
+        put_row(q, blockIdx.x, E, sums);
+        if (!last_of(tickets + 1 + fold, min(kFold, groups - row0), &s_last)) return;
+        add_rows<EP>(q, row0, min(kFold, groups - row0), E, sums, scratch);
+        if (folds > 1) {
+            const Parts r = parts_of((char*)(tickets + kTickets) + parts_bytes(groups, E), folds, E);
+            put_row(r, fold, E, sums);
+            if (!last_of(tickets, folds, &s_last)) return;
+            add_rows<EP>(r, 0, folds, E, sums, scratch);
+        }
+    }
     finish(a, sums, g);
-}
-
-// Many workgroups' sums of many experts, kFold at a time, by several workgroups first: one workgroup alone reads them
-// at its CU's rate (256 workgroups' of 256 experts 11 us; 4 here, and 4 for the join of what is left).
-constexpr int kFold = 32;
-constexpr int kFoldThreads = 256;
-__global__ __launch_bounds__(kFoldThreads) void balance_fold_kernel(void* from, int groups, void* to, int E) {
-    constexpr int J = kFoldThreads / 64, PER = kFold / J;
-    __shared__ double s_p[J][64];
-    __shared__ int s_c[J][64];
-    const int lane = threadIdx.x & 63, j = threadIdx.x >> 6, e = blockIdx.y * 64 + lane;
-    const int g0 = blockIdx.x * kFold + j * PER;
-    const Parts a = parts_of(from, groups, E), b = parts_of(to, gridDim.x, E);
-    float pv[PER];
-    int cv[PER];
-    double p = 0.0;
-    int c = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const size_t g = min(g0 + i, groups - 1);
-        pv[i] = a.p[g * E + min(e, E - 1)];
-        cv[i] = a.c[g * (E + 1) + min(e, E)];
-    }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const bool in = g0 + i < groups;
-        p += in ? (double)pv[i] : 0.0;
-        c += in ? cv[i] : 0;
-    }
-    s_p[j][lane] = p;
-    s_c[j][lane] = c;
-    __syncthreads();
-    if (j == 0) {
-#pragma unroll
-        for (int i = 1; i < J; ++i) {
-            p += s_p[i][lane];
-            c += s_c[i][lane];
-        }
-        if (e < E) b.p[(size_t)blockIdx.x * E + e] = (float)p;
-        if (e <= E) b.c[(size_t)blockIdx.x * (E + 1) + e] = c;
-        if (e == 0) {
-            double z = 0.0;
-            for (int g = blockIdx.x * kFold; g < min((int)(blockIdx.x + 1) * kFold, groups); ++g) z += a.z[g];
-            b.z[blockIdx.x] = z;
-        }
-    }
-}
-
-// The workgroups' sums, in order. ep: a power of two, E or more.
-__global__ __launch_bounds__(kThreads) void balance_join_kernel(BalanceArgs a, void* parts, int groups, int ep) {
-    __shared__ Sums sums;
-    __shared__ double s_p[kThreads];
-    __shared__ int s_c[kThreads];
-    const int tid = threadIdx.x, E = a.E, e = tid % ep, j = tid / ep, J = kThreads / ep;
-    const Parts q = parts_of(parts, groups, E);
-    const int group = group_of(a.e2g, E, a.G, tid);
-    double p = 0.0;
-    int c = 0;
-    // (one workgroup's latency: kAhead loads of each in flight, those past the end of the last row instead of branches)
-    constexpr int kAhead = 16;
-    if (e < E)
-        for (int g0 = j; g0 < groups; g0 += J * kAhead) {
-            float pv[kAhead];
-            int cv[kAhead];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int g = min(g0 + J * i, groups - 1);
-                pv[i] = q.p[(size_t)g * E + e];
-                cv[i] = q.c[(size_t)g * (E + 1) + e];
-            }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const bool in = g0 + J * i < groups;
-                p += in ? (double)pv[i] : 0.0;
-                c += in ? cv[i] : 0;
-            }
-        }
-    s_p[tid] = p;
-    s_c[tid] = c;
-    // tokens that count, and the z loss: the first wave
-    int n = 0;
-    double z = 0.0;
-    if (tid < 64) {
-        for (int g = tid; g < groups; g += 64) {
-            n += q.c[(size_t)g * (E + 1) + E];
-            z += q.z[g];
-        }
-#pragma unroll
-        for (int off = 32; off; off >>= 1) {
-            n += __shfl_xor(n, off);
-            z += __shfl_xor(z, off);
-        }
-    }
-    __syncthreads();
-    if (tid < E) {  // (e == tid)
-        for (int i = 1; i < J; ++i) {
-            p += s_p[i * ep + tid];
-            c += s_c[i * ep + tid];
-        }
-        sums.p[tid] = p;
-        sums.c[tid] = c;
-    }
-    if (tid == 0) {
-        sums.c[E] = n;
-        sums.z = z;
-    }
-    __syncthreads();
-    finish(a, sums, group);
 }
 
 template <int S, int V, int B>
@@ -400,10 +400,10 @@ __global__ __launch_bounds__(kGradThreads) void balance_grad_kernel(BalanceGradA
 int forward_groups(int T, int E) {
     const int per = kWaves * (E <= 16 ? 16 : 4);  // tokens of a workgroup at a time
     if (T <= kOneGroup * per) return 1;
-    return (int)min((int64_t)kMaxGroups, ceil_div64(T, per));
+    // (up to 64 experts no more workgroups than one fold, up to four rounds each: 8192 tokens 9.0 us in 64, 11.2 in 128)
+    const int most = E <= 64 && T <= 4 * 64 * per ? 64 : kMaxGroups;
+    return (int)min((int64_t)most, ceil_div64(T, per));
 }
-
-bool folds(int groups, int E) { return groups * E > 40960; }
 
 bool whole_chunks(int E, const void* a, const void* b) {
     return E % 4 == 0 && (((uintptr_t)a | (uintptr_t)b) & 15u) == 0;
@@ -413,19 +413,6 @@ template <int S, int V, int B>
 hipError_t forward(const BalanceArgs& a, hipStream_t s) {
     const int groups = forward_groups(a.T, a.E);
     hipLaunchKernelGGL((balance_kernel<S, V, B>), dim3(groups), dim3(kThreads), 0, s, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || groups == 1) return e;
-    int ep = 64;  // (fewer would leave one thread many sums to add)
-    while (ep < a.E) ep *= 2;
-    if (!folds(groups, a.E)) {
-        hipLaunchKernelGGL(balance_join_kernel, dim3(1), dim3(kThreads), 0, s, a, a.ws, groups, ep);
-        return hipGetLastError();
-    }
-    void* folded = (char*)a.ws + parts_bytes(groups, a.E);
-    const int left = ceil_div(groups, kFold);
-    hipLaunchKernelGGL(balance_fold_kernel, dim3(left, ceil_div(a.E + 1, 64)), dim3(kFoldThreads), 0, s, a.ws, groups, folded,
-                       a.E);
-    hipLaunchKernelGGL(balance_join_kernel, dim3(1), dim3(kThreads), 0, s, a, folded, left, ep);
     return hipGetLastError();
 }
 
@@ -457,7 +444,7 @@ hipError_t pick(const BalanceGradArgs& a, hipStream_t s) {
 
 size_t balance_ws_bytes(int T, int E) {
     const int g = forward_groups(T, E);
-    return g == 1 ? 0 : parts_bytes(g, E) + (folds(g, E) ? parts_bytes(ceil_div(g, kFold), E) : 0);
+    return g == 1 ? 0 : 4 * kTickets + parts_bytes(g, E) + parts_bytes(ceil_div(g, fold_of(E)), E);
 }
 
 hipError_t launch_balance(const BalanceArgs& a, hipStream_t s) {

@@ -247,11 +247,31 @@ def test_results_do_not_depend_on_the_run():
     ws, bufs = B.new_balance_workspace(30000, 60, "cuda"), B.new_balance_buffers(60, "cuda")
     first = {n: t.clone() for n, t in B.balance(zd, id_, valid=vd).items()}
     for fill in (0, 255):
-        ws.fill_(fill)
-        o = B.balance(zd, id_, valid=vd, out=bufs, workspace=ws)
-        assert o["losses"] is bufs["losses"]
-        for n in first:
-            assert torch.equal(o[n], first[n]), n
+        ws[B.BALANCE_ZERO_BYTES:].fill_(fill)
+        for _ in range(20):
+            o = B.balance(zd, id_, valid=vd, out=bufs, workspace=ws)
+            assert o["losses"] is bufs["losses"]
+            for n in first:
+                assert torch.equal(o[n], first[n]), n
+            assert not ws[:B.BALANCE_ZERO_BYTES].any()
+    # a workspace of more tokens
+    few = {n: t.clone() for n, t in B.balance(zd[:9000], id_[:9000], valid=vd[:9000]).items()}
+    B.balance(zd[:9000], id_[:9000], valid=vd[:9000], out=bufs, workspace=ws)
+    assert all(torch.equal(bufs[n], few[n]) for n in few)
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each."""
+    sets = [device(*make(i, 20000 + i, 60, 4)) for i in range(2)]
+    want = [{n: t.clone() for n, t in B.balance(z, i, valid=v).items()} for z, i, v in sets]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [B.new_balance_workspace(z.shape[0], 60, "cuda") for z, _, _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        got = [B.balance(z, i, valid=v, workspace=w, stream=s) for (z, i, v), w, s in zip(sets, spaces, streams)]
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert all(torch.equal(a[n], b[n]) for n in b)
 
 
 @pytest.mark.parametrize("T", [100, 5000])
@@ -318,6 +338,7 @@ def test_stream_and_graph(T):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, dz) and all(torch.equal(bufs[n], want[n]) for n in want), f"replay {rep}"
+        assert not ws[:B.BALANCE_ZERO_BYTES].any()
 
 
 def test_argument_refusals():

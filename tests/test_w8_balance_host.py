@@ -25,6 +25,7 @@ def test_header_constants():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     text = open(os.path.join(root, "include", "brownout_moe.h")).read()
     assert int(re.search(r"#define BMOE_W8_MAX_K (\d+)", text).group(1)) == B.W8_MAX_K
+    assert int(re.search(r"#define BMOE_BALANCE_ZERO_BYTES (\d+)", text).group(1)) == B.BALANCE_ZERO_BYTES
     assert [B.w8_row_bytes(K) for K in (8, 128, 136, 4096)] == [128, 128, 256, 4096]
 
 
