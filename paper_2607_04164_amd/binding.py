@@ -1164,7 +1164,9 @@ class LayerForward:
     8-bit weights: the FFN matrices (the shared ones too) given as W8 objects, bf16 layers, any number of tokens. The
     products run in 8-bit integers on the activations rounded token by token (brownout_moe_w8_ffn); the routed FFN
     gathers its rows (fused_gather), stream_k lets the tiles be split (the same bits either way). fold_combine and
-    few_tokens do not go with them; `device` as for 4-bit weights.
+    few_tokens do not go with them; `device` as for 4-bit weights. The layer above, bf16 / 8 bits / 4 bits: 1 token 38 /
+    32 / 32 us, 64 tokens 69 / 62 / 58, 256 tokens 110 / 83 / 107, 4096 tokens 313 / 233; d 4096, d_ff 14336, 4 segments,
+    top-2: 1 token 148 / 91 / 76, 64 tokens 303 / 173 / 238, 4096 tokens 2087 / 1209.
 
     balance=True: route keeps its logits (bufs["route"]["logits"]), and the method balance() gives the picks per
     expert and the balance and z losses of the last forward (bufs["balance"]). Not with few_tokens.
