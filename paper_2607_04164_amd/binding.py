@@ -1036,7 +1036,8 @@ class _BalanceLoss(torch.autograd.Function):
 def balance_loss(logits: torch.Tensor, topk_idx: torch.Tensor, *, valid: Optional[torch.Tensor] = None,
                  e2g: Optional[torch.Tensor] = None, G: Optional[int] = None):
     """balance for training: (losses, counts, prob), where losses [2] can be differentiated by the logits, once. On
-    the current stream."""
+    the current stream. In a captured graph call balance and balance_grad, or capture forward and backward together
+    with torch.autograd.grad while no eager graph of the same leaves lives."""
     return _BalanceLoss.apply(logits, topk_idx, valid, e2g, G)
 
 

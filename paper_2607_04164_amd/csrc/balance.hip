@@ -9,8 +9,8 @@
 // permutations. A lane keeps the sums of p of its experts over its tokens; a workgroup's sums meet in LDS in wave order.
 // The last of every fold_of(E) workgroups to finish adds their sums, the last of those the rest, in 64 bits and by
 // workgroup (arrival counters say who is last, the sums' order does not depend on it; no float atomics). That is one
-// launch: a second one for these sums takes the host longer than them (8192 tokens of 60 experts 12.2 -> 10.5 us a call,
-// though 9.2 and 9.0 in a graph). Up to kOneGroup rounds of tokens one workgroup does it all.
+// launch: a second one for these sums takes the host longer than them (8192 tokens of 60 experts 12.2 -> 8.9 us a call; in a
+// graph 9.2 and 9.0). Up to kOneGroup rounds of tokens one workgroup does it all.
 //
 // Bound by memory where there are many tokens (131072 of 256 experts: 36 us, 3.9 TB/s of 4.9; the read of the logits
 // alone 29), by the host's call for few (64 tokens: kernel 4.5 us, call 8), and between them by two or three round trips
@@ -273,7 +273,7 @@ template <int S, int V, int B>
 __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     constexpr int PER = 64 / S;  // tokens of a wave at a time
     __shared__ float s_p[kWaves][S * V];
-    __shared__ float s_z[kWaves];
+    __shared__ double s_z[kWaves];
     __shared__ Sums sums;
     __shared__ Scratch scratch;
     __shared__ int s_last;
@@ -286,7 +286,8 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     const int g = group_of(a.e2g, E, a.G, tid);
     for (int e = tid; e <= E; e += kThreads) sums.c[e] = 0;
     __syncthreads();
-    float p[V], z2 = 0.f;
+    float p[V];
+    double z2 = 0.0;  // (squares may leave fp32 where their mean does not)
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = 0.f;
     // (the lanes of a wave stay together: the permutations read their neighbours)
@@ -298,7 +299,7 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
         if (now.valid) {
 #pragma unroll
             for (int v = 0; v < V; ++v) p[v] += now.z[v];
-            z2 = fmaf(lse, lse, z2);
+            z2 = fma((double)lse, (double)lse, z2);
 #pragma unroll
             for (int i = 0; i < BMOE_MAX_TOPK / S; ++i)
                 if (now.pick[i] >= 0 && now.pick[i] < E) atomicAdd(&sums.c[now.pick[i]], 1);
@@ -324,7 +325,7 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     }
     if (tid == 0) {
         double sum = 0.0;
-        for (int w = 0; w < kWaves; ++w) sum += (double)s_z[w];
+        for (int w = 0; w < kWaves; ++w) sum += s_z[w];
         sums.z = sum;
     }
     __syncthreads();

@@ -241,6 +241,15 @@ def test_rows_off_16_byte_chunks(T, E, k):
         torch.testing.assert_close(B.balance_grad(src, a["counts"], k, d, valid=vd, out=dst), g, rtol=0, atol=8 * tol * size)
 
 
+@pytest.mark.parametrize("T", [7, 900, 5000])
+def test_squares_past_fp32(T):
+    """The sum of the squares leaves fp32, their mean does not."""
+    z = torch.full((T, 12), 1.5e19, device="cuda")
+    idx = torch.zeros((T, 1), dtype=torch.int32, device="cuda")
+    lse = float(np.float32(1.5e19))  # (log 12 is far below its last bit)
+    assert abs(float(B.balance(z, idx)["losses"][1]) / lse ** 2 - 1) <= 2 * F32
+
+
 def test_results_do_not_depend_on_the_run():
     z, idx, valid = make(2, 30000, 60, 4)
     zd, id_, vd = device(z, idx, valid)
