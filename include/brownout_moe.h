@@ -613,8 +613,8 @@ BMOE_API bmoe_status brownout_moe_w8_ffn(int32_t dtype, int32_t n_seg, int32_t r
  * d_logits [T,E] float, which may be logits itself (other shared memory is BMOE_ERR_UNSUPPORTED).
  * Logits of tokens that do not count may hold anything. -infinity is an expert of probability 0; a
  * token of nothing else has no probabilities, adds nothing to the losses and gets gradient 0,
- * though it counts in V. With V == 0 losses and prob are 0. Sums in a fixed order: results are
- * deterministic. E in 1..256, k in 1..16, G in 1..256.
+ * though it counts in V. With V == 0 losses and prob are 0 (T == 0 writes nothing). Sums in a
+ * fixed order: results are deterministic. E in 1..256, k in 1..16, G in 1..256.
  * workspace: bmoe_balance_workspace_bytes(T, E) bytes (0 for few tokens), 8-byte aligned. Its
  * first BMOE_BALANCE_ZERO_BYTES bytes (arrival counters) are zero before the first call that uses
  * it; every call leaves them zero; the rest needs no initialisation. Calls that can overlap in

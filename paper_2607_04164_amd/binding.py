@@ -972,9 +972,9 @@ def balance(logits: torch.Tensor, topk_idx: torch.Tensor, *, valid: Optional[tor
             workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
     """How evenly route's picks fall on the experts, or on the G groups of e2g: losses (balance loss, z loss),
     counts (picks per expert, then the number of tokens that count) and prob (mean probabilities). logits [T, E] and
-    topk_idx [T, k] as route writes them; valid [T] uint8: the tokens that count (None: all). workspace:
-    new_balance_workspace's for these T and E (or more tokens), or None (memory of the call's own stream, cleared by a
-    launch of its own)."""
+    topk_idx [T, k] as route writes them; valid [T] uint8: the tokens that count (None: all). T = 0 writes nothing.
+    workspace: new_balance_workspace's for these T and E (or more tokens), or None (memory of the call's own stream,
+    cleared by a launch of its own)."""
     T, E, G, device, lp, vp, gp = _balance_args(logits, valid, e2g, G)
     if not isinstance(topk_idx, torch.Tensor) or topk_idx.dim() != 2:
         raise ValueError("topk_idx must be [T, k]")

@@ -9,8 +9,8 @@
 // permutations. A lane keeps the sums of p of its experts over its tokens; a workgroup's sums meet in LDS in wave order.
 // The last of every fold_of(E) workgroups to finish adds their sums, the last of those the rest, in 64 bits and by
 // workgroup (arrival counters say who is last, the sums' order does not depend on it; no float atomics). That is one
-// launch: a second one for these sums takes the host longer than them (8192 tokens of 60 experts 12.2 -> 8.9 us a call; in a
-// graph 9.2 and 9.0). Up to kOneGroup rounds of tokens one workgroup does it all.
+// launch: a second one for these sums takes the host longer than them (8192 tokens of 60 experts 12.2 -> 8.9 us a call;
+// in a graph 9.2 and 9.0). Up to kOneGroup rounds of tokens one workgroup does it all.
 //
 // Bound by memory where there are many tokens (131072 of 256 experts: 36 us, 3.9 TB/s of 4.9; the read of the logits
 // alone 29), by the host's call for few (64 tokens: kernel 4.5 us, call 8), and between them by two or three round trips
@@ -165,6 +165,7 @@ __device__ __forceinline__ void finish(const BalanceArgs& a, Sums& s, int g) {
 // Rows of sums in the workspace: z [rows] double, p [rows, E] float, c [rows, E + 1] int32. They are written and read
 // past the XCDs' own L2 caches (relaxed atomics of device scope: sc1 stores and loads); a row is complete before its
 // workgroup counts itself in.
+//
 // Rows a workgroup adds at a time. More make fewer levels (3 us each) but longer ones: up to 64 experts 4096 tokens in 64
 // workgroups 7.8 us, in two levels of 32 9.9; 256 workgroups of 256 experts by 32 36 us, by 64 40.
 __host__ __device__ constexpr int fold_of(int E) { return E <= 64 ? 64 : 32; }

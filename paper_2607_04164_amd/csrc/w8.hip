@@ -65,7 +65,7 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void q8_rows_kernel(W8Quantize
     constexpr int R = NT > 256 ? 1 : 256 / NT;  // rows of a workgroup
     constexpr int W = NT / 64;
     __shared__ uint32_t part[W];
-    int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / NT;
+    const int64_t r = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * R + threadIdx.x / NT;
     // (one row of a workgroup where its threads have a barrier: they leave together)
     if (r >= a.rows) return;
     const int K = a.K, t = threadIdx.x % NT;
@@ -115,9 +115,10 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void q8_rows_kernel(W8Quantize
 template <typename E, int NT, int CH>
 hipError_t launch_q8(const W8QuantizeArgs& a, hipStream_t s) {
     constexpr int R = NT > 256 ? 1 : 256 / NT;
-    const int64_t blocks = ceil_div64(a.rows, R);
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((q8_rows_kernel<E, NT, CH>), dim3((unsigned)blocks), dim3(NT > 256 ? NT : 256), 0, s, a);
+    // (one dimension of a grid has room for less than 2^32 threads: 2^24 of these workgroups are too many)
+    const int64_t blocks = ceil_div64(a.rows, R), across = min(blocks, (int64_t)1 << 22);
+    hipLaunchKernelGGL((q8_rows_kernel<E, NT, CH>), dim3((unsigned)across, (unsigned)ceil_div64(blocks, across)),
+                       dim3(NT > 256 ? NT : 256), 0, s, a);
     return hipGetLastError();
 }
 

@@ -111,6 +111,19 @@ def test_quantize(rows, K, dtype):
         assert torch.equal(w.codes.view_as(q.codes), q.codes) and torch.equal(w.scales.view(-1), q.scales)
 
 
+@pytest.mark.parametrize("rows,K", [((1 << 26) + 5, 8), ((1 << 24) + 3, 1032)])
+def test_quantize_more_workgroups_than_a_grid_dimension_holds(rows, K):
+    """Rows of one power of two each, and its half: codes 127 and -64 (fp32's 1/127 is below 1/127, so just past -63.5)."""
+    x = torch.zeros((rows, K), dtype=torch.bfloat16, device="cuda")
+    exponent = (torch.arange(rows, device="cuda") % 7).to(torch.bfloat16)
+    x[:, 0], x[:, K - 1] = torch.exp2(exponent), -torch.exp2(exponent) / 2
+    q = B.a8_quantize(x)
+    assert torch.equal(q.scales, torch.exp2(exponent.float()) / 127)
+    assert bool((q.codes[:, 0] == 127).all()) and bool((q.codes[:, K - 1] == -64).all())
+    for part in (slice(0, 9), slice((1 << 24) - 4, (1 << 24) + 4), slice(rows - 9, rows)):
+        assert int(q.codes[part].ne(0).sum()) == 2 * q.codes[part].shape[0]
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 def test_quantize_ties_go_to_even(dtype):
     """Scale 1 (a row whose largest is 127) and powers of two beside it: every half is a tie."""
