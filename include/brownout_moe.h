@@ -540,7 +540,9 @@ BMOE_API bmoe_status brownout_moe_few(const bmoe_desc* desc, const bmoe_few_weig
  * [rows, K] by token. A stack of rows of K values (K a multiple of 8, at most BMOE_W8_MAX_K) is
  *   codes  [rows, P] int8, P = 128 * ceil(K/128): the codes of a row, then zeros
  *   scales [rows] float
- * and stands for x = scale * code. Both 16-byte aligned.
+ * and stands for x = scale * code. Both 16-byte aligned. Where they were made elsewhere, scales may
+ * have either sign; codes of -128 may be in one operand of a product (in both, sums of K =
+ * BMOE_W8_MAX_K can leave int32).
  *
  * brownout_moe_w8_quantize -- rounds x [rows, K] (dtype) to that format: scale = max|x| / 127 in
  * fp32, code = round(x / scale) to nearest even, of the true quotient. A row whose scale would be

@@ -98,11 +98,15 @@ struct OpI8 {
 };
 
 // a scale with which sum * a * b cannot leave fp32 on the way
-__device__ __forceinline__ bool plain_scale(float s) { return s == 0.f || (s >= 0x1p-60f && s <= 0x1p60f); }
-// sum * a * b. Scales far from 1: the smaller first, so that |sum| >= 1 neither under- nor overflows on the way to a
-// result that does not. A scale that is not a number makes the result one (fminf would drop it).
+__device__ __forceinline__ bool plain_scale(float s) {
+    const float size = fabsf(s);
+    return size == 0.f || (size >= 0x1p-60f && size <= 0x1p60f);
+}
+// sum * a * b. Scales far from 1: the smaller in size first (either may be negative where codes were made elsewhere), so
+// that |sum| >= 1 neither under- nor overflows on the way to a result that does not. A scale that is not a number makes
+// the result one (fminf would drop it).
 __device__ __forceinline__ float scaled(int sum, float a, float b) {
-    const bool swap = !(plain_scale(a) && plain_scale(b)) && !(a < b);
+    const bool swap = !(plain_scale(a) && plain_scale(b)) && !(fabsf(a) < fabsf(b));
     return (float)sum * (swap ? b : a) * (swap ? a : b);
 }
 

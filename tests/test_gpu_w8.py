@@ -339,6 +339,34 @@ def test_scales_far_apart(rows):
 
 
 @pytest.mark.parametrize("rows", [3, 300, 60000])
+@pytest.mark.parametrize("given", [False, True], ids=["a", "a8"])
+def test_scales_far_apart_of_either_sign(rows, given):
+    """Scales may be negative where the codes were made elsewhere: their sizes say which product is formed first."""
+    K, N = 128, 8
+    a = torch.zeros((rows, K), dtype=torch.bfloat16, device="cuda")
+    a[0, :] = 127 * 2.0 ** -100
+    a[1, :] = 127 * 2.0 ** 110
+    a[2, :] = 127.0
+    codes = torch.full((1, N, 128), 127, dtype=torch.int8, device="cuda")
+    scales = torch.tensor([[-2.0 ** 110, -2.0 ** -100, 2.0 ** 110, 2.0 ** -120, -2.0 ** 60, -1.5, -0.0, -2.0 ** -126]],
+                          device="cuda")
+    w = B.W8(codes, scales, K=K)
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    q, s = rounded64(a)
+    if given:
+        a = B.A8(q.to(torch.int8), s.float() * torch.tensor([-1.0, 1.0, -1.0] + [1.0] * (rows - 3), device="cuda"), K=K)
+        s = a.scales.double()
+    y = B.w8_matmul(off, a, w)
+    want = products64(q, s, [0, rows], w)
+    fits = want.abs() < torch.finfo(torch.bfloat16).max
+    assert bool(fits[0].all()) and fits[1].tolist() == [False, True, False, True, False, False, True, True]
+    assert torch.equal(y[~fits].double(), torch.sign(want[~fits]) * float("inf"))
+    # (the sum and the scales are powers of two but for 127^2 128 and 1.5: fp32 holds every product, the rounding to bf16 is
+    # the only one; below the smallest normal value it is an absolute one)
+    assert bool(((y.double() - want).abs() <= want.abs() * BF16 + 2.0 ** -133)[fits].all())
+
+
+@pytest.mark.parametrize("rows", [3, 300, 60000])
 def test_gated_scales_far_apart(rows):
     """Activations of 2^70 and of 2^-60 beside ordinary ones, weights that bring them back."""
     K, N = 128, 16
@@ -359,6 +387,22 @@ def test_gated_scales_far_apart(rows):
     assert bool(inside[0, :4].all()) and bool(inside[1, :8].all()) and not bool(inside[0].all())
     big = torch.where(inside, gate, torch.zeros_like(gate)), torch.where(inside, up, torch.zeros_like(up))
     check_hidden(torch.where(inside, h, torch.zeros_like(h)), *big, "h")
+
+
+@pytest.mark.parametrize("n,rows,N,K", [(1, 3, 264, 1048), (5, 777, 1000, 1048), (15, 6000, 520, 264), (1, 4000, 1032, 8192)])
+def test_negative_scales(n, rows, N, K):
+    """Every product with one scale negated is the product negated, on each kernel."""
+    g = gen(rows + N)
+    w = weights(g, n, N, K)
+    o = torch.from_numpy(segments(rows, rows, n)).cuda()
+    a8 = B.a8_quantize(randn(g, rows, K))
+    ws = B.new_w8_workspace(0, K, "cuda")
+    y = B.w8_matmul(o, a8, w, workspace=ws)
+    sign = torch.where(torch.rand(w.scales.shape, generator=g, device="cuda") < 0.5, -1.0, 1.0)
+    col = torch.repeat_interleave(sign, torch.diff(o.long()), dim=0, output_size=rows)
+    row = torch.where(torch.rand((rows,), generator=g, device="cuda") < 0.5, -1.0, 1.0)
+    back = B.w8_matmul(o, B.A8(a8.codes, a8.scales * row, K=K), B.W8(w.codes, w.scales * sign, K=K), workspace=ws)
+    assert torch.equal(back.float(), y.float() * col * row[:, None])
 
 
 @pytest.mark.parametrize("n,rows,d", [(2, 5, 256), (3, 60, 264), (2, 9000, 392)])
