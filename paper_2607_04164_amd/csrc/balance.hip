@@ -6,11 +6,14 @@
 //
 // S lanes of a wave hold a token's row (lane s: experts s, s + S, .., or four neighbours at a time where rows are whole
 // 16-byte chunks), so a wave takes 64 / S neighbouring rows at a time and a row's maximum and sums are register
-// permutations. A lane keeps the sums of p of its experts over its tokens; a workgroup's sums meet in LDS in wave order.
-// The last of every fold_of(E) workgroups to finish adds their sums, the last of those the rest, in 64 bits and by
-// workgroup (arrival counters say who is last, the sums' order does not depend on it; no float atomics). That is one
-// launch: a second one for these sums takes the host longer than them (8192 tokens of 60 experts 12.2 -> 8.9 us a call;
-// in a graph 9.2 and 9.0). Up to kOneGroup rounds of tokens one workgroup does it all.
+// permutations. A lane keeps the sums of p of its experts over its tokens, in fp32 for kRounds of them; longer sums are
+// kept in 64 bits in LDS. A workgroup's sums meet in LDS in wave order, in fp32. The last of every fold_of(E) workgroups
+// to finish adds their sums, the last of those the rest, in 64 bits and by workgroup (arrival counters say who is last,
+// the sums' order does not depend on it; no float atomics); a sum is rounded to fp32 where it is put away for the next
+// level. So a sum of p is off by at most kRounds + 24 roundings of 2^-24, however many tokens there are; the z loss's
+// squares are summed in 64 bits. That is one launch: a second one for these sums takes the host longer than them (8192
+// tokens of 60 experts 12.2 -> 8.9 us a call; in a graph 9.2 and 9.0). Up to kOneGroup rounds of tokens one workgroup
+// does it all.
 //
 // Bound by memory where there are many tokens (131072 of 256 experts: 36 us, 3.9 TB/s of 4.9; the read of the logits
 // alone 29), by the host's call for few (64 tokens: kernel 4.5 us, call 8), and between them by two or three round trips
@@ -24,6 +27,8 @@ constexpr int kThreads = 1024;  // of the forward's workgroups
 constexpr int kWaves = kThreads / 64;
 constexpr int kMaxGroups = 256;  // workgroups of the forward, at most
 constexpr int kOneGroup = 8;     // rounds of tokens that one workgroup takes by itself
+constexpr int kRounds = 32;      // tokens of a lane that are added in fp32 (a running sum of thousands loses what its steps
+                                 // round off, 3e-5 of it after 2048)
 constexpr int kGradThreads = 256;
 
 // sum / maximum over the S lanes of a token, the same bits in each of them
@@ -270,10 +275,20 @@ __device__ __forceinline__ void add_rows(const Parts& q, int row0, int n, int E,
     __syncthreads();
 }
 
+// the sums over a wave's tokens of what its lanes hold, in all of them
+template <int S, int V>
+__device__ __forceinline__ void wave_sums(float (&p)[V]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int off = S; off < 64; off *= 2) p[v] += __shfl_xor(p[v], off);
+}
+
 template <int S, int V, int B>
 __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     constexpr int PER = 64 / S;  // tokens of a wave at a time
     __shared__ float s_p[kWaves][S * V];
+    __shared__ double s_long[kWaves][S * V];  // sums of p of a wave's whole kRounds (is_long; a wave's own until the end)
     __shared__ double s_z[kWaves];
     __shared__ Sums sums;
     __shared__ Scratch scratch;
@@ -286,13 +301,25 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
     next.load(a.logits, a.topk_idx, a.valid, t, a.T, s, E, k);
     const int g = group_of(a.e2g, E, a.G, tid);
     for (int e = tid; e <= E; e += kThreads) sums.c[e] = 0;
+    const bool is_long = a.T > kRounds * step;
+    if (is_long)
+        for (int i = tid; i < kWaves * S * V; i += kThreads) s_long[i / (S * V)][i % (S * V)] = 0.0;
     __syncthreads();
     float p[V];
     double z2 = 0.0;  // (squares may leave fp32 where their mean does not)
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = 0.f;
     // (the lanes of a wave stay together: the permutations read their neighbours)
-    for (; __any(t < a.T); t += step) {
+    for (int round = 0; __any(t < a.T); t += step, ++round) {
+        if (round == kRounds) {
+            wave_sums<S, V>(p);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (lane < S) s_long[wave][expert_of<S, B>(s, v)] += (double)p[v];
+                p[v] = 0.f;
+            }
+            round = 0;
+        }
         Token<S, V, B, BMOE_MAX_TOPK / S> now = next;
         next.load(a.logits, a.topk_idx, a.valid, t + step, a.T, s, E, k);
         now.mask();
@@ -308,12 +335,10 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
         }
     }
     // the wave's tokens, then the waves in order
+    wave_sums<S, V>(p);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-#pragma unroll
-        for (int off = S; off < 64; off *= 2) p[v] += __shfl_xor(p[v], off);
+    for (int v = 0; v < V; ++v)
         if (lane < S) s_p[wave][expert_of<S, B>(s, v)] = p[v];
-    }
 #pragma unroll
     for (int off = S; off < 64; off *= 2) z2 += __shfl_xor(z2, off);
     if (lane == 0) s_z[wave] = z2;
@@ -322,7 +347,10 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a) {
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) sum += s_p[w][tid];
-        sums.p[tid] = (double)sum;
+        double all = (double)sum;
+        if (is_long)
+            for (int w = 0; w < kWaves; ++w) all += s_long[w][tid];
+        sums.p[tid] = all;
     }
     if (tid == 0) {
         double sum = 0.0;

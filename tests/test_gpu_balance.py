@@ -250,6 +250,32 @@ def test_squares_past_fp32(T):
     assert abs(float(B.balance(z, idx)["losses"][1]) / lse ** 2 - 1) <= 2 * F32
 
 
+# 65536 (E <= 16) and 16384 tokens a round of 256 workgroups: 2048 rounds and some, or 128; sums of two levels
+@pytest.mark.parametrize("T,E", [((1 << 27) + 77, 2), ((1 << 25) + 5, 17), ((1 << 21) + 3, 100), ((1 << 21) + 1, 251)])
+def test_long_batches_add_as_well_as_short_ones(T, E):
+    """A lane takes thousands of tokens; what it adds in fp32 is bounded all the same. Rows alike, so that every
+    rounding of a running sum would go the same way for long."""
+    row = np.zeros(E, np.float32)
+    row[0], row[1] = (3.0, 0.0) if E == 2 else (5.0, 2.0)
+    z = torch.from_numpy(row).cuda().expand(T, E).contiguous()
+    idx = torch.zeros((T, 1), dtype=torch.int32, device="cuda")
+    valid = torch.ones(T, dtype=torch.uint8, device="cuda")
+    valid[::1001] = 0
+    o = B.balance(z, idx, valid=valid)
+    want = losses64(row[None], np.zeros((1, 1), np.int32), None, np.arange(E), E, 1)
+    V = T - -(-T // 1001)
+    assert o["counts"].tolist() == [V] + [0] * (E - 1) + [V]
+    # fp32 sums of a lane up to 32 tokens, rounded once more; over 4 or 16 lanes' tokens and 16 waves; rounded where
+    # they are put away, twice, and at the end
+    tol = row_error(row[None])[0] + (32 + 1 + 4 + 16 + 3) * F32
+    np.testing.assert_allclose(o["prob"].double().cpu().numpy(), want[2], rtol=tol, atol=0)
+    got = o["losses"].double().cpu().numpy()
+    assert abs(got[0] / want[0][0] - 1) <= tol + F32
+    # (lse: the sum's error relative to its argument, its own roundings by its size, and the square)
+    size = float(want[4][0]) + 1
+    assert abs(got[1] - want[0][1]) <= 2 * size * (row_error(row[None])[0] + 8 * size * F32) + want[0][1] * 4 * F32
+
+
 def test_results_do_not_depend_on_the_run():
     z, idx, valid = make(2, 30000, 60, 4)
     zd, id_, vd = device(z, idx, valid)
