@@ -112,6 +112,8 @@ __device__ __forceinline__ float scaled(int sum, float a, float b) {
 
 __host__ __device__ constexpr int ceil_div(int a, int b) { return (a + b - 1) / b; }
 __host__ __device__ constexpr int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// whether one dimension of a grid holds these workgroups: it has room for less than 2^32 threads
+constexpr bool grid_holds(int64_t workgroups, int threads) { return workgroups * threads < (int64_t)1 << 32; }
 
 // ---- direct global->LDS loads and the waits that go with them
 //

@@ -662,6 +662,12 @@ bool skinny_dma_fits(const SkinnyParams& sp) {
     return sp.K % kS2KC == 0 && a_rows * sp.K * 2 < ((int64_t)1 << 31) && (int64_t)kSkCols * sp.K * 2 < ((int64_t)1 << 31);
 }
 
+// int8: workgroups of the segments' passes. A segment has one for its rows up to kSkRows, and at most one for every
+// kSkRows more.
+int64_t skinny_passes(const SkinnyParams& sp) {
+    return ((int64_t)sp.n_seg + sp.rows_cap / kSkRows) * ceil_div(sp.N, kSkCols);
+}
+
 template <bool GATED, int PAIRS, class OP>
 void launch_reg(const SkinnyParams& sp, int64_t blocks, hipStream_t s) {
     hipLaunchKernelGGL((skinny_reg_kernel<GATED, PAIRS, OP>), dim3((unsigned)blocks), dim3(kSkThreads), 0, s, sp);
@@ -671,19 +677,16 @@ template <bool GATED, class OP = OpBf16>
 hipError_t launch_skinny(const SkinnyParams& sp, hipStream_t s) {
     const int64_t blocks = (int64_t)sp.n_seg * ceil_div(sp.N, kSkCols);
     if (blocks <= 0) return hipSuccess;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    if (!grid_holds(blocks, kSkThreads)) return hipErrorInvalidValue;  // (2^22 of them: sizes are checked)
     const int64_t narrow = (int64_t)sp.n_seg * ceil_div(sp.N, kRgCols);
-    if (takes_reg<GATED>(sp) && narrow <= 0x7fffffff) {
+    if (takes_reg<GATED>(sp) && grid_holds(narrow, kSkThreads)) {
         if constexpr (GATED) launch_reg<GATED, 8, OP>(sp, narrow, s);
         else if (sp.K > 4 * 4 * 64 && sp.K <= 6 * 4 * 64) launch_reg<GATED, 6, OP>(sp, narrow, s);
         else launch_reg<GATED, 4, OP>(sp, narrow, s);
         return hipGetLastError();
     }
     if (OP::kScales) {
-        // a segment's passes: one for its rows up to kSkRows, and at most one for every kSkRows more
-        const int64_t passes = ((int64_t)sp.n_seg + sp.rows_cap / kSkRows) * ceil_div(sp.N, kSkCols);
-        if (passes > 0x7fffffff) return hipErrorInvalidValue;
-        hipLaunchKernelGGL((skinny_dma_kernel<GATED, OP>), dim3((unsigned)passes), dim3(kSkThreads), 0, s, sp);
+        hipLaunchKernelGGL((skinny_dma_kernel<GATED, OP>), dim3((unsigned)skinny_passes(sp)), dim3(kSkThreads), 0, s, sp);
     } else if (skinny_dma_fits(sp))
         hipLaunchKernelGGL((skinny_dma_kernel<GATED, OP>), dim3((unsigned)blocks), dim3(kSkThreads), 0, s, sp);
     else
@@ -739,7 +742,8 @@ hipError_t launch_ffn_skinny(const FfnArgs& a, hipStream_t s, int part) {
 //     segments, 1920 rows 18.5 / 21.5, 3000 rows 27.9 / 26.0; N = 4096, K = 14336 (split): 1 segment, 192 rows 36.1 /
 //     42.6, 384 rows 70.0 / 53.9; 4 segments, 300 rows 70.4 / 96.9, 600 rows 103.7 / 105.3
 bool w8_skinny_fits(const W8GemmArgs& a) {
-    if (!skinny_dma_fits(w8_params(a))) return false;
+    const SkinnyParams sp = w8_params(a);
+    if (!skinny_dma_fits(sp) || !grid_holds(skinny_passes(sp), kSkThreads)) return false;
     const int64_t rows = a.rows_cap, n = a.n_seg;
     if (rows <= kSkRows * n) return true;
     const bool gated = a.w1.codes != nullptr;

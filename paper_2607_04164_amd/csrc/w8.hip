@@ -115,7 +115,7 @@ __global__ __launch_bounds__(NT > 256 ? NT : 256) void q8_rows_kernel(W8Quantize
 template <typename E, int NT, int CH>
 hipError_t launch_q8(const W8QuantizeArgs& a, hipStream_t s) {
     constexpr int R = NT > 256 ? 1 : 256 / NT;
-    // (one dimension of a grid has room for less than 2^32 threads: 2^24 of these workgroups are too many)
+    // (2^24 of these workgroups are too many for one dimension of a grid)
     const int64_t blocks = ceil_div64(a.rows, R), across = min(blocks, (int64_t)1 << 22);
     hipLaunchKernelGGL((q8_rows_kernel<E, NT, CH>), dim3((unsigned)across, (unsigned)ceil_div64(blocks, across)),
                        dim3(NT > 256 ? NT : 256), 0, s, a);
@@ -300,6 +300,8 @@ hipError_t launch_few8(const Few8Params& p, hipStream_t s) {
 // 15 segments, gate/up 4 rows 9.9 / 12.2, 8 rows 11.5 / 17.2, down 8 rows 8.8 / 11.1; 4 segments, N = K = 4096, 4 rows
 // 13.8 / 14.7. (Room for 32768 values costs the smaller calls 0.3 to 1 us by its registers.)
 bool w8_few_fits(const W8GemmArgs& a) {
+    // (the most segments of the widest matrices: the other kernels' workgroups have more columns)
+    if (!grid_holds((int64_t)a.n_seg * ceil_div(a.N, 16), kFewThreads)) return false;
     return a.rows_cap <= kFewRows && a.rows_cap * w8_pitch(a.K) <= (a.n_seg == 1 ? kFewValues / 2 : kFewValues);
 }
 

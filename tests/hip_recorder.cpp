@@ -30,6 +30,7 @@ void* cfg_stream;
 int g_device = 0, g_device_status = 0, g_cus = 256, g_cus_status = 0;
 char g_array[1 << 21];
 void* g_module;
+int last_error = 0;
 }  // namespace
 
 extern "C" {
@@ -63,7 +64,11 @@ int hipDeviceGetAttribute(int* v, int, int) {
     *v = g_cus;
     return g_cus_status;
 }
-int hipGetLastError() { return 0; }
+int hipGetLastError() {
+    const int e = last_error;
+    last_error = 0;
+    return e;
+}
 int hipFuncSetAttribute(const void*, int, int) { return 0; }
 int hipGetSymbolAddress(void** p, const void*) {
     *p = g_array;
@@ -83,7 +88,10 @@ int __hipPopCallConfiguration(Dim* g, Dim* b, size_t* shmem, void** stream) {
     *stream = cfg_stream;
     return 0;
 }
-int hipLaunchKernel(const void* f, Dim g, Dim, void**, size_t, void*) {
+int hipLaunchKernel(const void* f, Dim g, Dim b, void**, size_t, void*) {
+    // (a dimension of 2^32 threads or more: hipErrorInvalidConfiguration, as the runtime answers)
+    const uint64_t most = (uint64_t)1 << 32;
+    if ((uint64_t)g.x * b.x >= most || (uint64_t)g.y * b.y >= most || (uint64_t)g.z * b.z >= most) return last_error = 9;
     launches.push_back({names()[f], g.x, g.y, g.z});
     return 0;
 }

@@ -297,3 +297,22 @@ def test_route_two_workgroups_per_cu_repeats(E, d, T):
         for k, v in first.items():
             assert torch.equal(r[k], v), (i, k)
     del b
+
+
+def test_most_segments_of_the_widest_matrices():
+    """256 segments of 2^20 columns: as 2^24 workgroups of 16 columns they are more threads than one dimension of a
+    grid has."""
+    g = torch.Generator(device="cuda").manual_seed(20)
+    n, d, f, rows = 256, 1 << 20, 24, 6
+    w = torch.empty((n, d, f), dtype=torch.bfloat16, device="cuda")
+    at, ends = [0, 1, 131, 255], (1, 3, 5, 6)
+    offs = np.zeros(n + 1, np.int32)
+    for i, e in zip(at, ends):
+        w[i] = torch.randn((d, f), generator=g, device="cuda").to(torch.bfloat16)
+        offs[i + 1:] = e
+    h = torch.randn((rows, f), generator=g, device="cuda").to(torch.bfloat16)
+    y = B.ffn_down(torch.from_numpy(offs).cuda(), h, w)
+    for i, b, e in zip(at, (0, *ends), ends):
+        want, size = h[b:e].double() @ w[i].double().t(), h[b:e].double().abs() @ w[i].double().abs().t()
+        # products of bf16 values are exact in fp32; their sum in any order, then one rounding to bf16
+        assert bool(((y[b:e].double() - want).abs() <= want.abs() * 2.0 ** -8 + size * (f + 1) * 2.0 ** -24).all()), i

@@ -444,6 +444,25 @@ def test_largest_sums():
         check_product(y, products64(*rounded64(a), [0, rows], w), f"{rows} rows")
 
 
+@pytest.mark.parametrize("given", [False, True], ids=["a", "a8"])
+def test_most_segments_of_the_widest_matrices(given):
+    """256 segments of 2^20 columns (34 GB of codes): 2^24 workgroups of 16 columns are more threads than one dimension of
+    a grid has."""
+    g = gen(20)
+    n, N, K, rows = 256, 1 << 20, 64, 6
+    codes = torch.empty((n, N, 128), dtype=torch.int8, device="cuda")
+    at = [0, 1, 131, 255]
+    codes[at] = torch.randint(-127, 128, (len(at), N, 128), generator=g, device="cuda", dtype=torch.int8)
+    w = B.W8(codes, torch.rand((n, N), generator=g, device="cuda") + 0.5, K=K)
+    offs = np.zeros(n + 1, np.int32)
+    for i, e in zip(at, (1, 3, 5, 6)):
+        offs[i + 1:] = e
+    a = randn(g, rows, K)
+    q, s = rounded64(a)
+    y = B.w8_matmul(torch.from_numpy(offs).cuda(), B.a8_quantize(a) if given else a, w)
+    check_product(y, products64(q, s, offs, w), "y")
+
+
 @pytest.mark.parametrize("n,rows,f,d", [(3, 9, 96, 256), (4, 40, 96, 256), (3, 9000, 520, 136)])
 def test_stream_and_graph(n, rows, f, d):
     g = gen(9)

@@ -7,7 +7,7 @@ import shutil
 
 import pytest
 
-from launch_record import PTR, kernels, record, struct
+from launch_record import PTR, ffn_part, kernels, record, struct
 from paper_2607_04164_amd import binding as B
 
 OK, NULL, SHAPE, ALIGN, UNSUP, WS = 0, 1, 2, 3, 5, 6
@@ -232,6 +232,26 @@ def test_product_choice(tmp_path):
     # a source too large for the few-row copies' 32-bit offsets
     ls, = launched([product(256, 256 * 64, 64, 131072, a8=True)], tmp_path)
     assert "grouped_gemm_dma_kernel" in ls[0][0]
+
+
+@needs_recorder
+def test_largest_sizes_are_launched(tmp_path):
+    """The widest matrices of the most segments: no dimension of a grid holds 2^32 threads (the runtime refuses them)."""
+    sizes = [(256, rows, N, K) for rows in (1, 16, 200, 20000) for N in ((1 << 20) - 8, 1 << 20) for K in (8, 128, 4096)]
+    sizes += [(1, 1 << 30, 64, 128), (256, 1 << 30, 8, 8), (256, 16384, 1 << 20, 131072)]
+    calls = [product(*c, gated=gated, a8=a8, ws=1 << 44) for c in sizes for gated in (False, True) for a8 in (False, True)]
+    calls += [{"fn": "brownout_moe_w8_quantize", "args": [*ints(t, 1 << 30, K), ["p", PTR], ["p", 1 << 50], ["p", 1 << 55],
+                                                          ["p", 0]]} for t in (0, 1) for K in (8, 4096, 131072)]
+    # a narrow matrix with a long K, where the few-row tiles are taken for any number of rows (gathered from few)
+    for rows in (1 << 25, (1 << 30) - 64, 1 << 30):
+        c = product(1, rows, 8, 12800, a8=True, ws=0)
+        c["args"][6:8] = [["p", PTR], ["i", 100]]
+        calls.append(c)
+    # bf16, on the same kernels
+    calls += [ffn_part("down", 256, rows, 1 << 20, f) for rows in (1, 16, 200) for f in (8, 64, 4096)]
+    calls += [ffn_part("up", 256, rows, d, 1 << 20) for rows in (1, 16, 200) for d in (8, 512, 4096)]
+    for c, ls in zip(calls, launched(calls, tmp_path)):
+        assert ls, c
 
 
 @needs_recorder
