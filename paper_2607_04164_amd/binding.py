@@ -1336,7 +1336,7 @@ class LayerForward:
         fused = self.fused_gather
         self._dispatch_args = (ptr(dp["counts"]), ptr(dp["offsets"]), ptr(dp["perm_token"]), ptr(dp["slot_row"]),
                                None if fused else ptr(dp["x_perm"]), ptr(self.ws), self.ws.numel())
-        rows = max(T * k, 1)
+        rows = T * k  # (0: the calls return before they look at anything)
         # fused: (.., offsets, a_rows, a_count) then x's pointer at call time
         a_src = (ptr(dp["perm_token"]), T) if fused else (ptr(dp["x_perm"]),)
         self._gate_up_args = (dtype, G, rows, d, f, ptr(dp["offsets"]), *a_src, ptr(w["w_gate"]),

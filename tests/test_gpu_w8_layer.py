@@ -141,6 +141,26 @@ def test_block_captured(name):
         assert torch.equal(r, wr) and torch.equal(a, wa) and all(torch.equal(o[n], wo[n]) for n in wo), f"replay {rep}"
 
 
+@pytest.mark.parametrize("kind", ["bf16", "w4", "w8"])
+@pytest.mark.parametrize("name", ["one-token", "prefill", "shared"])
+def test_layer_of_no_tokens(name, kind):
+    """Nothing is written, nothing is refused."""
+    cfg, desc, x, plain, w = made(name)
+    w = {"bf16": plain, "w8": w,
+         "w4": {n: B.w4_quantize(t, 64) if n in MATRICES else t for n, t in plain.items()}}[kind]
+    more = {"bf16": ({"fused_gather": True}, {"fused_gather": False}, {"fold_combine": True}, {"few_tokens": True}),
+            "w4": ({"few_tokens": True},), "w8": ({"concurrent_shared": False},)}[kind]
+    for kw in ({}, *more):
+        layer = B.LayerForward(desc.replace(T=0), w, **kw)
+        assert layer(x[:0]).shape == (0, desc.d), kw
+        if "few_tokens" not in kw:
+            for buf in ("h", "y"):
+                layer.bufs[buf].fill_(7.0)
+            layer(x[:0])
+            assert bool((layer.bufs["h"] == 7).all()) and bool((layer.bufs["y"] == 7).all())
+    torch.cuda.synchronize()
+
+
 def test_layer_refusals():
     cfg, desc, x, plain, w = made("shared")
     first = B.W8(w["w_gate"].codes[:1].contiguous(), w["w_gate"].scales[:1].contiguous(), K=w["w_gate"].shape[2])
