@@ -1162,10 +1162,11 @@ class LayerForward:
     above: 64 tokens 57 us against 68, 256 tokens 116 against 114, 4096 tokens 1162
     against 324). The layer's device is its weights': `device` must name it.
 
-    8-bit weights: the FFN matrices (the shared ones too) given as W8 objects, bf16 layers, any number of tokens. The
-    products run in 8-bit integers on the activations rounded token by token (brownout_moe_w8_ffn); the routed FFN
-    gathers its rows (fused_gather), stream_k lets the tiles be split (the same bits either way). fold_combine and
-    few_tokens do not go with them; `device` as for 4-bit weights. The layer above, bf16 / 8 bits / 4 bits: 1 token 38 /
+    8-bit weights: the FFN matrices (the shared ones too) given as W8 objects, bf16 layers, any number of tokens whose
+    8-bit rows are below 4 GiB (the gathered copies address them with 32-bit byte offsets). The products run in 8-bit
+    integers on the activations rounded token by token (brownout_moe_w8_ffn); the routed FFN gathers its rows
+    (fused_gather), stream_k lets the tiles be split (the same bits either way). fold_combine and few_tokens do not go
+    with them; `device` as for 4-bit weights. The layer above, bf16 / 8 bits / 4 bits: 1 token 38 /
     32 / 32 us, 64 tokens 69 / 62 / 58, 256 tokens 110 / 83 / 107, 4096 tokens 313 / 233; d 4096, d_ff 14336, 4 segments,
     top-2: 1 token 148 / 91 / 76, 64 tokens 303 / 173 / 238, 4096 tokens 2087 / 1209.
 
@@ -1192,6 +1193,8 @@ class LayerForward:
             return
         if self.w4 or self.w8:
             fused_gather = True
+        if self.w8 and desc.T * w8_row_bytes(desc.d) >= 1 << 32:
+            raise ValueError(f"{desc.T} tokens of {desc.d} columns: their 8-bit rows must be below 4 GiB")
         if fused_gather is None:
             # (the gathered copies address x with 32-bit byte offsets)
             x_bytes = desc.T * desc.d * (2 if desc.dtype == BMOE_BF16 else 4)

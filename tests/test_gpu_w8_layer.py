@@ -161,6 +161,12 @@ def test_layer_of_no_tokens(name, kind):
     torch.cuda.synchronize()
 
 
+def test_rows_past_the_copies_offsets_are_refused():
+    cfg, desc, x, _, w = made("one-token")
+    with pytest.raises(ValueError, match="4 GiB"):
+        B.LayerForward(desc.replace(T=1 << 23), w)
+
+
 def test_layer_refusals():
     cfg, desc, x, plain, w = made("shared")
     first = B.W8(w["w_gate"].codes[:1].contiguous(), w["w_gate"].scales[:1].contiguous(), K=w["w_gate"].shape[2])
