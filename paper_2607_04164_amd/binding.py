@@ -1166,9 +1166,11 @@ class LayerForward:
     8-bit rows are below 4 GiB (the gathered copies address them with 32-bit byte offsets). The products run in 8-bit
     integers on the activations rounded token by token (brownout_moe_w8_ffn); the routed FFN gathers its rows
     (fused_gather), stream_k lets the tiles be split (the same bits either way). fold_combine and few_tokens do not go
-    with them; `device` as for 4-bit weights. The layer above, bf16 / 8 bits / 4 bits: 1 token 38 /
-    32 / 32 us, 64 tokens 69 / 62 / 58, 256 tokens 110 / 83 / 107, 4096 tokens 313 / 233; d 4096, d_ff 14336, 4 segments,
-    top-2: 1 token 148 / 91 / 76, 64 tokens 303 / 173 / 238, 4096 tokens 2087 / 1209.
+    with them; `device` as for 4-bit weights. The layer above, bf16 / 8 bits / 4 bits (in brackets
+    few_tokens in bf16 and 4 bits, which up to 16 tokens of such narrow experts is faster than 8 bits): 1 token 38 / 32 /
+    32 us (26, 19), 4 tokens 43 / 42 / 37 (37, 28), 16 tokens 57 / 50 / 44 (46, 34), 64 tokens 69 / 62 / 57, 256 tokens 110 /
+    83 / 107, 4096 tokens 313 / 233; d 4096, d_ff 14336, 4 segments, top-2: 1 token 148 / 92 / 76 (132, 57), 16 tokens 299 /
+    164 / 140 (295, 126), 64 tokens 303 / 173 / 238, 4096 tokens 2087 / 1209.
 
     balance=True: route keeps its logits (bufs["route"]["logits"]), and the method balance() gives the picks per
     expert and the balance and z losses of the last forward (bufs["balance"]). Not with few_tokens.

@@ -16,7 +16,7 @@
 // does it all.
 //
 // Bound by memory where there are many tokens (131072 of 256 experts: 36 us, 3.9 TB/s of 4.9; the read of the logits
-// alone 29), by the host's call for few (64 tokens: kernel 4.5 us, call 8), and between them by two or three round trips
+// alone 29), by the host's call for few (64 tokens: kernel 4.3 us, call 8 to 9), and between them by two or three round trips
 // past the caches for the sums.
 #include "bmoe_common.h"
 

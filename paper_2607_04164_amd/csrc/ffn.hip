@@ -328,10 +328,12 @@ hipError_t launch_gemm(const GemmParams& g, hipStream_t s) {
 // not by latency. K that is not whole K-steps: tail_cols, below.
 //
 // int8 operands (OpI8): the same kernel, each K-step twice the columns, 32x32x32 int8 MFMA with int32 accumulators, and
-// the scales of the tile's rows and columns in LDS. Tiles of 16 K-steps and more run at 2.0 to 2.4 POP/s, above the
-// library's 1.97 (a K-step 1.43 us as in bf16, at a higher clock: 1.19 without its copies, 1.43 without the waits for
-// them), with 7 to 9 us of epilogue a tile: 8192 rows of 4 segments, d = 4096, d_ff = 14336 gate/up 840, down 372 us
-// (plus 20 of fixup); 30000 rows of 15 segments, d = 2048, d_ff = 1408 191 to 221 and 100 to 115.
+// the scales of the tile's rows and columns in LDS. A K-step takes 1.43 us as in bf16, at a higher clock (1.19 without its
+// copies, 1.43 without the waits for them), and the epilogue 7 to 9 us a tile, which K of 2048 and less does not hide.
+// Kernel times, and the rate of the rows' own operations (a library product of 8192 x 28672 x 4096: 1.97 POP/s): 8192
+// rows of 4 segments, d = 4096, d_ff = 14336 gate/up 840 us, 2.3 POP/s, down 372 us and 20 of fixup, 2.5; 4096 rows
+// through 14336 x 4096 219 to 247 us, 1.9 to 2.2; 30000 rows of 15 segments, d = 2048, d_ff = 1408 gate/up (16 K-steps)
+// 191 to 221 us, 1.6 to 1.8, down (11 K-steps) 98 to 115 us, 1.5 to 1.8.
 //
 // Work distribution: one workgroup per CU, rounds of one tile per workgroup.
 // With a workspace (stream-K) the K-steps of the last tiles may be split evenly

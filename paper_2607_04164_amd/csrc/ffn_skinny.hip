@@ -631,6 +631,18 @@ __global__ __launch_bounds__(kSkThreads, 2) void skinny_reg_kernel(SkinnyParams 
 // The rule counts on a spread. All rows in one segment (no routing of several
 // picks does that) cost two passes from 33 rows on: 64 rows in one of 15 segments
 // 8.9 / 11.9, of 60 segments 9.5 / 16.4; up to 32 rows 8.7 / 7.2 and 9.3 / 9.1.
+//
+// int8 (K counts pairs, so a bound on K is one of twice the columns) goes by the same rule. us, ring / this kernel, rows
+// spread at random, weights of three sets in turn, captured; * where the rule takes the slower one by more than 5 %:
+//  gate/up: 15 segments 1 row 9.8 / 5.7, 4 rows 10.2 / 8.2, 16 rows 13.8 / 15.7, 32 rows 23.2 / 20.4*, 64 rows 22.7 / 20.4,
+//   240 rows 23.6 / 24.7; 60 segments 4 rows 10.2 / 10.3, 8 rows 11.5 / 15.0, 96 rows 61.5 / 67.9; one segment 4 rows 9.5 /
+//   5.5, 32 rows 10.0 / 6.9*; d = 4096, d_ff = 14336, 4 segments 1 row 28.1 / 30.9, 64 rows 104 / 114; d_ff = 3584, 8
+//   segments 1 row 16.2 / 9.4, 4 rows 18.9 / 22.3, 32 rows 50.1 / 53.2*, 96 rows 50.4 / 56.3; d_ff = 176, 15 segments 9.5
+//   to 10.2 / 5.3 to 6.7;
+//  down: 15 segments 1 row 6.0 / 3.7, 16 rows 11.9 / 7.9, 96 rows 13.3 / 11.5, 128 rows 13.4 / 11.5*, 240 rows 13.8 / 13.9;
+//   60 segments 4 rows 8.8 / 6.5, 96 rows 40.9 / 27.7, 128 rows 41.4 / 27.9*, 240 rows 46.4 / 31.5*; one segment 16 rows
+//   6.1 / 4.0, 32 rows 6.3 / 4.7*; d = 4096, d_ff = 14336, 4 segments 1 row 33.5 / 12.1, 16 rows 42.4 / 44.1, 96 rows 43.9 /
+//   73.9; d_ff = 3584, 8 segments 1 row 10.9 / 5.8, 8 rows 13.7 / 14.5, 48 rows 25.7 / 26.3, 240 rows 27.1 / 45.0.
 template <bool GATED>
 bool takes_reg(const SkinnyParams& p) {
     const int64_t n = p.n_seg, rows = p.rows_cap, cols = ceil_div(p.N, kSkCols);
